@@ -291,6 +291,94 @@ int spts_msdp_compact_batched(spts_ctx *ctx, const void *x_in, const int32_t *po
                               int32_t protect_last, void *x_out, int32_t *pos_out,
                               int32_t *map_new2old, int32_t *map_old2new);
 
+/* ---- decode in 4 bits ------------------------------------------------------------------------
+ * The 4-bit form (a storage choice of this library, not part of the method): blocks of 32 consecutive values along a
+ * row of a matrix, or along the head dimension of a cached key or value, share the smallest power of two 2^e,
+ * -126 <= e <= 125, with max|v| <= 6 * 2^e; a value is stored as the nearest of +-{0, 1/2, 1, 3/2, 2, 3, 4, 6} * 2^e, ties to
+ * the even code, larger magnitudes (above 6 * 2^125) as 6 * 2^125.  A block that holds a NaN reads as NaN.  17/32 of a
+ * byte per value; a stored value is exact in bf16 and fp32, so products with it are those of the rounded matrix. */
+
+/* One matrix [rows, K] (y = x * W^T, as all matrices here) in 4 bits: two caller-owned device buffers of the sizes that
+ * spts_q4_bytes gives, in a layout of this library (strips of 16 rows by slabs of 512 columns).  K % 8 == 0. */
+typedef struct {
+    void *codes, *scales;
+    int64_t rows, K;
+} spts_q4;
+/* Bytes of the two buffers.  SPTS_EINVAL on rows or K < 1 or a NULL pointer, SPTS_ESHAPE on K % 8 != 0 or K >= 2^31. */
+int spts_q4_bytes(int64_t rows, int64_t K, size_t *code_bytes, size_t *scale_bytes);
+/* Packs W [out->rows, out->K] of the context's element type (device, row-major, 16-byte aligned) into out's buffers. */
+int spts_q4_pack(spts_ctx *ctx, const void *W, const spts_q4 *out);
+/* y[b, r] = sum_k W[r, k] x[b, k] for b < batch <= SPTS_MAX_DECODE_BATCH: x [batch, K] of the element type, y
+ * [batch, rows] of the element type, or fp32 where y_f32 != 0 (logits).  fp32 sums whose order depends on neither batch nor
+ * position in it: a vector has the same product alone and in any batch.  y must not overlap x.  batch == 0 does nothing. */
+int spts_matvec_q4(spts_ctx *ctx, const spts_q4 *W, const void *x, int32_t batch, void *y, int32_t y_f32);
+
+/* KV cache of one layer and sequence in 4 bits: post-rotary keys and values of the context's Hkv heads of d dimensions
+ * (d = 32, 64 or 128: SPTS_ESHAPE otherwise), blocks along d.  Device buffers of the sizes that spts_kv4_bytes gives
+ * (k and v: code_bytes each, k_scale and v_scale: scale_bytes each; 16-byte aligned), pos [capacity] int32; capacity a
+ * multiple of 8.  count lives on the host, as in spts_kv_out.  What lies behind the first count rows is never read as a
+ * value: the buffers need no initialisation. */
+typedef struct {
+    void *k, *v, *k_scale, *v_scale;
+    int32_t *pos;
+    int64_t capacity;
+    int64_t count;
+} spts_kv4;
+int spts_kv4_bytes(const spts_model_desc *model, int64_t capacity, size_t *code_bytes, size_t *scale_bytes);
+/* Appends rows to the caches of `batch` sequences (<= SPTS_MAX_DECODE_BATCH, distinct buffers): rows
+ * [offsets[b], offsets[b+1]) of k, v [rows, Hkv, d] (element type) and pos [rows] (all device) go behind caches[b]'s count,
+ * which is increased.  offsets [batch+1] is a HOST array, offsets[0] = 0, ascending.  A prefill's spts_kv_out is converted
+ * with batch = 1 and offsets {0, count}; a decode step appends one row to each.  SPTS_EINVAL where a capacity is exceeded. */
+int spts_kv4_append(spts_ctx *ctx, const void *k, const void *v, const int32_t *pos, const int64_t *offsets, int32_t batch,
+                    spts_kv4 *caches);
+/* The stored values back: rows first[b] .. first[b] + offsets[b+1] - offsets[b] of caches[b] (first: HOST [batch], NULL =
+ * from row 0; within count) to rows [offsets[b], offsets[b+1]) of k_out, v_out [rows, Hkv, d]. */
+int spts_kv4_read(spts_ctx *ctx, const spts_kv4 *caches, const int64_t *first, const int64_t *offsets, int32_t batch,
+                  void *k_out, void *v_out);
+/* Decode attention over 4-bit caches: out[b, h] = softmax(q[b, h] K_b^T / sqrt(d)) V_b over all count rows of caches[b];
+ * q, out [batch, H, d] of the element type, query head h reads key/value head h / (H / Hkv).  H / Hkv <= 16.  An empty
+ * cache gives zeros.  The same cache may be given to several queries.  Uses the context's workspace. */
+int spts_kv4_attn(spts_ctx *ctx, const void *q, int32_t batch, const spts_kv4 *caches, void *out);
+
+/* One layer's parameters for a decode step in 4 bits (layouts as in spts_layer_weights; gains in the element type). */
+typedef struct {
+    spts_q4 Wq, Wk, Wv, Wo, Wgate, Wup, Wdown;
+    const void *gamma1, *gamma2;
+} spts_layer_q4;
+/* spts_decode_layer_batched with weights and caches in 4 bits: one new token for each of `batch` sequences, x [batch, D]
+ * in/out, pos HOST [batch].  The new pair is rounded to the element type, then stored in 4 bits, and attended to as stored.
+ * Every row of x is treated alike whatever the batch.  D, H * d and Dff multiples of 8, d and H / Hkv as in
+ * spts_kv4_attn, count < capacity. */
+int spts_decode_layer_q4(spts_ctx *ctx, void *x, const int32_t *pos, int32_t batch, const spts_layer_q4 *w,
+                         spts_kv4 *caches);
+/* RMSNorm with gamma [D] of x [batch, D] into xn [batch, D] (element type; batch <= SPTS_MAX_DECODE_BATCH): the
+ * final norm in front of a head that is a spts_q4 matrix. */
+int spts_rmsnorm(spts_ctx *ctx, const void *x, const void *gamma, int32_t batch, void *xn);
+
+/* What is done to the logits of a step before the next token is chosen.  Everything is optional (NULL = off).  Device:
+ * history, bias, mask; HOST [batch]: history_len, prompt_len, repetition, frequency, presence. */
+typedef struct {
+    const int32_t *history;        /* [batch, history_stride] token ids: the prompt, then the answer so far; ids outside
+                                    * [0, V) are skipped (padding)                                               */
+    int64_t history_stride;
+    const int64_t *history_len;    /* ids of each row that count (needed with history)                           */
+    const int64_t *prompt_len;     /* the first of them that are the prompt (NULL = 0)                           */
+    const float *repetition;       /* > 0; l > 0 ? l / r : l * r for every word in the history (NULL = 1)        */
+    const float *frequency;        /* l - f * (times that the word is in the answer) (NULL = 0)                  */
+    const float *presence;         /* l - p for every word in the answer (NULL = 0)                              */
+    const float *bias;             /* l + bias[word]; row b at bias + b * bias_stride, 0 = one row for all       */
+    int64_t bias_stride;
+    const uint32_t *mask;          /* bit (word % 32) of mask[word / 32] set = allowed, others become -inf; row  */
+    int64_t mask_stride;           /* b at mask + b * mask_stride, 0 = one row for all                           */
+} spts_logits_rules;
+/* Applies the rules in the order of the struct's fields to logits [batch, V] (fp32) and writes logits_out [batch, V] (may
+ * be logits itself).  token_out [batch] (NULL = not wanted): the allowed word with the largest result, ties to the lowest
+ * id; -1 where no word is allowed (or all that are allowed are NaN); a masked NaN or infinity does not matter.
+ * x_next [batch, D] (NULL = not wanted; needs token_out and table [V, D]): row token of the table, zeros for -1.
+ * batch <= SPTS_MAX_DECODE_BATCH.  spts_greedy_token_batched's logits_out are such logits. */
+int spts_process_logits(spts_ctx *ctx, const float *logits, int32_t V, int32_t batch, const spts_logits_rules *rules,
+                        float *logits_out, int32_t *token_out, const void *table, void *x_next);
+
 /* Per-phase timing for benchmarks.  Between spts_profile_begin and spts_profile_end every phase of
  * every call on this context (k_proj, probe_attn, topk, attention, ffn_gate_up, ...) is bracketed
  * by two HIP events on the context's stream.  Products that share a launch are one phase (qv_proj:

@@ -23,6 +23,8 @@ EXPORTS = (
     "spts_probe_attn", "spts_probe_ffn", "spts_select_topk", "spts_select_topk_static", "spts_select_topk_batched", "spts_select_topk_segmented", "spts_layer_prefill", "spts_layer_prefill_batched", "spts_msdp_compact", "spts_msdp_compact_batched",
     "spts_decode_layer", "spts_decode_layer_batched", "spts_greedy_token", "spts_greedy_token_batched", "spts_channel_importance",
     "spts_pack_slab32",
+    "spts_q4_bytes", "spts_q4_pack", "spts_matvec_q4", "spts_kv4_bytes", "spts_kv4_append", "spts_kv4_read", "spts_kv4_attn",
+    "spts_decode_layer_q4", "spts_rmsnorm", "spts_process_logits",
     "spts_profile_begin", "spts_profile_end", "spts_profile_count", "spts_profile_get",
 )
 
@@ -46,6 +48,40 @@ class spts_layer_cfg(C.Structure):
 
 class spts_kv_out(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("pos", C.c_void_p), ("capacity", C.c_int64), ("count", C.c_int64)]
+
+
+class spts_q4(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("rows", C.c_int64), ("K", C.c_int64)]
+
+
+class spts_kv4(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("pos", C.c_void_p),
+                ("capacity", C.c_int64), ("count", C.c_int64)]
+
+
+class spts_layer_q4(C.Structure):
+    _fields_ = [(n, spts_q4) for n in ("Wq", "Wk", "Wv", "Wo", "Wgate", "Wup", "Wdown")] + [("gamma1", C.c_void_p), ("gamma2", C.c_void_p)]
+
+
+class spts_logits_rules(C.Structure):
+    _fields_ = [("history", C.c_void_p), ("history_stride", C.c_int64), ("history_len", C.POINTER(C.c_int64)),
+                ("prompt_len", C.POINTER(C.c_int64)), ("repetition", C.POINTER(C.c_float)), ("frequency", C.POINTER(C.c_float)),
+                ("presence", C.POINTER(C.c_float)), ("bias", C.c_void_p), ("bias_stride", C.c_int64), ("mask", C.c_void_p),
+                ("mask_stride", C.c_int64)]
+
+
+def host_i64(values):
+    """A host int64 array as the C calls take it (to be built once and passed to several calls); such an array is returned as it is."""
+    if isinstance(values, C.Array):
+        return values
+    return (C.c_int64 * max(len(values), 1))(*[int(v) for v in values])
+
+
+def kv4_array(caches):
+    """(array of spts_kv4, whether it is a copy): a ctypes array is passed on and its counts change in place, a list is copied."""
+    if isinstance(caches, C.Array):
+        return caches, False
+    return (spts_kv4 * max(len(caches), 1))(*caches), True
 
 
 _lib = None
@@ -107,6 +143,26 @@ def load() -> C.CDLL:
     lib.spts_channel_importance.argtypes = [vp, vp, i64, C.POINTER(spts_layer_weights), i64, vp]
     lib.spts_pack_slab32.restype = C.c_int
     lib.spts_pack_slab32.argtypes = [vp, vp, i64, i64, vp]
+    lib.spts_q4_bytes.restype = C.c_int
+    lib.spts_q4_bytes.argtypes = [i64, i64, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]
+    lib.spts_q4_pack.restype = C.c_int
+    lib.spts_q4_pack.argtypes = [vp, vp, C.POINTER(spts_q4)]
+    lib.spts_matvec_q4.restype = C.c_int
+    lib.spts_matvec_q4.argtypes = [vp, C.POINTER(spts_q4), vp, i32, vp, i32]
+    lib.spts_kv4_bytes.restype = C.c_int
+    lib.spts_kv4_bytes.argtypes = [C.POINTER(spts_model_desc), i64, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]
+    lib.spts_kv4_append.restype = C.c_int
+    lib.spts_kv4_append.argtypes = [vp, vp, vp, vp, C.POINTER(i64), i32, C.POINTER(spts_kv4)]
+    lib.spts_kv4_read.restype = C.c_int
+    lib.spts_kv4_read.argtypes = [vp, C.POINTER(spts_kv4), C.POINTER(i64), C.POINTER(i64), i32, vp, vp]
+    lib.spts_kv4_attn.restype = C.c_int
+    lib.spts_kv4_attn.argtypes = [vp, vp, i32, C.POINTER(spts_kv4), vp]
+    lib.spts_decode_layer_q4.restype = C.c_int
+    lib.spts_decode_layer_q4.argtypes = [vp, vp, C.POINTER(i32), i32, C.POINTER(spts_layer_q4), C.POINTER(spts_kv4)]
+    lib.spts_rmsnorm.restype = C.c_int
+    lib.spts_rmsnorm.argtypes = [vp, vp, vp, i32, vp]
+    lib.spts_process_logits.restype = C.c_int
+    lib.spts_process_logits.argtypes = [vp, vp, i32, i32, C.POINTER(spts_logits_rules), vp, vp, vp, vp]
     lib.spts_profile_begin.restype = C.c_int
     lib.spts_profile_begin.argtypes = [vp]
     lib.spts_profile_end.restype = C.c_int
@@ -159,6 +215,20 @@ def layer_weights(tensors: dict, r: int = 0, Dlow: int = 0, ud_orthonormal: bool
 
 def spts_workspace_bytes(model: spts_model_desc, max_tokens: int, max_probe: int, max_r: int, max_dlow: int) -> int:
     return int(load().spts_workspace_bytes(C.byref(model), max_tokens, max_probe, max_r, max_dlow))
+
+
+def spts_q4_bytes(rows: int, K: int):
+    """(code bytes, scale bytes) of a matrix [rows, K] in 4 bits."""
+    c, s = C.c_size_t(), C.c_size_t()
+    _check(load().spts_q4_bytes(rows, K, C.byref(c), C.byref(s)), "spts_q4_bytes")
+    return int(c.value), int(s.value)
+
+
+def spts_kv4_bytes(model: spts_model_desc, capacity: int):
+    """(code bytes, scale bytes) of one layer's keys, and of its values, in 4 bits."""
+    c, s = C.c_size_t(), C.c_size_t()
+    _check(load().spts_kv4_bytes(C.byref(model), capacity, C.byref(c), C.byref(s)), "spts_kv4_bytes")
+    return int(c.value), int(s.value)
 
 
 SPTS_TOPK_STATIC_MAX_N = 1048576
@@ -288,6 +358,48 @@ class Context:
 
     def spts_pack_slab32(self, W, rows: int, K: int, out):
         _check(load().spts_pack_slab32(self.handle, _ptr(W), rows, K, _ptr(out)), "spts_pack_slab32")
+
+    # ---- decode in 4 bits
+    def spts_q4_pack(self, W, out: spts_q4):
+        _check(load().spts_q4_pack(self.handle, _ptr(W), C.byref(out)), "spts_q4_pack")
+
+    def spts_matvec_q4(self, W: spts_q4, x, batch: int, y, y_f32: int = 0):
+        _check(load().spts_matvec_q4(self.handle, C.byref(W), _ptr(x), batch, _ptr(y), y_f32), "spts_matvec_q4")
+
+    def spts_kv4_append(self, k, v, pos, offsets, caches):
+        """offsets [batch+1]: host integers or binding.host_i64; caches: a list of spts_kv4 (count fields updated in place)
+        or a ctypes array of them."""
+        off = host_i64(offsets)
+        arr, copied = kv4_array(caches)
+        _check(load().spts_kv4_append(self.handle, _ptr(k), _ptr(v), _ptr(pos), off, len(caches), arr), "spts_kv4_append")
+        if copied:
+            for dst, src in zip(caches, arr):
+                dst.count = src.count
+
+    def spts_kv4_read(self, caches, offsets, k_out, v_out, first=None):
+        arr, _ = kv4_array(caches)
+        _check(load().spts_kv4_read(self.handle, arr, None if first is None else host_i64(first), host_i64(offsets), len(caches),
+                                    _ptr(k_out), _ptr(v_out)), "spts_kv4_read")
+
+    def spts_kv4_attn(self, q, caches, out):
+        arr, _ = kv4_array(caches)
+        _check(load().spts_kv4_attn(self.handle, _ptr(q), len(caches), arr, _ptr(out)), "spts_kv4_attn")
+
+    def spts_decode_layer_q4(self, x, pos, w: spts_layer_q4, caches):
+        """x [batch, D] device tensor; pos: host integers; caches as in spts_kv4_append."""
+        arr, copied = kv4_array(caches)
+        pa = pos if isinstance(pos, C.Array) else (C.c_int32 * max(len(pos), 1))(*[int(v) for v in pos])
+        _check(load().spts_decode_layer_q4(self.handle, _ptr(x), pa, len(caches), C.byref(w), arr), "spts_decode_layer_q4")
+        if copied:
+            for dst, src in zip(caches, arr):
+                dst.count = src.count
+
+    def spts_rmsnorm(self, x, gamma, batch: int, xn):
+        _check(load().spts_rmsnorm(self.handle, _ptr(x), _ptr(gamma), batch, _ptr(xn)), "spts_rmsnorm")
+
+    def spts_process_logits(self, logits, V: int, batch: int, rules: spts_logits_rules, logits_out, token_out=None, table=None, x_next=None):
+        _check(load().spts_process_logits(self.handle, _ptr(logits), V, batch, C.byref(rules), _ptr(logits_out), _ptr(token_out),
+                                          _ptr(table), _ptr(x_next)), "spts_process_logits")
 
     def spts_msdp_compact(self, x_in, pos_in, s_mha, N, N_next, protect_last, x_out, pos_out, map_new2old,
                           map_old2new=None):

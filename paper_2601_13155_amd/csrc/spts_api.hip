@@ -4,6 +4,7 @@
 #include "spts_internal.h"
 
 #include <algorithm>
+#include <cmath>
 #include <new>
 #include <vector>
 
@@ -97,8 +98,8 @@ struct spts_ctx {
     size_t ev_used = 0;
     struct Rec { int phase; hipEvent_t a, b; };
     std::vector<Rec> recs;
-    double phase_ms[32] = {};
-    int64_t phase_n[32] = {};
+    double phase_ms[64] = {};
+    int64_t phase_n[64] = {};
     template <typename T> T* p(size_t o) const { return reinterpret_cast<T*>(ws + o); }
 };
 
@@ -107,13 +108,15 @@ enum PhaseId {
     PH_ATTENTION, PH_O_PROJ, PH_PROXY_IN, PH_PROXY_MID, PH_PROXY_Z, PH_PROXY_OUT, PH_FFN_GATE_UP, PH_FFN_DOWN,
     PH_COMPACT, PH_DEC_NORM, PH_DEC_QKV, PH_DEC_ROPE_APPEND, PH_DEC_ATTN, PH_DEC_O, PH_DEC_GATE_UP, PH_DEC_DOWN, PH_DEC_HEAD,
     PH_BUILD_SALIENCY, PH_BUILD_TOPMEAN, PH_QV_PROJ, PH_KQV_PROJ,
+    PH_Q4_PACK, PH_Q4_MATVEC, PH_KV4_APPEND, PH_KV4_READ, PH_KV4_ATTN, PH_LOGITS_RULES,
     PH_COUNT
 };
 static const char* const kPhaseNames[PH_COUNT] = {
     "rmsnorm", "k_proj", "probe_q", "probe_attn", "topk", "gather", "q_proj", "v_proj",
     "attention", "o_proj", "proxy_in", "proxy_mid", "proxy_z", "proxy_out", "ffn_gate_up", "ffn_down", "compact",
     "dec_rmsnorm", "dec_qkv", "dec_rope_append", "dec_attention", "dec_o_proj", "dec_gate_up", "dec_down", "dec_head",
-    "build_saliency", "build_topmean", "qv_proj", "kqv_proj"};
+    "build_saliency", "build_topmean", "qv_proj", "kqv_proj",
+    "q4_pack", "q4_matvec", "kv4_append", "kv4_read", "kv4_attn", "logits_rules"};
 
 // Brackets the launches issued during its lifetime with two events when profiling is on.
 struct PhaseScope {
@@ -1293,6 +1296,266 @@ int spts_layer_prefill_batched(spts_ctx* c, void* x, const int32_t* pos, const i
     hidden_slab(c, gh, gd);
     { PHASE(c, PH_FFN_GATE_UP); SPTS_TRY(run_gemm(c, gh)); }
     { PHASE(c, PH_FFN_DOWN); SPTS_TRY(run_gemm(c, gd)); }
+    return SPTS_OK;
+}
+
+// ---- decode in 4 bits ---------------------------------------------------------------------------
+namespace {
+
+int check_q4(const spts_q4* w) {
+    if (!w || !w->codes || !w->scales || w->rows < 1 || w->K < 1) return SPTS_EINVAL;
+    if (!aligned16(w->codes) || !aligned16(w->scales)) return SPTS_EALIGN;
+    if (w->K % 8 != 0 || w->K > INT32_MAX || w->rows > INT32_MAX) return SPTS_ESHAPE;
+    return SPTS_OK;
+}
+
+bool kv4_shape_ok(const spts_model_desc& m) { return m.d == 32 || m.d == 64 || m.d == 128; }
+
+// the descriptor of a call's caches; rows: what is read or written of each starts there
+int kv4_batch(const spts_ctx* c, const spts_kv4* caches, int32_t batch, Kv4Batch* kb) {
+    if (!kv4_shape_ok(c->m)) return SPTS_ESHAPE;
+    kb->n = batch;
+    for (int b = 0; b < batch; ++b) {
+        const spts_kv4& k = caches[b];
+        if (!k.k || !k.v || !k.k_scale || !k.v_scale || !k.pos || k.capacity < 1 || k.count < 0 || k.count > k.capacity) return SPTS_EINVAL;
+        if (!aligned16(k.k) || !aligned16(k.v) || !aligned16(k.k_scale) || !aligned16(k.v_scale) || !aligned16(k.pos)) return SPTS_EALIGN;
+        if (k.capacity % 8 != 0) return SPTS_ESHAPE;
+        kb->k[b] = k.k; kb->v[b] = k.v; kb->ks[b] = k.k_scale; kb->vs[b] = k.v_scale; kb->pos[b] = k.pos;
+        kb->cap[b] = k.capacity; kb->count[b] = k.count;
+    }
+    return SPTS_OK;
+}
+
+int kv4_distinct(const spts_kv4* caches, int32_t batch) {
+    for (int b = 0; b < batch; ++b)
+        for (int o = 0; o < b; ++o)
+            if (caches[o].k == caches[b].k || caches[o].v == caches[b].v || caches[o].k_scale == caches[b].k_scale ||
+                caches[o].v_scale == caches[b].v_scale || caches[o].pos == caches[b].pos)
+                return SPTS_EINVAL;
+    return SPTS_OK;
+}
+
+int kv4_offsets(const int64_t* offsets, int32_t batch, Kv4Batch* kb) {
+    if (!offsets || offsets[0] != 0) return SPTS_EINVAL;
+    for (int b = 0; b < batch; ++b)
+        if (offsets[b + 1] < offsets[b]) return SPTS_EINVAL;
+    if (offsets[batch] > INT32_MAX) return SPTS_ESHAPE;
+    for (int b = 0; b <= batch; ++b) kb->off[b] = offsets[b];
+    return SPTS_OK;
+}
+
+}  // namespace
+
+int spts_q4_bytes(int64_t rows, int64_t K, size_t* code_bytes, size_t* scale_bytes) {
+    if (rows < 1 || K < 1 || !code_bytes || !scale_bytes) return SPTS_EINVAL;
+    if (K % 8 != 0 || K > INT32_MAX || rows > INT32_MAX) return SPTS_ESHAPE;
+    *code_bytes = (size_t)q4_code_bytes(rows, K);
+    *scale_bytes = (size_t)q4_scale_bytes(rows, K);
+    return SPTS_OK;
+}
+
+int spts_q4_pack(spts_ctx* c, const void* W, const spts_q4* out) {
+    if (!c || !W) return SPTS_EINVAL;
+    SPTS_TRY(check_q4(out));
+    if (!aligned16(W)) return SPTS_EALIGN;
+    PHASE(c, PH_Q4_PACK);
+    SPTS_HIP(c, launch_q4_pack(W, out->rows, out->K, out->codes, out->scales, c->bf16, c->stream));
+    return SPTS_OK;
+}
+
+int spts_matvec_q4(spts_ctx* c, const spts_q4* W, const void* x, int32_t batch, void* y, int32_t y_f32) {
+    if (!c || batch < 0 || batch > SPTS_MAX_DECODE_BATCH) return SPTS_EINVAL;
+    SPTS_TRY(check_q4(W));
+    if (batch == 0) return SPTS_OK;
+    if (!x || !y || x == y) return SPTS_EINVAL;
+    if (!aligned16(x) || !aligned16(y)) return SPTS_EALIGN;
+    Q4Args a{};
+    a.codes[0] = W->codes; a.scales[0] = W->scales; a.rows[0] = W->rows; a.y[0] = y;
+    a.x = x; a.K = W->K; a.nb = batch; a.mode = y_f32 ? Q4_F32 : Q4_STORE;
+    PHASE(c, PH_Q4_MATVEC);
+    SPTS_HIP(c, launch_q4_matvec(a, c->bf16, c->stream));
+    return SPTS_OK;
+}
+
+int spts_kv4_bytes(const spts_model_desc* model, int64_t capacity, size_t* code_bytes, size_t* scale_bytes) {
+    int st;
+    if (!model_ok(model, &st)) return st;
+    if (capacity < 1 || !code_bytes || !scale_bytes) return SPTS_EINVAL;
+    if (!kv4_shape_ok(*model) || capacity % 8 != 0) return SPTS_ESHAPE;
+    *code_bytes = (size_t)capacity * model->Hkv * (model->d / 2);
+    *scale_bytes = (size_t)capacity * model->Hkv * (model->d / 32);
+    return SPTS_OK;
+}
+
+int spts_kv4_append(spts_ctx* c, const void* k, const void* v, const int32_t* pos, const int64_t* offsets, int32_t batch,
+                    spts_kv4* caches) {
+    if (!c || batch < 0 || batch > SPTS_MAX_DECODE_BATCH) return SPTS_EINVAL;
+    if (batch == 0) return SPTS_OK;
+    if (!caches) return SPTS_EINVAL;
+    Kv4Batch kb{};
+    SPTS_TRY(kv4_batch(c, caches, batch, &kb));
+    SPTS_TRY(kv4_offsets(offsets, batch, &kb));
+    SPTS_TRY(kv4_distinct(caches, batch));
+    for (int b = 0; b < batch; ++b)
+        if (offsets[b + 1] - offsets[b] > kb.cap[b] - kb.count[b]) return SPTS_EINVAL;
+    if (offsets[batch] == 0) return SPTS_OK;
+    if (!k || !v || !pos) return SPTS_EINVAL;
+    if (!aligned16(k) || !aligned16(v) || !aligned16(pos)) return SPTS_EALIGN;
+    PHASE(c, PH_KV4_APPEND);
+    SPTS_HIP(c, launch_kv4_append(k, v, pos, kb, c->m.Hkv, c->m.d, c->bf16, c->stream));
+    for (int b = 0; b < batch; ++b) caches[b].count += offsets[b + 1] - offsets[b];
+    return SPTS_OK;
+}
+
+int spts_kv4_read(spts_ctx* c, const spts_kv4* caches, const int64_t* first, const int64_t* offsets, int32_t batch, void* k_out,
+                  void* v_out) {
+    if (!c || batch < 0 || batch > SPTS_MAX_DECODE_BATCH) return SPTS_EINVAL;
+    if (batch == 0) return SPTS_OK;
+    if (!caches) return SPTS_EINVAL;
+    Kv4Batch kb{};
+    SPTS_TRY(kv4_batch(c, caches, batch, &kb));
+    SPTS_TRY(kv4_offsets(offsets, batch, &kb));
+    for (int b = 0; b < batch; ++b) {
+        const int64_t at = first ? first[b] : 0;
+        if (at < 0 || at > kb.count[b] || offsets[b + 1] - offsets[b] > kb.count[b] - at) return SPTS_EINVAL;
+        kb.count[b] = at;
+    }
+    if (offsets[batch] == 0) return SPTS_OK;
+    if (!k_out || !v_out) return SPTS_EINVAL;
+    if (!aligned16(k_out) || !aligned16(v_out)) return SPTS_EALIGN;
+    PHASE(c, PH_KV4_READ);
+    SPTS_HIP(c, launch_kv4_read(kb, k_out, v_out, c->m.Hkv, c->m.d, c->bf16, c->stream));
+    return SPTS_OK;
+}
+
+int spts_kv4_attn(spts_ctx* c, const void* q, int32_t batch, const spts_kv4* caches, void* out) {
+    if (!c || batch < 0 || batch > SPTS_MAX_DECODE_BATCH) return SPTS_EINVAL;
+    if (batch == 0) return SPTS_OK;
+    if (!q || !caches || !out) return SPTS_EINVAL;
+    if (!aligned16(q) || !aligned16(out)) return SPTS_EALIGN;
+    const auto& m = c->m;
+    if (m.H / m.Hkv > KV4_MAX_GROUP) return SPTS_ESHAPE;
+    Kv4Batch kb{};
+    SPTS_TRY(kv4_batch(c, caches, batch, &kb));
+    PHASE(c, PH_KV4_ATTN);
+    SPTS_HIP(c, launch_kv4_attn(q, kb, m.H, m.Hkv, m.d, c->p<float>(c->off.tmp32), (c->off.qp - c->off.tmp32) / sizeof(float), out,
+                                c->bf16, c->stream));
+    return SPTS_OK;
+}
+
+int spts_rmsnorm(spts_ctx* c, const void* x, const void* gamma, int32_t batch, void* xn) {
+    if (!c || batch < 0 || batch > SPTS_MAX_DECODE_BATCH) return SPTS_EINVAL;
+    if (batch == 0) return SPTS_OK;
+    if (!x || !gamma || !xn) return SPTS_EINVAL;
+    if (!aligned16(x) || !aligned16(gamma) || !aligned16(xn)) return SPTS_EALIGN;
+    PHASE(c, PH_DEC_NORM);
+    SPTS_HIP(c, launch_rmsnorm(x, gamma, c->m.rms_eps, xn, batch, c->m.D, c->bf16, c->stream));
+    return SPTS_OK;
+}
+
+int spts_decode_layer_q4(spts_ctx* c, void* x, const int32_t* pos, int32_t batch, const spts_layer_q4* w, spts_kv4* caches) {
+    if (!c || batch < 0 || batch > SPTS_MAX_DECODE_BATCH) return SPTS_EINVAL;
+    if (batch == 0) return SPTS_OK;
+    if (!x || !pos || !w || !caches || !w->gamma1 || !w->gamma2) return SPTS_EINVAL;
+    if (!aligned16(x) || !aligned16(w->gamma1) || !aligned16(w->gamma2)) return SPTS_EALIGN;
+    const auto& m = c->m;
+    const int64_t QD = (int64_t)m.H * m.d, KV = (int64_t)m.Hkv * m.d;
+    const struct { const spts_q4* w; int64_t rows, K; } want[7] = {{&w->Wq, QD, m.D}, {&w->Wk, KV, m.D}, {&w->Wv, KV, m.D}, {&w->Wo, m.D, QD},
+                                                                  {&w->Wgate, m.Dff, m.D}, {&w->Wup, m.Dff, m.D}, {&w->Wdown, m.D, m.Dff}};
+    for (const auto& e : want) {
+        SPTS_TRY(check_q4(e.w));
+        if (e.w->rows != e.rows || e.w->K != e.K) return SPTS_ESHAPE;
+    }
+    if (m.H / m.Hkv > KV4_MAX_GROUP) return SPTS_ESHAPE;
+    if (batch > c->lim.max_tokens) return SPTS_EWORKSPACE;
+    Kv4Batch kb{};
+    SPTS_TRY(kv4_batch(c, caches, batch, &kb));
+    SPTS_TRY(kv4_distinct(caches, batch));
+    for (int b = 0; b < batch; ++b)
+        if (pos[b] < 0 || kb.count[b] >= kb.cap[b]) return SPTS_EINVAL;
+    // the projections' fp32 sums, in the FFN's hidden buffer (free until gate/up)
+    if ((size_t)batch * (QD + 2 * KV) * sizeof(float) > c->off.misc - c->off.big) return SPTS_EWORKSPACE;
+    float* q32 = c->p<float>(c->off.big);
+    float* k32 = q32 + batch * QD;
+    float* v32 = k32 + batch * KV;
+    void* xn = c->p<void>(c->off.xn);
+    void* q = c->p<void>(c->off.q);
+    void* att = c->p<void>(c->off.att);
+    void* hbuf = c->p<void>(c->off.big);
+    const size_t eb = c->bf16 ? 2 : 4;
+    hipStream_t st = c->stream;
+    auto args = [&](const spts_q4& a, const void* in, void* out, int mode) {
+        Q4Args g{};
+        g.codes[0] = a.codes; g.scales[0] = a.scales; g.rows[0] = a.rows; g.y[0] = out; g.x = in; g.K = a.K; g.nb = batch; g.mode = mode;
+        return g;
+    };
+    auto also = [](Q4Args& g, int i, const spts_q4& a, void* out) { g.codes[i] = a.codes; g.scales[i] = a.scales; g.rows[i] = a.rows; g.y[i] = out; };
+    { PHASE(c, PH_DEC_NORM); SPTS_HIP(c, launch_rmsnorm(x, w->gamma1, m.rms_eps, xn, batch, m.D, c->bf16, st)); }
+    Q4Args qkv = args(w->Wq, xn, q32, Q4_F32);
+    also(qkv, 1, w->Wk, k32);
+    also(qkv, 2, w->Wv, v32);
+    { PHASE(c, PH_DEC_QKV); SPTS_HIP(c, launch_q4_matvec(qkv, c->bf16, st)); }
+    {   // the new pairs, rotated and rounded to the element type, as rows of one each, then into the caches
+        PHASE(c, PH_DEC_ROPE_APPEND);
+        DecodeBatch db{};
+        db.n = batch;
+        for (int b = 0; b < batch; ++b) {
+            db.cache_k[b] = c->p<char>(c->off.khat) + b * KV * eb; db.cache_v[b] = c->p<char>(c->off.vhat) + b * KV * eb;
+            db.cache_pos[b] = c->p<int32_t>(c->off.posA) + b; db.pos[b] = pos[b];
+            kb.off[b + 1] = b + 1;
+        }
+        SPTS_HIP(c, launch_decode_rope_append_batched(q32, k32, v32, q, m.H, m.Hkv, m.d, m.rope_base, db, c->bf16, st));
+        SPTS_HIP(c, launch_kv4_append(c->p<void>(c->off.khat), c->p<void>(c->off.vhat), c->p<int32_t>(c->off.posA), kb, m.Hkv, m.d, c->bf16, st));
+    }
+    for (int b = 0; b < batch; ++b) kb.count[b] += 1;
+    { PHASE(c, PH_DEC_ATTN);
+      SPTS_HIP(c, launch_kv4_attn(q, kb, m.H, m.Hkv, m.d, c->p<float>(c->off.tmp32), (c->off.qp - c->off.tmp32) / sizeof(float), att, c->bf16, st)); }
+    { PHASE(c, PH_DEC_O); SPTS_HIP(c, launch_q4_matvec(args(w->Wo, att, x, Q4_RESID), c->bf16, st)); }
+    { PHASE(c, PH_DEC_NORM); SPTS_HIP(c, launch_rmsnorm(x, w->gamma2, m.rms_eps, xn, batch, m.D, c->bf16, st)); }
+    Q4Args gu = args(w->Wgate, xn, hbuf, Q4_SILU);
+    also(gu, 1, w->Wup, nullptr);
+    { PHASE(c, PH_DEC_GATE_UP); SPTS_HIP(c, launch_q4_matvec(gu, c->bf16, st)); }
+    { PHASE(c, PH_DEC_DOWN); SPTS_HIP(c, launch_q4_matvec(args(w->Wdown, hbuf, x, Q4_RESID), c->bf16, st)); }
+    for (int b = 0; b < batch; ++b) caches[b].count += 1;
+    return SPTS_OK;
+}
+
+int spts_process_logits(spts_ctx* c, const float* logits, int32_t V, int32_t batch, const spts_logits_rules* rules, float* logits_out,
+                        int32_t* token_out, const void* table, void* x_next) {
+    if (!c || V < 1 || batch < 0 || batch > SPTS_MAX_DECODE_BATCH || !rules) return SPTS_EINVAL;
+    if (batch == 0) return SPTS_OK;
+    if (!logits || !logits_out || (x_next && (!token_out || !table))) return SPTS_EINVAL;
+    if (!aligned16(logits) || !aligned16(logits_out) || (token_out && !aligned16(token_out)) || (x_next && (!aligned16(x_next) || !aligned16(table))))
+        return SPTS_EALIGN;
+    LogitsRules r{};
+    if (rules->history) {
+        if (!rules->history_len || rules->history_stride < 0) return SPTS_EINVAL;
+        if (!aligned16(rules->history)) return SPTS_EALIGN;
+        r.history = rules->history; r.history_stride = rules->history_stride;
+    }
+    if (rules->bias) {
+        if (rules->bias_stride != 0 && rules->bias_stride < V) return SPTS_EINVAL;
+        if (!aligned16(rules->bias)) return SPTS_EALIGN;
+        r.bias = rules->bias; r.bias_stride = rules->bias_stride;
+    }
+    if (rules->mask) {
+        if (rules->mask_stride != 0 && rules->mask_stride < ((int64_t)V + 31) / 32) return SPTS_EINVAL;
+        if (!aligned16(rules->mask)) return SPTS_EALIGN;
+        r.mask = rules->mask; r.mask_stride = rules->mask_stride;
+    }
+    for (int b = 0; b < batch; ++b) {
+        r.repetition[b] = rules->repetition ? rules->repetition[b] : 1.f;
+        r.frequency[b] = rules->frequency ? rules->frequency[b] : 0.f;
+        r.presence[b] = rules->presence ? rules->presence[b] : 0.f;
+        if (!(r.repetition[b] > 0.f) || !std::isfinite(r.repetition[b]) || !std::isfinite(r.frequency[b]) || !std::isfinite(r.presence[b])) return SPTS_EINVAL;
+        if (!r.history) continue;
+        r.len[b] = rules->history_len[b];
+        r.prompt[b] = rules->prompt_len ? rules->prompt_len[b] : 0;
+        if (r.len[b] < 0 || r.len[b] > INT32_MAX || r.prompt[b] < 0 || (batch > 1 && r.len[b] > r.history_stride)) return SPTS_EINVAL;
+    }
+    if (token_out && logits_scratch_bytes(V, batch) > c->off.qp - c->off.tmp32) return SPTS_EWORKSPACE;
+    PHASE(c, PH_LOGITS_RULES);
+    SPTS_HIP(c, launch_process_logits(logits, V, batch, r, logits_out, token_out, table, c->m.D, x_next, c->bf16, c->p<void>(c->off.tmp32), c->stream));
     return SPTS_OK;
 }
 

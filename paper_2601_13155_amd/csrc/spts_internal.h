@@ -334,4 +334,53 @@ constexpr size_t ARGMAX_SCRATCH_BYTES = 4096;
 hipError_t launch_argmax_rows(const float* logits, int V, int nrows, int32_t* token, const void* table, int D, void* x_next, bool bf16,
                               void* scratch, hipStream_t s);
 
+// ------------------------------------------------------------------ 4-bit matrices (spts_fp4.h has the form of the values)
+// Layout of a matrix [rows, K]: strips of 16 rows, each a sequence of 512-wide slabs of K (zeros beyond the matrix).  A slab is 4 tiles of 16 rows x
+// 128 k; a tile is 64 pieces of 16 bytes, piece 16 (k % 128 / 32) + row % 16 holding one block of 32 values, so that a wavefront's 16-byte load is a
+// tile and a lane holds one block of one row.  Scales: [strip][slab][piece][tile], four bytes a lane.
+constexpr int Q4_SLAB = 512;
+inline int64_t q4_slabs(int64_t K) { return (K + Q4_SLAB - 1) / Q4_SLAB; }
+inline int64_t q4_code_bytes(int64_t rows, int64_t K) { return (rows + 15) / 16 * q4_slabs(K) * 4096; }
+inline int64_t q4_scale_bytes(int64_t rows, int64_t K) { return (rows + 15) / 16 * q4_slabs(K) * 256; }
+hipError_t launch_q4_pack(const void* W, int64_t rows, int64_t K, void* codes, void* scales, bool bf16, hipStream_t s);
+enum Q4Mode : int {
+    Q4_STORE = 0,   // y[b, r] = W[r,:] . x[b,:]        (the element type)
+    Q4_F32 = 1,     // the same in fp32
+    Q4_RESID = 2,   // y[b, r] += W[r,:] . x[b,:]       (the element type)
+    Q4_SILU = 3,    // y[b, r] = silu(W0[r,:] . x[b,:]) * (W1[r,:] . x[b,:])
+};
+// Up to three packed matrices of row length K that share the vectors x [nb, K]; y[i] [nb, rows[i]].  Q4_SILU: two matrices of rows[0] rows, y[0].
+struct Q4Args {
+    const void* codes[3]; const void* scales[3]; void* y[3]; int64_t rows[3];
+    const void* x; int64_t K; int nb; int mode;
+};
+hipError_t launch_q4_matvec(const Q4Args& a, bool bf16, hipStream_t s);
+
+// ------------------------------------------------------------------ 4-bit caches
+// Of one layer and sequence, by key/value head and key (cap = capacity, a multiple of 8): keys [Hkv][cap][d / 2] bytes, blocks of 32 along d, scales
+// [Hkv][cap][d / 32]; values [Hkv][cap / 8][16][8][d / 32], i.e. of eight consecutive keys the d / 16 values that one lane multiplies, scales
+// [Hkv][cap / 8][d / 32][8].
+constexpr int KV4_MAX_GROUP = 16;   // query heads per key/value head
+struct Kv4Batch {
+    void* k[DECODE_MAX_BATCH]; void* v[DECODE_MAX_BATCH]; void* ks[DECODE_MAX_BATCH]; void* vs[DECODE_MAX_BATCH]; int32_t* pos[DECODE_MAX_BATCH];
+    int64_t cap[DECODE_MAX_BATCH]; int64_t count[DECODE_MAX_BATCH]; int64_t off[DECODE_MAX_BATCH + 1]; int32_t n;
+};
+// rows off[b] .. off[b + 1] of k, v [.., Hkv, d] and pos into rows count[b] .. of cache b; and back
+hipError_t launch_kv4_append(const void* k, const void* v, const int32_t* pos, const Kv4Batch& kb, int Hkv, int d, bool bf16, hipStream_t s);
+hipError_t launch_kv4_read(const Kv4Batch& kb, void* k, void* v, int Hkv, int d, bool bf16, hipStream_t s);
+// out [n, H, d] = softmax(q k^T / sqrt(d)) v over the first count[b] pairs of cache b (zeros where count is 0); part: fp32 scratch
+hipError_t launch_kv4_attn(const void* q, const Kv4Batch& kb, int H, int Hkv, int d, float* part, size_t part_floats, void* out, bool bf16, hipStream_t s);
+
+// ------------------------------------------------------------------ rules on logits
+struct LogitsRules {
+    const int32_t* history; int64_t history_stride; const float* bias; int64_t bias_stride; const uint32_t* mask; int64_t mask_stride;
+    int64_t len[DECODE_MAX_BATCH]; int64_t prompt[DECODE_MAX_BATCH];
+    float repetition[DECODE_MAX_BATCH], frequency[DECODE_MAX_BATCH], presence[DECODE_MAX_BATCH];
+};
+// token (may be NULL, and x_next with it): scratch of LOGITS_SCRATCH_BYTES
+constexpr int LOGITS_TILE = 4096;
+size_t logits_scratch_bytes(int V, int nrows);
+hipError_t launch_process_logits(const float* in, int V, int nrows, const LogitsRules& r, float* out, int32_t* token, const void* table, int D,
+                                 void* x_next, bool bf16, void* scratch, hipStream_t s);
+
 }  // namespace spts

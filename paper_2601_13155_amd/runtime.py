@@ -205,6 +205,160 @@ class BatchedDecodeRunner:
             self.x.copy_(self.x_next)
 
 
+# ------------------------------------------------------------------------------------------- decode in 4 bits
+class Q4Matrix:
+    """A matrix [rows, K] packed into 4 bits (spts_q4_pack); W: device tensor of the context's element type."""
+
+    def __init__(self, ctx: binding.Context, W):
+        torch = _torch()
+        rows, K = (int(n) for n in W.shape)
+        cb, sb = binding.spts_q4_bytes(rows, K)
+        self.codes = torch.empty(cb, dtype=torch.uint8, device=W.device)
+        self.scales = torch.empty(sb, dtype=torch.uint8, device=W.device)
+        self.struct = binding.spts_q4(self.codes.data_ptr(), self.scales.data_ptr(), rows, K)
+        ctx.spts_q4_pack(W.contiguous(), self.struct)
+
+
+def pack_layer_q4(ctx: binding.Context, w: binding.spts_layer_weights) -> binding.spts_layer_q4:
+    """The 4-bit form of a layer that upload_layer has put on the device (gains are shared with it, not copied)."""
+    t, out = w._keepalive, binding.spts_layer_q4()
+    out._keepalive = {n: Q4Matrix(ctx, t[n]) for n in ("Wq", "Wk", "Wv", "Wo", "Wgate", "Wup", "Wdown")}
+    for n, m in out._keepalive.items():
+        setattr(out, n, m.struct)
+    out.gamma1, out.gamma2 = t["gamma1"].data_ptr(), t["gamma2"].data_ptr()
+    out._keepalive.update(gamma1=t["gamma1"], gamma2=t["gamma2"])
+    return out
+
+
+class KV4Batch:
+    """One layer's caches of several sequences in 4 bits; capacities are rounded up to a multiple of 8.  `structs` is what
+    the calls take (a ctypes array of spts_kv4, its counts kept up to date by them)."""
+
+    def __init__(self, shape, capacities):
+        torch = _torch()
+        m = binding.model_desc(shape)
+        self.structs = (binding.spts_kv4 * len(capacities))()
+        self.tensors = []
+        for s, cap in zip(self.structs, capacities):
+            cap = max(8, (int(cap) + 7) // 8 * 8)
+            cb, sb = binding.spts_kv4_bytes(m, cap)
+            t = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in (cb, cb, sb, sb)] + [torch.empty(cap, dtype=torch.int32, device="cuda")]
+            self.tensors.append(t)
+            s.k, s.v, s.k_scale, s.v_scale, s.pos = (x.data_ptr() for x in t)
+            s.capacity = cap
+
+    @property
+    def counts(self) -> List[int]:
+        return [int(s.count) for s in self.structs]
+
+    def clear(self):
+        for s in self.structs:
+            s.count = 0
+
+    def append_cache(self, ctx: binding.Context, b: int, cache: "KVCache"):
+        """Appends every pair of a prefill's cache to sequence b's."""
+        one = [self.structs[b]]
+        ctx.spts_kv4_append(cache.k, cache.v, cache.pos, [0, cache.count], one)
+        self.structs[b].count = one[0].count
+
+    def host(self, ctx: binding.Context, shape, b: int):
+        """(k, v, pos) that sequence b's filled rows stand for, as host arrays (fp64 / int32)."""
+        torch = _torch()
+        n = self.counts[b]
+        k = torch.empty((max(n, 1), shape.Hkv, shape.d), dtype=torch.bfloat16 if shape.dtype == "bf16" else torch.float32, device="cuda")
+        v = torch.empty_like(k)
+        ctx.spts_kv4_read([self.structs[b]], [0, n], k, v)
+        return to_host(k[:n]).astype(np.float64), to_host(v[:n]).astype(np.float64), self.tensors[b][4][:n].cpu().numpy()
+
+
+class LogitsRules:
+    """spts_logits_rules for a batch of sequences.  history, bias, mask: device tensors (int32 [batch, n], fp32 and int32 of one
+    row or one per sequence); the rest: host sequences of one value per sequence.  history_len and prompt_len may be
+    changed between calls through the arrays of the same name."""
+
+    def __init__(self, batch: int, history=None, history_len=None, prompt_len=None, repetition=None, frequency=None, presence=None,
+                 bias=None, mask=None):
+        import ctypes as C
+        self.struct = s = binding.spts_logits_rules()
+        self._keepalive = (history, bias, mask)
+
+        def host(values, typ):
+            if values is None:
+                return None
+            if len(values) != batch:
+                raise ValueError(f"one value per sequence: got {len(values)} for a batch of {batch}")
+            return (typ * batch)(*values)
+
+        def rows(t):
+            if t.dim() not in (1, 2) or not t.is_contiguous() or (t.dim() == 2 and t.shape[0] not in (1, batch)):
+                raise ValueError("bias and mask: one contiguous row, or one per sequence")
+            return t.data_ptr(), 0 if t.dim() == 1 or t.shape[0] == 1 else t.shape[1]
+
+        if history is not None:
+            if history.dim() != 2 or history.shape[0] != batch or not history.is_contiguous() or history_len is None:
+                raise ValueError("history: a contiguous [batch, n] tensor, with history_len")
+            if any(n > history.shape[1] for n in history_len):
+                raise ValueError("history_len exceeds the history's rows")
+            s.history, s.history_stride = history.data_ptr(), history.shape[1]
+        self.history_len, self.prompt_len = host(history_len, C.c_int64), host(prompt_len, C.c_int64)
+        self.repetition, self.frequency, self.presence = (host(v, C.c_float) for v in (repetition, frequency, presence))
+        for name in ("history_len", "prompt_len", "repetition", "frequency", "presence"):
+            if getattr(self, name) is not None:
+                setattr(s, name, getattr(self, name))
+        if bias is not None:
+            s.bias, s.bias_stride = rows(bias)
+        if mask is not None:
+            s.mask, s.mask_stride = rows(mask)
+
+
+class Q4DecodeRunner:
+    """Decode phase with weights and caches in 4 bits for a batch of sequences: per step one spts_decode_layer_q4 per layer,
+    the final norm, the head's 4-bit matrix and spts_process_logits.  Only enqueues work; tokens stay on the device.
+
+    caches: one KV4Batch per layer; table [V, D]: the embedding (element type); head: its 4-bit form or another
+    output matrix's; rules: LogitsRules, whose history the runner extends by the tokens it decodes (None = plain argmax)."""
+
+    def __init__(self, ctx: binding.Context, shape, layers: List[binding.spts_layer_q4], caches: List[KV4Batch], gamma_f, table,
+                 head: Q4Matrix, rules: Optional[LogitsRules] = None):
+        torch = _torch()
+        self.ctx, self.shape, self.layers, self.caches = ctx, shape, layers, caches
+        self.gamma_f, self.table, self.head = gamma_f, table, head
+        self.batch = len(caches[0].structs)
+        self.rules = rules if rules is not None else LogitsRules(self.batch)
+        tdt = torch.bfloat16 if shape.dtype == "bf16" else torch.float32
+        self.x = torch.zeros((self.batch, shape.D), dtype=tdt, device="cuda")
+        self.x_next, self.xn = torch.zeros_like(self.x), torch.zeros_like(self.x)
+        self.tokens = torch.zeros(self.batch, dtype=torch.int32, device="cuda")
+        self.logits = torch.zeros((self.batch, int(table.shape[0])), dtype=torch.float32, device="cuda")
+
+    def step(self, pos):
+        """Runs self.x (in place) through every layer as the tokens at the host positions pos."""
+        for w, c in zip(self.layers, self.caches):
+            self.ctx.spts_decode_layer_q4(self.x, pos, w, c.structs)
+
+    def next_token(self):
+        """self.tokens and self.x_next from self.x: final norm, logits, rules, argmax, table row."""
+        V = int(self.table.shape[0])
+        self.ctx.spts_rmsnorm(self.x, self.gamma_f, self.batch, self.xn)
+        self.ctx.spts_matvec_q4(self.head.struct, self.xn, self.batch, self.logits, 1)
+        self.ctx.spts_process_logits(self.logits, V, self.batch, self.rules.struct, self.logits, self.tokens, self.table, self.x_next)
+
+    def generate(self, pos0: List[int], steps: int, tokens_out=None):
+        """steps decode steps from self.x at positions pos0; tokens_out [batch, steps] int32 device.  With a history in the
+        rules every token joins it (SPTS_EINVAL from the call once a row is full)."""
+        hist, lens = self.rules._keepalive[0], self.rules.history_len
+        for t in range(steps):
+            self.step([p + t for p in pos0])
+            self.next_token()
+            if hist is not None:
+                for b in range(self.batch):
+                    hist[b, lens[b]:lens[b] + 1].copy_(self.tokens[b:b + 1])
+                    lens[b] += 1
+            if tokens_out is not None:
+                tokens_out[:, t].copy_(self.tokens)
+            self.x.copy_(self.x_next)
+
+
 class StackRunner:
     """Runs Alg. 1's outer loop on the GPU: per layer one spts_layer_prefill, at stage ends one
     spts_msdp_compact.  Buffers are allocated once; run() only enqueues work (no host sync)."""
