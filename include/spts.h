@@ -316,7 +316,7 @@ int spts_matvec_q4(spts_ctx *ctx, const spts_q4 *W, const void *x, int32_t batch
 /* KV cache of one layer and sequence in 4 bits: post-rotary keys and values of the context's Hkv heads of d dimensions
  * (d = 32, 64 or 128: SPTS_ESHAPE otherwise), blocks along d.  Device buffers of the sizes that spts_kv4_bytes gives
  * (k and v: code_bytes each, k_scale and v_scale: scale_bytes each; 16-byte aligned), pos [capacity] int32; capacity a
- * multiple of 8.  count lives on the host, as in spts_kv_out.  What lies behind the first count rows is never read as a
+ * multiple of 8 below 2^31.  count lives on the host, as in spts_kv_out.  What lies behind the first count rows is never read as a
  * value: the buffers need no initialisation. */
 typedef struct {
     void *k, *v, *k_scale, *v_scale;

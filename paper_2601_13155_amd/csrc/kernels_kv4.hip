@@ -1,6 +1,8 @@
 // Caches in 4 bits: appending pairs, reading them back, and the attention of one query per sequence over them.
 #include "spts_fp4.h"
 
+#include <type_traits>
+
 namespace spts {
 
 namespace {
@@ -96,60 +98,318 @@ hipError_t launch_kv4_read(const Kv4Batch& kb, void* k, void* v, int Hkv, int d,
     return hipGetLastError();
 }
 
-// One workgroup per query head and sequence, 256 keys at a time with the running maximum and sum: a thread takes a key's score, then a thread takes
-// a dimension of the weighted values.
-template <typename T>
-__global__ void __launch_bounds__(256) kv4_attn_kernel(const T* __restrict__ q, Kv4Batch kb, int H, int Hkv, int d, float scale_log2e, T* __restrict__ out) {
-    __shared__ float sp[256], sq[128], red[4];
-    const int h = blockIdx.x, b = blockIdx.y, g = h / (H / Hkv), tid = threadIdx.x;
-    const int64_t n = kb.count[b], cap = kb.cap[b];
-    if (tid < d) sq[tid] = to_f32(q[((int64_t)b * H + h) * d + tid]);
-    float m = -INFINITY, l = 0.f, o = 0.f;
-    for (int64_t k0 = 0; k0 < n; k0 += 256) {
-        __syncthreads();
-        float s = -INFINITY;
-        if (k0 + tid < n) {
-            s = 0.f;
-            for (int c = 0; c < d / 8; ++c) {
-                float f[8];
-                const uint32_t w = *reinterpret_cast<const uint32_t*>((const char*)kb.k[b] + key_at(g, cap, k0 + tid, d) + c * 4);
-                fp4_decode8(w, __uint_as_float((uint32_t)((const uint8_t*)kb.ks[b])[key_scale_at(g, cap, k0 + tid, c / 4, d)] << 23), f);
-                for (int j = 0; j < 8; ++j) s = fmaf(f[j], sq[c * 8 + j], s);
+// ------------------------------------------------------------------------------------------------- attention
+typedef __bf16 mfma_bf16x8 __attribute__((ext_vector_type(8)));
+typedef float mfma_f32x4 __attribute__((ext_vector_type(4)));
+
+__device__ inline mfma_f32x4 mfma16(u32x4 a, u32x4 b, mfma_f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(mfma_bf16x8, a), __builtin_bit_cast(mfma_bf16x8, b), c, 0, 0, 0);
+}
+
+// eight fp32 values as N bf16 vectors whose sum they are (to 8 N bits)
+template <int N>
+__device__ inline void bf16_parts(const float* v, u32x4 (&out)[N]) {
+    float r[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r[j] = v[j];
+#pragma unroll
+    for (int p = 0; p < N; ++p)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t w = cvt_pk_bf16(r[2 * j], r[2 * j + 1]);
+            out[p][j] = w;
+            if (p + 1 < N) {
+                r[2 * j] -= __uint_as_float(w << 16);
+                r[2 * j + 1] -= __uint_as_float(w & 0xffff0000u);
             }
-            s *= scale_log2e;
         }
-        float mx = s;
-        for (int off = 32; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor(mx, off));
-        if ((tid & 63) == 0) red[tid >> 6] = mx;
-        __syncthreads();
-        const float mn = fmaxf(m, fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
-        const float alpha = exp2f(m - mn);
-        m = mn;
-        sp[tid] = exp2f(s - mn);
-        __syncthreads();
-        l *= alpha;
-        o *= alpha;
-        const int64_t left = n - k0 < 256 ? n - k0 : 256;
-        for (int j = 0; j < left; ++j) {
-            l += sp[j];
-            if (tid < d) {
-                const int per = d / 16;   // values of a piece
-                const uint8_t byte = ((const uint8_t*)kb.v[b])[value_at(g, cap, k0 + j, tid / per, d) + tid % per / 2];
-                const fp4_f32x2 f = fp4_pair<0>(byte, __uint_as_float((uint32_t)((const uint8_t*)kb.vs[b])[value_scale_at(g, cap, k0 + j, tid / 32, d)] << 23));
-                o = fmaf(sp[j], f[tid & 1], o);
+}
+
+// W dwords from p
+template <int W> __device__ inline void load_words(const char* p, uint32_t (&w)[W]) {
+    if constexpr (W == 8) {
+        const u32x4 a = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)), b = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p) + 1);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { w[i] = a[i]; w[4 + i] = b[i]; }
+    } else if constexpr (W == 4) {
+        const u32x4 a = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = a[i];
+    } else if constexpr (W == 2) {
+        const u32x2 a = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p));
+        w[0] = a[0]; w[1] = a[1];
+    } else {
+        w[0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(p));
+    }
+}
+
+// pair I (two dimensions) of key J in a lane's piece of values: D / 32 bytes a key, eight keys
+template <int D, int J, int I> __device__ inline uint32_t value_pair(const uint32_t* w, float scale) {
+    constexpr int byte = J * (D / 32) + I;
+    return fp4_pair_bf16<byte % 4>(w[byte / 4], scale);
+}
+
+struct Kv4Splits { int32_t first[DECODE_MAX_BATCH + 1]; int32_t per; };   // splits of sequence b: first[b] .. first[b + 1], of `per` keys (a multiple of 32)
+
+// what one lane needs of 32 keys
+template <int D> struct Kv4Step {
+    uint32_t k[2][D / 32], v[D / 16], vs[2];
+    uint32_t ks[2];
+};
+
+// One workgroup of four wavefronts per split of a sequence's keys and key/value head; a wavefront takes 32 keys at a time with its own running maximum
+// and sum, all query heads of the head at once on the matrix cores:
+//   S^T = K Q^T: a key is an operand row (lane l16 = key, lane group kg = a quarter of the dimensions, one stored block), a query head a column.
+//     Of the two products of 16 keys, operand row m of product t is key 8 (m / 4) + 4 t + m % 4: lane group kg then holds the scores of the keys 8 kg .. 8 kg + 7.
+//   O^T = V^T P^T: these eight scores are already the second operand's eight values of the lane, no exchange needed; the first needs eight keys of one dimension in
+//     a lane, which is how the values are stored (piece n of eight keys: D / 16 dimensions): decoding gives pairs of dimensions, two byte permutes pairs of keys.
+//   In both results a column, i.e. lane % 16, is a query head, so the running maximum, the sum and the rescaling are the lane's own.
+// The maximum moves only when a score is 2^8 times above it (the sums stand that easily), so most steps have no rescaling.
+template <typename T, int D>
+__global__ void __launch_bounds__(256, 2) kv4_attn_kernel(const T* __restrict__ q, Kv4Batch kb, Kv4Splits sp, int H, int Hkv, float scale_log2e, float* __restrict__ part,
+                                                          T* __restrict__ out) {
+    constexpr bool F32 = sizeof(T) == 4;
+    constexpr int NP = F32 ? 3 : 1;                       // bf16 parts of a query or weight
+    constexpr int KW = D / 32, VM = D / 16, LD = D + 4;
+    __shared__ float so[4][16][LD];
+    __shared__ float sml[4][16][2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, kg = lane >> 4;
+    const int g = blockIdx.y, grp = H / Hkv;
+    int b = 0;
+    while (b + 1 < kb.n && (int)blockIdx.x >= sp.first[b + 1]) ++b;
+    const int ns = sp.first[b + 1] - sp.first[b], split = (int)blockIdx.x - sp.first[b];
+    const int64_t n = kb.count[b], cap = kb.cap[b], m0 = (int64_t)split * sp.per, m1 = m0 + sp.per < n ? m0 + sp.per : n;
+
+    // the queries, columns beyond the group zero
+    u32x4 qf[NP][KW];
+    {
+        const T* qh = q + ((int64_t)b * H + g * grp + (l16 < grp ? l16 : 0)) * D + kg * (D / 4);
+#pragma unroll
+        for (int i = 0; i < KW; ++i) {
+            if constexpr (F32) {
+                float v[8];
+                u32x4 parts[NP];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = l16 < grp ? qh[8 * i + j] : 0.f;
+                bf16_parts<NP>(v, parts);
+#pragma unroll
+                for (int p = 0; p < NP; ++p) qf[p][i] = parts[p];
+            } else {
+                qf[0][i] = l16 < grp ? *reinterpret_cast<const u32x4*>(qh + 8 * i) : u32x4{0, 0, 0, 0};
             }
         }
     }
-    if (tid < d) out[((int64_t)b * H + h) * d + tid] = from_f32<T>(n > 0 ? o / l : 0.f);
+    // a head's rows; a lane's offsets within 32 keys
+    const char* const kh = (const char*)kb.k[b] + (int64_t)g * cap * (D / 2);
+    const char* const vh = (const char*)kb.v[b] + (int64_t)g * cap * (D / 2);
+    const uint8_t* const ksh = (const uint8_t*)kb.ks[b] + (int64_t)g * cap * (D / 32);
+    const uint8_t* const vsh = (const uint8_t*)kb.vs[b] + (int64_t)g * cap * (D / 32);
+    const int kblk = kg * (D / 4) / 32, vblk = l16 * (D / 16) / 32;
+    int krow[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) krow[t] = 8 * (l16 >> 2) + 4 * t + (l16 & 3);
+
+    // keys from key0 on (a multiple of 32, below m1); rows at and beyond n are not read
+    auto load = [&](int64_t key0, Kv4Step<D>& s) {
+        const int left = (int)(n - key0 < 32 ? n - key0 : 32);
+        const char* kp = kh + key0 * (D / 2);
+        const uint8_t* ksp = ksh + key0 * (D / 32);
+        const char* vp = vh + key0 * (D / 2);
+        const uint8_t* vsp = vsh + key0 * (D / 32);
+        int row[2] = {krow[0], krow[1]}, grp8 = kg;
+        if (left < 32) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) row[t] = row[t] < left ? row[t] : left - 1;
+            grp8 = grp8 < (left + 7) / 8 ? grp8 : (left - 1) / 8;
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            load_words<KW>(kp + (uint32_t)(row[t] * (D / 2) + kg * (D / 8)), s.k[t]);
+            s.ks[t] = ksp[(uint32_t)(row[t] * (D / 32) + kblk)];
+        }
+        load_words<D / 16>(vp + (uint32_t)((grp8 * 16 + l16) * (D / 4)), s.v);
+        load_words<2>((const char*)vsp + (uint32_t)((grp8 * (D / 32) + vblk) * 8), s.vs);
+    };
+
+    float m = -INFINITY, l = 0.f;
+    mfma_f32x4 acc[VM];
+#pragma unroll
+    for (int i = 0; i < VM; ++i) acc[i] = mfma_f32x4{0.f, 0.f, 0.f, 0.f};
+    Kv4Step<D> next;
+    int64_t key0 = m0 + wave * 32;
+    if (key0 < m1) load(key0, next);
+    for (; key0 < m1; key0 += 128) {
+        Kv4Step<D> cur = next;
+        if (key0 + 128 < m1) load(key0 + 128, next);
+        const int left = (int)(n - key0 < 32 ? n - key0 : 32);
+        mfma_f32x4 s[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            s[t] = mfma_f32x4{0.f, 0.f, 0.f, 0.f};
+            const float sc = __uint_as_float(cur.ks[t] << 23);
+#pragma unroll
+            for (int i = 0; i < KW; ++i) {
+                const u32x4 kf = fp4_decode8_bf16(cur.k[t][i], sc);
+#pragma unroll
+                for (int p = NP - 1; p >= 0; --p) s[t] = mfma16(kf, qf[p][i], s[t]);
+            }
+        }
+        if (left < 32) {
+            // the last keys: weights of rows that are not there are 0, and so are their values (the bytes may be anything)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (kg * 8 + j >= left) {
+                    s[j / 4][j % 4] = -INFINITY;
+                    const uint32_t clear = 0xffu << (8 * (j % 4));
+                    cur.vs[j / 4] = (cur.vs[j / 4] & ~clear) | (0x7f7f7f7fu & clear);
+                    if constexpr (D == 128) cur.v[j] = 0;
+                    else if constexpr (D == 64) cur.v[j / 2] &= j % 2 ? 0xffffu : 0xffff0000u;
+                    else cur.v[j / 4] &= ~clear;
+                }
+            }
+        }
+        float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]))) * scale_log2e;
+        if (__ballot(mx > m + 8.0f) != 0) {
+            mx = fmaxf(mx, __shfl_xor(mx, 16));
+            mx = fmaxf(mx, __shfl_xor(mx, 32));
+            const float mn = fmaxf(m, mx), alpha = __builtin_amdgcn_exp2f(m - mn);
+            m = mn;
+            l *= alpha;
+#pragma unroll
+            for (int i = 0; i < VM; ++i) acc[i] *= alpha;
+        }
+        float p[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j / 4][j % 4], scale_log2e, -m));
+        l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+        u32x4 pf[NP];
+        bf16_parts<NP>(p, pf);   // bf16 output: weights are rounded to bf16 for the matrix core; fp32: three parts are all of a weight's 24 bits
+        float vsc[8];
+        vsc[0] = fp4_scale_of<0>(cur.vs[0]); vsc[1] = fp4_scale_of<1>(cur.vs[0]); vsc[2] = fp4_scale_of<2>(cur.vs[0]); vsc[3] = fp4_scale_of<3>(cur.vs[0]);
+        vsc[4] = fp4_scale_of<0>(cur.vs[1]); vsc[5] = fp4_scale_of<1>(cur.vs[1]); vsc[6] = fp4_scale_of<2>(cur.vs[1]); vsc[7] = fp4_scale_of<3>(cur.vs[1]);
+        auto weigh = [&](auto at) {   // dimensions 2 I and 2 I + 1 of the lane's piece
+            constexpr int I = decltype(at)::value;
+            const uint32_t d[8] = {value_pair<D, 0, I>(cur.v, vsc[0]), value_pair<D, 1, I>(cur.v, vsc[1]), value_pair<D, 2, I>(cur.v, vsc[2]), value_pair<D, 3, I>(cur.v, vsc[3]),
+                                   value_pair<D, 4, I>(cur.v, vsc[4]), value_pair<D, 5, I>(cur.v, vsc[5]), value_pair<D, 6, I>(cur.v, vsc[6]), value_pair<D, 7, I>(cur.v, vsc[7])};
+            u32x4 lo, hi;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                lo[j] = __builtin_amdgcn_perm(d[2 * j + 1], d[2 * j], 0x05040100);
+                hi[j] = __builtin_amdgcn_perm(d[2 * j + 1], d[2 * j], 0x07060302);
+            }
+#pragma unroll
+            for (int p2 = NP - 1; p2 >= 0; --p2) {
+                acc[2 * I] = mfma16(lo, pf[p2], acc[2 * I]);
+                acc[2 * I + 1] = mfma16(hi, pf[p2], acc[2 * I + 1]);
+            }
+        };
+        weigh(std::integral_constant<int, 0>{});
+        if constexpr (D >= 64) weigh(std::integral_constant<int, 1>{});
+        if constexpr (D >= 128) { weigh(std::integral_constant<int, 2>{}); weigh(std::integral_constant<int, 3>{}); }
+    }
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    // the four wavefronts meet.  acc[i][r]: head l16, dimension (4 kg + r) D / 16 + i
+    if (l16 < grp) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int i = 0; i < VM; ++i) so[wave][l16][(4 * kg + r) * VM + i] = acc[i][r];
+        if (kg == 0) { sml[wave][l16][0] = m; sml[wave][l16][1] = l; }
+    }
+    __syncthreads();
+    for (int t = tid; t < grp * D; t += 256) {
+        const int hg = t / D, e = t % D;
+        float mn = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) mn = fmaxf(mn, sml[w][hg][0]);
+        const float mu = mn == -INFINITY ? 0.f : mn;
+        float ls = 0.f, o = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float a = __builtin_amdgcn_exp2f(sml[w][hg][0] - mu);
+            ls += sml[w][hg][1] * a;
+            o += so[w][hg][e] * a;
+        }
+        if (ns == 1) {
+            out[((int64_t)b * H + g * grp + hg) * D + e] = from_f32<T>(ls == 0.f ? 0.f : o / ls);
+        } else {
+            float* dst = part + (((int64_t)blockIdx.x * Hkv + g) * grp + hg) * (D + 2);
+            if (e == 0) { dst[0] = mn; dst[1] = ls; }
+            dst[2 + e] = o;
+        }
+    }
+}
+
+// The splits of one query head meet: blockIdx.x = head, blockIdx.y = sequence; 512 / D groups of threads walk the splits.
+constexpr int KV4_MAX_SPLITS = 256;
+template <typename T, int D>
+__global__ void __launch_bounds__(512) kv4_merge_kernel(const float* __restrict__ part, Kv4Splits sp, int H, int Hkv, T* __restrict__ out) {
+    constexpr int GROUPS = 512 / D;
+    __shared__ float sa[KV4_MAX_SPLITS], red[2][8], so[512];
+    const int h = blockIdx.x, b = blockIdx.y, grp = H / Hkv, g = h / grp, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int ns = sp.first[b + 1] - sp.first[b];
+    if (ns == 1) return;
+    const float* base = part + (((int64_t)sp.first[b] * Hkv + g) * grp + h % grp) * (D + 2);
+    const int64_t stride = (int64_t)H * (D + 2);
+    const float m = tid < ns ? base[tid * stride] : -INFINITY, l = tid < ns ? base[tid * stride + 1] : 0.f;
+    float mx = m;
+    for (int off = 32; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor(mx, off));
+    if (lane == 0) red[0][wave] = mx;
+    __syncthreads();
+    mx = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+    const float mu = mx == -INFINITY ? 0.f : mx, a = __builtin_amdgcn_exp2f(m - mu);
+    if (tid < ns) sa[tid] = a;
+    float ls = l * a;
+    for (int off = 32; off > 0; off >>= 1) ls += __shfl_xor(ls, off);
+    if (lane == 0) red[1][wave] = ls;
+    __syncthreads();
+    const float L = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
+    float o = 0.f;
+#pragma unroll 8
+    for (int s = tid / D; s < ns; s += GROUPS) o += base[s * stride + 2 + tid % D] * sa[s];
+    so[tid] = o;
+    __syncthreads();
+    if (tid >= D) return;
+    float t = 0.f;
+#pragma unroll
+    for (int k = 0; k < GROUPS; ++k) t += so[k * D + tid];
+    out[((int64_t)b * H + h) * D + tid] = from_f32<T>(L == 0.f ? 0.f : t / L);
+}
+
+template <typename T, int D>
+static hipError_t launch_kv4_attn_t(const T* q, const Kv4Batch& kb, int H, int Hkv, float* part, size_t part_floats, T* out, hipStream_t s) {
+    // shares of equal length over all sequences: as many as make two workgroups per CU over all heads, none below 128 keys
+    int64_t total = 0, longest = 1;
+    for (int b = 0; b < kb.n; ++b) { total += kb.count[b]; longest = kb.count[b] > longest ? kb.count[b] : longest; }
+    int64_t per = (total * Hkv + 511) / 512;
+    per = per < 128 ? 128 : per;
+    const int64_t room = (int64_t)(part_floats / ((size_t)H * (D + 2)));
+    Kv4Splits sp{};
+    for (;; per += per / 8 + 32) {
+        per = (per + 31) / 32 * 32;
+        if (longest > per * KV4_MAX_SPLITS) continue;
+        sp.per = (int32_t)per;
+        for (int b = 0; b < kb.n; ++b) sp.first[b + 1] = sp.first[b] + (int32_t)(kb.count[b] > per ? (kb.count[b] + per - 1) / per : 1);
+        if (sp.first[kb.n] == kb.n || sp.first[kb.n] <= room) break;
+    }
+    const float c = 1.4426950408889634f / sqrtf((float)D);
+    kv4_attn_kernel<T, D><<<dim3((unsigned)sp.first[kb.n], (unsigned)Hkv), dim3(256), 0, s>>>(q, kb, sp, H, Hkv, c, part, out);
+    if (sp.first[kb.n] > kb.n) kv4_merge_kernel<T, D><<<dim3((unsigned)H, (unsigned)kb.n), dim3(512), 0, s>>>(part, sp, H, Hkv, out);
+    return hipGetLastError();
 }
 
 hipError_t launch_kv4_attn(const void* q, const Kv4Batch& kb, int H, int Hkv, int d, float* part, size_t part_floats, void* out, bool bf16, hipStream_t s) {
-    (void)part; (void)part_floats;
-    const float c = 1.4426950408889634f / sqrtf((float)d);
-    const dim3 g((unsigned)H, (unsigned)kb.n), b(256);
-    if (bf16) kv4_attn_kernel<bf16_t><<<g, b, 0, s>>>((const bf16_t*)q, kb, H, Hkv, d, c, (bf16_t*)out);
-    else kv4_attn_kernel<float><<<g, b, 0, s>>>((const float*)q, kb, H, Hkv, d, c, (float*)out);
-    return hipGetLastError();
+#define SPTS_KV4_ATTN(D_)                                                                                                                   \
+    return bf16 ? launch_kv4_attn_t<bf16_t, D_>((const bf16_t*)q, kb, H, Hkv, part, part_floats, (bf16_t*)out, s)                           \
+                : launch_kv4_attn_t<float, D_>((const float*)q, kb, H, Hkv, part, part_floats, (float*)out, s);
+    switch (d) {
+        case 128: SPTS_KV4_ATTN(128)
+        case 64: SPTS_KV4_ATTN(64)
+        case 32: SPTS_KV4_ATTN(32)
+        default: return hipErrorInvalidValue;
+    }
+#undef SPTS_KV4_ATTN
 }
 
 }  // namespace spts

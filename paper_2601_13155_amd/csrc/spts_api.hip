@@ -1319,7 +1319,7 @@ int kv4_batch(const spts_ctx* c, const spts_kv4* caches, int32_t batch, Kv4Batch
         const spts_kv4& k = caches[b];
         if (!k.k || !k.v || !k.k_scale || !k.v_scale || !k.pos || k.capacity < 1 || k.count < 0 || k.count > k.capacity) return SPTS_EINVAL;
         if (!aligned16(k.k) || !aligned16(k.v) || !aligned16(k.k_scale) || !aligned16(k.v_scale) || !aligned16(k.pos)) return SPTS_EALIGN;
-        if (k.capacity % 8 != 0) return SPTS_ESHAPE;
+        if (k.capacity % 8 != 0 || k.capacity > INT32_MAX) return SPTS_ESHAPE;
         kb->k[b] = k.k; kb->v[b] = k.v; kb->ks[b] = k.k_scale; kb->vs[b] = k.v_scale; kb->pos[b] = k.pos;
         kb->cap[b] = k.capacity; kb->count[b] = k.count;
     }
@@ -1381,7 +1381,7 @@ int spts_kv4_bytes(const spts_model_desc* model, int64_t capacity, size_t* code_
     int st;
     if (!model_ok(model, &st)) return st;
     if (capacity < 1 || !code_bytes || !scale_bytes) return SPTS_EINVAL;
-    if (!kv4_shape_ok(*model) || capacity % 8 != 0) return SPTS_ESHAPE;
+    if (!kv4_shape_ok(*model) || capacity % 8 != 0 || capacity > INT32_MAX) return SPTS_ESHAPE;
     *code_bytes = (size_t)capacity * model->Hkv * (model->d / 2);
     *scale_bytes = (size_t)capacity * model->Hkv * (model->d / 32);
     return SPTS_OK;

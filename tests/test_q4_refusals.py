@@ -67,7 +67,7 @@ def test_sizes(lib):
     m = binding.model_desc(synth.TINY)
     assert binding.spts_kv4_bytes(m, 24) == (24 * 2 * 32, 24 * 2 * 2)
     assert lib.spts_kv4_bytes(None, 8, C.byref(c), C.byref(s)) == INVAL
-    for cap, why in ((0, INVAL), (-8, INVAL), (12, SHAPE)):
+    for cap, why in ((0, INVAL), (-8, INVAL), (12, SHAPE), (1 << 31, SHAPE)):
         assert lib.spts_kv4_bytes(C.byref(m), cap, C.byref(c), C.byref(s)) == why
     for d in (16, 96, 256):
         bad = binding.model_desc(synth.TINY)
@@ -105,7 +105,7 @@ def test_caches(lib, ctx):
         assert app(i64(0, 1), 1, kv4(**{name: None})) == INVAL
         assert app(i64(0, 1), 1, kv4(**{name: A + 4})) == ALIGN
         assert app(i64(0, 1, 2), 2, kv4(2, **{name: A})) == INVAL                                # the same buffer twice
-    for kw, why in ((dict(capacity=0), INVAL), (dict(count=-1), INVAL), (dict(count=65), INVAL), (dict(capacity=60), SHAPE)):
+    for kw, why in ((dict(capacity=0), INVAL), (dict(count=-1), INVAL), (dict(count=65), INVAL), (dict(capacity=60), SHAPE), (dict(capacity=1 << 31), SHAPE)):
         assert app(i64(0, 1), 1, kv4(**kw)) == why
     for d in (16, 256):
         assert app(i64(0, 1), 1, kv4(), at=ctx(d=d)) == SHAPE
