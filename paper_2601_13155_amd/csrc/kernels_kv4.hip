@@ -99,32 +99,6 @@ hipError_t launch_kv4_read(const Kv4Batch& kb, void* k, void* v, int Hkv, int d,
 }
 
 // ------------------------------------------------------------------------------------------------- attention
-typedef __bf16 mfma_bf16x8 __attribute__((ext_vector_type(8)));
-typedef float mfma_f32x4 __attribute__((ext_vector_type(4)));
-
-__device__ inline mfma_f32x4 mfma16(u32x4 a, u32x4 b, mfma_f32x4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(mfma_bf16x8, a), __builtin_bit_cast(mfma_bf16x8, b), c, 0, 0, 0);
-}
-
-// eight fp32 values as N bf16 vectors whose sum they are (to 8 N bits)
-template <int N>
-__device__ inline void bf16_parts(const float* v, u32x4 (&out)[N]) {
-    float r[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) r[j] = v[j];
-#pragma unroll
-    for (int p = 0; p < N; ++p)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t w = cvt_pk_bf16(r[2 * j], r[2 * j + 1]);
-            out[p][j] = w;
-            if (p + 1 < N) {
-                r[2 * j] -= __uint_as_float(w << 16);
-                r[2 * j + 1] -= __uint_as_float(w & 0xffff0000u);
-            }
-        }
-}
-
 // W dwords from p
 template <int W> __device__ inline void load_words(const char* p, uint32_t (&w)[W]) {
     if constexpr (W == 8) {
