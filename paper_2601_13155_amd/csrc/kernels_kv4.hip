@@ -21,81 +21,132 @@ __device__ inline int cache_of(const Kv4Batch& kb, int64_t row, int64_t* at) {
 }
 }  // namespace
 
-// One thread per row, head and block of 32, keys (blockIdx.y = 0) or values.
-template <typename T>
-__global__ void __launch_bounds__(256) kv4_append_kernel(const T* __restrict__ k, const T* __restrict__ v, const int32_t* __restrict__ pos, Kv4Batch kb, int Hkv, int d) {
-    const int blocks = Hkv * (d / 32);
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / blocks;
-    if (row >= kb.off[kb.n]) return;
-    const int g = (int)(i % blocks) / (d / 32), blk = (int)(i % blocks) % (d / 32);
-    int64_t key;
-    const int b = cache_of(kb, row, &key);
-    const T* src = (blockIdx.y ? v : k) + (row * Hkv + g) * d + blk * 32;
-    float f[32];
+// Eight dimensions of one row and head per thread, of the key and of the value: 16 bytes of bf16 in, a dword of codes out.  A workgroup takes 2048 / D
+// consecutive rows of one head (blockIdx.y), so that rows arrive in whole pieces of 2 D bytes and the codes of a head leave in one stretch; the four lanes of a block
+// find its largest value by two exchanges.
+template <typename T> __device__ inline void load8(const T* p, float (&v)[8]) {
+    if constexpr (sizeof(T) == 2) {
+        const u32x4 w = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+    } else {
+        const u32x4 a = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)), b = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p) + 1);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[i] = __uint_as_float(a[i]); v[4 + i] = __uint_as_float(b[i]); }
+    }
+}
+
+// codes of eight values and their block's scale byte; the block is the quad of lanes
+__device__ inline uint32_t encode_quad(const float (&v)[8], uint32_t* byte) {
     uint32_t top = 0;
 #pragma unroll
-    for (int j = 0; j < 32; ++j) {
-        f[j] = to_f32(src[j]);
-        const uint32_t m = __float_as_uint(f[j]) & 0x7fffffffu;
+    for (int j = 0; j < 8; ++j) {
+        const uint32_t m = __float_as_uint(v[j]) & 0x7fffffffu;
         top = m > top ? m : top;
     }
-    const uint32_t byte = fp4_scale_byte(top);
-    u32x4 c;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) c[q] = fp4_encode8(f + 8 * q, __uint_as_float(byte << 23));
-    if (blockIdx.y == 0) {
-        *reinterpret_cast<u32x4*>((char*)kb.k[b] + key_at(g, kb.cap[b], key, d) + blk * 16) = c;
-        ((uint8_t*)kb.ks[b])[key_scale_at(g, kb.cap[b], key, blk, d)] = (uint8_t)byte;
-        if (i % blocks == 0) kb.pos[b][key] = pos[row];
+    uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xF, 0xF, true);   // quad_perm [1, 0, 3, 2]
+    top = o > top ? o : top;
+    o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x4E, 0xF, 0xF, true);            // quad_perm [2, 3, 0, 1]
+    top = o > top ? o : top;
+    *byte = fp4_scale_byte(top);
+    return fp4_encode8(v, __uint_as_float(*byte << 23));
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(256) kv4_append_kernel(const T* __restrict__ k, const T* __restrict__ v, const int32_t* __restrict__ pos, Kv4Batch kb, int Hkv) {
+    constexpr int CH = D / 8, PB = D / 32;   // threads of a row, bytes of a piece of values
+    const int g = blockIdx.y, c = threadIdx.x % CH;
+    const int64_t row = (int64_t)blockIdx.x * (256 / CH) + threadIdx.x / CH;
+    if (row >= kb.off[kb.n]) return;         // (whole quads)
+    const T* const ks = k + (row * Hkv + g) * D + 8 * c;
+    const T* const vs = v + (row * Hkv + g) * D + 8 * c;
+    float kf[8], vf[8];
+    load8(ks, kf);
+    load8(vs, vf);
+    int64_t key;
+    const int b = cache_of(kb, row, &key);
+    const int64_t cap = kb.cap[b];
+    uint32_t kbyte, vbyte;
+    const uint32_t kc = encode_quad(kf, &kbyte), vc = encode_quad(vf, &vbyte);
+    *reinterpret_cast<uint32_t*>((char*)kb.k[b] + key_at(g, cap, key, D) + 4 * c) = kc;
+    char* const vp = (char*)kb.v[b] + value_at(g, cap, key, c * 4 / PB, D);   // pieces of one key are 8 PB bytes apart
+    if constexpr (PB == 4) *reinterpret_cast<uint32_t*>(vp) = vc;
+    else if constexpr (PB == 2) {
+        *reinterpret_cast<uint16_t*>(vp) = (uint16_t)vc;
+        *reinterpret_cast<uint16_t*>(vp + 16) = (uint16_t)(vc >> 16);
     } else {
-        const int per = d / 32;   // bytes of a piece
-        for (int j = 0; j < 16; ++j) ((uint8_t*)kb.v[b])[value_at(g, kb.cap[b], key, (blk * 16 + j) / per, d) + j % per] = (uint8_t)(c[j / 4] >> (8 * (j % 4)));
-        ((uint8_t*)kb.vs[b])[value_scale_at(g, kb.cap[b], key, blk, d)] = (uint8_t)byte;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) vp[8 * j] = (char)(vc >> (8 * j));
+    }
+    if (c % 4 == 0) {
+        ((uint8_t*)kb.ks[b])[key_scale_at(g, cap, key, c / 4, D)] = (uint8_t)kbyte;
+        ((uint8_t*)kb.vs[b])[value_scale_at(g, cap, key, c / 4, D)] = (uint8_t)vbyte;
+    }
+    if (g == 0 && c == 0) kb.pos[b][key] = pos[row];
+}
+
+template <typename T> __device__ inline void store8(T* p, const float (&v)[8]) {
+    if constexpr (sizeof(T) == 2) {
+        const u32x4 w{cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3]), cvt_pk_bf16(v[4], v[5]), cvt_pk_bf16(v[6], v[7])};
+        __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(p));
+    } else {
+        const u32x4 a{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])},
+            b{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])};
+        __builtin_nontemporal_store(a, reinterpret_cast<u32x4*>(p));
+        __builtin_nontemporal_store(b, reinterpret_cast<u32x4*>(p) + 1);
+    }
+}
+
+// The way back, same threads.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) kv4_read_kernel(Kv4Batch kb, T* __restrict__ k, T* __restrict__ v, int Hkv) {
+    constexpr int CH = D / 8, PB = D / 32;
+    const int g = blockIdx.y, c = threadIdx.x % CH;
+    const int64_t row = (int64_t)blockIdx.x * (256 / CH) + threadIdx.x / CH;
+    if (row >= kb.off[kb.n]) return;
+    int64_t key;
+    const int b = cache_of(kb, row, &key);
+    const int64_t cap = kb.cap[b];
+    const uint32_t kc = *reinterpret_cast<const uint32_t*>((const char*)kb.k[b] + key_at(g, cap, key, D) + 4 * c);
+    const char* const vp = (const char*)kb.v[b] + value_at(g, cap, key, c * 4 / PB, D);
+    uint32_t vc;
+    if constexpr (PB == 4) vc = *reinterpret_cast<const uint32_t*>(vp);
+    else if constexpr (PB == 2) vc = (uint32_t)*reinterpret_cast<const uint16_t*>(vp) | (uint32_t)*reinterpret_cast<const uint16_t*>(vp + 16) << 16;
+    else vc = (uint32_t)(uint8_t)vp[0] | (uint32_t)(uint8_t)vp[8] << 8 | (uint32_t)(uint8_t)vp[16] << 16 | (uint32_t)(uint8_t)vp[24] << 24;
+    const uint32_t kbyte = ((const uint8_t*)kb.ks[b])[key_scale_at(g, cap, key, c / 4, D)], vbyte = ((const uint8_t*)kb.vs[b])[value_scale_at(g, cap, key, c / 4, D)];
+    float f[8];
+    fp4_decode8(kc, __uint_as_float(kbyte << 23), f);
+    store8(k + (row * Hkv + g) * D + 8 * c, f);
+    fp4_decode8(vc, __uint_as_float(vbyte << 23), f);
+    store8(v + (row * Hkv + g) * D + 8 * c, f);
+}
+
+template <typename T, int D>
+static hipError_t launch_kv4_rows(const T* k, const T* v, const int32_t* pos, T* k_out, T* v_out, const Kv4Batch& kb, int Hkv, hipStream_t s) {
+    const int64_t rows = kb.off[kb.n];
+    if (rows == 0) return hipSuccess;
+    const dim3 g((unsigned)((rows + 2048 / D - 1) / (2048 / D)), (unsigned)Hkv), b(256);
+    if (k) kv4_append_kernel<T, D><<<g, b, 0, s>>>(k, v, pos, kb, Hkv);
+    else kv4_read_kernel<T, D><<<g, b, 0, s>>>(kb, k_out, v_out, Hkv);
+    return hipGetLastError();
+}
+
+template <typename T>
+static hipError_t launch_kv4_rows_t(const void* k, const void* v, const int32_t* pos, void* k_out, void* v_out, const Kv4Batch& kb, int Hkv, int d, hipStream_t s) {
+    switch (d) {
+        case 128: return launch_kv4_rows<T, 128>((const T*)k, (const T*)v, pos, (T*)k_out, (T*)v_out, kb, Hkv, s);
+        case 64: return launch_kv4_rows<T, 64>((const T*)k, (const T*)v, pos, (T*)k_out, (T*)v_out, kb, Hkv, s);
+        case 32: return launch_kv4_rows<T, 32>((const T*)k, (const T*)v, pos, (T*)k_out, (T*)v_out, kb, Hkv, s);
+        default: return hipErrorInvalidValue;
     }
 }
 
 hipError_t launch_kv4_append(const void* k, const void* v, const int32_t* pos, const Kv4Batch& kb, int Hkv, int d, bool bf16, hipStream_t s) {
-    const int64_t items = kb.off[kb.n] * Hkv * (d / 32);
-    if (items == 0) return hipSuccess;
-    const dim3 g((unsigned)((items + 255) / 256), 2), b(256);
-    if (bf16) kv4_append_kernel<bf16_t><<<g, b, 0, s>>>((const bf16_t*)k, (const bf16_t*)v, pos, kb, Hkv, d);
-    else kv4_append_kernel<float><<<g, b, 0, s>>>((const float*)k, (const float*)v, pos, kb, Hkv, d);
-    return hipGetLastError();
-}
-
-template <typename T>
-__global__ void __launch_bounds__(256) kv4_read_kernel(Kv4Batch kb, T* __restrict__ k, T* __restrict__ v, int Hkv, int d) {
-    const int blocks = Hkv * (d / 32);
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / blocks;
-    if (row >= kb.off[kb.n]) return;
-    const int g = (int)(i % blocks) / (d / 32), blk = (int)(i % blocks) % (d / 32);
-    int64_t key;
-    const int b = cache_of(kb, row, &key);
-    T* dst = (blockIdx.y ? v : k) + (row * Hkv + g) * d + blk * 32;
-    u32x4 c{0, 0, 0, 0};
-    uint32_t byte;
-    if (blockIdx.y == 0) {
-        c = *reinterpret_cast<const u32x4*>((const char*)kb.k[b] + key_at(g, kb.cap[b], key, d) + blk * 16);
-        byte = ((const uint8_t*)kb.ks[b])[key_scale_at(g, kb.cap[b], key, blk, d)];
-    } else {
-        const int per = d / 32;
-        for (int j = 0; j < 16; ++j) c[j / 4] |= (uint32_t)((const uint8_t*)kb.v[b])[value_at(g, kb.cap[b], key, (blk * 16 + j) / per, d) + j % per] << (8 * (j % 4));
-        byte = ((const uint8_t*)kb.vs[b])[value_scale_at(g, kb.cap[b], key, blk, d)];
-    }
-    for (int q = 0; q < 4; ++q) {
-        float f[8];
-        fp4_decode8(c[q], __uint_as_float(byte << 23), f);
-        for (int j = 0; j < 8; ++j) dst[8 * q + j] = from_f32<T>(f[j]);
-    }
+    return bf16 ? launch_kv4_rows_t<bf16_t>(k, v, pos, nullptr, nullptr, kb, Hkv, d, s) : launch_kv4_rows_t<float>(k, v, pos, nullptr, nullptr, kb, Hkv, d, s);
 }
 
 hipError_t launch_kv4_read(const Kv4Batch& kb, void* k, void* v, int Hkv, int d, bool bf16, hipStream_t s) {
-    const int64_t items = kb.off[kb.n] * Hkv * (d / 32);
-    if (items == 0) return hipSuccess;
-    const dim3 g((unsigned)((items + 255) / 256), 2), b(256);
-    if (bf16) kv4_read_kernel<bf16_t><<<g, b, 0, s>>>(kb, (bf16_t*)k, (bf16_t*)v, Hkv, d);
-    else kv4_read_kernel<float><<<g, b, 0, s>>>(kb, (float*)k, (float*)v, Hkv, d);
-    return hipGetLastError();
+    return bf16 ? launch_kv4_rows_t<bf16_t>(nullptr, nullptr, nullptr, k, v, kb, Hkv, d, s) : launch_kv4_rows_t<float>(nullptr, nullptr, nullptr, k, v, kb, Hkv, d, s);
 }
 
 // ------------------------------------------------------------------------------------------------- attention
