@@ -12,11 +12,30 @@ __device__ inline int64_t key_scale_at(int g, int64_t cap, int64_t key, int blk,
 __device__ inline int64_t value_at(int g, int64_t cap, int64_t key, int n, int d) { return ((((int64_t)g * cap + key) >> 3) * 16 + n) * (d / 4) + (key & 7) * (d / 32); }
 __device__ inline int64_t value_scale_at(int g, int64_t cap, int64_t key, int blk, int d) { return ((((int64_t)g * cap + key) >> 3) * (d / 32) + blk) * 8 + (key & 7); }
 
-// the cache that row `row` of a call belongs to, and the row's place in it
-__device__ inline int cache_of(const Kv4Batch& kb, int64_t row, int64_t* at) {
+// A kernel's view of up to NB caches.  Arguments beyond some 100 bytes cost every launch 0.6 us, beyond 800 another 0.5 (measured with empty kernels:
+// 2.65 / 3.3 / 3.8 us a launch), so a single sequence has a descriptor of its own and sixteen fit 800 bytes.
+template <int NB> struct Kv4Rows {
+    char *k[NB], *v[NB];
+    uint8_t *ks[NB], *vs[NB];
+    int32_t* pos[NB];
+    int32_t cap[NB], at[NB], end[NB];   // capacity, cache row of the sequence's first row, its end among the call's rows
+    int32_t rows;
+};
+template <int NB> struct Kv4Caches {
+    const char *k[NB], *v[NB];
+    const uint8_t *ks[NB], *vs[NB];
+    int32_t cap[NB], n[NB];
+    int32_t end[NB];                    // splits of sequence b: those before end[b] that are none of b - 1's; behind the last sequence its end
+    int32_t per;                        // keys of a split, a multiple of 32
+};
+
+// the sequence that item i is in, and the first item of that sequence
+template <int NB> __device__ inline int sequence_of(const int32_t (&end)[NB], int i, int* first) {
     int b = 0;
-    while (b + 1 < kb.n && row >= kb.off[b + 1]) ++b;
-    *at = kb.count[b] + (row - kb.off[b]);
+    *first = 0;
+#pragma unroll
+    for (int j = 0; j + 1 < NB; ++j)
+        if (i >= end[j]) { b = j + 1; *first = end[j]; }
     return b;
 }
 }  // namespace
@@ -52,24 +71,24 @@ __device__ inline uint32_t encode_quad(const float (&v)[8], uint32_t* byte) {
     return fp4_encode8(v, __uint_as_float(*byte << 23));
 }
 
-template <typename T, int D>
-__global__ void __launch_bounds__(256) kv4_append_kernel(const T* __restrict__ k, const T* __restrict__ v, const int32_t* __restrict__ pos, Kv4Batch kb, int Hkv) {
+template <typename T, int D, int NB>
+__global__ void __launch_bounds__(256) kv4_append_kernel(const T* __restrict__ k, const T* __restrict__ v, const int32_t* __restrict__ pos, Kv4Rows<NB> kb, int Hkv) {
     constexpr int CH = D / 8, PB = D / 32;   // threads of a row, bytes of a piece of values
     const int g = blockIdx.y, c = threadIdx.x % CH;
     const int64_t row = (int64_t)blockIdx.x * (256 / CH) + threadIdx.x / CH;
-    if (row >= kb.off[kb.n]) return;         // (whole quads)
+    if (row >= kb.rows) return;         // (whole quads)
     const T* const ks = k + (row * Hkv + g) * D + 8 * c;
     const T* const vs = v + (row * Hkv + g) * D + 8 * c;
     float kf[8], vf[8];
     load8(ks, kf);
     load8(vs, vf);
-    int64_t key;
-    const int b = cache_of(kb, row, &key);
-    const int64_t cap = kb.cap[b];
+    int first;
+    const int b = sequence_of(kb.end, (int)row, &first);
+    const int64_t cap = kb.cap[b], key = kb.at[b] + (row - first);
     uint32_t kbyte, vbyte;
     const uint32_t kc = encode_quad(kf, &kbyte), vc = encode_quad(vf, &vbyte);
-    *reinterpret_cast<uint32_t*>((char*)kb.k[b] + key_at(g, cap, key, D) + 4 * c) = kc;
-    char* const vp = (char*)kb.v[b] + value_at(g, cap, key, c * 4 / PB, D);   // pieces of one key are 8 PB bytes apart
+    *reinterpret_cast<uint32_t*>(kb.k[b] + key_at(g, cap, key, D) + 4 * c) = kc;
+    char* const vp = kb.v[b] + value_at(g, cap, key, c * 4 / PB, D);   // pieces of one key are 8 PB bytes apart
     if constexpr (PB == 4) *reinterpret_cast<uint32_t*>(vp) = vc;
     else if constexpr (PB == 2) {
         *reinterpret_cast<uint16_t*>(vp) = (uint16_t)vc;
@@ -79,8 +98,8 @@ __global__ void __launch_bounds__(256) kv4_append_kernel(const T* __restrict__ k
         for (int j = 0; j < 4; ++j) vp[8 * j] = (char)(vc >> (8 * j));
     }
     if (c % 4 == 0) {
-        ((uint8_t*)kb.ks[b])[key_scale_at(g, cap, key, c / 4, D)] = (uint8_t)kbyte;
-        ((uint8_t*)kb.vs[b])[value_scale_at(g, cap, key, c / 4, D)] = (uint8_t)vbyte;
+        kb.ks[b][key_scale_at(g, cap, key, c / 4, D)] = (uint8_t)kbyte;
+        kb.vs[b][value_scale_at(g, cap, key, c / 4, D)] = (uint8_t)vbyte;
     }
     if (g == 0 && c == 0) kb.pos[b][key] = pos[row];
 }
@@ -98,22 +117,22 @@ template <typename T> __device__ inline void store8(T* p, const float (&v)[8]) {
 }
 
 // The way back, same threads.
-template <typename T, int D>
-__global__ void __launch_bounds__(256) kv4_read_kernel(Kv4Batch kb, T* __restrict__ k, T* __restrict__ v, int Hkv) {
+template <typename T, int D, int NB>
+__global__ void __launch_bounds__(256) kv4_read_kernel(Kv4Rows<NB> kb, T* __restrict__ k, T* __restrict__ v, int Hkv) {
     constexpr int CH = D / 8, PB = D / 32;
     const int g = blockIdx.y, c = threadIdx.x % CH;
     const int64_t row = (int64_t)blockIdx.x * (256 / CH) + threadIdx.x / CH;
-    if (row >= kb.off[kb.n]) return;
-    int64_t key;
-    const int b = cache_of(kb, row, &key);
-    const int64_t cap = kb.cap[b];
-    const uint32_t kc = *reinterpret_cast<const uint32_t*>((const char*)kb.k[b] + key_at(g, cap, key, D) + 4 * c);
-    const char* const vp = (const char*)kb.v[b] + value_at(g, cap, key, c * 4 / PB, D);
+    if (row >= kb.rows) return;
+    int first;
+    const int b = sequence_of(kb.end, (int)row, &first);
+    const int64_t cap = kb.cap[b], key = kb.at[b] + (row - first);
+    const uint32_t kc = *reinterpret_cast<const uint32_t*>(kb.k[b] + key_at(g, cap, key, D) + 4 * c);
+    const char* const vp = kb.v[b] + value_at(g, cap, key, c * 4 / PB, D);
     uint32_t vc;
     if constexpr (PB == 4) vc = *reinterpret_cast<const uint32_t*>(vp);
     else if constexpr (PB == 2) vc = (uint32_t)*reinterpret_cast<const uint16_t*>(vp) | (uint32_t)*reinterpret_cast<const uint16_t*>(vp + 16) << 16;
     else vc = (uint32_t)(uint8_t)vp[0] | (uint32_t)(uint8_t)vp[8] << 8 | (uint32_t)(uint8_t)vp[16] << 16 | (uint32_t)(uint8_t)vp[24] << 24;
-    const uint32_t kbyte = ((const uint8_t*)kb.ks[b])[key_scale_at(g, cap, key, c / 4, D)], vbyte = ((const uint8_t*)kb.vs[b])[value_scale_at(g, cap, key, c / 4, D)];
+    const uint32_t kbyte = kb.ks[b][key_scale_at(g, cap, key, c / 4, D)], vbyte = kb.vs[b][value_scale_at(g, cap, key, c / 4, D)];
     float f[8];
     fp4_decode8(kc, __uint_as_float(kbyte << 23), f);
     store8(k + (row * Hkv + g) * D + 8 * c, f);
@@ -121,14 +140,26 @@ __global__ void __launch_bounds__(256) kv4_read_kernel(Kv4Batch kb, T* __restric
     store8(v + (row * Hkv + g) * D + 8 * c, f);
 }
 
+template <typename T, int D, int NB>
+static hipError_t launch_kv4_rows_n(const T* k, const T* v, const int32_t* pos, T* k_out, T* v_out, const Kv4Batch& kb, int Hkv, hipStream_t s) {
+    Kv4Rows<NB> r{};
+    for (int b = 0; b < NB; ++b) {
+        const int i = b < kb.n ? b : kb.n - 1;
+        r.k[b] = (char*)kb.k[i]; r.v[b] = (char*)kb.v[i]; r.ks[b] = (uint8_t*)kb.ks[i]; r.vs[b] = (uint8_t*)kb.vs[i]; r.pos[b] = kb.pos[i];
+        r.cap[b] = (int32_t)kb.cap[i]; r.at[b] = (int32_t)kb.count[i]; r.end[b] = (int32_t)kb.off[i + 1];
+    }
+    r.rows = (int32_t)kb.off[kb.n];
+    const dim3 g((unsigned)((r.rows + 2048 / D - 1) / (2048 / D)), (unsigned)Hkv), t(256);
+    if (k) kv4_append_kernel<T, D, NB><<<g, t, 0, s>>>(k, v, pos, r, Hkv);
+    else kv4_read_kernel<T, D, NB><<<g, t, 0, s>>>(r, k_out, v_out, Hkv);
+    return hipGetLastError();
+}
+
 template <typename T, int D>
 static hipError_t launch_kv4_rows(const T* k, const T* v, const int32_t* pos, T* k_out, T* v_out, const Kv4Batch& kb, int Hkv, hipStream_t s) {
-    const int64_t rows = kb.off[kb.n];
-    if (rows == 0) return hipSuccess;
-    const dim3 g((unsigned)((rows + 2048 / D - 1) / (2048 / D)), (unsigned)Hkv), b(256);
-    if (k) kv4_append_kernel<T, D><<<g, b, 0, s>>>(k, v, pos, kb, Hkv);
-    else kv4_read_kernel<T, D><<<g, b, 0, s>>>(kb, k_out, v_out, Hkv);
-    return hipGetLastError();
+    if (kb.off[kb.n] == 0) return hipSuccess;
+    return kb.n == 1 ? launch_kv4_rows_n<T, D, 1>(k, v, pos, k_out, v_out, kb, Hkv, s)
+                     : launch_kv4_rows_n<T, D, DECODE_MAX_BATCH>(k, v, pos, k_out, v_out, kb, Hkv, s);
 }
 
 template <typename T>
@@ -174,8 +205,6 @@ template <int D, int J, int I> __device__ inline uint32_t value_pair(const uint3
     return fp4_pair_bf16<byte % 4>(w[byte / 4], scale);
 }
 
-struct Kv4Splits { int32_t first[DECODE_MAX_BATCH + 1]; int32_t per; };   // splits of sequence b: first[b] .. first[b + 1], of `per` keys (a multiple of 32)
-
 // what one lane needs of 32 keys
 template <int D> struct Kv4Step {
     uint32_t k[2][D / 32], v[D / 16], vs[2];
@@ -190,20 +219,20 @@ template <int D> struct Kv4Step {
 //     a lane, which is how the values are stored (piece n of eight keys: D / 16 dimensions): decoding gives pairs of dimensions, two byte permutes pairs of keys.
 //   In both results a column, i.e. lane % 16, is a query head, so the running maximum, the sum and the rescaling are the lane's own.
 // The maximum moves only when a score is 2^8 times above it (the sums stand that easily), so most steps have no rescaling.
-template <typename T, int D>
-__global__ void __launch_bounds__(256, 2) kv4_attn_kernel(const T* __restrict__ q, Kv4Batch kb, Kv4Splits sp, int H, int Hkv, float scale_log2e, float* __restrict__ part,
-                                                          T* __restrict__ out) {
+template <typename T, int D, int NW, int NB>
+__global__ void __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) kv4_attn_kernel(const T* __restrict__ q, Kv4Caches<NB> kb, int H, int Hkv, float scale_log2e, float* __restrict__ part,
+                                                                          T* __restrict__ out) {
     constexpr bool F32 = sizeof(T) == 4;
     constexpr int NP = F32 ? 3 : 1;                       // bf16 parts of a query or weight
     constexpr int KW = D / 32, VM = D / 16, LD = D + 4;
-    __shared__ float so[4][16][LD];
-    __shared__ float sml[4][16][2];
+    extern __shared__ __attribute__((aligned(16))) float lds[];   // [NW][group][LD] weighted values, then [NW][16][2] maximum and sum
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, kg = lane >> 4;
     const int g = blockIdx.y, grp = H / Hkv;
-    int b = 0;
-    while (b + 1 < kb.n && (int)blockIdx.x >= sp.first[b + 1]) ++b;
-    const int ns = sp.first[b + 1] - sp.first[b], split = (int)blockIdx.x - sp.first[b];
-    const int64_t n = kb.count[b], cap = kb.cap[b], m0 = (int64_t)split * sp.per, m1 = m0 + sp.per < n ? m0 + sp.per : n;
+    float* const sml = lds + NW * grp * LD;
+    int first;
+    const int b = sequence_of(kb.end, (int)blockIdx.x, &first);
+    const int ns = kb.end[b] - first, split = (int)blockIdx.x - first;
+    const int64_t n = kb.n[b], cap = kb.cap[b], m0 = (int64_t)split * kb.per, m1 = m0 + kb.per < n ? m0 + kb.per : n;
 
     // the queries, columns beyond the group zero
     u32x4 qf[NP][KW];
@@ -225,10 +254,10 @@ __global__ void __launch_bounds__(256, 2) kv4_attn_kernel(const T* __restrict__ 
         }
     }
     // a head's rows; a lane's offsets within 32 keys
-    const char* const kh = (const char*)kb.k[b] + (int64_t)g * cap * (D / 2);
-    const char* const vh = (const char*)kb.v[b] + (int64_t)g * cap * (D / 2);
-    const uint8_t* const ksh = (const uint8_t*)kb.ks[b] + (int64_t)g * cap * (D / 32);
-    const uint8_t* const vsh = (const uint8_t*)kb.vs[b] + (int64_t)g * cap * (D / 32);
+    const char* const kh = kb.k[b] + (int64_t)g * cap * (D / 2);
+    const char* const vh = kb.v[b] + (int64_t)g * cap * (D / 2);
+    const uint8_t* const ksh = kb.ks[b] + (int64_t)g * cap * (D / 32);
+    const uint8_t* const vsh = kb.vs[b] + (int64_t)g * cap * (D / 32);
     const int kblk = kg * (D / 4) / 32, vblk = l16 * (D / 16) / 32;
     int krow[2];
 #pragma unroll
@@ -263,9 +292,9 @@ __global__ void __launch_bounds__(256, 2) kv4_attn_kernel(const T* __restrict__ 
     Kv4Step<D> next;
     int64_t key0 = m0 + wave * 32;
     if (key0 < m1) load(key0, next);
-    for (; key0 < m1; key0 += 128) {
+    for (; key0 < m1; key0 += NW * 32) {
         Kv4Step<D> cur = next;
-        if (key0 + 128 < m1) load(key0 + 128, next);
+        if (key0 + NW * 32 < m1) load(key0 + NW * 32, next);
         const int left = (int)(n - key0 < 32 ? n - key0 : 32);
         mfma_f32x4 s[2];
 #pragma unroll
@@ -334,27 +363,28 @@ __global__ void __launch_bounds__(256, 2) kv4_attn_kernel(const T* __restrict__ 
     }
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
-    // the four wavefronts meet.  acc[i][r]: head l16, dimension (4 kg + r) D / 16 + i
+    // the wavefronts meet.  acc[i][r]: head l16, dimension (4 kg + r) D / 16 + i
     if (l16 < grp) {
+        float* const to = lds + (wave * grp + l16) * LD + 4 * kg * VM;
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int i = 0; i < VM; ++i) so[wave][l16][(4 * kg + r) * VM + i] = acc[i][r];
-        if (kg == 0) { sml[wave][l16][0] = m; sml[wave][l16][1] = l; }
+            for (int i = 0; i < VM; ++i) to[r * VM + i] = acc[i][r];
+        if (kg == 0) { sml[(wave * 16 + l16) * 2] = m; sml[(wave * 16 + l16) * 2 + 1] = l; }
     }
     __syncthreads();
-    for (int t = tid; t < grp * D; t += 256) {
+    for (int t = tid; t < grp * D; t += NW * 64) {
         const int hg = t / D, e = t % D;
         float mn = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) mn = fmaxf(mn, sml[w][hg][0]);
+        for (int w = 0; w < NW; ++w) mn = fmaxf(mn, sml[(w * 16 + hg) * 2]);
         const float mu = mn == -INFINITY ? 0.f : mn;
         float ls = 0.f, o = 0.f;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const float a = __builtin_amdgcn_exp2f(sml[w][hg][0] - mu);
-            ls += sml[w][hg][1] * a;
-            o += so[w][hg][e] * a;
+#pragma unroll 4
+        for (int w = 0; w < NW; ++w) {
+            const float a = __builtin_amdgcn_exp2f(sml[(w * 16 + hg) * 2] - mu);
+            ls += sml[(w * 16 + hg) * 2 + 1] * a;
+            o += lds[(w * grp + hg) * LD + e] * a;
         }
         if (ns == 1) {
             out[((int64_t)b * H + g * grp + hg) * D + e] = from_f32<T>(ls == 0.f ? 0.f : o / ls);
@@ -368,14 +398,15 @@ __global__ void __launch_bounds__(256, 2) kv4_attn_kernel(const T* __restrict__ 
 
 // The splits of one query head meet: blockIdx.x = head, blockIdx.y = sequence; 512 / D groups of threads walk the splits.
 constexpr int KV4_MAX_SPLITS = 256;
-template <typename T, int D>
-__global__ void __launch_bounds__(512) kv4_merge_kernel(const float* __restrict__ part, Kv4Splits sp, int H, int Hkv, T* __restrict__ out) {
+template <int NB> struct Kv4Ends { int32_t end[NB]; };
+template <typename T, int D, int NB>
+__global__ void __launch_bounds__(512) kv4_merge_kernel(const float* __restrict__ part, Kv4Ends<NB> sp, int H, int Hkv, T* __restrict__ out) {
     constexpr int GROUPS = 512 / D;
     __shared__ float sa[KV4_MAX_SPLITS], red[2][8], so[512];
     const int h = blockIdx.x, b = blockIdx.y, grp = H / Hkv, g = h / grp, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int ns = sp.first[b + 1] - sp.first[b];
+    const int first = NB > 1 && b > 0 ? sp.end[NB > 1 ? b - 1 : 0] : 0, ns = sp.end[NB > 1 ? b : 0] - first;
     if (ns == 1) return;
-    const float* base = part + (((int64_t)sp.first[b] * Hkv + g) * grp + h % grp) * (D + 2);
+    const float* base = part + (((int64_t)first * Hkv + g) * grp + h % grp) * (D + 2);
     const int64_t stride = (int64_t)H * (D + 2);
     const float m = tid < ns ? base[tid * stride] : -INFINITY, l = tid < ns ? base[tid * stride + 1] : 0.f;
     float mx = m;
@@ -402,26 +433,48 @@ __global__ void __launch_bounds__(512) kv4_merge_kernel(const float* __restrict_
     out[((int64_t)b * H + h) * D + tid] = from_f32<T>(L == 0.f ? 0.f : t / L);
 }
 
+template <typename T, int D, int NW, int NB>
+static hipError_t launch_kv4_attn_n(const T* q, const Kv4Batch& kb, int64_t per, int H, int Hkv, float* part, T* out, hipStream_t s) {
+    Kv4Caches<NB> c{};
+    Kv4Ends<NB> ends{};
+    for (int b = 0; b < NB; ++b) {
+        const int i = b < kb.n ? b : kb.n - 1;
+        c.k[b] = (const char*)kb.k[i]; c.v[b] = (const char*)kb.v[i]; c.ks[b] = (const uint8_t*)kb.ks[i]; c.vs[b] = (const uint8_t*)kb.vs[i];
+        c.cap[b] = (int32_t)kb.cap[i]; c.n[b] = (int32_t)kb.count[i];
+        ends.end[b] = c.end[b] = (b > 0 ? c.end[b - 1] : 0) + (b < kb.n ? (int32_t)(kb.count[b] > per ? (kb.count[b] + per - 1) / per : 1) : 0);
+    }
+    c.per = (int32_t)per;
+    const int splits = c.end[NB - 1], lds = (NW * (H / Hkv) * (D + 4) + NW * 32) * (int)sizeof(float);
+    const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(&kv4_attn_kernel<T, D, NW, NB>), (NW * KV4_MAX_GROUP * (D + 4) + NW * 32) * (int)sizeof(float));
+    if (e != hipSuccess) return e;
+    kv4_attn_kernel<T, D, NW, NB><<<dim3((unsigned)splits, (unsigned)Hkv), dim3(NW * 64), lds, s>>>(q, c, H, Hkv, 1.4426950408889634f / sqrtf((float)D), part, out);
+    if (splits > kb.n) kv4_merge_kernel<T, D, NB><<<dim3((unsigned)H, (unsigned)kb.n), dim3(512), 0, s>>>(part, ends, H, Hkv, out);
+    return hipGetLastError();
+}
+
 template <typename T, int D>
 static hipError_t launch_kv4_attn_t(const T* q, const Kv4Batch& kb, int H, int Hkv, float* part, size_t part_floats, T* out, hipStream_t s) {
-    // shares of equal length over all sequences: as many as make two workgroups per CU over all heads, none below 128 keys
+    constexpr int WIDE = sizeof(T) == 4 ? 8 : 16;   // wavefronts that a CU's registers hold
     int64_t total = 0, longest = 1;
     for (int b = 0; b < kb.n; ++b) { total += kb.count[b]; longest = kb.count[b] > longest ? kb.count[b] : longest; }
+    // short caches whole, by one wide workgroup each: no second launch
+    if (longest <= WIDE * 64) {
+        return kb.n == 1 ? launch_kv4_attn_n<T, D, WIDE, 1>(q, kb, WIDE * 64, H, Hkv, part, out, s)
+                         : launch_kv4_attn_n<T, D, WIDE, DECODE_MAX_BATCH>(q, kb, WIDE * 64, H, Hkv, part, out, s);
+    }
+    // shares of equal length over all sequences: as many as make two workgroups per CU over all heads, none below 128 keys
     int64_t per = (total * Hkv + 511) / 512;
-    per = per < 128 ? 128 : per;
+    per = per < 128 ? 128 : per > (1 << 30) ? (1 << 30) : per;
     const int64_t room = (int64_t)(part_floats / ((size_t)H * (D + 2)));
-    Kv4Splits sp{};
     for (;; per += per / 8 + 32) {
         per = (per + 31) / 32 * 32;
         if (longest > per * KV4_MAX_SPLITS) continue;
-        sp.per = (int32_t)per;
-        for (int b = 0; b < kb.n; ++b) sp.first[b + 1] = sp.first[b] + (int32_t)(kb.count[b] > per ? (kb.count[b] + per - 1) / per : 1);
-        if (sp.first[kb.n] == kb.n || sp.first[kb.n] <= room) break;
+        int64_t splits = 0;
+        for (int b = 0; b < kb.n; ++b) splits += kb.count[b] > per ? (kb.count[b] + per - 1) / per : 1;
+        if (splits == kb.n || splits <= room) break;
     }
-    const float c = 1.4426950408889634f / sqrtf((float)D);
-    kv4_attn_kernel<T, D><<<dim3((unsigned)sp.first[kb.n], (unsigned)Hkv), dim3(256), 0, s>>>(q, kb, sp, H, Hkv, c, part, out);
-    if (sp.first[kb.n] > kb.n) kv4_merge_kernel<T, D><<<dim3((unsigned)H, (unsigned)kb.n), dim3(512), 0, s>>>(part, sp, H, Hkv, out);
-    return hipGetLastError();
+    return kb.n == 1 ? launch_kv4_attn_n<T, D, 4, 1>(q, kb, per, H, Hkv, part, out, s)
+                     : launch_kv4_attn_n<T, D, 4, DECODE_MAX_BATCH>(q, kb, per, H, Hkv, part, out, s);
 }
 
 hipError_t launch_kv4_attn(const void* q, const Kv4Batch& kb, int H, int Hkv, int d, float* part, size_t part_floats, void* out, bool bf16, hipStream_t s) {
