@@ -43,18 +43,6 @@ template <int NB> __device__ inline int sequence_of(const int32_t (&end)[NB], in
 // Eight dimensions of one row and head per thread, of the key and of the value: 16 bytes of bf16 in, a dword of codes out.  A workgroup takes 2048 / D
 // consecutive rows of one head (blockIdx.y), so that rows arrive in whole pieces of 2 D bytes and the codes of a head leave in one stretch; the four lanes of a block
 // find its largest value by two exchanges.
-template <typename T> __device__ inline void load8(const T* p, float (&v)[8]) {
-    if constexpr (sizeof(T) == 2) {
-        const u32x4 w = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
-    } else {
-        const u32x4 a = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)), b = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p) + 1);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { v[i] = __uint_as_float(a[i]); v[4 + i] = __uint_as_float(b[i]); }
-    }
-}
-
 // codes of eight values and their block's scale byte; the block is the quad of lanes
 __device__ inline uint32_t encode_quad(const float (&v)[8], uint32_t* byte) {
     uint32_t top = 0;

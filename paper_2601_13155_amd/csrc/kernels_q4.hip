@@ -4,34 +4,40 @@
 
 namespace spts {
 
-// One thread per piece and slab: four blocks of one row, 128 values apart.
+// One thread per piece and slab: eight values of sixteen blocks of one row; the other values of a block are 16, 32 and 48 lanes away.
 template <typename T>
 __global__ void __launch_bounds__(256) q4_pack_kernel(const T* __restrict__ W, int64_t rows, int64_t K, int64_t slabs, int64_t pieces,
                                                       u32x4* __restrict__ codes, uint32_t* __restrict__ scales) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= pieces) return;
-    const int lane = (int)(i & 63);
+    if (i >= pieces) return;                      // (whole wavefronts)
+    const int lane = (int)(i & 63), kg = lane >> 4;
     const int64_t slab = (i >> 6) % slabs, strip = (i >> 6) / slabs, row = strip * 16 + (lane & 15);
-    uint32_t sc = 0;
+    u32x4 sc{0, 0, 0, 0};
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-        const int64_t k0 = slab * Q4_SLAB + t * 128 + (lane >> 4) * 32;
-        float v[32];
-        uint32_t top = 0;
-#pragma unroll
-        for (int j = 0; j < 32; ++j) {
-            v[j] = row < rows && k0 + j < K ? to_f32(W[row * K + k0 + j]) : 0.f;
-            const uint32_t m = __float_as_uint(v[j]) & 0x7fffffffu;
-            top = m > top ? m : top;
-        }
-        const uint32_t byte = fp4_scale_byte(top);
         u32x4 c;
 #pragma unroll
-        for (int g = 0; g < 4; ++g) c[g] = fp4_encode8(v + 8 * g, __uint_as_float(byte << 23));
+        for (int j = 0; j < 4; ++j) {
+            const int64_t k = slab * Q4_SLAB + t * 128 + j * 32 + kg * 8;
+            float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            if (row < rows && k < K) load8(W + row * K + k, v);   // K % 8 == 0
+            uint32_t top = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t m = __float_as_uint(v[e]) & 0x7fffffffu;
+                top = m > top ? m : top;
+            }
+            uint32_t o = (uint32_t)__shfl_xor((int)top, 16);
+            top = o > top ? o : top;
+            o = (uint32_t)__shfl_xor((int)top, 32);
+            top = o > top ? o : top;
+            const uint32_t byte = fp4_scale_byte(top);
+            c[j] = fp4_encode8(v, __uint_as_float(byte << 23));
+            sc[t] |= byte << (8 * j);
+        }
         codes[((i >> 6) * 4 + t) * 64 + lane] = c;
-        sc |= byte << (8 * t);
     }
-    scales[i] = sc;
+    scales[i] = kg == 0 ? sc[0] : kg == 1 ? sc[1] : kg == 2 ? sc[2] : sc[3];   // (all four lanes of a row have all four)
 }
 
 hipError_t launch_q4_pack(const void* W, int64_t rows, int64_t K, void* codes, void* scales, bool bf16, hipStream_t s) {
@@ -42,33 +48,41 @@ hipError_t launch_q4_pack(const void* W, int64_t rows, int64_t K, void* codes, v
     return hipGetLastError();
 }
 
-// y = x W^T on the matrix cores for up to 16 vectors: a row of W is an operand row (lane l16), a vector a column, and lane group kg takes 32 of a tile's 128 k:
-// one stored block, so that a 16-byte load brings four operands of one scale each, already where the matrix core wants them, and the decoder's
-// bf16 pairs are the operand.  Vectors are read from the caches (lanes without a vector feed zeros); an fp32 vector is taken as three bf16 parts, which is all
-// of its 24 bits.  The NW wavefronts of a workgroup share the slabs of NS strips in turn and meet in LDS; the order of a row's sum depends on K alone.
-template <typename T, int MODE, int NS, int NW>
-__global__ void __launch_bounds__(NW * 64) q4_matvec_kernel(Q4Args a) {
+// y = x W^T on the matrix cores for up to 16 vectors: a row of W is an operand row (lane l16), a vector a column; a dword of codes is an operand's eight values of a
+// lane, and the decoder's bf16 pairs are the operand.  Vectors are read from the caches, 64 bytes of each per load; an fp32 vector is taken as three bf16
+// parts, which is all of its 24 bits.  The NW wavefronts of a workgroup share the slabs of NS strips in turn, each with the codes and scales of its next slab on
+// their way while it works on one, and meet in LDS.  The order of a row's sum depends on K and NW alone, not on the vectors.  (Vectors asked for a slab ahead too take
+// 200 registers a lane, which halves the wavefronts on a CU: 28672 x 4096, one vector, 16.0 -> 22.6 us.)
+template <int NM> struct Q4Mats { const u32x4* codes[NM]; const uint32_t* scales[NM]; void* y[NM]; int32_t rows[NM]; const void* x; int32_t K, nb; };   // (few arguments: quick launches)
+
+template <typename T, int MODE, int NM, int NS, int NW>
+__global__ void __launch_bounds__(NW * 64) q4_matvec_kernel(Q4Mats<NM> a) {
     constexpr bool F32 = sizeof(T) == 4;
-    constexpr int NP = F32 ? 3 : 1;
+    constexpr int NP = F32 ? 3 : 1, OWN = MODE == Q4_SILU ? NS / 2 : NS;   // strips of one matrix (SiLU: half are gate rows, half the same up rows)
     __shared__ __attribute__((aligned(16))) float sred[NW][NS][16][20];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, kg = lane >> 4;
-    const int slabs = (int)((a.K + Q4_SLAB - 1) / Q4_SLAB), K = (int)a.K;
-    int64_t blk = blockIdx.x;
+    const int slabs = (a.K + Q4_SLAB - 1) / Q4_SLAB, K = a.K;
+    int blk = blockIdx.x;
     int which = 0;
-    if (MODE != Q4_SILU)
-        while (which < 2 && blk >= (a.rows[which] + 16 * NS - 1) / (16 * NS)) blk -= (a.rows[which++] + 16 * NS - 1) / (16 * NS);
+    if (MODE != Q4_SILU) {
+#pragma unroll
+        for (int i = 0; i + 1 < NM; ++i) {
+            const int n = (a.rows[i] + 16 * NS - 1) / (16 * NS);
+            if (which == i && blk >= n) { blk -= n; which = i + 1; }
+        }
+    }
     const u32x4* codes[NS];
     const uint32_t* scales[NS];
-    const int64_t last = (a.rows[which] + 15) / 16 - 1;
+    const int last = (a.rows[which] + 15) / 16 - 1;
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
-        const int64_t strip = MODE == Q4_SILU ? blk : blk * NS + s < last ? blk * NS + s : last;
-        const int m = MODE == Q4_SILU ? s : which;
-        codes[s] = (const u32x4*)a.codes[m] + strip * slabs * 256;
-        scales[s] = (const uint32_t*)a.scales[m] + strip * slabs * 64;
+        const int at = blk * OWN + s % OWN, m = MODE == Q4_SILU ? s / OWN : which;
+        const int64_t strip = at < last ? at : last;
+        codes[s] = a.codes[m] + strip * slabs * 256;
+        scales[s] = a.scales[m] + strip * slabs * 64;
     }
     const bool vec = l16 < a.nb;
-    const T* const x = (const T*)a.x + (int64_t)(vec ? l16 : 0) * K + kg * 32;
+    const T* const x = (const T*)a.x + (int64_t)(vec ? l16 : 0) * K + kg * 8;
     mfma_f32x4 acc[NS];
 #pragma unroll
     for (int s = 0; s < NS; ++s) acc[s] = mfma_f32x4{0.f, 0.f, 0.f, 0.f};
@@ -93,63 +107,53 @@ __global__ void __launch_bounds__(NW * 64) q4_matvec_kernel(Q4Args a) {
             sc[s] = sn[s];
         }
         const int k0 = slab * Q4_SLAB;
-        auto multiply = [&](int t, int i, const u32x4 (&xf)[NP]) {
-#pragma unroll
-            for (int s = 0; s < NS; ++s) {
-                const float scale = __uint_as_float(t == 0 ? sc[s] << 23 : t == 1 ? sc[s] << 15 : t == 2 ? sc[s] << 7 : sc[s] >> 1);
-                const u32x4 w = fp4_decode8_bf16(c[s][t][i], scale);
-#pragma unroll
-                for (int p = NP - 1; p >= 0; --p) acc[s] = mfma16(w, xf[p], acc[s]);
-            }
-        };
-        if constexpr (F32) {
-            if (slab + NW < slabs) load(slab + NW);
+        u32x4 xv[F32 ? 1 : 4][4];
+        if constexpr (!F32) {
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int k = t * 128 + 8 * i;
-                    const bool in = vec && k0 + kg * 32 + k < K;
-                    const f32x4* p = reinterpret_cast<const f32x4*>(x + k0 + k);
+                for (int i = 0; i < 4; ++i)
+                    xv[t][i] = vec && k0 + t * 128 + i * 32 + kg * 8 < K ? *reinterpret_cast<const u32x4*>(x + k0 + t * 128 + i * 32) : u32x4{0, 0, 0, 0};
+        }
+        if (slab + NW < slabs) load(slab + NW);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            uint32_t w4[NS];   // the tile's four scales of the lane's row, which lane 16 t + l16 has loaded
+#pragma unroll
+            for (int s = 0; s < NS; ++s) w4[s] = (uint32_t)__builtin_amdgcn_ds_bpermute((16 * t + l16) * 4, (int)sc[s]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                u32x4 xf[NP];
+                if constexpr (F32) {
+                    const int k = k0 + t * 128 + i * 32;
+                    const bool in = vec && k + kg * 8 < K;
+                    const f32x4* p = reinterpret_cast<const f32x4*>(x + k);
                     const f32x4 lo = in ? p[0] : f32x4{0.f, 0.f, 0.f, 0.f}, hi = in ? p[1] : f32x4{0.f, 0.f, 0.f, 0.f};
                     const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-                    u32x4 xf[NP];
                     bf16_parts<NP>(v, xf);
-                    multiply(t, i, xf);
+                } else xf[0] = xv[t][i];
+#pragma unroll
+                for (int s = 0; s < NS; ++s) {
+                    const u32x4 w = fp4_decode8_bf16(c[s][t][i], i == 0 ? fp4_scale_of<0>(w4[s]) : i == 1 ? fp4_scale_of<1>(w4[s]) : i == 2 ? fp4_scale_of<2>(w4[s]) : fp4_scale_of<3>(w4[s]));
+#pragma unroll
+                    for (int p = NP - 1; p >= 0; --p) acc[s] = mfma16(w, xf[p], acc[s]);
                 }
-        } else {
-            u32x4 xv[4][4];
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int k = t * 128 + 8 * i;
-                    xv[t][i] = vec && k0 + kg * 32 + k < K ? *reinterpret_cast<const u32x4*>(x + k0 + k) : u32x4{0, 0, 0, 0};
-                }
-            if (slab + NW < slabs) load(slab + NW);
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const u32x4 xf[NP] = {xv[t][i]};
-                    multiply(t, i, xf);
-                }
+            }
         }
     }
     // lane (vector l16, row group kg) holds rows 4 kg .. 4 kg + 3 of its strips
 #pragma unroll
     for (int s = 0; s < NS; ++s) *reinterpret_cast<mfma_f32x4*>(&sred[wave][s][l16][4 * kg]) = acc[s];
     __syncthreads();
-    constexpr int OUT = MODE == Q4_SILU ? 1 : NS;
-    for (int t = tid; t < OUT * 256; t += NW * 64) {
-        const int r = t & 15, s = (t >> 4) % OUT, b = t / (16 * OUT);
-        const int64_t row = (MODE == Q4_SILU ? blk : blk * NS + s) * 16 + r;
+    for (int t = tid; t < OWN * 256; t += NW * 64) {
+        const int r = t & 15, s = (t >> 4) % OWN, b = t / (16 * OWN);
+        const int64_t row = ((int64_t)blk * OWN + s) * 16 + r;
         if (b >= a.nb || row >= a.rows[which]) continue;
         float v = 0.f, u = 0.f;
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
             v += sred[w][s][b][r];
-            if (MODE == Q4_SILU) u += sred[w][NS - 1][b][r];
+            if (MODE == Q4_SILU) u += sred[w][NS - OWN + s][b][r];
         }
         const int64_t at = (int64_t)b * a.rows[which] + row;
         if (MODE == Q4_F32) ((float*)a.y[which])[at] = v;
@@ -160,30 +164,49 @@ __global__ void __launch_bounds__(NW * 64) q4_matvec_kernel(Q4Args a) {
     }
 }
 
-template <typename T>
-static hipError_t launch_q4_matvec_t(const Q4Args& a, hipStream_t s) {
-    constexpr int NW = 8;
-    auto blocks = [&](int ns) {
-        int64_t n = 0;
-        for (int i = 0; i < 3; ++i) n += (a.rows[i] + 16 * ns - 1) / (16 * ns);
-        return n;
-    };
-    const dim3 b(NW * 64);
-    if (a.mode == Q4_SILU) {
-        if (a.rows[0] > 0) q4_matvec_kernel<T, Q4_SILU, 2, NW><<<dim3((unsigned)((a.rows[0] + 15) / 16)), b, 0, s>>>(a);
-        return hipGetLastError();
+template <typename T, int MODE, int NM, int NS, int NW>
+static hipError_t launch_q4_matvec_n(const Q4Args& a, hipStream_t s) {
+    constexpr int OWN = MODE == Q4_SILU ? NS / 2 : NS;   // strips of one matrix
+    Q4Mats<NM> m{};
+    int64_t blocks = 0;
+    for (int i = 0; i < NM; ++i) {
+        m.codes[i] = (const u32x4*)a.codes[i]; m.scales[i] = (const uint32_t*)a.scales[i]; m.y[i] = a.y[i]; m.rows[i] = (int32_t)a.rows[i];
+        if (MODE != Q4_SILU || i == 0) blocks += (a.rows[i] + 16 * OWN - 1) / (16 * OWN);
     }
-    if (blocks(1) == 0) return hipSuccess;
-    const dim3 g((unsigned)blocks(1));
-    switch (a.mode) {
-        case Q4_STORE: q4_matvec_kernel<T, Q4_STORE, 1, NW><<<g, b, 0, s>>>(a); break;
-        case Q4_F32: q4_matvec_kernel<T, Q4_F32, 1, NW><<<g, b, 0, s>>>(a); break;
-        case Q4_RESID: q4_matvec_kernel<T, Q4_RESID, 1, NW><<<g, b, 0, s>>>(a); break;
-        default: return hipErrorInvalidValue;
-    }
+    m.x = a.x; m.K = (int32_t)a.K; m.nb = a.nb;
+    if (blocks == 0) return hipSuccess;
+    q4_matvec_kernel<T, MODE, NM, NS, NW><<<dim3((unsigned)blocks), dim3(NW * 64), 0, s>>>(m);
     return hipGetLastError();
 }
 
+template <typename T, int NS, int NW>
+static hipError_t launch_q4_matvec_m(const Q4Args& a, hipStream_t s) {
+    switch (a.mode) {
+        case Q4_STORE: return launch_q4_matvec_n<T, Q4_STORE, 1, NS, NW>(a, s);
+        case Q4_F32: return a.rows[1] || a.rows[2] ? launch_q4_matvec_n<T, Q4_F32, 3, NS, NW>(a, s) : launch_q4_matvec_n<T, Q4_F32, 1, NS, NW>(a, s);
+        case Q4_RESID: return launch_q4_matvec_n<T, Q4_RESID, 1, NS, NW>(a, s);
+        case Q4_SILU: return launch_q4_matvec_n<T, Q4_SILU, 2, (NS < 2 ? 2 : NS), NW>(a, s);
+        default: return hipErrorInvalidValue;
+    }
+}
+
+// How many strips a workgroup takes.  A launch costs 4 us before the codes stream at 6 TB/s, so few strips are spread over the chip, one or two
+// workgroups of eight wavefronts to a CU; of many, fewer and longer workgroups lose less on their ends, and several strips share what is read of the vectors,
+// which many vectors feel most.  bf16, us for 1 / 2 / 4 strips with 8, 8 / 4 wavefronts: 4096 x 4096, one vector 4.3 / 5.0 / 7.5, sixteen 6.7 / 7.4 / 9.9; 6144 rows 5.9 / 5.3 / 7.8
+// and 10.8 / 7.6 / 10.1; 8192 x 8192, sixteen 19.4 / 13.9 / 16.5; 12288 x 4096 8.8 / 9.2 / 8.6 (two strips, 4 wavefronts 8.5) and 14.7 / 14.1 / 10.9 (13.2);
+// 28672 x 4096 16.3 / 17.9 / 15.0 (14.7) and 30.6 / 27.8 / 18.7 (22.7); 128256 x 4096 58.6 / 66.2 / 46.5 (48.0) and 128 / 106 / 60.0 (79).
+// The number of wavefronts, and with it the order of a sum, goes by the matrices alone.
+template <typename T>
+static hipError_t launch_q4_matvec_t(const Q4Args& a, hipStream_t s) {
+    int64_t strips = 0;
+    for (int i = 0; i < 3; ++i) strips += (a.rows[i] + 15) / 16;
+    if (a.mode == Q4_SILU) strips = 2 * ((a.rows[0] + 15) / 16);
+    if (strips <= 256) return launch_q4_matvec_m<T, 1, 8>(a, s);
+    if (strips <= 512) return launch_q4_matvec_m<T, 2, 8>(a, s);
+    return a.nb <= 2 ? launch_q4_matvec_m<T, 2, 4>(a, s) : launch_q4_matvec_m<T, 4, 4>(a, s);
+}
+
+// a: Q4_STORE and Q4_RESID take one matrix, Q4_SILU two, Q4_F32 up to three
 hipError_t launch_q4_matvec(const Q4Args& a, bool bf16, hipStream_t s) {
     if (a.nb < 1 || a.nb > DECODE_MAX_BATCH) return hipErrorInvalidValue;
     return bf16 ? launch_q4_matvec_t<bf16_t>(a, s) : launch_q4_matvec_t<float>(a, s);

@@ -49,6 +49,19 @@ __device__ inline u32x4 fp4_decode8_bf16(uint32_t w, float scale) {
     return u32x4{fp4_pair_bf16<0>(w, scale), fp4_pair_bf16<1>(w, scale), fp4_pair_bf16<2>(w, scale), fp4_pair_bf16<3>(w, scale)};
 }
 
+// eight consecutive values of T that are read once
+template <typename T> __device__ inline void load8(const T* p, float (&v)[8]) {
+    if constexpr (sizeof(T) == 2) {
+        const u32x4 w = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+    } else {
+        const u32x4 a = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)), b = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p) + 1);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[i] = __uint_as_float(a[i]); v[4 + i] = __uint_as_float(b[i]); }
+    }
+}
+
 // ------------------------------------------------------------------ matrix cores
 typedef __bf16 mfma_bf16x8 __attribute__((ext_vector_type(8)));
 typedef float mfma_f32x4 __attribute__((ext_vector_type(4)));

@@ -336,8 +336,9 @@ hipError_t launch_argmax_rows(const float* logits, int V, int nrows, int32_t* to
 
 // ------------------------------------------------------------------ 4-bit matrices (spts_fp4.h has the form of the values)
 // Layout of a matrix [rows, K]: strips of 16 rows, each a sequence of 512-wide slabs of K (zeros beyond the matrix).  A slab is 4 tiles of 16 rows x
-// 128 k; a tile is 64 pieces of 16 bytes, piece 16 (k % 128 / 32) + row % 16 holding one block of 32 values, so that a wavefront's 16-byte load is a
-// tile and a lane holds one block of one row.  Scales: [strip][slab][piece][tile], four bytes a lane.
+// 128 k; a tile is 64 pieces of 16 bytes, piece 16 g + r of row r with the codes k = 32 i + 8 g .. + 7 of the tile in dword i, so that a wavefront's 16-byte
+// load is a tile and dword i is the lane's operand of the tile's i-th matrix instruction.  Scales: [strip][slab][tile][row][block], a dword of four
+// blocks for each row and tile.
 constexpr int Q4_SLAB = 512;
 inline int64_t q4_slabs(int64_t K) { return (K + Q4_SLAB - 1) / Q4_SLAB; }
 inline int64_t q4_code_bytes(int64_t rows, int64_t K) { return (rows + 15) / 16 * q4_slabs(K) * 4096; }
@@ -349,7 +350,7 @@ enum Q4Mode : int {
     Q4_RESID = 2,   // y[b, r] += W[r,:] . x[b,:]       (the element type)
     Q4_SILU = 3,    // y[b, r] = silu(W0[r,:] . x[b,:]) * (W1[r,:] . x[b,:])
 };
-// Up to three packed matrices of row length K that share the vectors x [nb, K]; y[i] [nb, rows[i]].  Q4_SILU: two matrices of rows[0] rows, y[0].
+// One packed matrix of row length K, or (Q4_F32) up to three that share the vectors x [nb, K]; y[i] [nb, rows[i]].  Q4_SILU: two matrices of rows[0] rows, y[0].
 struct Q4Args {
     const void* codes[3]; const void* scales[3]; void* y[3]; int64_t rows[3];
     const void* x; int64_t K; int nb; int mode;

@@ -50,7 +50,8 @@ def rounded(a, dtype):
 # ----------------------------------------------------------------------------------------------------------- matrices
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("rows,K,nb", [(1, 8, 1), (16, 32, 2), (17, 40, 3), (15, 512, 16), (64, 520, 5), (33, 688, 7), (100, 1032, 4), (48, 2048, 8),
-                                       (16, 4096, 1), (1003, 688, 16), (5, 18944, 9)])
+                                       (16, 4096, 1), (1003, 688, 16), (5, 18944, 9),
+                                       (4090, 520, 3), (4100, 1032, 1), (8200, 520, 2), (8216, 1544, 3)])
 def test_product_of_whole_numbers_is_exact(torch, dtype, rows, K, nb):
     """Grid values times small whole numbers: every sum is a multiple of 1/2 below 2^23 whatever its order, so each output has one
     right bit pattern, and a missed, doubled or misplaced term shows."""
@@ -391,12 +392,17 @@ def layer_for(torch, ctx, shape, seed):
     return dw, {n: back[n] if same[n] else np.ascontiguousarray(back[n].T) for n in back}
 
 
+# (D, H, Hkv, d, Dff): the rows of each product, in strips of 16, on either side of where the kernels change
+LAYERS = [(256, 4, 2, 64, 688), (64, 64, 16, 128, 8704), (4224, 4, 2, 32, 64), (8320, 4, 2, 32, 64), (64, 48, 6, 128, 2104)]
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("nseq", [1, 2, 5, 16])
-def test_decode_layer_lockstep(torch, dtype, nseq):
+@pytest.mark.parametrize("nseq,dims", [(1, 0), (2, 0), (5, 0), (16, 0), (1, 1), (3, 1), (2, 2), (2, 3), (3, 3), (4, 4)])
+def test_decode_layer_lockstep(torch, dtype, nseq, dims):
     """Caches of different lengths filled from random pairs, three steps of the layer: the appended pair against the oracle's (to the
     element type's rounding, then one of 4 bits), the state against the oracle's over the pairs as stored."""
-    ctx, shape = ctx_for(dtype)
+    D, heads, Hkv, d, Dff = LAYERS[dims]
+    ctx, shape = ctx_for(dtype, H=heads, Hkv=Hkv, d=d, D=D, Dff=Dff)
     mdl, rnd, tol = H.oracle_model(shape), H.rnd_for(dtype), H.TOL[dtype]["hidden"]
     rng = np.random.default_rng(nseq)
     dw, w = layer_for(torch, ctx, shape, 31)
