@@ -442,13 +442,14 @@ static hipError_t launch_kv4_attn_n(const T* q, const Kv4Batch& kb, int64_t per,
 
 template <typename T, int D>
 static hipError_t launch_kv4_attn_t(const T* q, const Kv4Batch& kb, int H, int Hkv, float* part, size_t part_floats, T* out, hipStream_t s) {
-    constexpr int WIDE = sizeof(T) == 4 ? 8 : 16;   // wavefronts that a CU's registers hold
+    constexpr int WIDE = sizeof(T) == 4 && D == 128 ? 8 : 16;   // wavefronts that a CU's registers hold
+    constexpr int SHORT = WIDE * 64;
     int64_t total = 0, longest = 1;
     for (int b = 0; b < kb.n; ++b) { total += kb.count[b]; longest = kb.count[b] > longest ? kb.count[b] : longest; }
     // short caches whole, by one wide workgroup each: no second launch
-    if (longest <= WIDE * 64) {
-        return kb.n == 1 ? launch_kv4_attn_n<T, D, WIDE, 1>(q, kb, WIDE * 64, H, Hkv, part, out, s)
-                         : launch_kv4_attn_n<T, D, WIDE, DECODE_MAX_BATCH>(q, kb, WIDE * 64, H, Hkv, part, out, s);
+    if (longest <= SHORT) {
+        return kb.n == 1 ? launch_kv4_attn_n<T, D, WIDE, 1>(q, kb, SHORT, H, Hkv, part, out, s)
+                         : launch_kv4_attn_n<T, D, WIDE, DECODE_MAX_BATCH>(q, kb, SHORT, H, Hkv, part, out, s);
     }
     // shares of equal length over all sequences: as many as make two workgroups per CU over all heads, none below 128 keys
     int64_t per = (total * Hkv + 511) / 512;

@@ -17,41 +17,37 @@ __device__ inline Best wave_best(Best a) {
 constexpr uint32_t IN_PROMPT = 0x80000000u;
 }  // namespace
 
-// A workgroup owns LOGITS_TILE words of one sequence, four of them a thread: their logits, biases and mask words are asked for first, then it goes over the
-// sequence's whole history (a few hundred KB at most, from the caches for all workgroups but one) and counts the ids that are its own in LDS; integers, so
-// the order does not matter.  No table of counts is kept between calls or cleared in memory.
-constexpr int LT = 1024, LW = LOGITS_TILE / LT;   // threads, words of each
-__global__ void __launch_bounds__(LT) process_logits_kernel(const float* in, int V, LogitsRules r, float* out, Best* __restrict__ part) {
-    __shared__ uint32_t cnt[LOGITS_TILE];
+// A kernel's view of up to NB sequences' rules (few arguments make quick launches, hence one for a single sequence)
+template <int NB> struct Rules {
+    const int32_t* history; int64_t history_stride; const float* bias; int64_t bias_stride; const uint32_t* mask; int64_t mask_stride;
+    int32_t len[NB], prompt[NB];
+    float repetition[NB], frequency[NB], presence[NB];
+};
+
+// A workgroup owns 1024 LW words of one sequence: their logits, biases and mask words are asked for first, then it goes over the sequence's whole history (a few
+// hundred KB at most, from the caches for all workgroups but one) and counts the ids that are its own in LDS; integers, so the order does not matter.  No
+// table of counts is kept between calls or cleared in memory.  ONE: the workgroup has all words of a sequence without a history, and chooses the token itself.
+constexpr int LT = 1024;
+template <typename T, int LW, int NB, bool ONE>
+__global__ void __launch_bounds__(LT) process_logits_kernel(const float* in, int V, Rules<NB> r, float* out, Best* __restrict__ part, int32_t* __restrict__ token,
+                                                            const T* __restrict__ table, int D, T* __restrict__ x_next) {
+    __shared__ uint32_t cnt[ONE ? 1 : LT * LW];
     __shared__ Best sb[LT / 64];
-    const int b = blockIdx.y, tid = threadIdx.x, v0 = (int)blockIdx.x * LOGITS_TILE;
-    const int n = V - v0 < LOGITS_TILE ? V - v0 : LOGITS_TILE;
+    const int b = blockIdx.y, rb = NB > 1 ? b : 0, tid = threadIdx.x, v0 = (int)blockIdx.x * (LT * LW);
+    const int n = V - v0 < LT * LW ? V - v0 : LT * LW;
     const int64_t row = (int64_t)b * V + v0;
-    float x[LW], bias[LW];
-    uint32_t word[LW];
+    float x[LW];
 #pragma unroll
     for (int j = 0; j < LW; ++j) {
         const int i = tid + j * LT;
         x[j] = i < n ? in[row + i] : 0.f;
-        bias[j] = 0.f;
-        word[j] = ~0u;
     }
-    if (r.bias) {
-#pragma unroll
-        for (int j = 0; j < LW; ++j)
-            if (tid + j * LT < n) bias[j] = r.bias[b * r.bias_stride + v0 + tid + j * LT];
-    }
-    if (r.mask) {
-#pragma unroll
-        for (int j = 0; j < LW; ++j)
-            if (tid + j * LT < n) word[j] = r.mask[b * r.mask_stride + (uint32_t)(v0 + tid + j * LT) / 32];
-    }
-    if (r.history) {
+    if (!ONE && r.history) {
 #pragma unroll
         for (int j = 0; j < LW; ++j) cnt[tid + j * LT] = 0;
         __syncthreads();
         const int32_t* const ids = r.history + b * r.history_stride;
-        const int len = (int)r.len[b], prompt = (int)(r.prompt[b] < len ? r.prompt[b] : len);
+        const int len = r.len[rb], prompt = r.prompt[rb];
         auto count = [&](int32_t id, int at) {
             const uint32_t w = (uint32_t)id - (uint32_t)v0;
             if (w < (uint32_t)n) {
@@ -76,7 +72,7 @@ __global__ void __launch_bounds__(LT) process_logits_kernel(const float* in, int
                 for (int e = 0; e < 4; ++e) count((int32_t)w[u][e], head + 4 * (i0 + u * LT) + e);
         }
         __syncthreads();
-        const float rep = r.repetition[b], freq = r.frequency[b], pres = r.presence[b];
+        const float rep = r.repetition[rb], freq = r.frequency[rb], pres = r.presence[rb];
 #pragma unroll
         for (int j = 0; j < LW; ++j) {
             const uint32_t c = cnt[tid + j * LT], said = c & ~IN_PROMPT;
@@ -87,23 +83,43 @@ __global__ void __launch_bounds__(LT) process_logits_kernel(const float* in, int
             }
         }
     }
+    if (r.bias) {
+        const float* const bias = r.bias + b * r.bias_stride + v0;
+#pragma unroll
+        for (int j = 0; j < LW; ++j) x[j] = x[j] + (tid + j * LT < n ? bias[tid + j * LT] : 0.f);
+    }
+    uint32_t word[LW];
+#pragma unroll
+    for (int j = 0; j < LW; ++j) word[j] = ~0u;
+    if (r.mask) {
+        const uint32_t* const mask = r.mask + b * r.mask_stride + v0 / 32;   // (v0 is a multiple of 32)
+#pragma unroll
+        for (int j = 0; j < LW; ++j)
+            if (tid + j * LT < n) word[j] = mask[(tid + j * LT) / 32];
+    }
     Best best{-INFINITY, NONE};
 #pragma unroll
     for (int j = 0; j < LW; ++j) {
         const int i = tid + j * LT;
-        if (r.bias) x[j] = x[j] + bias[j];   // (without a bias -0 stays -0)
-        const bool allowed = i < n && (word[j] >> ((v0 + i) & 31) & 1u) != 0;
+        const bool allowed = i < n && (word[j] >> (i & 31) & 1u) != 0;
         x[j] = allowed ? x[j] : -INFINITY;
         if (i < n) out[row + i] = x[j];
         best = better(best, Best{x[j], allowed ? v0 + i : NONE});
     }
-    if (!part) return;
+    if (ONE ? !token : !part) return;
     best = wave_best(best);
     if ((tid & 63) == 0) sb[tid >> 6] = best;
     __syncthreads();
-    if (tid >= 64) return;
-    best = wave_best(tid < LT / 64 ? sb[tid] : Best{-INFINITY, NONE});
-    if (tid == 0) part[(int64_t)b * gridDim.x + blockIdx.x] = best;
+    if (!ONE && tid >= 64) return;
+    best = wave_best((tid & 63) < LT / 64 ? sb[tid & 63] : Best{-INFINITY, NONE});
+    if (!ONE) {
+        if (tid == 0) part[(int64_t)b * gridDim.x + blockIdx.x] = best;
+        return;
+    }
+    const int tok = best.i == NONE ? -1 : best.i;
+    if (tid == 0) token[b] = tok;
+    if (x_next)
+        for (int i = tid; i < D; i += LT) x_next[(int64_t)b * D + i] = tok < 0 ? T{} : table[(int64_t)tok * D + i];
 }
 
 template <typename T>
@@ -125,19 +141,44 @@ __global__ void __launch_bounds__(1024) pick_token_kernel(const Best* __restrict
     for (int i = threadIdx.x; i < D; i += blockDim.x) x_next[(int64_t)b * D + i] = stok < 0 ? T{} : table[(int64_t)stok * D + i];
 }
 
-size_t logits_scratch_bytes(int V, int nrows) { return (size_t)((V + LOGITS_TILE - 1) / LOGITS_TILE) * nrows * sizeof(Best); }
+// Words of a thread: without a history 32 where that makes one workgroup per sequence and saves the second launch (us for one sequence of 4000 / 32000 words 7.7 -> 6.7,
+// 7.8 -> 7.2; with a history of 500 ids 8.1 -> 11.0, of 32768 9.7 -> 15.9), otherwise 4, so that the words are spread over the chip (16 sequences of
+// 128256 words, histories of up to 32768 ids: 2 / 4 / 8 / 16 words 16.9 / 13.4 / 13.1 / 14.8; one sequence 8.4 / 8.9 / 9.8 / 12.0)
+constexpr int LW_ONE = 32, LW_MANY = 4;
+
+size_t logits_scratch_bytes(int V, int nrows) { return (size_t)((V + LT * LW_MANY - 1) / (LT * LW_MANY)) * nrows * sizeof(Best); }
+
+template <typename T, int NB>
+static hipError_t launch_process_logits_n(const float* in, int V, int nrows, const LogitsRules& r, float* out, int32_t* token, const T* table, int D, T* x_next,
+                                          Best* part, hipStream_t s) {
+    Rules<NB> d{r.history, r.history_stride, r.bias, r.bias_stride, r.mask, r.mask_stride, {}, {}, {}, {}, {}};
+    for (int b = 0; b < nrows; ++b) {
+        d.len[b] = (int32_t)r.len[b]; d.prompt[b] = (int32_t)(r.prompt[b] < r.len[b] ? r.prompt[b] : r.len[b]);
+        d.repetition[b] = r.repetition[b]; d.frequency[b] = r.frequency[b]; d.presence[b] = r.presence[b];
+    }
+    if (V <= LT * LW_ONE && !r.history) {
+        process_logits_kernel<T, LW_ONE, NB, true><<<dim3(1, (unsigned)nrows), dim3(LT), 0, s>>>(in, V, d, out, nullptr, token, table, D, x_next);
+        return hipGetLastError();
+    }
+    const int nparts = (V + LT * LW_MANY - 1) / (LT * LW_MANY);
+    process_logits_kernel<T, LW_MANY, NB, false><<<dim3((unsigned)nparts, (unsigned)nrows), dim3(LT), 0, s>>>(
+        in, V, d, out, token ? part : nullptr, nullptr, nullptr, 0, nullptr);
+    if (token) pick_token_kernel<T><<<dim3((unsigned)nrows), dim3(x_next ? 1024 : 64), 0, s>>>(part, nparts, token, table, D, x_next);
+    return hipGetLastError();
+}
+
+template <typename T>
+static hipError_t launch_process_logits_t(const float* in, int V, int nrows, const LogitsRules& r, float* out, int32_t* token, const T* table, int D, T* x_next,
+                                          Best* part, hipStream_t s) {
+    return nrows == 1 ? launch_process_logits_n<T, 1>(in, V, nrows, r, out, token, table, D, x_next, part, s)
+                      : launch_process_logits_n<T, DECODE_MAX_BATCH>(in, V, nrows, r, out, token, table, D, x_next, part, s);
+}
 
 hipError_t launch_process_logits(const float* in, int V, int nrows, const LogitsRules& r, float* out, int32_t* token, const void* table, int D,
                                  void* x_next, bool bf16, void* scratch, hipStream_t s) {
-    const int nparts = (V + LOGITS_TILE - 1) / LOGITS_TILE;
-    Best* part = token ? (Best*)scratch : nullptr;
-    process_logits_kernel<<<dim3((unsigned)nparts, (unsigned)nrows), dim3(LT), 0, s>>>(in, V, r, out, part);
-    if (token) {
-        const dim3 g((unsigned)nrows), t(x_next ? 1024 : 64);
-        if (bf16) pick_token_kernel<bf16_t><<<g, t, 0, s>>>(part, nparts, token, (const bf16_t*)table, D, (bf16_t*)x_next);
-        else pick_token_kernel<float><<<g, t, 0, s>>>(part, nparts, token, (const float*)table, D, (float*)x_next);
-    }
-    return hipGetLastError();
+    if (nrows < 1 || nrows > DECODE_MAX_BATCH) return hipErrorInvalidValue;
+    return bf16 ? launch_process_logits_t<bf16_t>(in, V, nrows, r, out, token, (const bf16_t*)table, D, (bf16_t*)x_next, (Best*)scratch, s)
+                : launch_process_logits_t<float>(in, V, nrows, r, out, token, (const float*)table, D, (float*)x_next, (Best*)scratch, s);
 }
 
 }  // namespace spts

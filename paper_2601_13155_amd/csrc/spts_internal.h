@@ -378,8 +378,7 @@ struct LogitsRules {
     int64_t len[DECODE_MAX_BATCH]; int64_t prompt[DECODE_MAX_BATCH];
     float repetition[DECODE_MAX_BATCH], frequency[DECODE_MAX_BATCH], presence[DECODE_MAX_BATCH];
 };
-// token (may be NULL, and x_next with it): scratch of LOGITS_SCRATCH_BYTES
-constexpr int LOGITS_TILE = 4096;
+// token (may be NULL, and x_next with it): scratch of logits_scratch_bytes
 size_t logits_scratch_bytes(int V, int nrows);
 hipError_t launch_process_logits(const float* in, int V, int nrows, const LogitsRules& r, float* out, int32_t* token, const void* table, int D,
                                  void* x_next, bool bf16, void* scratch, hipStream_t s);

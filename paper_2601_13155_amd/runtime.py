@@ -4,6 +4,7 @@ Marshalling and sequencing only: every arithmetic step of the path runs inside l
 """
 from __future__ import annotations
 
+import ctypes
 from typing import Dict, List, Optional
 
 import numpy as np
@@ -246,14 +247,14 @@ class KV4Batch:
             self.tensors.append(t)
             s.k, s.v, s.k_scale, s.v_scale, s.pos = (x.data_ptr() for x in t)
             s.capacity = cap
+        self._empty = bytes(self.structs)
 
     @property
     def counts(self) -> List[int]:
         return [int(s.count) for s in self.structs]
 
     def clear(self):
-        for s in self.structs:
-            s.count = 0
+        ctypes.memmove(self.structs, self._empty, len(self._empty))
 
     def append_cache(self, ctx: binding.Context, b: int, cache: "KVCache"):
         """Appends every pair of a prefill's cache to sequence b's."""
@@ -278,7 +279,6 @@ class LogitsRules:
 
     def __init__(self, batch: int, history=None, history_len=None, prompt_len=None, repetition=None, frequency=None, presence=None,
                  bias=None, mask=None):
-        import ctypes as C
         self.struct = s = binding.spts_logits_rules()
         self._keepalive = (history, bias, mask)
 
@@ -300,8 +300,8 @@ class LogitsRules:
             if any(n > history.shape[1] for n in history_len):
                 raise ValueError("history_len exceeds the history's rows")
             s.history, s.history_stride = history.data_ptr(), history.shape[1]
-        self.history_len, self.prompt_len = host(history_len, C.c_int64), host(prompt_len, C.c_int64)
-        self.repetition, self.frequency, self.presence = (host(v, C.c_float) for v in (repetition, frequency, presence))
+        self.history_len, self.prompt_len = host(history_len, ctypes.c_int64), host(prompt_len, ctypes.c_int64)
+        self.repetition, self.frequency, self.presence = (host(v, ctypes.c_float) for v in (repetition, frequency, presence))
         for name in ("history_len", "prompt_len", "repetition", "frequency", "presence"):
             if getattr(self, name) is not None:
                 setattr(s, name, getattr(self, name))
