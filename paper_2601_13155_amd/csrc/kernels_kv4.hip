@@ -128,8 +128,7 @@ __global__ void __launch_bounds__(256) kv4_read_kernel(Kv4Rows<NB> kb, T* __rest
     store8(v + (row * Hkv + g) * D + 8 * c, f);
 }
 
-template <typename T, int D, int NB>
-static hipError_t launch_kv4_rows_n(const T* k, const T* v, const int32_t* pos, T* k_out, T* v_out, const Kv4Batch& kb, int Hkv, hipStream_t s) {
+template <int NB> static Kv4Rows<NB> rows_of(const Kv4Batch& kb) {
     Kv4Rows<NB> r{};
     for (int b = 0; b < NB; ++b) {
         const int i = b < kb.n ? b : kb.n - 1;
@@ -137,6 +136,12 @@ static hipError_t launch_kv4_rows_n(const T* k, const T* v, const int32_t* pos, 
         r.cap[b] = (int32_t)kb.cap[i]; r.at[b] = (int32_t)kb.count[i]; r.end[b] = (int32_t)kb.off[i + 1];
     }
     r.rows = (int32_t)kb.off[kb.n];
+    return r;
+}
+
+template <typename T, int D, int NB>
+static hipError_t launch_kv4_rows_n(const T* k, const T* v, const int32_t* pos, T* k_out, T* v_out, const Kv4Batch& kb, int Hkv, hipStream_t s) {
+    const Kv4Rows<NB> r = rows_of<NB>(kb);
     const dim3 g((unsigned)((r.rows + 2048 / D - 1) / (2048 / D)), (unsigned)Hkv), t(256);
     if (k) kv4_append_kernel<T, D, NB><<<g, t, 0, s>>>(k, v, pos, r, Hkv);
     else kv4_read_kernel<T, D, NB><<<g, t, 0, s>>>(r, k_out, v_out, Hkv);
@@ -166,6 +171,96 @@ hipError_t launch_kv4_append(const void* k, const void* v, const int32_t* pos, c
 
 hipError_t launch_kv4_read(const Kv4Batch& kb, void* k, void* v, int Hkv, int d, bool bf16, hipStream_t s) {
     return bf16 ? launch_kv4_rows_t<bf16_t>(nullptr, nullptr, nullptr, k, v, kb, Hkv, d, s) : launch_kv4_rows_t<float>(nullptr, nullptr, nullptr, k, v, kb, Hkv, d, s);
+}
+
+// The pairs of one new token per sequence, from the projections' fp32 sums q32 [n, H, D], k32 / v32 [n, Hkv, D]: queries and keys are rotated, everything is rounded to T
+// once, keys and values then go into the caches (blockIdx.y = sequence).  A thread has the dimensions j and j + D / 2 of a head, 32 lanes a block of each half (both halves
+// one block for D = 32); neighbours share a byte.  The angle is formed in fp64, as everywhere here.
+template <int NB> struct Kv4Tokens { Kv4Rows<NB> rows; int32_t pos[NB]; double neg2_over_d_log2base; };
+template <typename T, int D, int NB>
+__global__ void __launch_bounds__(256) kv4_rope_append_kernel(const float* __restrict__ q32, const float* __restrict__ k32, const float* __restrict__ v32, T* __restrict__ q,
+                                                              int H, int Hkv, Kv4Tokens<NB> tk) {
+    constexpr int HALF = D / 2, PB = D / 32;
+    const int b = NB > 1 ? (int)blockIdx.y : 0, i = blockIdx.x * 256 + threadIdx.x, j = i % HALF;
+    int head = i / HALF;
+    if (i == 0) tk.rows.pos[b][tk.rows.at[b]] = tk.pos[b];
+    if (head >= H + 2 * Hkv) return;                  // (whole heads: the lanes of a block leave together)
+    const bool is_q = head < H, is_v = head >= H + Hkv;
+    head -= is_q ? 0 : is_v ? H + Hkv : H;
+    const float* src = (is_q ? q32 + (int64_t)b * H * D : (is_v ? v32 : k32) + (int64_t)b * Hkv * D) + (int64_t)head * D + j;
+    float x0 = src[0], x1 = src[HALF];
+    if (!is_v) {
+        double sn, cs;
+        sincos((double)tk.pos[b] * exp2((double)j * tk.neg2_over_d_log2base), &sn, &cs);
+        const float c = (float)cs, s = (float)sn, r0 = x0 * c - x1 * s;
+        x1 = x1 * c + x0 * s;
+        x0 = r0;
+    }
+    const T t0 = from_f32<T>(x0), t1 = from_f32<T>(x1);
+    if (is_q) {
+        T* to = q + ((int64_t)b * H + head) * D + j;
+        to[0] = t0;
+        to[HALF] = t1;
+    }
+    x0 = to_f32(t0); x1 = to_f32(t1);
+    uint32_t top0 = __float_as_uint(x0) & 0x7fffffffu, top1 = __float_as_uint(x1) & 0x7fffffffu;
+    if (D == 32) top0 = top1 = top0 > top1 ? top0 : top1;
+#pragma unroll
+    for (int off = 1; off < (D == 32 ? 16 : 32); off <<= 1) {
+        const uint32_t o0 = (uint32_t)__shfl_xor((int)top0, off), o1 = (uint32_t)__shfl_xor((int)top1, off);
+        top0 = o0 > top0 ? o0 : top0;
+        top1 = o1 > top1 ? o1 : top1;
+    }
+    const float n0 = __shfl_xor(x0, 1), n1 = __shfl_xor(x1, 1);
+    if (is_q || (j & 1)) return;
+    const uint32_t byte0 = fp4_scale_byte(top0), byte1 = fp4_scale_byte(top1);
+    const uint32_t c0 = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, x0, n0, __uint_as_float(byte0 << 23), 0);
+    const uint32_t c1 = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, x1, n1, __uint_as_float(byte1 << 23), 0);
+    const int64_t cap = tk.rows.cap[b], key = tk.rows.at[b];
+    const int p0 = j / 2, p1 = (j + HALF) / 2;        // bytes of the row
+    if (!is_v) {
+        char* const to = tk.rows.k[b] + key_at(head, cap, key, D);
+        to[p0] = (char)c0;
+        to[p1] = (char)c1;
+    } else {
+        tk.rows.v[b][value_at(head, cap, key, p0 / PB, D) + p0 % PB] = (char)c0;
+        tk.rows.v[b][value_at(head, cap, key, p1 / PB, D) + p1 % PB] = (char)c1;
+    }
+    if (j % 32 == 0) {
+        uint8_t* const to = is_v ? tk.rows.vs[b] : tk.rows.ks[b];
+        const int b0 = j / 32, b1 = (j + HALF) / 32;
+        to[is_v ? value_scale_at(head, cap, key, b0, D) : key_scale_at(head, cap, key, b0, D)] = (uint8_t)byte0;
+        if (D > 32) to[is_v ? value_scale_at(head, cap, key, b1, D) : key_scale_at(head, cap, key, b1, D)] = (uint8_t)byte1;
+    }
+}
+
+template <typename T, int D, int NB>
+static hipError_t launch_kv4_rope_append_n(const float* q32, const float* k32, const float* v32, void* q, int H, int Hkv, float base, const Kv4Batch& kb, const int32_t* pos,
+                                           hipStream_t s) {
+    Kv4Tokens<NB> tk{rows_of<NB>(kb), {}, -2.0 / (double)D * log2((double)base)};
+    for (int b = 0; b < kb.n; ++b) tk.pos[b] = pos[b];
+    kv4_rope_append_kernel<T, D, NB><<<dim3((unsigned)(((H + 2 * Hkv) * (D / 2) + 255) / 256), (unsigned)kb.n), dim3(256), 0, s>>>(q32, k32, v32, (T*)q, H, Hkv, tk);
+    return hipGetLastError();
+}
+
+template <typename T>
+static hipError_t launch_kv4_rope_append_t(const float* q32, const float* k32, const float* v32, void* q, int H, int Hkv, int d, float base, const Kv4Batch& kb,
+                                           const int32_t* pos, hipStream_t s) {
+#define SPTS_KV4_ROPE(D_)                                                                                                                          \
+    return kb.n == 1 ? launch_kv4_rope_append_n<T, D_, 1>(q32, k32, v32, q, H, Hkv, base, kb, pos, s)                                              \
+                     : launch_kv4_rope_append_n<T, D_, DECODE_MAX_BATCH>(q32, k32, v32, q, H, Hkv, base, kb, pos, s);
+    switch (d) {
+        case 128: SPTS_KV4_ROPE(128)
+        case 64: SPTS_KV4_ROPE(64)
+        case 32: SPTS_KV4_ROPE(32)
+        default: return hipErrorInvalidValue;
+    }
+#undef SPTS_KV4_ROPE
+}
+
+hipError_t launch_kv4_rope_append(const float* q32, const float* k32, const float* v32, void* q, int H, int Hkv, int d, float base, const Kv4Batch& kb, const int32_t* pos,
+                                  bool bf16, hipStream_t s) {
+    return bf16 ? launch_kv4_rope_append_t<bf16_t>(q32, k32, v32, q, H, Hkv, d, base, kb, pos, s) : launch_kv4_rope_append_t<float>(q32, k32, v32, q, H, Hkv, d, base, kb, pos, s);
 }
 
 // ------------------------------------------------------------------------------------------------- attention

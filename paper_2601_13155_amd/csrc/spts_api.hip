@@ -1482,7 +1482,6 @@ int spts_decode_layer_q4(spts_ctx* c, void* x, const int32_t* pos, int32_t batch
     void* q = c->p<void>(c->off.q);
     void* att = c->p<void>(c->off.att);
     void* hbuf = c->p<void>(c->off.big);
-    const size_t eb = c->bf16 ? 2 : 4;
     hipStream_t st = c->stream;
     auto args = [&](const spts_q4& a, const void* in, void* out, int mode) {
         Q4Args g{};
@@ -1495,18 +1494,7 @@ int spts_decode_layer_q4(spts_ctx* c, void* x, const int32_t* pos, int32_t batch
     also(qkv, 1, w->Wk, k32);
     also(qkv, 2, w->Wv, v32);
     { PHASE(c, PH_DEC_QKV); SPTS_HIP(c, launch_q4_matvec(qkv, c->bf16, st)); }
-    {   // the new pairs, rotated and rounded to the element type, as rows of one each, then into the caches
-        PHASE(c, PH_DEC_ROPE_APPEND);
-        DecodeBatch db{};
-        db.n = batch;
-        for (int b = 0; b < batch; ++b) {
-            db.cache_k[b] = c->p<char>(c->off.khat) + b * KV * eb; db.cache_v[b] = c->p<char>(c->off.vhat) + b * KV * eb;
-            db.cache_pos[b] = c->p<int32_t>(c->off.posA) + b; db.pos[b] = pos[b];
-            kb.off[b + 1] = b + 1;
-        }
-        SPTS_HIP(c, launch_decode_rope_append_batched(q32, k32, v32, q, m.H, m.Hkv, m.d, m.rope_base, db, c->bf16, st));
-        SPTS_HIP(c, launch_kv4_append(c->p<void>(c->off.khat), c->p<void>(c->off.vhat), c->p<int32_t>(c->off.posA), kb, m.Hkv, m.d, c->bf16, st));
-    }
+    { PHASE(c, PH_DEC_ROPE_APPEND); SPTS_HIP(c, launch_kv4_rope_append(q32, k32, v32, q, m.H, m.Hkv, m.d, m.rope_base, kb, pos, c->bf16, st)); }
     for (int b = 0; b < batch; ++b) kb.count[b] += 1;
     { PHASE(c, PH_DEC_ATTN);
       SPTS_HIP(c, launch_kv4_attn(q, kb, m.H, m.Hkv, m.d, c->p<float>(c->off.tmp32), (c->off.qp - c->off.tmp32) / sizeof(float), att, c->bf16, st)); }

@@ -369,6 +369,9 @@ struct Kv4Batch {
 // rows off[b] .. off[b + 1] of k, v [.., Hkv, d] and pos into rows count[b] .. of cache b; and back
 hipError_t launch_kv4_append(const void* k, const void* v, const int32_t* pos, const Kv4Batch& kb, int Hkv, int d, bool bf16, hipStream_t s);
 hipError_t launch_kv4_read(const Kv4Batch& kb, void* k, void* v, int Hkv, int d, bool bf16, hipStream_t s);
+// one new token per sequence, at position pos[b]: q [n, H, d] rotated, its rotated key and its value into row count[b] of cache b, from the projections' fp32 sums
+hipError_t launch_kv4_rope_append(const float* q32, const float* k32, const float* v32, void* q, int H, int Hkv, int d, float base, const Kv4Batch& kb, const int32_t* pos,
+                                  bool bf16, hipStream_t s);
 // out [n, H, d] = softmax(q k^T / sqrt(d)) v over the first count[b] pairs of cache b (zeros where count is 0); part: fp32 scratch
 hipError_t launch_kv4_attn(const void* q, const Kv4Batch& kb, int H, int Hkv, int d, float* part, size_t part_floats, void* out, bool bf16, hipStream_t s);
 
