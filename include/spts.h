@@ -304,7 +304,8 @@ typedef struct {
     void *codes, *scales;
     int64_t rows, K;
 } spts_q4;
-/* Bytes of the two buffers.  SPTS_EINVAL on rows or K < 1 or a NULL pointer, SPTS_ESHAPE on K % 8 != 0 or K >= 2^31. */
+/* Bytes of the two buffers.  SPTS_EINVAL on rows or K < 1 or a NULL pointer, SPTS_ESHAPE on K % 8 != 0, K > 2^30 or
+ * rows > 2^28 (as for the calls that take such a matrix). */
 int spts_q4_bytes(int64_t rows, int64_t K, size_t *code_bytes, size_t *scale_bytes);
 /* Packs W [out->rows, out->K] of the context's element type (device, row-major, 16-byte aligned) into out's buffers. */
 int spts_q4_pack(spts_ctx *ctx, const void *W, const spts_q4 *out);
@@ -347,8 +348,7 @@ typedef struct {
 } spts_layer_q4;
 /* spts_decode_layer_batched with weights and caches in 4 bits: one new token for each of `batch` sequences, x [batch, D]
  * in/out, pos HOST [batch].  The new pair is rounded to the element type, then stored in 4 bits, and attended to as stored.
- * Every row of x is treated alike whatever the batch.  D, H * d and Dff multiples of 8, d and H / Hkv as in
- * spts_kv4_attn, count < capacity. */
+ * D, H * d and Dff multiples of 8, d and H / Hkv as in spts_kv4_attn, count < capacity, distinct caches. */
 int spts_decode_layer_q4(spts_ctx *ctx, void *x, const int32_t *pos, int32_t batch, const spts_layer_q4 *w,
                          spts_kv4 *caches);
 /* RMSNorm with gamma [D] of x [batch, D] into xn [batch, D] (element type; batch <= SPTS_MAX_DECODE_BATCH): the
@@ -375,7 +375,7 @@ typedef struct {
  * be logits itself).  token_out [batch] (NULL = not wanted): the allowed word with the largest result, ties to the lowest
  * id; -1 where no word is allowed (or all that are allowed are NaN); a masked NaN or infinity does not matter.
  * x_next [batch, D] (NULL = not wanted; needs token_out and table [V, D]): row token of the table, zeros for -1.
- * batch <= SPTS_MAX_DECODE_BATCH.  spts_greedy_token_batched's logits_out are such logits. */
+ * batch <= SPTS_MAX_DECODE_BATCH, V <= 2^28.  spts_greedy_token_batched's logits_out are such logits. */
 int spts_process_logits(spts_ctx *ctx, const float *logits, int32_t V, int32_t batch, const spts_logits_rules *rules,
                         float *logits_out, int32_t *token_out, const void *table, void *x_next);
 

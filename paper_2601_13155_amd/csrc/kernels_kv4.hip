@@ -19,7 +19,7 @@ template <int NB> struct Kv4Rows {
     uint8_t *ks[NB], *vs[NB];
     int32_t* pos[NB];
     int32_t cap[NB], at[NB], end[NB];   // capacity, cache row of the sequence's first row, its end among the call's rows
-    int32_t rows;
+    int32_t row0, rows;                 // rows of this launch
 };
 template <int NB> struct Kv4Caches {
     const char *k[NB], *v[NB];
@@ -63,7 +63,7 @@ template <typename T, int D, int NB>
 __global__ void __launch_bounds__(256) kv4_append_kernel(const T* __restrict__ k, const T* __restrict__ v, const int32_t* __restrict__ pos, Kv4Rows<NB> kb, int Hkv) {
     constexpr int CH = D / 8, PB = D / 32;   // threads of a row, bytes of a piece of values
     const int g = blockIdx.y, c = threadIdx.x % CH;
-    const int64_t row = (int64_t)blockIdx.x * (256 / CH) + threadIdx.x / CH;
+    const int64_t row = kb.row0 + (int64_t)blockIdx.x * (256 / CH) + threadIdx.x / CH;
     if (row >= kb.rows) return;         // (whole quads)
     const T* const ks = k + (row * Hkv + g) * D + 8 * c;
     const T* const vs = v + (row * Hkv + g) * D + 8 * c;
@@ -109,7 +109,7 @@ template <typename T, int D, int NB>
 __global__ void __launch_bounds__(256) kv4_read_kernel(Kv4Rows<NB> kb, T* __restrict__ k, T* __restrict__ v, int Hkv) {
     constexpr int CH = D / 8, PB = D / 32;
     const int g = blockIdx.y, c = threadIdx.x % CH;
-    const int64_t row = (int64_t)blockIdx.x * (256 / CH) + threadIdx.x / CH;
+    const int64_t row = kb.row0 + (int64_t)blockIdx.x * (256 / CH) + threadIdx.x / CH;
     if (row >= kb.rows) return;
     int first;
     const int b = sequence_of(kb.end, (int)row, &first);
@@ -128,6 +128,8 @@ __global__ void __launch_bounds__(256) kv4_read_kernel(Kv4Rows<NB> kb, T* __rest
     store8(v + (row * Hkv + g) * D + 8 * c, f);
 }
 
+constexpr int64_t KV4_LAUNCH_ROWS = 1 << 24;   // a launch has fewer than 2^32 threads along a dimension; a row of a head has at most 16
+
 template <int NB> static Kv4Rows<NB> rows_of(const Kv4Batch& kb) {
     Kv4Rows<NB> r{};
     for (int b = 0; b < NB; ++b) {
@@ -141,11 +143,18 @@ template <int NB> static Kv4Rows<NB> rows_of(const Kv4Batch& kb) {
 
 template <typename T, int D, int NB>
 static hipError_t launch_kv4_rows_n(const T* k, const T* v, const int32_t* pos, T* k_out, T* v_out, const Kv4Batch& kb, int Hkv, hipStream_t s) {
-    const Kv4Rows<NB> r = rows_of<NB>(kb);
-    const dim3 g((unsigned)((r.rows + 2048 / D - 1) / (2048 / D)), (unsigned)Hkv), t(256);
-    if (k) kv4_append_kernel<T, D, NB><<<g, t, 0, s>>>(k, v, pos, r, Hkv);
-    else kv4_read_kernel<T, D, NB><<<g, t, 0, s>>>(r, k_out, v_out, Hkv);
-    return hipGetLastError();
+    Kv4Rows<NB> r = rows_of<NB>(kb);
+    const int64_t rows = r.rows;
+    for (int64_t r0 = 0; r0 < rows; r0 += KV4_LAUNCH_ROWS) {
+        const int64_t n = rows - r0 < KV4_LAUNCH_ROWS ? rows - r0 : KV4_LAUNCH_ROWS;
+        r.row0 = (int32_t)r0; r.rows = (int32_t)(r0 + n);
+        const dim3 g((unsigned)((n + 2048 / D - 1) / (2048 / D)), (unsigned)Hkv), t(256);
+        if (k) kv4_append_kernel<T, D, NB><<<g, t, 0, s>>>(k, v, pos, r, Hkv);
+        else kv4_read_kernel<T, D, NB><<<g, t, 0, s>>>(r, k_out, v_out, Hkv);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 template <typename T, int D>

@@ -53,9 +53,46 @@ hipError_t launch_q4_pack(const void* W, int64_t rows, int64_t K, void* codes, v
 // parts, which is all of its 24 bits.  The NW wavefronts of a workgroup share the slabs of NS strips in turn, each with the codes and scales of its next slab on
 // their way while it works on one, and meet in LDS.  The order of a row's sum depends on K and NW alone, not on the vectors.  (Vectors asked for a slab ahead too take
 // 200 registers a lane, which halves the wavefronts on a CU: 28672 x 4096, one vector, 16.0 -> 22.6 us.)
-template <int NM> struct Q4Mats { const u32x4* codes[NM]; const uint32_t* scales[NM]; void* y[NM]; int32_t rows[NM]; const void* x; int32_t K, nb; };   // (few arguments: quick launches)
+// (few arguments: quick launches)
+template <int NM> struct Q4Mats { const u32x4* codes[NM]; const uint32_t* scales[NM]; void* y[NM]; int32_t rows[NM]; const void* x; int32_t K, nb; const void* gamma; float eps; };
 
-template <typename T, int MODE, int NM, int NS, int NW>
+// One vector x [K] normalised on its way in: every workgroup takes its sum of squares and leaves the normalised vector, rounded as rmsnorm_kernel does it, in LDS
+// (zeros up to whole slabs), where the products read it.  The first codes are already on their way; a norm of its own would be a launch of 3 us.
+template <int NW>
+__device__ inline void norm_to_lds(const bf16_t* __restrict__ x, const bf16_t* __restrict__ gamma, float eps, int K, int slabs, u32x4* xl, float* red) {
+    const int tid = threadIdx.x, chunks = K / 8;
+    float ss = 0.f;
+    for (int c = tid; c < chunks; c += NW * 64) {
+        const u32x4 w = reinterpret_cast<const u32x4*>(x)[c];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float a = __uint_as_float(w[i] << 16), b = __uint_as_float(w[i] & 0xffff0000u);
+            ss += a * a; ss += b * b;
+        }
+    }
+    ss = wave_sum(ss);
+    if ((tid & 63) == 0) red[tid >> 6] = ss;
+    __syncthreads();
+    ss = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) ss += red[w];
+    const float inv = 1.0f / sqrtf(ss / (float)K + eps);
+    for (int c = tid; c < slabs * (Q4_SLAB / 8); c += NW * 64) {
+        u32x4 o{0, 0, 0, 0};
+        if (c < chunks) {
+            const u32x4 w = reinterpret_cast<const u32x4*>(x)[c], g = reinterpret_cast<const u32x4*>(gamma)[c];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                o[i] = cvt_pk_bf16(__uint_as_float(w[i] << 16) * inv * __uint_as_float(g[i] << 16),
+                                   __uint_as_float(w[i] & 0xffff0000u) * inv * __uint_as_float(g[i] & 0xffff0000u));
+        }
+        xl[c] = o;
+    }
+    __syncthreads();
+}
+constexpr int Q4_NORM_K = 16384;   // longest: 32 KB of LDS
+
+template <typename T, int MODE, int NM, int NS, int NW, bool NORM>
 __global__ void __launch_bounds__(NW * 64) q4_matvec_kernel(Q4Mats<NM> a) {
     constexpr bool F32 = sizeof(T) == 4;
     constexpr int NP = F32 ? 3 : 1, OWN = MODE == Q4_SILU ? NS / 2 : NS;   // strips of one matrix (SiLU: half are gate rows, half the same up rows)
@@ -97,6 +134,8 @@ __global__ void __launch_bounds__(NW * 64) q4_matvec_kernel(Q4Mats<NM> a) {
         }
     };
     if (wave < slabs) load(wave);
+    extern __shared__ u32x4 xl[];
+    if constexpr (NORM) norm_to_lds<NW>((const bf16_t*)a.x, (const bf16_t*)a.gamma, a.eps, K, slabs, xl, &sred[0][0][0][0]);
     for (int slab = wave; slab < slabs; slab += NW) {
         u32x4 c[NS][4];
         uint32_t sc[NS];
@@ -113,7 +152,8 @@ __global__ void __launch_bounds__(NW * 64) q4_matvec_kernel(Q4Mats<NM> a) {
             for (int t = 0; t < 4; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    xv[t][i] = vec && k0 + t * 128 + i * 32 + kg * 8 < K ? *reinterpret_cast<const u32x4*>(x + k0 + t * 128 + i * 32) : u32x4{0, 0, 0, 0};
+                    if constexpr (NORM) xv[t][i] = vec ? xl[(k0 + t * 128 + i * 32) / 8 + kg] : u32x4{0, 0, 0, 0};
+                    else xv[t][i] = vec && k0 + t * 128 + i * 32 + kg * 8 < K ? *reinterpret_cast<const u32x4*>(x + k0 + t * 128 + i * 32) : u32x4{0, 0, 0, 0};
         }
         if (slab + NW < slabs) load(slab + NW);
 #pragma unroll
@@ -121,15 +161,21 @@ __global__ void __launch_bounds__(NW * 64) q4_matvec_kernel(Q4Mats<NM> a) {
             uint32_t w4[NS];   // the tile's four scales of the lane's row, which lane 16 t + l16 has loaded
 #pragma unroll
             for (int s = 0; s < NS; ++s) w4[s] = (uint32_t)__builtin_amdgcn_ds_bpermute((16 * t + l16) * 4, (int)sc[s]);
+            f32x4 xw[F32 ? 4 : 1][2];
+            if constexpr (F32) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int k = k0 + t * 128 + i * 32;
+                    const bool in = vec && k + kg * 8 < K;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) xw[i][h] = in ? reinterpret_cast<const f32x4*>(x + k)[h] : f32x4{0.f, 0.f, 0.f, 0.f};
+                }
+            }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 u32x4 xf[NP];
                 if constexpr (F32) {
-                    const int k = k0 + t * 128 + i * 32;
-                    const bool in = vec && k + kg * 8 < K;
-                    const f32x4* p = reinterpret_cast<const f32x4*>(x + k);
-                    const f32x4 lo = in ? p[0] : f32x4{0.f, 0.f, 0.f, 0.f}, hi = in ? p[1] : f32x4{0.f, 0.f, 0.f, 0.f};
-                    const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+                    const float v[8] = {xw[i][0][0], xw[i][0][1], xw[i][0][2], xw[i][0][3], xw[i][1][0], xw[i][1][1], xw[i][1][2], xw[i][1][3]};
                     bf16_parts<NP>(v, xf);
                 } else xf[0] = xv[t][i];
 #pragma unroll
@@ -141,7 +187,7 @@ __global__ void __launch_bounds__(NW * 64) q4_matvec_kernel(Q4Mats<NM> a) {
             }
         }
     }
-    // lane (vector l16, row group kg) holds rows 4 kg .. 4 kg + 3 of its strips
+    // lane (vector l16, row group kg) holds rows 4 kg .. 4 kg + 3 of its strips.  (NORM: everyone has read the norm's sums, which stood here, before the second barrier)
 #pragma unroll
     for (int s = 0; s < NS; ++s) *reinterpret_cast<mfma_f32x4*>(&sred[wave][s][l16][4 * kg]) = acc[s];
     __syncthreads();
@@ -175,7 +221,15 @@ static hipError_t launch_q4_matvec_n(const Q4Args& a, hipStream_t s) {
     }
     m.x = a.x; m.K = (int32_t)a.K; m.nb = a.nb;
     if (blocks == 0) return hipSuccess;
-    q4_matvec_kernel<T, MODE, NM, NS, NW><<<dim3((unsigned)blocks), dim3(NW * 64), 0, s>>>(m);
+    if constexpr (sizeof(T) == 2 && (MODE == Q4_F32 || MODE == Q4_SILU) && NM > 1 && NS <= 2) {   // (a single vector never takes four strips)
+        if (a.gamma) {
+            m.gamma = a.gamma; m.eps = a.eps;
+            const int lds = (m.K + Q4_SLAB - 1) / Q4_SLAB * Q4_SLAB * 2;
+            q4_matvec_kernel<T, MODE, NM, NS, NW, true><<<dim3((unsigned)blocks), dim3(NW * 64), lds, s>>>(m);
+            return hipGetLastError();
+        }
+    }
+    q4_matvec_kernel<T, MODE, NM, NS, NW, false><<<dim3((unsigned)blocks), dim3(NW * 64), 0, s>>>(m);
     return hipGetLastError();
 }
 
@@ -207,8 +261,11 @@ static hipError_t launch_q4_matvec_t(const Q4Args& a, hipStream_t s) {
 }
 
 // a: Q4_STORE and Q4_RESID take one matrix, Q4_SILU two, Q4_F32 up to three
+bool q4_norm_inside(int64_t K, int nb, bool bf16) { return bf16 && nb == 1 && K <= Q4_NORM_K; }
+
 hipError_t launch_q4_matvec(const Q4Args& a, bool bf16, hipStream_t s) {
     if (a.nb < 1 || a.nb > DECODE_MAX_BATCH) return hipErrorInvalidValue;
+    if (a.gamma && (!q4_norm_inside(a.K, a.nb, bf16) || (a.mode != Q4_SILU && !(a.mode == Q4_F32 && (a.rows[1] || a.rows[2]))))) return hipErrorInvalidValue;
     return bf16 ? launch_q4_matvec_t<bf16_t>(a, s) : launch_q4_matvec_t<float>(a, s);
 }
 

@@ -1305,7 +1305,7 @@ namespace {
 int check_q4(const spts_q4* w) {
     if (!w || !w->codes || !w->scales || w->rows < 1 || w->K < 1) return SPTS_EINVAL;
     if (!aligned16(w->codes) || !aligned16(w->scales)) return SPTS_EALIGN;
-    if (w->K % 8 != 0 || w->K > INT32_MAX || w->rows > INT32_MAX) return SPTS_ESHAPE;
+    if (w->K % 8 != 0 || w->K > Q4_MAX_K || w->rows > Q4_MAX_ROWS) return SPTS_ESHAPE;
     return SPTS_OK;
 }
 
@@ -1348,7 +1348,7 @@ int kv4_offsets(const int64_t* offsets, int32_t batch, Kv4Batch* kb) {
 
 int spts_q4_bytes(int64_t rows, int64_t K, size_t* code_bytes, size_t* scale_bytes) {
     if (rows < 1 || K < 1 || !code_bytes || !scale_bytes) return SPTS_EINVAL;
-    if (K % 8 != 0 || K > INT32_MAX || rows > INT32_MAX) return SPTS_ESHAPE;
+    if (K % 8 != 0 || K > Q4_MAX_K || rows > Q4_MAX_ROWS) return SPTS_ESHAPE;
     *code_bytes = (size_t)q4_code_bytes(rows, K);
     *scale_bytes = (size_t)q4_scale_bytes(rows, K);
     return SPTS_OK;
@@ -1489,8 +1489,11 @@ int spts_decode_layer_q4(spts_ctx* c, void* x, const int32_t* pos, int32_t batch
         return g;
     };
     auto also = [](Q4Args& g, int i, const spts_q4& a, void* out) { g.codes[i] = a.codes; g.scales[i] = a.scales; g.rows[i] = a.rows; g.y[i] = out; };
-    { PHASE(c, PH_DEC_NORM); SPTS_HIP(c, launch_rmsnorm(x, w->gamma1, m.rms_eps, xn, batch, m.D, c->bf16, st)); }
+    const bool inside = q4_norm_inside(m.D, batch, c->bf16);
+    auto normed = [&](Q4Args& g, const void* gamma) { g.x = x; g.gamma = gamma; g.eps = m.rms_eps; };
+    if (!inside) { PHASE(c, PH_DEC_NORM); SPTS_HIP(c, launch_rmsnorm(x, w->gamma1, m.rms_eps, xn, batch, m.D, c->bf16, st)); }
     Q4Args qkv = args(w->Wq, xn, q32, Q4_F32);
+    if (inside) normed(qkv, w->gamma1);
     also(qkv, 1, w->Wk, k32);
     also(qkv, 2, w->Wv, v32);
     { PHASE(c, PH_DEC_QKV); SPTS_HIP(c, launch_q4_matvec(qkv, c->bf16, st)); }
@@ -1499,8 +1502,9 @@ int spts_decode_layer_q4(spts_ctx* c, void* x, const int32_t* pos, int32_t batch
     { PHASE(c, PH_DEC_ATTN);
       SPTS_HIP(c, launch_kv4_attn(q, kb, m.H, m.Hkv, m.d, c->p<float>(c->off.tmp32), (c->off.qp - c->off.tmp32) / sizeof(float), att, c->bf16, st)); }
     { PHASE(c, PH_DEC_O); SPTS_HIP(c, launch_q4_matvec(args(w->Wo, att, x, Q4_RESID), c->bf16, st)); }
-    { PHASE(c, PH_DEC_NORM); SPTS_HIP(c, launch_rmsnorm(x, w->gamma2, m.rms_eps, xn, batch, m.D, c->bf16, st)); }
+    if (!inside) { PHASE(c, PH_DEC_NORM); SPTS_HIP(c, launch_rmsnorm(x, w->gamma2, m.rms_eps, xn, batch, m.D, c->bf16, st)); }
     Q4Args gu = args(w->Wgate, xn, hbuf, Q4_SILU);
+    if (inside) normed(gu, w->gamma2);
     also(gu, 1, w->Wup, nullptr);
     { PHASE(c, PH_DEC_GATE_UP); SPTS_HIP(c, launch_q4_matvec(gu, c->bf16, st)); }
     { PHASE(c, PH_DEC_DOWN); SPTS_HIP(c, launch_q4_matvec(args(w->Wdown, hbuf, x, Q4_RESID), c->bf16, st)); }
@@ -1511,6 +1515,7 @@ int spts_decode_layer_q4(spts_ctx* c, void* x, const int32_t* pos, int32_t batch
 int spts_process_logits(spts_ctx* c, const float* logits, int32_t V, int32_t batch, const spts_logits_rules* rules, float* logits_out,
                         int32_t* token_out, const void* table, void* x_next) {
     if (!c || V < 1 || batch < 0 || batch > SPTS_MAX_DECODE_BATCH || !rules) return SPTS_EINVAL;
+    if (V > LOGITS_MAX_WORDS) return SPTS_ESHAPE;
     if (batch == 0) return SPTS_OK;
     if (!logits || !logits_out || (x_next && (!token_out || !table))) return SPTS_EINVAL;
     if (!aligned16(logits) || !aligned16(logits_out) || (token_out && !aligned16(token_out)) || (x_next && (!aligned16(x_next) || !aligned16(table))))

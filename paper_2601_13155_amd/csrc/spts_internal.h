@@ -340,6 +340,7 @@ hipError_t launch_argmax_rows(const float* logits, int V, int nrows, int32_t* to
 // load is a tile and dword i is the lane's operand of the tile's i-th matrix instruction.  Scales: [strip][slab][tile][row][block], a dword of four
 // blocks for each row and tile.
 constexpr int Q4_SLAB = 512;
+constexpr int64_t Q4_MAX_K = 1 << 30, Q4_MAX_ROWS = 1 << 28;   // 32-bit indexes of a row's slabs; a launch has fewer than 2^32 threads
 inline int64_t q4_slabs(int64_t K) { return (K + Q4_SLAB - 1) / Q4_SLAB; }
 inline int64_t q4_code_bytes(int64_t rows, int64_t K) { return (rows + 15) / 16 * q4_slabs(K) * 4096; }
 inline int64_t q4_scale_bytes(int64_t rows, int64_t K) { return (rows + 15) / 16 * q4_slabs(K) * 256; }
@@ -354,7 +355,9 @@ enum Q4Mode : int {
 struct Q4Args {
     const void* codes[3]; const void* scales[3]; void* y[3]; int64_t rows[3];
     const void* x; int64_t K; int nb; int mode;
+    const void* gamma; float eps;   // RMSNorm of x on its way in: Q4_SILU and Q4_F32 of several matrices, where q4_norm_inside
 };
+bool q4_norm_inside(int64_t K, int nb, bool bf16);
 hipError_t launch_q4_matvec(const Q4Args& a, bool bf16, hipStream_t s);
 
 // ------------------------------------------------------------------ 4-bit caches
@@ -382,6 +385,7 @@ struct LogitsRules {
     float repetition[DECODE_MAX_BATCH], frequency[DECODE_MAX_BATCH], presence[DECODE_MAX_BATCH];
 };
 // token (may be NULL, and x_next with it): scratch of logits_scratch_bytes
+constexpr int LOGITS_MAX_WORDS = 1 << 28;
 size_t logits_scratch_bytes(int V, int nrows);
 hipError_t launch_process_logits(const float* in, int V, int nrows, const LogitsRules& r, float* out, int32_t* token, const void* table, int D,
                                  void* x_next, bool bf16, void* scratch, hipStream_t s);

@@ -393,11 +393,12 @@ def layer_for(torch, ctx, shape, seed):
 
 
 # (D, H, Hkv, d, Dff): the rows of each product, in strips of 16, on either side of where the kernels change
-LAYERS = [(256, 4, 2, 64, 688), (64, 64, 16, 128, 8704), (4224, 4, 2, 32, 64), (8320, 4, 2, 32, 64), (64, 48, 6, 128, 2104)]
+LAYERS = [(256, 4, 2, 64, 688), (64, 64, 16, 128, 8704), (4224, 4, 2, 32, 64), (8320, 4, 2, 32, 64), (64, 48, 6, 128, 2104), (16392, 4, 2, 32, 64)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("nseq,dims", [(1, 0), (2, 0), (5, 0), (16, 0), (1, 1), (3, 1), (2, 2), (2, 3), (3, 3), (4, 4)])
+@pytest.mark.parametrize("nseq,dims", [(1, 0), (2, 0), (5, 0), (16, 0), (1, 1), (3, 1), (1, 2), (2, 2), (1, 3), (2, 3), (3, 3),
+                                       (1, 4), (4, 4), (1, 5)])
 def test_decode_layer_lockstep(torch, dtype, nseq, dims):
     """Caches of different lengths filled from random pairs, three steps of the layer: the appended pair against the oracle's (to the
     element type's rounding, then one of 4 bits), the state against the oracle's over the pairs as stored."""
