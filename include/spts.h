@@ -304,7 +304,7 @@ typedef struct {
     void *codes, *scales;
     int64_t rows, K;
 } spts_q4;
-/* Bytes of the two buffers.  SPTS_EINVAL on rows or K < 1 or a NULL pointer, SPTS_ESHAPE on K % 8 != 0, K > 2^30 or
+/* Bytes of the two buffers.  SPTS_EINVAL on rows or K < 1 or a NULL pointer, SPTS_ESHAPE on K % 8 != 0, K > 2^26 or
  * rows > 2^28 (as for the calls that take such a matrix). */
 int spts_q4_bytes(int64_t rows, int64_t K, size_t *code_bytes, size_t *scale_bytes);
 /* Packs W [out->rows, out->K] of the context's element type (device, row-major, 16-byte aligned) into out's buffers. */

@@ -92,34 +92,72 @@ __device__ inline void norm_to_lds(const bf16_t* __restrict__ x, const bf16_t* _
 }
 constexpr int Q4_NORM_K = 16384;   // longest: 32 KB of LDS
 
-template <typename T, int MODE, int NM, int NS, int NW, bool NORM>
-__global__ void __launch_bounds__(NW * 64) q4_matvec_kernel(Q4Mats<NM> a) {
-    constexpr bool F32 = sizeof(T) == 4;
-    constexpr int NP = F32 ? 3 : 1, OWN = MODE == Q4_SILU ? NS / 2 : NS;   // strips of one matrix (SiLU: half are gate rows, half the same up rows)
-    __shared__ __attribute__((aligned(16))) float sred[NW][NS][16][20];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, kg = lane >> 4;
-    const int slabs = (a.K + Q4_SLAB - 1) / Q4_SLAB, K = a.K;
-    int blk = blockIdx.x;
-    int which = 0;
+// which strips a workgroup has: NS consecutive ones of one matrix (SiLU: half are gate rows, half the same up rows); behind the last one, that again
+template <int NS> struct Q4Strips { const u32x4* codes[NS]; const uint32_t* scales[NS]; int blk, which; };
+template <int MODE, int NM, int NS>
+__device__ inline Q4Strips<NS> q4_strips(const Q4Mats<NM>& a, int slabs) {
+    constexpr int OWN = MODE == Q4_SILU ? NS / 2 : NS;
+    Q4Strips<NS> r;
+    r.blk = blockIdx.x;
+    r.which = 0;
     if (MODE != Q4_SILU) {
 #pragma unroll
         for (int i = 0; i + 1 < NM; ++i) {
             const int n = (a.rows[i] + 16 * NS - 1) / (16 * NS);
-            if (which == i && blk >= n) { blk -= n; which = i + 1; }
+            if (r.which == i && r.blk >= n) { r.blk -= n; r.which = i + 1; }
         }
     }
-    const u32x4* codes[NS];
-    const uint32_t* scales[NS];
-    const int last = (a.rows[which] + 15) / 16 - 1;
+    const int last = (a.rows[r.which] + 15) / 16 - 1;
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
-        const int at = blk * OWN + s % OWN, m = MODE == Q4_SILU ? s / OWN : which;
+        const int at = r.blk * OWN + s % OWN, m = MODE == Q4_SILU ? s / OWN : r.which;
         const int64_t strip = at < last ? at : last;
-        codes[s] = a.codes[m] + strip * slabs * 256;
-        scales[s] = a.scales[m] + strip * slabs * 64;
+        r.codes[s] = a.codes[m] + strip * slabs * 256;
+        r.scales[s] = a.scales[m] + strip * slabs * 64;
     }
+    return r;
+}
+
+// The wavefronts' partial tiles meet in LDS and leave.  Lane (vector l16, row group kg) holds rows 4 kg .. 4 kg + 3 of its strips.
+template <typename T, int MODE, int NM, int NS, int NW>
+__device__ inline void q4_finish(const Q4Mats<NM>& a, const Q4Strips<NS>& st, const mfma_f32x4 (&acc)[NS], float (*sred)[NS][16][20]) {
+    constexpr int OWN = MODE == Q4_SILU ? NS / 2 : NS;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) *reinterpret_cast<mfma_f32x4*>(&sred[wave][s][lane & 15][4 * (lane >> 4)]) = acc[s];
+    __syncthreads();
+    for (int t = tid; t < OWN * 256; t += NW * 64) {
+        const int r = t & 15, s = (t >> 4) % OWN, b = t / (16 * OWN);
+        const int64_t row = ((int64_t)st.blk * OWN + s) * 16 + r;
+        if (b >= a.nb || row >= a.rows[st.which]) continue;
+        float v = 0.f, u = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            v += sred[w][s][b][r];
+            if (MODE == Q4_SILU) u += sred[w][NS - OWN + s][b][r];
+        }
+        const int64_t at = (int64_t)b * a.rows[st.which] + row;
+        if (MODE == Q4_F32) ((float*)a.y[st.which])[at] = v;
+        else {
+            T* y = (T*)a.y[st.which] + at;
+            *y = from_f32<T>(MODE == Q4_SILU ? v / (1.0f + __expf(-v)) * u : MODE == Q4_RESID ? to_f32(*y) + v : v);
+        }
+    }
+}
+
+// y = x W^T on the matrix cores for up to 16 vectors: a row of W is an operand row (lane l16), a vector a column; a dword of codes is an operand's eight values of a
+// lane, and the decoder's bf16 pairs are the operand.  The NW wavefronts of a workgroup share the slabs of NS strips in turn and meet in LDS; the order of a
+// row's sum depends on K and NW alone, not on the vectors.
+// fp32 vectors are taken as three bf16 parts, which is all of their 24 bits, and are read from the caches a tile at a time; codes and scales of the next slab are on
+// their way while one is worked on.
+template <int MODE, int NM, int NS, int NW>
+__global__ void __launch_bounds__(NW * 64) q4_matvec_f32_kernel(Q4Mats<NM> a) {
+    __shared__ __attribute__((aligned(16))) float sred[NW][NS][16][20];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, kg = lane >> 4;
+    const int slabs = (a.K + Q4_SLAB - 1) / Q4_SLAB, K = a.K;
+    const Q4Strips<NS> st = q4_strips<MODE, NM, NS>(a, slabs);
     const bool vec = l16 < a.nb;
-    const T* const x = (const T*)a.x + (int64_t)(vec ? l16 : 0) * K + kg * 8;
+    const float* const x = (const float*)a.x + (int64_t)(vec ? l16 : 0) * K + kg * 8;
     mfma_f32x4 acc[NS];
 #pragma unroll
     for (int s = 0; s < NS; ++s) acc[s] = mfma_f32x4{0.f, 0.f, 0.f, 0.f};
@@ -129,13 +167,11 @@ __global__ void __launch_bounds__(NW * 64) q4_matvec_kernel(Q4Mats<NM> a) {
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
 #pragma unroll
-            for (int t = 0; t < 4; ++t) cn[s][t] = __builtin_nontemporal_load(codes[s] + (slab * 4 + t) * 64 + lane);
-            sn[s] = __builtin_nontemporal_load(scales[s] + slab * 64 + lane);
+            for (int t = 0; t < 4; ++t) cn[s][t] = __builtin_nontemporal_load(st.codes[s] + (slab * 4 + t) * 64 + lane);
+            sn[s] = __builtin_nontemporal_load(st.scales[s] + slab * 64 + lane);
         }
     };
     if (wave < slabs) load(wave);
-    extern __shared__ u32x4 xl[];
-    if constexpr (NORM) norm_to_lds<NW>((const bf16_t*)a.x, (const bf16_t*)a.gamma, a.eps, K, slabs, xl, &sred[0][0][0][0]);
     for (int slab = wave; slab < slabs; slab += NW) {
         u32x4 c[NS][4];
         uint32_t sc[NS];
@@ -145,69 +181,127 @@ __global__ void __launch_bounds__(NW * 64) q4_matvec_kernel(Q4Mats<NM> a) {
             for (int t = 0; t < 4; ++t) c[s][t] = cn[s][t];
             sc[s] = sn[s];
         }
-        const int k0 = slab * Q4_SLAB;
-        u32x4 xv[F32 ? 1 : 4][4];
-        if constexpr (!F32) {
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if constexpr (NORM) xv[t][i] = vec ? xl[(k0 + t * 128 + i * 32) / 8 + kg] : u32x4{0, 0, 0, 0};
-                    else xv[t][i] = vec && k0 + t * 128 + i * 32 + kg * 8 < K ? *reinterpret_cast<const u32x4*>(x + k0 + t * 128 + i * 32) : u32x4{0, 0, 0, 0};
-        }
         if (slab + NW < slabs) load(slab + NW);
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
             uint32_t w4[NS];   // the tile's four scales of the lane's row, which lane 16 t + l16 has loaded
 #pragma unroll
             for (int s = 0; s < NS; ++s) w4[s] = (uint32_t)__builtin_amdgcn_ds_bpermute((16 * t + l16) * 4, (int)sc[s]);
-            f32x4 xw[F32 ? 4 : 1][2];
-            if constexpr (F32) {
+            f32x4 xw[4][2];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int k = k0 + t * 128 + i * 32;
-                    const bool in = vec && k + kg * 8 < K;
+            for (int i = 0; i < 4; ++i) {
+                const int k = slab * Q4_SLAB + t * 128 + i * 32;
+                const bool in = vec && k + kg * 8 < K;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) xw[i][h] = in ? reinterpret_cast<const f32x4*>(x + k)[h] : f32x4{0.f, 0.f, 0.f, 0.f};
-                }
+                for (int h = 0; h < 2; ++h) xw[i][h] = in ? reinterpret_cast<const f32x4*>(x + k)[h] : f32x4{0.f, 0.f, 0.f, 0.f};
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                u32x4 xf[NP];
-                if constexpr (F32) {
-                    const float v[8] = {xw[i][0][0], xw[i][0][1], xw[i][0][2], xw[i][0][3], xw[i][1][0], xw[i][1][1], xw[i][1][2], xw[i][1][3]};
-                    bf16_parts<NP>(v, xf);
-                } else xf[0] = xv[t][i];
+                const float v[8] = {xw[i][0][0], xw[i][0][1], xw[i][0][2], xw[i][0][3], xw[i][1][0], xw[i][1][1], xw[i][1][2], xw[i][1][3]};
+                u32x4 xf[3];
+                bf16_parts<3>(v, xf);
 #pragma unroll
                 for (int s = 0; s < NS; ++s) {
                     const u32x4 w = fp4_decode8_bf16(c[s][t][i], i == 0 ? fp4_scale_of<0>(w4[s]) : i == 1 ? fp4_scale_of<1>(w4[s]) : i == 2 ? fp4_scale_of<2>(w4[s]) : fp4_scale_of<3>(w4[s]));
 #pragma unroll
-                    for (int p = NP - 1; p >= 0; --p) acc[s] = mfma16(w, xf[p], acc[s]);
+                    for (int p = 2; p >= 0; --p) acc[s] = mfma16(w, xf[p], acc[s]);
                 }
             }
         }
     }
-    // lane (vector l16, row group kg) holds rows 4 kg .. 4 kg + 3 of its strips.  (NORM: everyone has read the norm's sums, which stood here, before the second barrier)
+    q4_finish<float, MODE, NM, NS, NW>(a, st, acc, sred);
+}
+
+// bf16 vectors.  Read by lanes, an operand of 16 vectors is 16 half cache lines, of which a CU takes in 22 bytes a clock: a product of 4096 x 14336 took 0.55 us more with
+// every vector, on however many CUs.  So codes, scales and vectors go to LDS with loads that are laid out for memory, whole lines of 4 vectors an instruction, into a
+// ring of DEPTH tiles (128 k) of each wavefront; a wavefront reads only what it has loaded itself, after its own vmcnt wait, so there is no barrier in the loop.
+// Piece c (16 bytes) of vector r lies at slot c ^ r of its row, which spreads the 16 rows of an operand over the banks.  4096 x 14336, 2 / 4 / 8 / 16 vectors 9.7 / 10.9 /
+// 12.8 / 17.5 -> 7.1 / 7.9 / 9.3 / 11.9 us.  4 XI: vectors there is room for; 0: a single one that is normalised on its way in.
+template <int NS, int XI> constexpr int q4_stage_bytes() { return NS * (1024 + 256) + XI * 1024; }
+template <int MODE, int NM, int NS, int NW, int XI, int DEPTH>
+__global__ void __launch_bounds__(NW * 64) q4_matvec_kernel(Q4Mats<NM> a) {
+    constexpr bool NORM = XI == 0;
+    constexpr uint32_t STAGE = q4_stage_bytes<NS, XI>();
+    constexpr int NI = 2 * NS + XI;                // loads of a stage
+    static_assert((DEPTH - 1) * NI <= 63, "vmcnt field");
+    static_assert((size_t)DEPTH * STAGE >= sizeof(float) * NS * 16 * 20, "the partial tiles reuse the ring");
+    extern __shared__ __attribute__((aligned(16))) char ring[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, kg = lane >> 4;
+    const int K = a.K, slabs = (K + Q4_SLAB - 1) / Q4_SLAB, ntiles = (K + 127) / 128;
+    const Q4Strips<NS> st = q4_strips<MODE, NM, NS>(a, slabs);
+    // tile n of this wavefront: slab wave + NW (n / 4), tile n % 4 of it; those behind K are left out
+    const int mine = wave < slabs ? (slabs - wave + NW - 1) / NW : 0;
+    int N = mine * 4;
+    if (mine > 0 && wave + NW * (mine - 1) == slabs - 1) N -= slabs * 4 - ntiles;
+    int row[XI + NORM];
 #pragma unroll
-    for (int s = 0; s < NS; ++s) *reinterpret_cast<mfma_f32x4*>(&sred[wave][s][l16][4 * kg]) = acc[s];
-    __syncthreads();
-    for (int t = tid; t < OWN * 256; t += NW * 64) {
-        const int r = t & 15, s = (t >> 4) % OWN, b = t / (16 * OWN);
-        const int64_t row = ((int64_t)blk * OWN + s) * 16 + r;
-        if (b >= a.nb || row >= a.rows[which]) continue;
-        float v = 0.f, u = 0.f;
+    for (int j = 0; j < XI; ++j) row[j] = 4 * j + kg < a.nb ? 4 * j + kg : a.nb - 1;   // (behind the last vector any: its column is not stored)
+    const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)ring + (uint32_t)wave * (DEPTH * STAGE);
+    auto issue = [&](int n) {
+        const int tile = (wave + NW * (n >> 2)) * 4 + (n & 3), k0 = tile * 128;
+        const uint32_t slot = base + (uint32_t)(n % DEPTH) * STAGE;
 #pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            v += sred[w][s][b][r];
-            if (MODE == Q4_SILU) u += sred[w][NS - OWN + s][b][r];
+        for (int s = 0; s < NS; ++s) {
+            dma16s_nt((uint32_t)lane * 16, (const char*)st.codes[s] + (int64_t)tile * 1024, slot + s * 1024);
+            dma4s_nt((uint32_t)l16 * 4, (const char*)st.scales[s] + (int64_t)tile * 64, slot + NS * 1024 + s * 256);
         }
-        const int64_t at = (int64_t)b * a.rows[which] + row;
-        if (MODE == Q4_F32) ((float*)a.y[which])[at] = v;
-        else {
-            T* y = (T*)a.y[which] + at;
-            *y = from_f32<T>(MODE == Q4_SILU ? v / (1.0f + __expf(-v)) * u : MODE == Q4_RESID ? to_f32(*y) + v : v);
+#pragma unroll
+        for (int j = 0; j < XI; ++j) {
+            int piece = l16 ^ (4 * j + kg);        // the lane's 16 bytes go to row 4 j + kg, slot l16
+            piece = k0 + piece * 8 < K ? piece : 0;
+            dma16s(((uint32_t)row[j] * (uint32_t)K + (uint32_t)piece * 8) * 2, (const char*)a.x + (int64_t)k0 * 2, slot + NS * 1280 + j * 1024);
         }
+    };
+    mfma_f32x4 acc[NS];
+#pragma unroll
+    for (int s = 0; s < NS; ++s) acc[s] = mfma_f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int n = 0; n < (N < DEPTH ? N : DEPTH); ++n) issue(n);
+    const u32x4* const xl = reinterpret_cast<const u32x4*>(ring + NW * DEPTH * STAGE + 64);   // behind the rings: the norm's sums, the normalised vector
+    if constexpr (NORM) norm_to_lds<NW>((const bf16_t*)a.x, (const bf16_t*)a.gamma, a.eps, K, slabs, const_cast<u32x4*>(xl), (float*)(ring + NW * DEPTH * STAGE));
+    for (int n = 0; n < N; ++n) {
+        if (n + DEPTH <= N) SPTS_WAIT_VMCNT((DEPTH - 1) * NI); else SPTS_WAIT_VMCNT(0);
+        asm volatile("" ::: "memory");
+        const char* const slot = ring + (size_t)wave * (DEPTH * STAGE) + (size_t)(n % DEPTH) * STAGE;
+        u32x4 c[NS], xv[4];
+        uint32_t sc[NS];
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            c[s] = *reinterpret_cast<const u32x4*>(slot + s * 1024 + lane * 16);
+            sc[s] = *reinterpret_cast<const uint32_t*>(slot + NS * 1024 + s * 256 + lane * 4);
+        }
+        const int xr = l16 & (4 * XI - 1);         // (with room for 4 or 8 vectors the columns behind repeat them, with one alone all do)
+        const int k0 = ((wave + NW * (n >> 2)) * 4 + (n & 3)) * 128;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            xv[i] = NORM ? xl[k0 / 8 + 4 * i + kg] : *reinterpret_cast<const u32x4*>(slot + NS * 1280 + xr * 256 + (((4 * i + kg) ^ xr) * 16));
+        // the slot is filled again only after its operands have arrived in registers
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (n + DEPTH < N) issue(n + DEPTH);
+        if (!NORM && k0 + 128 > K) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) xv[i] = k0 + i * 32 + kg * 8 < K ? xv[i] : u32x4{0, 0, 0, 0};
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int s = 0; s < NS; ++s)
+                acc[s] = mfma16(fp4_decode8_bf16(c[s][i], i == 0 ? fp4_scale_of<0>(sc[s]) : i == 1 ? fp4_scale_of<1>(sc[s]) : i == 2 ? fp4_scale_of<2>(sc[s]) : fp4_scale_of<3>(sc[s])),
+                                xv[i], acc[s]);
     }
+    __syncthreads();   // every ring has drained: its last tile waited for vmcnt 0
+    q4_finish<bf16_t, MODE, NM, NS, NW>(a, st, acc, reinterpret_cast<float (*)[NS][16][20]>(ring));
+}
+
+// (Depth of the ring: four tiles where they are small, 4096 x 14336, one vector, 2 / 3 / 4 tiles 8.5 / 7.6 / 7.1 us; otherwise two, which leaves room for more workgroups:
+// 12288 x 4096, one vector 2 / 3 tiles 7.3 / 7.8, 128256 x 4096, sixteen 53.0 / 66.4.)
+template <int MODE, int NM, int NS, int NW, int XI>
+static hipError_t launch_q4_bf16(const Q4Mats<NM>& m, unsigned blocks, hipStream_t s) {
+    constexpr int DEPTH = NS == 1 && XI < 4 ? 4 : 2, RING = NW * DEPTH * q4_stage_bytes<NS, XI>(), MOST = RING + (XI ? 0 : 64 + Q4_NORM_K * 2);
+    const int lds = XI ? RING : RING + 64 + (m.K + Q4_SLAB - 1) / Q4_SLAB * Q4_SLAB * 2;
+    const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(&q4_matvec_kernel<MODE, NM, NS, NW, XI, DEPTH>), MOST);
+    if (e != hipSuccess) return e;
+    q4_matvec_kernel<MODE, NM, NS, NW, XI, DEPTH><<<dim3(blocks), dim3(NW * 64), lds, s>>>(m);
+    return hipGetLastError();
 }
 
 template <typename T, int MODE, int NM, int NS, int NW>
@@ -221,16 +315,19 @@ static hipError_t launch_q4_matvec_n(const Q4Args& a, hipStream_t s) {
     }
     m.x = a.x; m.K = (int32_t)a.K; m.nb = a.nb;
     if (blocks == 0) return hipSuccess;
-    if constexpr (sizeof(T) == 2 && (MODE == Q4_F32 || MODE == Q4_SILU) && NM > 1 && NS <= 2) {   // (a single vector never takes four strips)
-        if (a.gamma) {
-            m.gamma = a.gamma; m.eps = a.eps;
-            const int lds = (m.K + Q4_SLAB - 1) / Q4_SLAB * Q4_SLAB * 2;
-            q4_matvec_kernel<T, MODE, NM, NS, NW, true><<<dim3((unsigned)blocks), dim3(NW * 64), lds, s>>>(m);
-            return hipGetLastError();
+    const unsigned g = (unsigned)blocks;
+    if constexpr (sizeof(T) == 4) {
+        q4_matvec_f32_kernel<MODE, NM, NS, NW><<<dim3(g), dim3(NW * 64), 0, s>>>(m);
+        return hipGetLastError();
+    } else {
+        if constexpr (NM > 1) {
+            if (a.gamma) {
+                m.gamma = a.gamma; m.eps = a.eps;
+                return launch_q4_bf16<MODE, NM, NS, NW, 0>(m, g, s);
+            }
         }
+        return a.nb <= 4 ? launch_q4_bf16<MODE, NM, NS, NW, 1>(m, g, s) : a.nb <= 8 ? launch_q4_bf16<MODE, NM, NS, NW, 2>(m, g, s) : launch_q4_bf16<MODE, NM, NS, NW, 4>(m, g, s);
     }
-    q4_matvec_kernel<T, MODE, NM, NS, NW, false><<<dim3((unsigned)blocks), dim3(NW * 64), 0, s>>>(m);
-    return hipGetLastError();
 }
 
 template <typename T, int NS, int NW>
@@ -244,12 +341,11 @@ static hipError_t launch_q4_matvec_m(const Q4Args& a, hipStream_t s) {
     }
 }
 
-// How many strips a workgroup takes.  A launch costs 4 us before the codes stream at 6 TB/s, so few strips are spread over the chip, one or two
-// workgroups of eight wavefronts to a CU; of many, fewer and longer workgroups lose less on their ends, and several strips share what is read of the vectors,
-// which many vectors feel most.  bf16, us for 1 / 2 / 4 strips with 8, 8 / 4 wavefronts: 4096 x 4096, one vector 4.3 / 5.0 / 7.5, sixteen 6.7 / 7.4 / 9.9; 6144 rows 5.9 / 5.3 / 7.8
-// and 10.8 / 7.6 / 10.1; 8192 x 8192, sixteen 19.4 / 13.9 / 16.5; 12288 x 4096 8.8 / 9.2 / 8.6 (two strips, 4 wavefronts 8.5) and 14.7 / 14.1 / 10.9 (13.2);
-// 28672 x 4096 16.3 / 17.9 / 15.0 (14.7) and 30.6 / 27.8 / 18.7 (22.7); 128256 x 4096 58.6 / 66.2 / 46.5 (48.0) and 128 / 106 / 60.0 (79).
-// The number of wavefronts, and with it the order of a sum, goes by the matrices alone.
+// How many strips a workgroup takes.  A launch costs about 4 us before the codes stream at 6 TB/s, so few strips are spread over the chip, one or two workgroups
+// of eight wavefronts to a CU; of many, fewer and longer workgroups lose less on their ends, and several strips share what is read of the vectors.  bf16, us for
+// 1 / 2 strips with 8 / 4 strips with 4 wavefronts (2 with 4, 4 with 8): 6144 x 4096, one vector 5.3 / 5.0, sixteen 8.3 / 6.4; 8192 x 8192, sixteen 14.8 / 10.8; 12288 x
+// 4096 7.7 / 7.8 / 7.7 (7.3, 7.8) and 12.6 / 11.3 / 9.0 (10.0, 9.2); 28672 x 4096 14.6 / 14.8 / 12.7 (14.2, 16.3) and 27.0 / 22.4 / 15.3 (18.2, 18.4); 128256 x 4096
+// 57.0 / 49.2 / 45.2 (46.4, 55.1) and 118 / 83.6 / 53.6 (63.3, 66.7).  It goes by the matrices alone, and with it the order of a sum.
 template <typename T>
 static hipError_t launch_q4_matvec_t(const Q4Args& a, hipStream_t s) {
     int64_t strips = 0;
@@ -257,7 +353,7 @@ static hipError_t launch_q4_matvec_t(const Q4Args& a, hipStream_t s) {
     if (a.mode == Q4_SILU) strips = 2 * ((a.rows[0] + 15) / 16);
     if (strips <= 256) return launch_q4_matvec_m<T, 1, 8>(a, s);
     if (strips <= 512) return launch_q4_matvec_m<T, 2, 8>(a, s);
-    return a.nb <= 2 ? launch_q4_matvec_m<T, 2, 4>(a, s) : launch_q4_matvec_m<T, 4, 4>(a, s);
+    return launch_q4_matvec_m<T, 4, 4>(a, s);
 }
 
 // a: Q4_STORE and Q4_RESID take one matrix, Q4_SILU two, Q4_F32 up to three

@@ -55,6 +55,10 @@ __device__ inline void dma16s(uint32_t voff, const void* sbase, uint32_t lds_bas
 __device__ inline void dma16s_nt(uint32_t voff, const void* sbase, uint32_t lds_base) {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt\n\t" ::"v"(voff), "s"(sbase), "s"(lds_base) : "memory");
 }
+// One dword a lane (global_load_lds_dword), to lds_base + 4 * lane, of data that is read once
+__device__ inline void dma4s_nt(uint32_t voff, const void* sbase, uint32_t lds_base) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1 nt\n\t" ::"v"(voff), "s"(sbase), "s"(lds_base) : "memory");
+}
 // s_waitcnt vmcnt(n) only (expcnt / lgkmcnt fields left at "no wait")
 #define SPTS_WAIT_VMCNT(n) __builtin_amdgcn_s_waitcnt(0x0F70 | ((n) & 0xF) | (((n) >> 4) << 14))
 
@@ -340,7 +344,7 @@ hipError_t launch_argmax_rows(const float* logits, int V, int nrows, int32_t* to
 // load is a tile and dword i is the lane's operand of the tile's i-th matrix instruction.  Scales: [strip][slab][tile][row][block], a dword of four
 // blocks for each row and tile.
 constexpr int Q4_SLAB = 512;
-constexpr int64_t Q4_MAX_K = 1 << 30, Q4_MAX_ROWS = 1 << 28;   // 32-bit indexes of a row's slabs; a launch has fewer than 2^32 threads
+constexpr int64_t Q4_MAX_K = 1 << 26, Q4_MAX_ROWS = 1 << 28;   // 32-bit offsets of 16 vectors; a launch has fewer than 2^32 threads
 inline int64_t q4_slabs(int64_t K) { return (K + Q4_SLAB - 1) / Q4_SLAB; }
 inline int64_t q4_code_bytes(int64_t rows, int64_t K) { return (rows + 15) / 16 * q4_slabs(K) * 4096; }
 inline int64_t q4_scale_bytes(int64_t rows, int64_t K) { return (rows + 15) / 16 * q4_slabs(K) * 256; }

@@ -61,7 +61,7 @@ def test_sizes(lib):
     assert lib.spts_q4_bytes(1, 8, C.byref(c), C.byref(s)) == OK and (c.value, s.value) == (4096, 256)
     assert lib.spts_q4_bytes(4096, 14336, C.byref(c), C.byref(s)) == OK and (c.value, s.value) == (4096 * 14336 // 2, 4096 * 14336 // 32)
     assert lib.spts_q4_bytes(17, 520, C.byref(c), C.byref(s)) == OK and (c.value, s.value) == (4 * 4096, 4 * 256)
-    for rows, K, why in ((0, 8, INVAL), (1, 0, INVAL), (-1, 8, INVAL), (1, 12, SHAPE), (1, 1 << 31, SHAPE), (1, (1 << 30) + 8, SHAPE),
+    for rows, K, why in ((0, 8, INVAL), (1, 0, INVAL), (-1, 8, INVAL), (1, 12, SHAPE), (1, 1 << 31, SHAPE), (1, (1 << 26) + 8, SHAPE),
                          ((1 << 28) + 1, 8, SHAPE)):
         assert lib.spts_q4_bytes(rows, K, C.byref(c), C.byref(s)) == why, (rows, K)
     assert lib.spts_q4_bytes(1, 8, None, C.byref(s)) == INVAL and lib.spts_q4_bytes(1, 8, C.byref(c), None) == INVAL
@@ -83,7 +83,7 @@ def test_pack_and_matvec(lib, ctx):
     assert lib.spts_q4_pack(None, A, C.byref(w)) == INVAL
     mv = lambda m, x, n, y: lib.spts_matvec_q4(h, C.byref(m) if m is not None else None, x, n, y, 0)  # noqa: E731
     for m, why in ((q4(rows=0), INVAL), (q4(K=0), INVAL), (q4(K=-8), INVAL), (q4(K=60), SHAPE), (q4(codes=None), INVAL), (q4(scales=None), INVAL),
-                   (q4(codes=A + 4), ALIGN), (q4(scales=A + 4), ALIGN), (q4(rows=(1 << 28) + 1), SHAPE), (q4(K=(1 << 30) + 8), SHAPE)):
+                   (q4(codes=A + 4), ALIGN), (q4(scales=A + 4), ALIGN), (q4(rows=(1 << 28) + 1), SHAPE), (q4(K=(1 << 26) + 8), SHAPE)):
         assert pack(A, m) == why and mv(m, A, 1, 2 * A) == why
     assert mv(w, A, 0, None) == OK
     assert mv(w, A, -1, 2 * A) == INVAL and mv(w, A, 17, 2 * A) == INVAL
