@@ -338,7 +338,8 @@ int spts_kv4_read(spts_ctx *ctx, const spts_kv4 *caches, const int64_t *first, c
                   void *k_out, void *v_out);
 /* Decode attention over 4-bit caches: out[b, h] = softmax(q[b, h] K_b^T / sqrt(d)) V_b over all count rows of caches[b];
  * q, out [batch, H, d] of the element type, query head h reads key/value head h / (H / Hkv).  H / Hkv <= 16.  An empty
- * cache gives zeros.  The same cache may be given to several queries.  Uses the context's workspace. */
+ * cache gives zeros.  The same cache may be given to several queries.  out may be q itself, and must not overlap it otherwise.  Uses
+ * the context's workspace. */
 int spts_kv4_attn(spts_ctx *ctx, const void *q, int32_t batch, const spts_kv4 *caches, void *out);
 
 /* One layer's parameters for a decode step in 4 bits (layouts as in spts_layer_weights; gains in the element type). */
@@ -351,7 +352,7 @@ typedef struct {
  * D, H * d and Dff multiples of 8, d and H / Hkv as in spts_kv4_attn, count < capacity, distinct caches. */
 int spts_decode_layer_q4(spts_ctx *ctx, void *x, const int32_t *pos, int32_t batch, const spts_layer_q4 *w,
                          spts_kv4 *caches);
-/* RMSNorm with gamma [D] of x [batch, D] into xn [batch, D] (element type; batch <= SPTS_MAX_DECODE_BATCH): the
+/* RMSNorm with gamma [D] of x [batch, D] into xn [batch, D] (element type, not overlapping; batch <= SPTS_MAX_DECODE_BATCH): the
  * final norm in front of a head that is a spts_q4 matrix. */
 int spts_rmsnorm(spts_ctx *ctx, const void *x, const void *gamma, int32_t batch, void *xn);
 
@@ -361,7 +362,7 @@ typedef struct {
     const int32_t *history;        /* [batch, history_stride] token ids: the prompt, then the answer so far; ids outside
                                     * [0, V) are skipped (padding)                                               */
     int64_t history_stride;
-    const int64_t *history_len;    /* ids of each row that count (needed with history)                           */
+    const int64_t *history_len;    /* ids of each row that count, <= history_stride (needed with history)         */
     const int64_t *prompt_len;     /* the first of them that are the prompt (NULL = 0)                           */
     const float *repetition;       /* > 0; l > 0 ? l / r : l * r for every word in the history (NULL = 1)        */
     const float *frequency;        /* l - f * (times that the word is in the answer) (NULL = 0)                  */
@@ -372,7 +373,7 @@ typedef struct {
     int64_t mask_stride;           /* b at mask + b * mask_stride, 0 = one row for all                           */
 } spts_logits_rules;
 /* Applies the rules in the order of the struct's fields to logits [batch, V] (fp32) and writes logits_out [batch, V] (may
- * be logits itself).  token_out [batch] (NULL = not wanted): the allowed word with the largest result, ties to the lowest
+ * be logits itself, and must not overlap it otherwise).  token_out [batch] (NULL = not wanted): the allowed word with the largest result, ties to the lowest
  * id; -1 where no word is allowed (or all that are allowed are NaN); a masked NaN or infinity does not matter.
  * x_next [batch, D] (NULL = not wanted; needs token_out and table [V, D]): row token of the table, zeros for -1.
  * batch <= SPTS_MAX_DECODE_BATCH, V <= 2^28.  spts_greedy_token_batched's logits_out are such logits. */

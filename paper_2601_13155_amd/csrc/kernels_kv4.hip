@@ -26,7 +26,7 @@ template <int NB> struct Kv4Caches {
     const uint8_t *ks[NB], *vs[NB];
     int32_t cap[NB], n[NB];
     int32_t end[NB];                    // splits of sequence b: those before end[b] that are none of b - 1's; behind the last sequence its end
-    int32_t per;                        // keys of a split, a multiple of 32
+    uint32_t per;                       // keys of a split, a multiple of 32 (a little above 2^31 where one share takes the longest cache)
 };
 
 // the sequence that item i is in, and the first item of that sequence
@@ -303,7 +303,7 @@ template <int D> struct Kv4Step {
     uint32_t ks[2];
 };
 
-// One workgroup of four wavefronts per split of a sequence's keys and key/value head; a wavefront takes 32 keys at a time with its own running maximum
+// One workgroup of NW wavefronts per split of a sequence's keys and key/value head (4; 8 or 16 where one has a whole short cache); a wavefront takes 32 keys at a time with its own running maximum
 // and sum, all query heads of the head at once on the matrix cores:
 //   S^T = K Q^T: a key is an operand row (lane l16 = key, lane group kg = a quarter of the dimensions, one stored block), a query head a column.
 //     Of the two products of 16 keys, operand row m of product t is key 8 (m / 4) + 4 t + m % 4: lane group kg then holds the scores of the keys 8 kg .. 8 kg + 7.
@@ -312,8 +312,8 @@ template <int D> struct Kv4Step {
 //   In both results a column, i.e. lane % 16, is a query head, so the running maximum, the sum and the rescaling are the lane's own.
 // The maximum moves only when a score is 2^8 times above it (the sums stand that easily), so most steps have no rescaling.
 template <typename T, int D, int NW, int NB>
-__global__ void __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) kv4_attn_kernel(const T* __restrict__ q, Kv4Caches<NB> kb, int H, int Hkv, float scale_log2e, float* __restrict__ part,
-                                                                          T* __restrict__ out) {
+__global__ void __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) kv4_attn_kernel(const T* q, Kv4Caches<NB> kb, int H, int Hkv, float scale_log2e, float* __restrict__ part,
+                                                                          T* out) {   // (may be q: a workgroup has read its heads' queries before it writes them)
     constexpr bool F32 = sizeof(T) == 4;
     constexpr int NP = F32 ? 3 : 1;                       // bf16 parts of a query or weight
     constexpr int KW = D / 32, VM = D / 16, LD = D + 4;
@@ -535,7 +535,7 @@ static hipError_t launch_kv4_attn_n(const T* q, const Kv4Batch& kb, int64_t per,
         c.cap[b] = (int32_t)kb.cap[i]; c.n[b] = (int32_t)kb.count[i];
         ends.end[b] = c.end[b] = (b > 0 ? c.end[b - 1] : 0) + (b < kb.n ? (int32_t)(kb.count[b] > per ? (kb.count[b] + per - 1) / per : 1) : 0);
     }
-    c.per = (int32_t)per;
+    c.per = (uint32_t)per;
     const int splits = c.end[NB - 1], lds = (NW * (H / Hkv) * (D + 4) + NW * 32) * (int)sizeof(float);
     const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(&kv4_attn_kernel<T, D, NW, NB>), (NW * KV4_MAX_GROUP * (D + 4) + NW * 32) * (int)sizeof(float));
     if (e != hipSuccess) return e;

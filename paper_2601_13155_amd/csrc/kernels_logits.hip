@@ -88,7 +88,7 @@ __global__ void __launch_bounds__(LT) process_logits_kernel(const float* in, int
 #pragma unroll
         for (int j = 0; j < LW; ++j) x[j] = x[j] + (tid + j * LT < n ? bias[tid + j * LT] : 0.f);
     }
-    uint32_t word[LW];
+    uint32_t word[LW];   // (all ones without a mask: a condition `!mask || bit` came out wrong in the select below when the words beside it diverged)
 #pragma unroll
     for (int j = 0; j < LW; ++j) word[j] = ~0u;
     if (r.mask) {

@@ -48,12 +48,7 @@ hipError_t launch_q4_pack(const void* W, int64_t rows, int64_t K, void* codes, v
     return hipGetLastError();
 }
 
-// y = x W^T on the matrix cores for up to 16 vectors: a row of W is an operand row (lane l16), a vector a column; a dword of codes is an operand's eight values of a
-// lane, and the decoder's bf16 pairs are the operand.  Vectors are read from the caches, 64 bytes of each per load; an fp32 vector is taken as three bf16
-// parts, which is all of its 24 bits.  The NW wavefronts of a workgroup share the slabs of NS strips in turn, each with the codes and scales of its next slab on
-// their way while it works on one, and meet in LDS.  The order of a row's sum depends on K and NW alone, not on the vectors.  (Vectors asked for a slab ahead too take
-// 200 registers a lane, which halves the wavefronts on a CU: 28672 x 4096, one vector, 16.0 -> 22.6 us.)
-// (few arguments: quick launches)
+// A kernel's view of its matrices (few arguments make quick launches)
 template <int NM> struct Q4Mats { const u32x4* codes[NM]; const uint32_t* scales[NM]; void* y[NM]; int32_t rows[NM]; const void* x; int32_t K, nb; const void* gamma; float eps; };
 
 // One vector x [K] normalised on its way in: every workgroup takes its sum of squares and leaves the normalised vector, rounded as rmsnorm_kernel does it, in LDS
@@ -199,7 +194,7 @@ __global__ void __launch_bounds__(NW * 64) q4_matvec_f32_kernel(Q4Mats<NM> a) {
             for (int i = 0; i < 4; ++i) {
                 const float v[8] = {xw[i][0][0], xw[i][0][1], xw[i][0][2], xw[i][0][3], xw[i][1][0], xw[i][1][1], xw[i][1][2], xw[i][1][3]};
                 u32x4 xf[3];
-                bf16_parts<3>(v, xf);
+                bf16_parts<3, true>(v, xf);
 #pragma unroll
                 for (int s = 0; s < NS; ++s) {
                     const u32x4 w = fp4_decode8_bf16(c[s][t][i], i == 0 ? fp4_scale_of<0>(w4[s]) : i == 1 ? fp4_scale_of<1>(w4[s]) : i == 2 ? fp4_scale_of<2>(w4[s]) : fp4_scale_of<3>(w4[s]));

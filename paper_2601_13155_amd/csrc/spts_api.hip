@@ -1309,6 +1309,13 @@ int check_q4(const spts_q4* w) {
     return SPTS_OK;
 }
 
+// whether [a, a + na) and [b, b + nb) share a byte
+bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return x < y + (uintptr_t)nb && y < x + (uintptr_t)na;
+}
+int64_t elem_bytes(const spts_ctx* c) { return c->bf16 ? 2 : 4; }
+
 bool kv4_shape_ok(const spts_model_desc& m) { return m.d == 32 || m.d == 64 || m.d == 128; }
 
 // the descriptor of a call's caches; rows: what is read or written of each starts there
@@ -1369,6 +1376,7 @@ int spts_matvec_q4(spts_ctx* c, const spts_q4* W, const void* x, int32_t batch, 
     if (batch == 0) return SPTS_OK;
     if (!x || !y || x == y) return SPTS_EINVAL;
     if (!aligned16(x) || !aligned16(y)) return SPTS_EALIGN;
+    if (overlap(x, batch * W->K * elem_bytes(c), y, batch * W->rows * (y_f32 ? 4 : elem_bytes(c)))) return SPTS_EINVAL;
     Q4Args a{};
     a.codes[0] = W->codes; a.scales[0] = W->scales; a.rows[0] = W->rows; a.y[0] = y;
     a.x = x; a.K = W->K; a.nb = batch; a.mode = y_f32 ? Q4_F32 : Q4_STORE;
@@ -1435,6 +1443,8 @@ int spts_kv4_attn(spts_ctx* c, const void* q, int32_t batch, const spts_kv4* cac
     if (!aligned16(q) || !aligned16(out)) return SPTS_EALIGN;
     const auto& m = c->m;
     if (m.H / m.Hkv > KV4_MAX_GROUP) return SPTS_ESHAPE;
+    const int64_t bytes = (int64_t)batch * m.H * m.d * elem_bytes(c);
+    if (out != q && overlap(q, bytes, out, bytes)) return SPTS_EINVAL;
     Kv4Batch kb{};
     SPTS_TRY(kv4_batch(c, caches, batch, &kb));
     PHASE(c, PH_KV4_ATTN);
@@ -1448,6 +1458,8 @@ int spts_rmsnorm(spts_ctx* c, const void* x, const void* gamma, int32_t batch, v
     if (batch == 0) return SPTS_OK;
     if (!x || !gamma || !xn) return SPTS_EINVAL;
     if (!aligned16(x) || !aligned16(gamma) || !aligned16(xn)) return SPTS_EALIGN;
+    const int64_t bytes = (int64_t)batch * c->m.D * elem_bytes(c);
+    if (overlap(x, bytes, xn, bytes)) return SPTS_EINVAL;
     PHASE(c, PH_DEC_NORM);
     SPTS_HIP(c, launch_rmsnorm(x, gamma, c->m.rms_eps, xn, batch, c->m.D, c->bf16, c->stream));
     return SPTS_OK;
@@ -1520,6 +1532,7 @@ int spts_process_logits(spts_ctx* c, const float* logits, int32_t V, int32_t bat
     if (!logits || !logits_out || (x_next && (!token_out || !table))) return SPTS_EINVAL;
     if (!aligned16(logits) || !aligned16(logits_out) || (token_out && !aligned16(token_out)) || (x_next && (!aligned16(x_next) || !aligned16(table))))
         return SPTS_EALIGN;
+    if (logits_out != logits && overlap(logits, (int64_t)batch * V * 4, logits_out, (int64_t)batch * V * 4)) return SPTS_EINVAL;
     LogitsRules r{};
     if (rules->history) {
         if (!rules->history_len || rules->history_stride < 0) return SPTS_EINVAL;
@@ -1544,7 +1557,7 @@ int spts_process_logits(spts_ctx* c, const float* logits, int32_t V, int32_t bat
         if (!r.history) continue;
         r.len[b] = rules->history_len[b];
         r.prompt[b] = rules->prompt_len ? rules->prompt_len[b] : 0;
-        if (r.len[b] < 0 || r.len[b] > INT32_MAX || r.prompt[b] < 0 || (batch > 1 && r.len[b] > r.history_stride)) return SPTS_EINVAL;
+        if (r.len[b] < 0 || r.len[b] > INT32_MAX || r.prompt[b] < 0 || r.len[b] > r.history_stride) return SPTS_EINVAL;
     }
     if (token_out && logits_scratch_bytes(V, batch) > c->off.qp - c->off.tmp32) return SPTS_EWORKSPACE;
     PHASE(c, PH_LOGITS_RULES);

@@ -70,8 +70,9 @@ __device__ inline mfma_f32x4 mfma16(u32x4 a, u32x4 b, mfma_f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(mfma_bf16x8, a), __builtin_bit_cast(mfma_bf16x8, b), c, 0, 0, 0);
 }
 
-// eight fp32 values as N bf16 vectors whose sum they are (to 8 N bits)
-template <int N>
+// eight fp32 values as N bf16 vectors whose sum they are (to 8 N bits, three are exact): every part but the last is the upper half of what is left, so that no
+// finite value becomes infinite on the way.  INF: an infinity is its first part alone (the others would be NaN).
+template <int N, bool INF = false>
 __device__ inline void bf16_parts(const float* v, u32x4 (&out)[N]) {
     float r[8];
 #pragma unroll
@@ -80,11 +81,12 @@ __device__ inline void bf16_parts(const float* v, u32x4 (&out)[N]) {
     for (int p = 0; p < N; ++p)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const uint32_t w = cvt_pk_bf16(r[2 * j], r[2 * j + 1]);
-            out[p][j] = w;
-            if (p + 1 < N) {
-                r[2 * j] -= __uint_as_float(w << 16);
-                r[2 * j + 1] -= __uint_as_float(w & 0xffff0000u);
+            if (p + 1 == N) { out[p][j] = cvt_pk_bf16(r[2 * j], r[2 * j + 1]); continue; }
+            out[p][j] = __builtin_amdgcn_perm(__float_as_uint(r[2 * j + 1]), __float_as_uint(r[2 * j]), 0x07060302);
+#pragma unroll
+            for (int h = 2 * j; h < 2 * j + 2; ++h) {
+                const float rest = r[h] - __uint_as_float(__float_as_uint(r[h]) & 0xffff0000u);
+                r[h] = INF && p == 0 && fabsf(r[h]) == INFINITY ? 0.f : rest;
             }
         }
 }

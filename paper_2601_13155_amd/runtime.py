@@ -280,7 +280,7 @@ class LogitsRules:
     def __init__(self, batch: int, history=None, history_len=None, prompt_len=None, repetition=None, frequency=None, presence=None,
                  bias=None, mask=None):
         self.struct = s = binding.spts_logits_rules()
-        self._keepalive = (history, bias, mask)
+        self.batch, self._keepalive = batch, (history, bias, mask)
 
         def host(values, typ):
             if values is None:
@@ -294,6 +294,10 @@ class LogitsRules:
                 raise ValueError("bias and mask: one contiguous row, or one per sequence")
             return t.data_ptr(), 0 if t.dim() == 1 or t.shape[0] == 1 else t.shape[1]
 
+        torch = _torch()
+        for t, name, dts in ((history, "history", (torch.int32,)), (bias, "bias", (torch.float32,)), (mask, "mask", (torch.int32, torch.uint32))):
+            if t is not None and t.dtype not in dts:
+                raise ValueError(f"{name}: {dts[0]}, not {t.dtype}")
         if history is not None:
             if history.dim() != 2 or history.shape[0] != batch or not history.is_contiguous() or history_len is None:
                 raise ValueError("history: a contiguous [batch, n] tensor, with history_len")
@@ -325,6 +329,16 @@ class Q4DecodeRunner:
         self.gamma_f, self.table, self.head = gamma_f, table, head
         self.batch = len(caches[0].structs)
         self.rules = rules if rules is not None else LogitsRules(self.batch)
+        V = int(table.shape[0])
+        if len(layers) != len(caches) or any(len(c.structs) != self.batch for c in caches):
+            raise ValueError("one KV4Batch per layer, all of the same number of sequences")
+        if head.struct.rows != V or head.struct.K != shape.D or int(table.shape[1]) != shape.D:
+            raise ValueError("table and head: [V, D]")
+        if self.rules.batch != self.batch:
+            raise ValueError("rules for another number of sequences")
+        _, bias, mask = self.rules._keepalive
+        if (bias is not None and bias.shape[-1] < V) or (mask is not None and mask.shape[-1] < (V + 31) // 32):
+            raise ValueError(f"bias and mask: rows of {V} words")
         tdt = torch.bfloat16 if shape.dtype == "bf16" else torch.float32
         self.x = torch.zeros((self.batch, shape.D), dtype=tdt, device="cuda")
         self.x_next, self.xn = torch.zeros_like(self.x), torch.zeros_like(self.x)
@@ -345,8 +359,12 @@ class Q4DecodeRunner:
 
     def generate(self, pos0: List[int], steps: int, tokens_out=None):
         """steps decode steps from self.x at positions pos0; tokens_out [batch, steps] int32 device.  With a history in the
-        rules every token joins it (SPTS_EINVAL from the call once a row is full)."""
+        rules every token joins it: ValueError, before any step, if its rows or the caches have no room for that many."""
         hist, lens = self.rules._keepalive[0], self.rules.history_len
+        if hist is not None and any(n + steps > hist.shape[1] for n in lens):
+            raise ValueError(f"the history's rows of {hist.shape[1]} ids have no room for {steps} more")
+        if any(s.count + steps > s.capacity for c in self.caches for s in c.structs):
+            raise ValueError(f"a cache has no room for {steps} more pairs")
         for t in range(steps):
             self.step([p + t for p in pos0])
             self.next_token()

@@ -128,6 +128,38 @@ def test_pack_limits(torch, dtype):
     assert np.isnan(got[:, 6]).all()                   # a NaN block poisons the row's sums
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_product_with_infinities_and_the_largest_numbers(torch, dtype):
+    """A vector's infinity, NaN or largest number reaches the rows as IEEE arithmetic has it (an infinity times a stored zero is NaN), and no other
+    vector of the batch."""
+    ctx, _ = ctx_for(dtype)
+    rng = np.random.default_rng(8)
+    rows, K = 33, 600
+    W = rng.choice(np.array([0.0, 0.25, -0.25, 0.5, -0.5]), (rows, K)).astype(np.float32)
+    W[:, ::32] = 0.5                                    # exact in 4 bits
+    x = rng.integers(-8, 9, (6, K)).astype(np.float32)
+    top = np.float32(3.4028234e38) if dtype == "f32" else np.float32(3.3895314e38)
+    x[0, 37], x[1, 599], x[3, 0], x[4, 300], x[4, 301] = np.inf, -np.inf, top, top, -top
+    x[2, 5] = np.array([0x7f800001], dtype=np.uint32).view(np.float32)[0]               # a NaN whose upper half alone is an infinity
+    xd = runtime.to_device(x, dtype)
+    if dtype == "bf16":
+        xd[2, 5] = float("nan")
+    m = runtime.Q4Matrix(ctx, runtime.to_device(W, dtype))
+    y = torch.empty((6, rows), dtype=torch.float32, device="cuda")
+    ctx.spts_matvec_q4(m.struct, xd, 6, y, 1)
+    torch.cuda.synchronize()
+    got = y.cpu().numpy().astype(np.float64)
+    with np.errstate(invalid="ignore"):
+        x64 = x.astype(np.float64)
+        ref = np.array([[(W[r].astype(np.float64) * x64[b]).sum() for r in range(rows)] for b in range(6)])
+    assert np.isinf(ref[:2]).any() and np.isnan(ref[:2]).any() and np.isnan(ref[2]).all()
+    assert np.array_equal(np.isnan(got), np.isnan(ref)) and np.array_equal(got[np.isinf(ref)], ref[np.isinf(ref)])
+    fin = np.isfinite(ref)
+    mag = np.abs(np.where(np.isfinite(x64), x64, 0.0)) @ np.abs(W.astype(np.float64)).T
+    assert np.all(np.abs(got[fin] - ref[fin]) <= (SUM(K) * mag + 2.0 ** -24 * np.abs(np.where(fin, ref, 0)))[fin])
+    assert np.array_equal(got[5], ref[5])               # whole numbers and quarters
+
+
 # ------------------------------------------------------------------------------------------------------------- caches
 def make_pairs(rng, n, Hkv, d, dtype):
     k = rounded(rng.standard_normal((n, Hkv, d)) * np.exp(rng.standard_normal((1, Hkv, d))), dtype)
@@ -311,6 +343,37 @@ def test_attention_over_a_long_cache(torch):
     ctx.spts_kv4_read(caches.structs, [0, 3], back, vb, first=[n - 3])
     torch.cuda.synchronize()
     assert np.array_equal(runtime.to_host(vb), v) and np.array_equal(runtime.to_host(back), k)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_in_place_and_on_two_streams(torch, dtype):
+    """The output may be the queries' place; two contexts on streams of their own do not touch each other's shares (one launch and two)."""
+    rng = np.random.default_rng(77)
+    shape = synth.ModelShape(D=256, H=8, Hkv=2, d=64, Dff=688, dtype=dtype)
+    made = []
+    for lens in ([2100, 70, 4000], [100, 300, 9]):
+        for _ in range(2):
+            st = torch.cuda.Stream()
+            with torch.cuda.stream(st):
+                c = binding.Context(shape, 64, 1, 1, shape.Dff, stream=st)
+                caches = runtime.KV4Batch(shape, [n + 1 for n in lens])
+                append(torch, c, caches, [make_pairs(rng, n, 2, 64, dtype) + (np.arange(n),) for n in lens], dtype)
+                q = runtime.to_device(rounded(rng.standard_normal((3, 8, 64)), dtype), dtype)
+                alone = torch.empty_like(q)
+                c.spts_kv4_attn(q, caches.structs, alone)
+            torch.cuda.synchronize()
+            made.append((c, caches, q, alone, st))
+    for _ in range(20):
+        outs = [torch.full_like(m[2], 9.0) for m in made]
+        torch.cuda.synchronize()
+        for (c, caches, q, _, st), out in zip(made, outs):
+            c.spts_kv4_attn(q, caches.structs, out)
+        torch.cuda.synchronize()
+        assert all(torch.equal(out, m[3]) for out, m in zip(outs, made))
+    for c, caches, q, alone, _ in made:
+        c.spts_kv4_attn(q, caches.structs, q)
+    torch.cuda.synchronize()
+    assert all(torch.equal(m[2], m[3]) for m in made)
 
 
 # -------------------------------------------------------------------------------------------------------------- rules

@@ -89,6 +89,7 @@ def test_pack_and_matvec(lib, ctx):
     assert mv(w, A, -1, 2 * A) == INVAL and mv(w, A, 17, 2 * A) == INVAL
     assert mv(w, None, 1, A) == INVAL and mv(w, A, 1, None) == INVAL and mv(w, A, 1, A) == INVAL and mv(None, A, 1, 2 * A) == INVAL
     assert mv(w, A + 2, 1, 2 * A) == ALIGN and mv(w, A, 1, 2 * A + 4) == ALIGN
+    assert mv(w, A, 2, A + 496) == INVAL and mv(w, A + 112, 2, A) == INVAL            # 512 bytes of vectors, 128 of results: the last and the first overlap
 
 
 def test_caches(lib, ctx):
@@ -125,6 +126,7 @@ def test_attention(lib, ctx):
     assert att(0, None) == OK and att(-1, kv4(count=8)) == INVAL and att(17, kv4(17, count=8)) == INVAL
     assert att(1, None) == INVAL and att(1, kv4(count=8), q=None) == INVAL and att(1, kv4(count=8), out=None) == INVAL
     assert att(1, kv4(count=8), q=A + 4) == ALIGN and att(1, kv4(count=8), out=A + 4) == ALIGN
+    assert att(2, kv4(2, count=8), out=A + 2032) == INVAL and att(2, kv4(2, count=8), q=A + 1024) == INVAL   # out is q or lies apart
     assert att(1, kv4(count=65)) == INVAL and att(1, kv4(capacity=12, count=8)) == SHAPE
     assert att(1, kv4(count=8), at=ctx(H=17, Hkv=1)) == SHAPE and att(1, kv4(count=8), at=ctx(d=16)) == SHAPE
 
@@ -149,6 +151,7 @@ def test_layer(lib, ctx):
     assert run(layer(), 1, kv4(count=64)) == INVAL and run(layer(), 2, kv4(2, k=A)) == INVAL
     assert run(layer(), 2, kv4(2), p=(C.c_int32 * 2)(5, -1)) == INVAL
     m = binding.model_desc(synth.TINY)
+    assert lib.spts_rmsnorm(h, A, A, 2, A) == INVAL and lib.spts_rmsnorm(h, A, A, 2, A + 2032) == INVAL
     assert lib.spts_rmsnorm(h, A, A, 0, None) == OK and lib.spts_rmsnorm(h, A, A, 17, A) == INVAL
     assert lib.spts_rmsnorm(h, A, None, 1, A) == INVAL and lib.spts_rmsnorm(h, A, A + 4, 1, A) == ALIGN
     assert m.D == 256
@@ -174,6 +177,8 @@ def test_rules(lib, ctx):
     for n in (i64(-1, 0), i64(1 << 31, 0)):
         assert run(rules(history=A, history_stride=4, history_len=n)) == INVAL
     assert run(rules(history=A, history_stride=4, history_len=i64(5, 4)), n=2) == INVAL  # rows overlap
+    assert run(rules(history=A, history_stride=4, history_len=i64(5))) == INVAL
+    assert run(rules(), n=2, y=A + 496) == INVAL and run(rules(), x=A + 240) == INVAL       # results are the logits' own place or lie apart
     assert run(rules(history=A, history_stride=4, history_len=i64(4), prompt_len=i64(-1))) == INVAL
     assert run(rules(history=A + 4, history_stride=4, history_len=i64(4))) == ALIGN
     for name in ("repetition", "frequency", "presence"):
@@ -191,6 +196,31 @@ def test_runtime_checks_its_arguments():
     r = runtime.LogitsRules(2, history=hist, history_len=[3, 8], repetition=[1.1, 1.2], bias=torch.zeros(64))
     assert r.struct.history_stride == 8 and r.struct.bias_stride == 0 and list(r.struct.history_len[:2]) == [3, 8]
     for kw in (dict(history=hist), dict(history=hist, history_len=[3]), dict(history=hist, history_len=[3, 9]), dict(repetition=[1.0]),
-               dict(history=hist[:1], history_len=[3, 3]), dict(mask=torch.zeros((3, 2), dtype=torch.int32)), dict(bias=torch.zeros((64, 2)).t())):
+               dict(history=hist[:1], history_len=[3, 3]), dict(mask=torch.zeros((3, 2), dtype=torch.int32)), dict(bias=torch.zeros((64, 2)).t()),
+               dict(history=hist.long(), history_len=[3, 8]), dict(bias=torch.zeros(64, dtype=torch.float64)), dict(mask=torch.zeros(2, dtype=torch.int64))):
         with pytest.raises(ValueError):
             runtime.LogitsRules(2, **kw)
+
+
+def test_runner_checks_its_arguments(monkeypatch):
+    """What would write behind a buffer, or fail in the middle of a run, is refused before anything is done (host tensors: nothing is launched)."""
+    import types
+
+    import torch
+    from paper_2601_13155_amd import runtime
+    monkeypatch.setattr(torch, "zeros", lambda *a, device=None, _zeros=torch.zeros, **kw: _zeros(*a, **kw))
+    shape = synth.ModelShape(D=64, H=4, Hkv=2, d=32, Dff=64, dtype="f32")
+    caches = lambda n, count=0: types.SimpleNamespace(structs=kv4(n, capacity=16, count=count))  # noqa: E731
+    head = lambda rows, K=64: types.SimpleNamespace(struct=q4(rows, K))  # noqa: E731
+    table = torch.zeros((96, 64))
+    make = lambda cs, hd=head(96), layers=(None,), t=table, rules=None: runtime.Q4DecodeRunner(None, shape, list(layers), cs, None, t, hd, rules)  # noqa: E731
+    make([caches(2)])
+    hist = torch.zeros((2, 8), dtype=torch.int32)
+    for bad in (lambda: make([caches(2)], layers=(None, None)), lambda: make([caches(2), caches(3)], layers=(None, None)),
+                lambda: make([caches(2)], head(112)), lambda: make([caches(2)], head(96, 128)), lambda: make([caches(2)], t=torch.zeros((96, 32))),
+                lambda: make([caches(2)], rules=runtime.LogitsRules(3)), lambda: make([caches(2)], rules=runtime.LogitsRules(2, bias=torch.zeros(95))),
+                lambda: make([caches(2)], rules=runtime.LogitsRules(2, mask=torch.zeros((2, 2), dtype=torch.int32))),
+                lambda: make([caches(2)], rules=runtime.LogitsRules(2, history=hist, history_len=[3, 6])).generate([0, 0], 3),
+                lambda: make([caches(2, count=14)]).generate([0, 0], 3)):
+        with pytest.raises(ValueError):
+            bad()
