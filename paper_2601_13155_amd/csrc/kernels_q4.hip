@@ -141,15 +141,15 @@ __device__ inline void q4_finish(const Q4Mats<NM>& a, const Q4Strips<NS>& st, co
 }
 
 // y = x W^T on the matrix cores for up to 16 vectors: a row of W is an operand row (lane l16), a vector a column; a dword of codes is an operand's eight values of a
-// lane, and the decoder's bf16 pairs are the operand.  The NW wavefronts of a workgroup share the slabs of NS strips in turn and meet in LDS; the order of a
-// row's sum depends on K and NW alone, not on the vectors.
-// fp32 vectors are taken as three bf16 parts, which is all of their 24 bits, and are read from the caches a tile at a time; codes and scales of the next slab are on
-// their way while one is worked on.
+// lane, and the decoder's bf16 pairs are the operand.  The NW wavefronts of a workgroup share the tiles of NS strips in turn and meet in LDS, so the order of a
+// row's sum depends on K and NW alone, not on the vectors.  (A slab at a time instead of a tile: 28672 x 4096 12.8 instead of 12.1 us, 3584 x 18944 8.9 instead of 8.1.)
+// fp32 vectors are taken as three bf16 parts, which is all of their 24 bits, and are read from the caches a tile at a time; codes and scales of the next four tiles
+// are on their way while four are worked on.
 template <int MODE, int NM, int NS, int NW>
 __global__ void __launch_bounds__(NW * 64) q4_matvec_f32_kernel(Q4Mats<NM> a) {
     __shared__ __attribute__((aligned(16))) float sred[NW][NS][16][20];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, kg = lane >> 4;
-    const int slabs = (a.K + Q4_SLAB - 1) / Q4_SLAB, K = a.K;
+    const int K = a.K, slabs = (K + Q4_SLAB - 1) / Q4_SLAB, ntiles = (K + 127) / 128;
     const Q4Strips<NS> st = q4_strips<MODE, NM, NS>(a, slabs);
     const bool vec = l16 < a.nb;
     const float* const x = (const float*)a.x + (int64_t)(vec ? l16 : 0) * K + kg * 8;
@@ -158,16 +158,21 @@ __global__ void __launch_bounds__(NW * 64) q4_matvec_f32_kernel(Q4Mats<NM> a) {
     for (int s = 0; s < NS; ++s) acc[s] = mfma_f32x4{0.f, 0.f, 0.f, 0.f};
     u32x4 cn[NS][4];
     uint32_t sn[NS];
-    auto load = [&](int slab) {
+    // tiles first, first + NW, ...; behind the last one, that again
+    auto load = [&](int first) {
+        const int own = first + NW * kg;
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
 #pragma unroll
-            for (int t = 0; t < 4; ++t) cn[s][t] = __builtin_nontemporal_load(st.codes[s] + (slab * 4 + t) * 64 + lane);
-            sn[s] = __builtin_nontemporal_load(st.scales[s] + slab * 64 + lane);
+            for (int t = 0; t < 4; ++t) {
+                const int tile = first + NW * t;
+                cn[s][t] = __builtin_nontemporal_load(st.codes[s] + (tile < ntiles ? tile : ntiles - 1) * 64 + lane);
+            }
+            sn[s] = __builtin_nontemporal_load(st.scales[s] + (own < ntiles ? own : ntiles - 1) * 16 + l16);
         }
     };
-    if (wave < slabs) load(wave);
-    for (int slab = wave; slab < slabs; slab += NW) {
+    if (wave < ntiles) load(wave);
+    for (int first = wave; first < ntiles; first += 4 * NW) {
         u32x4 c[NS][4];
         uint32_t sc[NS];
 #pragma unroll
@@ -176,16 +181,18 @@ __global__ void __launch_bounds__(NW * 64) q4_matvec_f32_kernel(Q4Mats<NM> a) {
             for (int t = 0; t < 4; ++t) c[s][t] = cn[s][t];
             sc[s] = sn[s];
         }
-        if (slab + NW < slabs) load(slab + NW);
+        if (first + 4 * NW < ntiles) load(first + 4 * NW);
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
+            const int k0 = (first + NW * t) * 128;
+            if (k0 >= K) break;
             uint32_t w4[NS];   // the tile's four scales of the lane's row, which lane 16 t + l16 has loaded
 #pragma unroll
             for (int s = 0; s < NS; ++s) w4[s] = (uint32_t)__builtin_amdgcn_ds_bpermute((16 * t + l16) * 4, (int)sc[s]);
             f32x4 xw[4][2];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int k = slab * Q4_SLAB + t * 128 + i * 32;
+                const int k = k0 + i * 32;
                 const bool in = vec && k + kg * 8 < K;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) xw[i][h] = in ? reinterpret_cast<const f32x4*>(x + k)[h] : f32x4{0.f, 0.f, 0.f, 0.f};
@@ -211,7 +218,8 @@ __global__ void __launch_bounds__(NW * 64) q4_matvec_f32_kernel(Q4Mats<NM> a) {
 // every vector, on however many CUs.  So codes, scales and vectors go to LDS with loads that are laid out for memory, whole lines of 4 vectors an instruction, into a
 // ring of DEPTH tiles (128 k) of each wavefront; a wavefront reads only what it has loaded itself, after its own vmcnt wait, so there is no barrier in the loop.
 // Piece c (16 bytes) of vector r lies at slot c ^ r of its row, which spreads the 16 rows of an operand over the banks.  4096 x 14336, 2 / 4 / 8 / 16 vectors 9.7 / 10.9 /
-// 12.8 / 17.5 -> 7.1 / 7.9 / 9.3 / 11.9 us.  4 XI: vectors there is room for; 0: a single one that is normalised on its way in.
+// 12.8 / 17.5 -> 7.1 / 7.9 / 9.3 / 11.9 us; of sixteen a CU still takes in no more than 30 bytes a clock, with three tiles in flight or with workgroups
+// that begin at different tiles as well (14.8 / 14.9 / 14.8 us for 3584 x 18944).  4 XI: vectors there is room for; 0: a single one that is normalised on its way in.
 template <int NS, int XI> constexpr int q4_stage_bytes() { return NS * (1024 + 256) + XI * 1024; }
 template <int MODE, int NM, int NS, int NW, int XI, int DEPTH>
 __global__ void __launch_bounds__(NW * 64) q4_matvec_kernel(Q4Mats<NM> a) {
@@ -224,16 +232,13 @@ __global__ void __launch_bounds__(NW * 64) q4_matvec_kernel(Q4Mats<NM> a) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, kg = lane >> 4;
     const int K = a.K, slabs = (K + Q4_SLAB - 1) / Q4_SLAB, ntiles = (K + 127) / 128;
     const Q4Strips<NS> st = q4_strips<MODE, NM, NS>(a, slabs);
-    // tile n of this wavefront: slab wave + NW (n / 4), tile n % 4 of it; those behind K are left out
-    const int mine = wave < slabs ? (slabs - wave + NW - 1) / NW : 0;
-    int N = mine * 4;
-    if (mine > 0 && wave + NW * (mine - 1) == slabs - 1) N -= slabs * 4 - ntiles;
+    const int N = wave < ntiles ? (ntiles - wave + NW - 1) / NW : 0;   // tiles wave, wave + NW, ...
     int row[XI + NORM];
 #pragma unroll
     for (int j = 0; j < XI; ++j) row[j] = 4 * j + kg < a.nb ? 4 * j + kg : a.nb - 1;   // (behind the last vector any: its column is not stored)
     const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)ring + (uint32_t)wave * (DEPTH * STAGE);
     auto issue = [&](int n) {
-        const int tile = (wave + NW * (n >> 2)) * 4 + (n & 3), k0 = tile * 128;
+        const int tile = wave + NW * n, k0 = tile * 128;
         const uint32_t slot = base + (uint32_t)(n % DEPTH) * STAGE;
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
@@ -265,7 +270,7 @@ __global__ void __launch_bounds__(NW * 64) q4_matvec_kernel(Q4Mats<NM> a) {
             sc[s] = *reinterpret_cast<const uint32_t*>(slot + NS * 1024 + s * 256 + lane * 4);
         }
         const int xr = l16 & (4 * XI - 1);         // (with room for 4 or 8 vectors the columns behind repeat them, with one alone all do)
-        const int k0 = ((wave + NW * (n >> 2)) * 4 + (n & 3)) * 128;
+        const int k0 = (wave + NW * n) * 128;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             xv[i] = NORM ? xl[k0 / 8 + 4 * i + kg] : *reinterpret_cast<const u32x4*>(slot + NS * 1280 + xr * 256 + (((4 * i + kg) ^ xr) * 16));
@@ -338,9 +343,10 @@ static hipError_t launch_q4_matvec_m(const Q4Args& a, hipStream_t s) {
 
 // How many strips a workgroup takes.  A launch costs about 4 us before the codes stream at 6 TB/s, so few strips are spread over the chip, one or two workgroups
 // of eight wavefronts to a CU; of many, fewer and longer workgroups lose less on their ends, and several strips share what is read of the vectors.  bf16, us for
-// 1 / 2 strips with 8 / 4 strips with 4 wavefronts (2 with 4, 4 with 8): 6144 x 4096, one vector 5.3 / 5.0, sixteen 8.3 / 6.4; 8192 x 8192, sixteen 14.8 / 10.8; 12288 x
-// 4096 7.7 / 7.8 / 7.7 (7.3, 7.8) and 12.6 / 11.3 / 9.0 (10.0, 9.2); 28672 x 4096 14.6 / 14.8 / 12.7 (14.2, 16.3) and 27.0 / 22.4 / 15.3 (18.2, 18.4); 128256 x 4096
-// 57.0 / 49.2 / 45.2 (46.4, 55.1) and 118 / 83.6 / 53.6 (63.3, 66.7).  It goes by the matrices alone, and with it the order of a sum.
+// 1 / 2 strips with 8 / 4 strips with 4 wavefronts (2 with 4, 4 with 8): 4096 x 14336, one vector 7.2 / 9.0 / 15.8 (12.8, 13.8), sixteen 12.0 / 14.4 / 19.2; 6144 x
+// 4096 5.1 / 4.6 / 6.4 and 8.1 / 5.9 / 7.5; 8192 x 8192 9.6 / 7.6 / 10.7 and 13.9 / 9.8 / 12.5; 12288 x 4096 7.4 / 6.7 / 6.9 (6.5, 6.8) and 12.1 / 10.2 / 7.9 (9.3, 8.2);
+// 28672 x 4096 14.6 / 12.6 / 12.3 (12.4, 13.5) and 26.6 / 19.4 / 14.0 (16.1, 15.4); 128256 x 4096 56.1 / 42.2 / 43.2 (42.4, 49.9) and 117 / 76.2 / 49.5 (59.9, 59.4).
+// fp32, 28672 x 4096: 35.5 / 33.7 / 24.1 (28.6) and 55.9 / 43.4 / 28.2 (38.6).  It goes by the matrices alone, and with it the order of a sum.
 template <typename T>
 static hipError_t launch_q4_matvec_t(const Q4Args& a, hipStream_t s) {
     int64_t strips = 0;
