@@ -137,6 +137,8 @@ def main():
     ap.add_argument("--vocab", type=int, default=128256, help="rows of the synthetic vocabulary table of the decode leg")
     ap.add_argument("--decode-batch", type=int, default=8,
                     help="sequences of the batched decode leg (copies of the prefill caches decoded together, at most 16; 0 or 1 = skip it)")
+    ap.add_argument("--decode-q4", action="store_true",
+                    help="the decode leg once more with weights, vocabulary table and caches in 4 bits (one sequence and --decode-batch of them)")
     ap.add_argument("--builder-tokens", type=int, default=8192,
                     help="calibration tokens of the offline channel-importance leg (0 = skip it)")
     ap.add_argument("--batch-seqs", type=int, default=4,
@@ -391,6 +393,34 @@ def main():
                                  "gbs": btot / (bms * 1e-3) / 1e9, "hbm_frac": btot / (bms * 1e-3) / 1e9 / PEAK_HBM_GBS}
             log(f"[decode, batch of {nb}] {bms:.3f} ms/step = {nb * 1e3 / bms:.0f} tokens/s")
             del bc, bdec
+        # the same step in 4 bits, over the same pairs
+        if args.decode_q4:
+            packed = [runtime.pack_layer_q4(ctx, w) for w in dev_sets]
+            head = runtime.Q4Matrix(ctx, table)
+            decode["q4"] = {}
+            for nb in sorted({1, max(1, min(args.decode_batch, 16))}):
+                k4 = [runtime.KV4Batch(shape, [cn + steps_d + 1] * nb) for cn in cached]
+                for kb, c0, cn in zip(k4, caches, cached):
+                    for s in range(nb):
+                        one = [kb.structs[s]]
+                        ctx.spts_kv4_append(c0.k, c0.v, c0.pos, [0, cn], one)
+                        kb.structs[s].count = cn
+                qdec = runtime.Q4DecodeRunner(ctx, shape, [packed[l % pool] for l in range(wl.layers)], k4, gamma_f, table, head)
+                qdec.x.copy_(table[1:1 + nb])
+                qdec.generate([wl.N] * nb, 1)
+                torch.cuda.synchronize()
+                e0.record()
+                qdec.generate([wl.N + 1] * nb, steps_d)
+                e1.record()
+                torch.cuda.synchronize()
+                qms = e0.elapsed_time(e1) / steps_d
+                bits = 17.0 / 32.0 / b                  # bytes of a stored value against one of the element type
+                qtot = bits * (wbytes + nb * kvbytes + head_bytes)
+                decode["q4"][f"{nb}_sequences"] = {"steps": steps_d, "ms_per_step": qms, "tokens_per_s": nb * 1e3 / qms,
+                                                   "gbs": qtot / (qms * 1e-3) / 1e9, "hbm_frac": qtot / (qms * 1e-3) / 1e9 / PEAK_HBM_GBS}
+                log(f"[decode in 4 bits, {nb} sequence(s)] {qms:.3f} ms/step = {nb * 1e3 / qms:.0f} tokens/s")
+                del k4, qdec
+            del packed, head
         del caches, crunner, dec
         # the same decode over the full caches of a dense prefill (every layer keeps all N pairs): the library's own
         # baseline for the end-to-end figure

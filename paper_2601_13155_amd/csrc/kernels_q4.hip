@@ -51,41 +51,79 @@ hipError_t launch_q4_pack(const void* W, int64_t rows, int64_t K, void* codes, v
 // A kernel's view of its matrices (few arguments make quick launches)
 template <int NM> struct Q4Mats { const u32x4* codes[NM]; const uint32_t* scales[NM]; void* y[NM]; int32_t rows[NM]; const void* x; int32_t K, nb; const void* gamma; float eps; };
 
-// One vector x [K] normalised on its way in: every workgroup takes its sum of squares and leaves the normalised vector, rounded as rmsnorm_kernel does it, in LDS
-// (zeros up to whole slabs), where the products read it.  The first codes are already on their way; a norm of its own would be a launch of 3 us.
+// Up to four vectors normalised on their way in.  Every workgroup reads them and gamma into LDS (norm_load, a KB of a vector an instruction; ahead of the ring's
+// loads, which a load behind them would have to wait for), takes the sums of squares and leaves the normalised vectors, rounded as rmsnorm_kernel does it,
+// in their place (zeros up to whole slabs).  Piece c (16 bytes) of vector b lies at slot c ^ 4 b, which spreads the vectors of an operand over the banks.
+// A wavefront reads only what it has loaded itself until the sums meet.
+constexpr int Q4_NORM_NB = 4;
+constexpr int Q4_NORM_SLABS = 40;   // KB of LDS: the vectors and gamma
 template <int NW>
-__device__ inline void norm_to_lds(const bf16_t* __restrict__ x, const bf16_t* __restrict__ gamma, float eps, int K, int slabs, u32x4* xl, float* red) {
-    const int tid = threadIdx.x, chunks = K / 8;
-    float ss = 0.f;
-    for (int c = tid; c < chunks; c += NW * 64) {
-        const u32x4 w = reinterpret_cast<const u32x4*>(x)[c];
+__device__ inline void norm_load(const bf16_t* x, const bf16_t* gamma, int K, int slabs, int nb, uint32_t at) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    for (int b = 0; b <= nb; ++b)
+        for (int s = wave; s < slabs; s += NW) {
+            const int piece = s * 64 + (b < nb ? lane ^ (4 * b) : lane);
+            dma16s(piece * 8 < K ? (uint32_t)piece * 16 : 0u, b < nb ? x + (int64_t)b * K : gamma, at + (uint32_t)(b * slabs + s) * 1024);
+        }
+}
+// NV: vectors taken together, so that their latencies overlap (those behind the last repeat the first and are not stored)
+template <int NW, int NV>
+__device__ inline void norm_in_lds(u32x4* xl, float* red, float eps, int K, int slabs, int nb) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const u32x4* const gl = xl + nb * slabs * 64;
+    float ss[NV];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float a = __uint_as_float(w[i] << 16), b = __uint_as_float(w[i] & 0xffff0000u);
-            ss += a * a; ss += b * b;
+    for (int b = 0; b < NV; ++b) ss[b] = 0.f;
+    for (int s = wave; s < slabs; s += NW) {
+#pragma unroll
+        for (int b = 0; b < NV; ++b) {
+            const int at = b < nb ? b : 0, slot = s * 64 + lane;
+            u32x4 w = xl[at * slabs * 64 + slot];
+            w = (slot ^ (4 * at)) * 8 < K ? w : u32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float lo = __uint_as_float(w[i] << 16), hi = __uint_as_float(w[i] & 0xffff0000u);
+                ss[b] += lo * lo; ss[b] += hi * hi;
+            }
         }
     }
-    ss = wave_sum(ss);
-    if ((tid & 63) == 0) red[tid >> 6] = ss;
-    __syncthreads();
-    ss = 0.f;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) ss += red[w];
-    const float inv = 1.0f / sqrtf(ss / (float)K + eps);
-    for (int c = tid; c < slabs * (Q4_SLAB / 8); c += NW * 64) {
-        u32x4 o{0, 0, 0, 0};
-        if (c < chunks) {
-            const u32x4 w = reinterpret_cast<const u32x4*>(x)[c], g = reinterpret_cast<const u32x4*>(gamma)[c];
+    for (int b = 0; b < NV; ++b) {
+        ss[b] = group_sum<16>(ss[b]);
+        ss[b] += __shfl_xor(ss[b], 16);
+        ss[b] += __shfl_xor(ss[b], 32);
+    }
+#pragma unroll
+    for (int b = 0; b < NV; ++b)
+        if (lane == 0) red[b * NW + wave] = ss[b];
+    __syncthreads();
+    float inv[NV];
+#pragma unroll
+    for (int b = 0; b < NV; ++b) {
+        float sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) sum += red[b * NW + w];
+        inv[b] = 1.0f / sqrtf(sum / (float)K + eps);
+    }
+    for (int s = wave; s < slabs; s += NW) {
+        const int slot = s * 64 + lane;
+        u32x4 o[NV];
+#pragma unroll
+        for (int b = 0; b < NV; ++b) {
+            const int at = b < nb ? b : 0, piece = slot ^ (4 * at);
+            const u32x4 w = xl[at * slabs * 64 + slot], g = gl[piece];
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                o[i] = cvt_pk_bf16(__uint_as_float(w[i] << 16) * inv * __uint_as_float(g[i] << 16),
-                                   __uint_as_float(w[i] & 0xffff0000u) * inv * __uint_as_float(g[i] & 0xffff0000u));
+                o[b][i] = cvt_pk_bf16(__uint_as_float(w[i] << 16) * inv[b] * __uint_as_float(g[i] << 16),
+                                      __uint_as_float(w[i] & 0xffff0000u) * inv[b] * __uint_as_float(g[i] & 0xffff0000u));
+            o[b] = piece * 8 < K ? o[b] : u32x4{0, 0, 0, 0};
         }
-        xl[c] = o;
+#pragma unroll
+        for (int b = 0; b < NV; ++b)
+            if (b < nb) xl[b * slabs * 64 + slot] = o[b];
     }
     __syncthreads();
 }
-constexpr int Q4_NORM_K = 16384;   // longest: 32 KB of LDS
 
 // which strips a workgroup has: NS consecutive ones of one matrix (SiLU: half are gate rows, half the same up rows); behind the last one, that again
 template <int NS> struct Q4Strips { const u32x4* codes[NS]; const uint32_t* scales[NS]; int blk, which; };
@@ -219,14 +257,14 @@ __global__ void __launch_bounds__(NW * 64) q4_matvec_f32_kernel(Q4Mats<NM> a) {
 // ring of DEPTH tiles (128 k) of each wavefront; a wavefront reads only what it has loaded itself, after its own vmcnt wait, so there is no barrier in the loop.
 // Piece c (16 bytes) of vector r lies at slot c ^ r of its row, which spreads the 16 rows of an operand over the banks.  4096 x 14336, 2 / 4 / 8 / 16 vectors 9.7 / 10.9 /
 // 12.8 / 17.5 -> 7.1 / 7.9 / 9.3 / 11.9 us; of sixteen a CU still takes in no more than 30 bytes a clock, with three tiles in flight or with workgroups
-// that begin at different tiles as well (14.8 / 14.9 / 14.8 us for 3584 x 18944).  4 XI: vectors there is room for; 0: a single one that is normalised on its way in.
-template <int NS, int XI> constexpr int q4_stage_bytes() { return NS * (1024 + 256) + XI * 1024; }
+// that begin at different tiles as well (14.8 / 14.9 / 14.8 us for 3584 x 18944).  4 XI: vectors there is room for; 0: up to four that are normalised on their way in.
+template <int NS, int XI> constexpr int q4_stage_bytes() { return NS * 1024 + 256 + XI * 1024; }
 template <int MODE, int NM, int NS, int NW, int XI, int DEPTH>
 __global__ void __launch_bounds__(NW * 64) q4_matvec_kernel(Q4Mats<NM> a) {
     constexpr bool NORM = XI == 0;
     constexpr uint32_t STAGE = q4_stage_bytes<NS, XI>();
-    constexpr int NI = 2 * NS + XI;                // loads of a stage
-    static_assert((DEPTH - 1) * NI <= 63, "vmcnt field");
+    constexpr int NI = NS + 1 + XI;                // loads of a stage: codes of each strip, scales of all, vectors
+    static_assert(NS <= 4 && DEPTH * NI <= 63, "vmcnt field");
     static_assert((size_t)DEPTH * STAGE >= sizeof(float) * NS * 16 * 20, "the partial tiles reuse the ring");
     extern __shared__ __attribute__((aligned(16))) char ring[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, kg = lane >> 4;
@@ -237,27 +275,42 @@ __global__ void __launch_bounds__(NW * 64) q4_matvec_kernel(Q4Mats<NM> a) {
 #pragma unroll
     for (int j = 0; j < XI; ++j) row[j] = 4 * j + kg < a.nb ? 4 * j + kg : a.nb - 1;   // (behind the last vector any: its column is not stored)
     const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)ring + (uint32_t)wave * (DEPTH * STAGE);
+    const uint32_t* sp = st.scales[0];             // lane (kg, l16): scales of strip kg % NS, row l16
+#pragma unroll
+    for (int s = 1; s < NS; ++s) sp = kg % NS == s ? st.scales[s] : sp;
+    sp += l16;
     auto issue = [&](int n) {
         const int tile = wave + NW * n, k0 = tile * 128;
         const uint32_t slot = base + (uint32_t)(n % DEPTH) * STAGE;
 #pragma unroll
-        for (int s = 0; s < NS; ++s) {
-            dma16s_nt((uint32_t)lane * 16, (const char*)st.codes[s] + (int64_t)tile * 1024, slot + s * 1024);
-            dma4s_nt((uint32_t)l16 * 4, (const char*)st.scales[s] + (int64_t)tile * 64, slot + NS * 1024 + s * 256);
-        }
+        for (int s = 0; s < NS; ++s) dma16s_nt((uint32_t)lane * 16, (const char*)st.codes[s] + (int64_t)tile * 1024, slot + s * 1024);
+        dma4_nt(sp + (int64_t)tile * 16, slot + NS * 1024);
 #pragma unroll
         for (int j = 0; j < XI; ++j) {
             int piece = l16 ^ (4 * j + kg);        // the lane's 16 bytes go to row 4 j + kg, slot l16
             piece = k0 + piece * 8 < K ? piece : 0;
-            dma16s(((uint32_t)row[j] * (uint32_t)K + (uint32_t)piece * 8) * 2, (const char*)a.x + (int64_t)k0 * 2, slot + NS * 1280 + j * 1024);
+            dma16s(((uint32_t)row[j] * (uint32_t)K + (uint32_t)piece * 8) * 2, (const char*)a.x + (int64_t)k0 * 2, slot + NS * 1024 + 256 + j * 1024);
         }
     };
     mfma_f32x4 acc[NS];
 #pragma unroll
     for (int s = 0; s < NS; ++s) acc[s] = mfma_f32x4{0.f, 0.f, 0.f, 0.f};
+    int vx = 0;
+    // behind the rings: the vectors to normalise, gamma, the sums
+    u32x4* xl = reinterpret_cast<u32x4*>(ring + NW * DEPTH * STAGE);
+    if constexpr (NORM) norm_load<NW>((const bf16_t*)a.x, (const bf16_t*)a.gamma, K, slabs, a.nb, base + (uint32_t)(NW - wave) * (DEPTH * STAGE));
     for (int n = 0; n < (N < DEPTH ? N : DEPTH); ++n) issue(n);
-    const u32x4* const xl = reinterpret_cast<const u32x4*>(ring + NW * DEPTH * STAGE + 64);   // behind the rings: the norm's sums, the normalised vector
-    if constexpr (NORM) norm_to_lds<NW>((const bf16_t*)a.x, (const bf16_t*)a.gamma, a.eps, K, slabs, const_cast<u32x4*>(xl), (float*)(ring + NW * DEPTH * STAGE));
+    if constexpr (NORM) {
+        if (N >= DEPTH) SPTS_WAIT_VMCNT(DEPTH * NI); else SPTS_WAIT_VMCNT(0);
+        asm volatile("" ::: "memory");
+        float* const red = reinterpret_cast<float*>(xl + (a.nb + 1) * slabs * 64);
+        if (a.nb == 1) norm_in_lds<NW, 1>(xl, red, a.eps, K, slabs, 1);
+        else if (a.nb == 2) norm_in_lds<NW, 2>(xl, red, a.eps, K, slabs, 2);
+        else norm_in_lds<NW, Q4_NORM_NB>(xl, red, a.eps, K, slabs, a.nb);
+        const int v = (l16 & 3) < a.nb ? l16 & 3 : a.nb - 1;
+        xl += v * slabs * 64 + kg;
+        vx = v;
+    }
     for (int n = 0; n < N; ++n) {
         if (n + DEPTH <= N) SPTS_WAIT_VMCNT((DEPTH - 1) * NI); else SPTS_WAIT_VMCNT(0);
         asm volatile("" ::: "memory");
@@ -267,13 +320,13 @@ __global__ void __launch_bounds__(NW * 64) q4_matvec_kernel(Q4Mats<NM> a) {
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
             c[s] = *reinterpret_cast<const u32x4*>(slot + s * 1024 + lane * 16);
-            sc[s] = *reinterpret_cast<const uint32_t*>(slot + NS * 1024 + s * 256 + lane * 4);
+            sc[s] = *reinterpret_cast<const uint32_t*>(slot + NS * 1024 + s * 64 + l16 * 4);
         }
         const int xr = l16 & (4 * XI - 1);         // (with room for 4 or 8 vectors the columns behind repeat them, with one alone all do)
         const int k0 = (wave + NW * n) * 128;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            xv[i] = NORM ? xl[k0 / 8 + 4 * i + kg] : *reinterpret_cast<const u32x4*>(slot + NS * 1280 + xr * 256 + (((4 * i + kg) ^ xr) * 16));
+            xv[i] = NORM ? xl[k0 / 8 + 4 * (i ^ vx)] : *reinterpret_cast<const u32x4*>(slot + NS * 1024 + 256 + xr * 256 + (((4 * i + kg) ^ xr) * 16));
         // the slot is filled again only after its operands have arrived in registers
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         if (n + DEPTH < N) issue(n + DEPTH);
@@ -296,8 +349,9 @@ __global__ void __launch_bounds__(NW * 64) q4_matvec_kernel(Q4Mats<NM> a) {
 // 12288 x 4096, one vector 2 / 3 tiles 7.3 / 7.8, 128256 x 4096, sixteen 53.0 / 66.4.)
 template <int MODE, int NM, int NS, int NW, int XI>
 static hipError_t launch_q4_bf16(const Q4Mats<NM>& m, unsigned blocks, hipStream_t s) {
-    constexpr int DEPTH = NS == 1 && XI < 4 ? 4 : 2, RING = NW * DEPTH * q4_stage_bytes<NS, XI>(), MOST = RING + (XI ? 0 : 64 + Q4_NORM_K * 2);
-    const int lds = XI ? RING : RING + 64 + (m.K + Q4_SLAB - 1) / Q4_SLAB * Q4_SLAB * 2;
+    constexpr int DEPTH = NS == 1 && XI < 4 ? 4 : 2, RING = NW * DEPTH * q4_stage_bytes<NS, XI>(), SUMS = Q4_NORM_NB * NW * (int)sizeof(float),
+                  MOST = RING + (XI ? 0 : Q4_NORM_SLABS * 1024 + SUMS);
+    const int lds = XI ? RING : RING + (m.nb + 1) * (int)q4_slabs(m.K) * 1024 + SUMS;
     const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(&q4_matvec_kernel<MODE, NM, NS, NW, XI, DEPTH>), MOST);
     if (e != hipSuccess) return e;
     q4_matvec_kernel<MODE, NM, NS, NW, XI, DEPTH><<<dim3(blocks), dim3(NW * 64), lds, s>>>(m);
@@ -358,7 +412,7 @@ static hipError_t launch_q4_matvec_t(const Q4Args& a, hipStream_t s) {
 }
 
 // a: Q4_STORE and Q4_RESID take one matrix, Q4_SILU two, Q4_F32 up to three
-bool q4_norm_inside(int64_t K, int nb, bool bf16) { return bf16 && nb == 1 && K <= Q4_NORM_K; }
+bool q4_norm_inside(int64_t K, int nb, bool bf16) { return bf16 && nb <= Q4_NORM_NB && (nb + 1) * q4_slabs(K) <= Q4_NORM_SLABS; }
 
 hipError_t launch_q4_matvec(const Q4Args& a, bool bf16, hipStream_t s) {
     if (a.nb < 1 || a.nb > DECODE_MAX_BATCH) return hipErrorInvalidValue;
