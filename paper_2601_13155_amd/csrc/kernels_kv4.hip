@@ -1,6 +1,7 @@
 // Caches in 4 bits: appending pairs, reading them back, and the attention of one query per sequence over them.
 #include "spts_fp4.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace spts {
@@ -488,41 +489,47 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) kv4_attn_kernel(cons
     }
 }
 
-// The splits of one query head meet: blockIdx.x = head, blockIdx.y = sequence; 512 / D groups of threads walk the splits.
+// The splits of one query head meet: blockIdx.x = head, blockIdx.y = sequence, blockIdx.z = W of its dimensions; 512 / W groups of threads walk the splits.
 constexpr int KV4_MAX_SPLITS = 256;
 template <int NB> struct Kv4Ends { int32_t end[NB]; };
-template <typename T, int D, int NB>
+template <typename T, int D, int W, int NB>
 __global__ void __launch_bounds__(512) kv4_merge_kernel(const float* __restrict__ part, Kv4Ends<NB> sp, int H, int Hkv, T* __restrict__ out) {
-    constexpr int GROUPS = 512 / D;
+    constexpr int GROUPS = 512 / W, AHEAD = 4;
     __shared__ float sa[KV4_MAX_SPLITS], red[2][8], so[512];
-    const int h = blockIdx.x, b = blockIdx.y, grp = H / Hkv, g = h / grp, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int h = blockIdx.x, b = blockIdx.y, grp = H / Hkv, g = h / grp, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, e = blockIdx.z * W + tid % W;
     const int first = NB > 1 && b > 0 ? sp.end[NB > 1 ? b - 1 : 0] : 0, ns = sp.end[NB > 1 ? b : 0] - first;
     if (ns == 1) return;
     const float* base = part + (((int64_t)first * Hkv + g) * grp + h % grp) * (D + 2);
     const int64_t stride = (int64_t)H * (D + 2);
     const float m = tid < ns ? base[tid * stride] : -INFINITY, l = tid < ns ? base[tid * stride + 1] : 0.f;
+    float early[AHEAD];   // the first values, asked for before their weights are known
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) early[i] = tid / W + i * GROUPS < ns ? base[(tid / W + i * GROUPS) * stride + 2 + e] : 0.f;
     float mx = m;
     for (int off = 32; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor(mx, off));
     if (lane == 0) red[0][wave] = mx;
     __syncthreads();
     mx = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
     const float mu = mx == -INFINITY ? 0.f : mx, a = __builtin_amdgcn_exp2f(m - mu);
-    if (tid < ns) sa[tid] = a;
+    if (tid < KV4_MAX_SPLITS) sa[tid] = a;
     float ls = l * a;
     for (int off = 32; off > 0; off >>= 1) ls += __shfl_xor(ls, off);
     if (lane == 0) red[1][wave] = ls;
     __syncthreads();
     const float L = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
     float o = 0.f;
-#pragma unroll 8
-    for (int s = tid / D; s < ns; s += GROUPS) o += base[s * stride + 2 + tid % D] * sa[s];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+        if (tid / W + i * GROUPS < ns) o += early[i] * sa[tid / W + i * GROUPS];
+#pragma unroll 4
+    for (int s = tid / W + AHEAD * GROUPS; s < ns; s += GROUPS) o += base[s * stride + 2 + e] * sa[s];
     so[tid] = o;
     __syncthreads();
-    if (tid >= D) return;
+    if (tid >= W) return;
     float t = 0.f;
 #pragma unroll
-    for (int k = 0; k < GROUPS; ++k) t += so[k * D + tid];
-    out[((int64_t)b * H + h) * D + tid] = from_f32<T>(L == 0.f ? 0.f : t / L);
+    for (int k = 0; k < GROUPS; ++k) t += so[k * W + tid];
+    out[((int64_t)b * H + h) * D + e] = from_f32<T>(L == 0.f ? 0.f : t / L);
 }
 
 template <typename T, int D, int NW, int NB>
@@ -540,7 +547,14 @@ static hipError_t launch_kv4_attn_n(const T* q, const Kv4Batch& kb, int64_t per,
     const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(&kv4_attn_kernel<T, D, NW, NB>), (NW * KV4_MAX_GROUP * (D + 4) + NW * 32) * (int)sizeof(float));
     if (e != hipSuccess) return e;
     kv4_attn_kernel<T, D, NW, NB><<<dim3((unsigned)splits, (unsigned)Hkv), dim3(NW * 64), lds, s>>>(q, c, H, Hkv, 1.4426950408889634f / sqrtf((float)D), part, out);
-    if (splits > kb.n) kv4_merge_kernel<T, D, NB><<<dim3((unsigned)H, (unsigned)kb.n), dim3(512), 0, s>>>(part, ends, H, Hkv, out);
+    if (splits > kb.n) {
+        // Many shares are spread over four workgroups a head, of few one has all (us for 5000 / 13107 / 131072 keys of 32 heads, 40 or 64 shares, 32 or 128 dimensions a
+        // workgroup 8.2 / 9.2 / 27.4 and 9.2 / 10.9 / 28.3; 16 sequences of up to 3000 / 13107 keys, 12 shares 13.4 / 20.4 and 11.0 / 18.0)
+        int most = 1;
+        for (int b = 0; b < kb.n; ++b) most = std::max(most, ends.end[b] - (b > 0 ? ends.end[b - 1] : 0));
+        if (most > 16) kv4_merge_kernel<T, D, 32, NB><<<dim3((unsigned)H, (unsigned)kb.n, D / 32), dim3(512), 0, s>>>(part, ends, H, Hkv, out);
+        else kv4_merge_kernel<T, D, D, NB><<<dim3((unsigned)H, (unsigned)kb.n), dim3(512), 0, s>>>(part, ends, H, Hkv, out);
+    }
     return hipGetLastError();
 }
 
