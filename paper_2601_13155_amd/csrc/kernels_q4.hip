@@ -151,13 +151,16 @@ __device__ inline Q4Strips<NS> q4_strips(const Q4Mats<NM>& a, int slabs) {
     return r;
 }
 
-// The wavefronts' partial tiles meet in LDS and leave.  Lane (vector l16, row group kg) holds rows 4 kg .. 4 kg + 3 of its strips.
-template <typename T, int MODE, int NM, int NS, int NW>
-__device__ inline void q4_finish(const Q4Mats<NM>& a, const Q4Strips<NS>& st, const mfma_f32x4 (&acc)[NS], float (*sred)[NS][16][20]) {
+// The wavefronts' partial tiles meet in LDS and leave.  Lane (vector l16, row group kg) holds rows 4 kg .. 4 kg + 3 of its strips.  Sums of three parts of the
+// vectors are columns (4 part + vector, four vectors a tile) or tiles of their own, added in one order either way.
+template <typename T, int MODE, int NM, int NS, int NW, int TILES, int PARTS, bool APART>
+__device__ inline void q4_finish(const Q4Mats<NM>& a, const Q4Strips<NS>& st, const mfma_f32x4 (&acc)[TILES][NS], float (*sred)[TILES][NS][16][20]) {
     constexpr int OWN = MODE == Q4_SILU ? NS / 2 : NS;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
 #pragma unroll
-    for (int s = 0; s < NS; ++s) *reinterpret_cast<mfma_f32x4*>(&sred[wave][s][lane & 15][4 * (lane >> 4)]) = acc[s];
+    for (int p = 0; p < TILES; ++p)
+#pragma unroll
+        for (int s = 0; s < NS; ++s) *reinterpret_cast<mfma_f32x4*>(&sred[wave][p][s][lane & 15][4 * (lane >> 4)]) = acc[p][s];
     __syncthreads();
     for (int t = tid; t < OWN * 256; t += NW * 64) {
         const int r = t & 15, s = (t >> 4) % OWN, b = t / (16 * OWN);
@@ -165,10 +168,13 @@ __device__ inline void q4_finish(const Q4Mats<NM>& a, const Q4Strips<NS>& st, co
         if (b >= a.nb || row >= a.rows[st.which]) continue;
         float v = 0.f, u = 0.f;
 #pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            v += sred[w][s][b][r];
-            if (MODE == Q4_SILU) u += sred[w][NS - OWN + s][b][r];
-        }
+        for (int w = 0; w < NW; ++w)
+#pragma unroll
+            for (int p = PARTS - 1; p >= 0; --p) {
+                const int tile = APART ? b / 4 : p, col = APART ? 4 * p + b % 4 : b;
+                v += sred[w][tile][s][col][r];
+                if (MODE == Q4_SILU) u += sred[w][tile][NS - OWN + s][col][r];
+            }
         const int64_t at = (int64_t)b * a.rows[st.which] + row;
         if (MODE == Q4_F32) ((float*)a.y[st.which])[at] = v;
         else {
@@ -181,99 +187,36 @@ __device__ inline void q4_finish(const Q4Mats<NM>& a, const Q4Strips<NS>& st, co
 // y = x W^T on the matrix cores for up to 16 vectors: a row of W is an operand row (lane l16), a vector a column; a dword of codes is an operand's eight values of a
 // lane, and the decoder's bf16 pairs are the operand.  The NW wavefronts of a workgroup share the tiles of NS strips in turn and meet in LDS, so the order of a
 // row's sum depends on K and NW alone, not on the vectors.  (A slab at a time instead of a tile: 28672 x 4096 12.8 instead of 12.1 us, 3584 x 18944 8.9 instead of 8.1.)
-// fp32 vectors are taken as three bf16 parts, which is all of their 24 bits, and are read from the caches a tile at a time; codes and scales of the next four tiles
-// are on their way while four are worked on.
-template <int MODE, int NM, int NS, int NW>
-__global__ void __launch_bounds__(NW * 64) q4_matvec_f32_kernel(Q4Mats<NM> a) {
-    __shared__ __attribute__((aligned(16))) float sred[NW][NS][16][20];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, kg = lane >> 4;
-    const int K = a.K, slabs = (K + Q4_SLAB - 1) / Q4_SLAB, ntiles = (K + 127) / 128;
-    const Q4Strips<NS> st = q4_strips<MODE, NM, NS>(a, slabs);
-    const bool vec = l16 < a.nb;
-    const float* const x = (const float*)a.x + (int64_t)(vec ? l16 : 0) * K + kg * 8;
-    mfma_f32x4 acc[NS];
-#pragma unroll
-    for (int s = 0; s < NS; ++s) acc[s] = mfma_f32x4{0.f, 0.f, 0.f, 0.f};
-    u32x4 cn[NS][4];
-    uint32_t sn[NS];
-    // tiles first, first + NW, ...; behind the last one, that again
-    auto load = [&](int first) {
-        const int own = first + NW * kg;
-#pragma unroll
-        for (int s = 0; s < NS; ++s) {
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const int tile = first + NW * t;
-                cn[s][t] = __builtin_nontemporal_load(st.codes[s] + (tile < ntiles ? tile : ntiles - 1) * 64 + lane);
-            }
-            sn[s] = __builtin_nontemporal_load(st.scales[s] + (own < ntiles ? own : ntiles - 1) * 16 + l16);
-        }
-    };
-    if (wave < ntiles) load(wave);
-    for (int first = wave; first < ntiles; first += 4 * NW) {
-        u32x4 c[NS][4];
-        uint32_t sc[NS];
-#pragma unroll
-        for (int s = 0; s < NS; ++s) {
-#pragma unroll
-            for (int t = 0; t < 4; ++t) c[s][t] = cn[s][t];
-            sc[s] = sn[s];
-        }
-        if (first + 4 * NW < ntiles) load(first + 4 * NW);
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int k0 = (first + NW * t) * 128;
-            if (k0 >= K) break;
-            uint32_t w4[NS];   // the tile's four scales of the lane's row, which lane 16 t + l16 has loaded
-#pragma unroll
-            for (int s = 0; s < NS; ++s) w4[s] = (uint32_t)__builtin_amdgcn_ds_bpermute((16 * t + l16) * 4, (int)sc[s]);
-            f32x4 xw[4][2];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int k = k0 + i * 32;
-                const bool in = vec && k + kg * 8 < K;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) xw[i][h] = in ? reinterpret_cast<const f32x4*>(x + k)[h] : f32x4{0.f, 0.f, 0.f, 0.f};
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float v[8] = {xw[i][0][0], xw[i][0][1], xw[i][0][2], xw[i][0][3], xw[i][1][0], xw[i][1][1], xw[i][1][2], xw[i][1][3]};
-                u32x4 xf[3];
-                bf16_parts<3, true>(v, xf);
-#pragma unroll
-                for (int s = 0; s < NS; ++s) {
-                    const u32x4 w = fp4_decode8_bf16(c[s][t][i], i == 0 ? fp4_scale_of<0>(w4[s]) : i == 1 ? fp4_scale_of<1>(w4[s]) : i == 2 ? fp4_scale_of<2>(w4[s]) : fp4_scale_of<3>(w4[s]));
-#pragma unroll
-                    for (int p = 2; p >= 0; --p) acc[s] = mfma16(w, xf[p], acc[s]);
-                }
-            }
-        }
-    }
-    q4_finish<float, MODE, NM, NS, NW>(a, st, acc, sred);
-}
-
-// bf16 vectors.  Read by lanes, an operand of 16 vectors is 16 half cache lines, of which a CU takes in 22 bytes a clock: a product of 4096 x 14336 took 0.55 us more with
+// fp32 vectors are taken as three bf16 parts, which is all of their 24 bits.  Up to eight vectors are taken apart by all lanes together, eight values of four vectors
+// a lane, and the parts are columns of their own (4 part + vector), so that a matrix instruction does for all three; more are taken apart as operands are read.  (One kernel
+// that split operands of any number and read them from the caches: 28672 x 4096, 1 / 4 / 8 / 16 vectors 24.6 / 25.0 / 26.3 / 28.8 us; this way
+// 13.8 / 13.9 / 18.2 / 26.2.  Taking them apart is what bounds them: 7.5 instructions a value.)
+// Read by lanes, an operand of 16 vectors is 16 half cache lines, of which a CU takes in 22 bytes a clock: a product of 4096 x 14336 took 0.55 us more with
 // every vector, on however many CUs.  So codes, scales and vectors go to LDS with loads that are laid out for memory, whole lines of 4 vectors an instruction, into a
 // ring of DEPTH tiles (128 k) of each wavefront; a wavefront reads only what it has loaded itself, after its own vmcnt wait, so there is no barrier in the loop.
 // Piece c (16 bytes) of vector r lies at slot c ^ r of its row, which spreads the 16 rows of an operand over the banks.  4096 x 14336, 2 / 4 / 8 / 16 vectors 9.7 / 10.9 /
 // 12.8 / 17.5 -> 7.1 / 7.9 / 9.3 / 11.9 us; of sixteen a CU still takes in no more than 30 bytes a clock, with three tiles in flight or with workgroups
 // that begin at different tiles as well (14.8 / 14.9 / 14.8 us for 3584 x 18944).  4 XI: vectors there is room for; 0: up to four that are normalised on their way in.
-template <int NS, int XI> constexpr int q4_stage_bytes() { return NS * 1024 + 256 + XI * 1024; }
-template <int MODE, int NM, int NS, int NW, int XI, int DEPTH>
+constexpr int Q4_APART = 12 * 256;
+template <typename T, int NS, int XI> constexpr int q4_stage_bytes() { return NS * 1024 + 256 + XI * 512 * (int)sizeof(T); }
+template <typename T, int MODE, int NM, int NS, int NW, int XI, int DEPTH>
 __global__ void __launch_bounds__(NW * 64) q4_matvec_kernel(Q4Mats<NM> a) {
-    constexpr bool NORM = XI == 0;
-    constexpr uint32_t STAGE = q4_stage_bytes<NS, XI>();
-    constexpr int NI = NS + 1 + XI;                // loads of a stage: codes of each strip, scales of all, vectors
+    constexpr bool NORM = XI == 0, F32 = sizeof(T) == 4, APART = F32 && XI <= 2;
+    constexpr uint32_t STAGE = q4_stage_bytes<T, NS, XI>();
+    constexpr int RV = F32 ? 2 : 4, XN = 4 * XI / RV;   // vectors of a load, loads of all
+    constexpr int NI = NS + 1 + XN;                // loads of a stage: codes of each strip, scales of all, vectors
     static_assert(NS <= 4 && DEPTH * NI <= 63, "vmcnt field");
-    static_assert((size_t)DEPTH * STAGE >= sizeof(float) * NS * 16 * 20, "the partial tiles reuse the ring");
+    constexpr int TILES = APART ? XI : F32 ? 3 : 1;
+    static_assert((size_t)DEPTH * STAGE >= sizeof(float) * TILES * NS * 16 * 20, "the partial tiles reuse the ring");
     extern __shared__ __attribute__((aligned(16))) char ring[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, kg = lane >> 4;
     const int K = a.K, slabs = (K + Q4_SLAB - 1) / Q4_SLAB, ntiles = (K + 127) / 128;
     const Q4Strips<NS> st = q4_strips<MODE, NM, NS>(a, slabs);
     const int N = wave < ntiles ? (ntiles - wave + NW - 1) / NW : 0;   // tiles wave, wave + NW, ...
-    int row[XI + NORM];
+    const int lrow = lane * RV / 64;               // vector of a load that the lane has a part of
+    int row[XN + NORM];
 #pragma unroll
-    for (int j = 0; j < XI; ++j) row[j] = 4 * j + kg < a.nb ? 4 * j + kg : a.nb - 1;   // (behind the last vector any: its column is not stored)
+    for (int j = 0; j < XN; ++j) row[j] = RV * j + lrow < a.nb ? RV * j + lrow : a.nb - 1;   // (behind the last vector any: its column is not stored)
     const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)ring + (uint32_t)wave * (DEPTH * STAGE);
     const uint32_t* sp = st.scales[0];             // lane (kg, l16): scales of strip kg % NS, row l16
 #pragma unroll
@@ -286,18 +229,24 @@ __global__ void __launch_bounds__(NW * 64) q4_matvec_kernel(Q4Mats<NM> a) {
         for (int s = 0; s < NS; ++s) dma16s_nt((uint32_t)lane * 16, (const char*)st.codes[s] + (int64_t)tile * 1024, slot + s * 1024);
         dma4_nt(sp + (int64_t)tile * 16, slot + NS * 1024);
 #pragma unroll
-        for (int j = 0; j < XI; ++j) {
-            int piece = l16 ^ (4 * j + kg);        // the lane's 16 bytes go to row 4 j + kg, slot l16
+        for (int j = 0; j < XN; ++j) {
+            // the lane's 16 bytes go to row RV j + lrow, bf16: slot l16, fp32: half lane % 2 of slot l16
+            const int at = F32 ? lane % 32 / 2 : l16;
+            int piece = at ^ (RV * j + lrow);
             piece = k0 + piece * 8 < K ? piece : 0;
-            dma16s(((uint32_t)row[j] * (uint32_t)K + (uint32_t)piece * 8) * 2, (const char*)a.x + (int64_t)k0 * 2, slot + NS * 1024 + 256 + j * 1024);
+            dma16s(((uint32_t)row[j] * (uint32_t)K + (uint32_t)piece * 8) * (uint32_t)sizeof(T) + (F32 ? lane % 2 * 16 : 0), (const char*)a.x + (int64_t)k0 * (int)sizeof(T),
+                   slot + NS * 1024 + 256 + j * 1024);
         }
     };
-    mfma_f32x4 acc[NS];
+    mfma_f32x4 acc[TILES][NS];
 #pragma unroll
-    for (int s = 0; s < NS; ++s) acc[s] = mfma_f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int p = 0; p < TILES; ++p)
+#pragma unroll
+        for (int s = 0; s < NS; ++s) acc[p][s] = mfma_f32x4{0.f, 0.f, 0.f, 0.f};
     int vx = 0;
     // behind the rings: the vectors to normalise, gamma, the sums
     u32x4* xl = reinterpret_cast<u32x4*>(ring + NW * DEPTH * STAGE);
+    char* const apart = ring + NW * DEPTH * STAGE + wave * Q4_APART;   // or a tile's parts, of each wavefront
     if constexpr (NORM) norm_load<NW>((const bf16_t*)a.x, (const bf16_t*)a.gamma, K, slabs, a.nb, base + (uint32_t)(NW - wave) * (DEPTH * STAGE));
     for (int n = 0; n < (N < DEPTH ? N : DEPTH); ++n) issue(n);
     if constexpr (NORM) {
@@ -315,7 +264,7 @@ __global__ void __launch_bounds__(NW * 64) q4_matvec_kernel(Q4Mats<NM> a) {
         if (n + DEPTH <= N) SPTS_WAIT_VMCNT((DEPTH - 1) * NI); else SPTS_WAIT_VMCNT(0);
         asm volatile("" ::: "memory");
         const char* const slot = ring + (size_t)wave * (DEPTH * STAGE) + (size_t)(n % DEPTH) * STAGE;
-        u32x4 c[NS], xv[4];
+        u32x4 c[NS], xv[APART ? XI : 1][4], raw[F32 ? (APART ? 2 * XI : 8) : 1];
         uint32_t sc[NS];
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
@@ -325,36 +274,78 @@ __global__ void __launch_bounds__(NW * 64) q4_matvec_kernel(Q4Mats<NM> a) {
         const int xr = l16 & (4 * XI - 1);         // (with room for 4 or 8 vectors the columns behind repeat them, with one alone all do)
         const int k0 = (wave + NW * n) * 128;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            xv[i] = NORM ? xl[k0 / 8 + 4 * (i ^ vx)] : *reinterpret_cast<const u32x4*>(slot + NS * 1024 + 256 + xr * 256 + (((4 * i + kg) ^ xr) * 16));
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (NORM) xv[0][i] = xl[k0 / 8 + 4 * (i ^ vx)];
+            else if constexpr (!F32) xv[0][i] = *reinterpret_cast<const u32x4*>(slot + NS * 1024 + 256 + xr * 256 + (((4 * i + kg) ^ xr) * 16));
+            else if constexpr (!APART) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) raw[2 * i + h] = *reinterpret_cast<const u32x4*>(slot + NS * 1024 + 256 + xr * 512 + (((4 * i + kg) ^ xr) * 32) + h * 16);
+            }
+        }
+        if constexpr (APART) {                     // piece l16 of vectors 4 j + kg
+#pragma unroll
+            for (int j = 0; j < 2 * XI; ++j) {
+                const int r = j / 2 * 4 + kg;
+                raw[j] = *reinterpret_cast<const u32x4*>(slot + NS * 1024 + 256 + r * 512 + ((l16 ^ r) * 32) + j % 2 * 16);
+            }
+        }
         // the slot is filled again only after its operands have arrived in registers
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         if (n + DEPTH < N) issue(n + DEPTH);
         if (!NORM && k0 + 128 > K) {
+            const u32x4 none{0, 0, 0, 0};
+            if constexpr (APART) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) xv[i] = k0 + i * 32 + kg * 8 < K ? xv[i] : u32x4{0, 0, 0, 0};
+                for (int j = 0; j < 2 * XI; ++j) raw[j] = k0 + l16 * 8 < K ? raw[j] : none;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const bool in = k0 + i * 32 + kg * 8 < K;
+                    if constexpr (!F32) xv[0][i] = in ? xv[0][i] : none;
+                    else { raw[2 * i] = in ? raw[2 * i] : none; raw[2 * i + 1] = in ? raw[2 * i + 1] : none; }
+                }
+            }
+        }
+        if constexpr (APART) {
+            const int col = l16 < 12 ? l16 : l16 - 4;
+#pragma unroll
+            for (int j = 0; j < XI; ++j) {
+                u32x4 xf[3];
+                bf16_parts3(raw[2 * j], raw[2 * j + 1], xf);
+#pragma unroll
+                for (int p = 0; p < 3; ++p) *reinterpret_cast<u32x4*>(apart + (4 * p + kg) * 256 + ((l16 ^ (4 * p + kg)) * 16)) = xf[p];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) xv[j][i] = *reinterpret_cast<const u32x4*>(apart + col * 256 + (((4 * i + kg) ^ col) * 16));
+            }
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 4; ++i) {
+            u32x4 xf[3];
+            if constexpr (F32 && !APART) bf16_parts3(raw[2 * i], raw[2 * i + 1], xf);
 #pragma unroll
-            for (int s = 0; s < NS; ++s)
-                acc[s] = mfma16(fp4_decode8_bf16(c[s][i], i == 0 ? fp4_scale_of<0>(sc[s]) : i == 1 ? fp4_scale_of<1>(sc[s]) : i == 2 ? fp4_scale_of<2>(sc[s]) : fp4_scale_of<3>(sc[s])),
-                                xv[i], acc[s]);
+            for (int s = 0; s < NS; ++s) {
+                const u32x4 w = fp4_decode8_bf16(c[s][i], i == 0 ? fp4_scale_of<0>(sc[s]) : i == 1 ? fp4_scale_of<1>(sc[s]) : i == 2 ? fp4_scale_of<2>(sc[s]) : fp4_scale_of<3>(sc[s]));
+#pragma unroll
+                for (int p = 0; p < TILES; ++p) acc[p][s] = mfma16(w, F32 && !APART ? xf[p] : xv[APART ? p : 0][i], acc[p][s]);
+            }
+        }
     }
     __syncthreads();   // every ring has drained: its last tile waited for vmcnt 0
-    q4_finish<bf16_t, MODE, NM, NS, NW>(a, st, acc, reinterpret_cast<float (*)[NS][16][20]>(ring));
+    q4_finish<T, MODE, NM, NS, NW, TILES, F32 ? 3 : 1, APART>(a, st, acc, reinterpret_cast<float (*)[TILES][NS][16][20]>(ring));
 }
 
 // (Depth of the ring: four tiles where they are small, 4096 x 14336, one vector, 2 / 3 / 4 tiles 8.5 / 7.6 / 7.1 us; otherwise two, which leaves room for more workgroups:
-// 12288 x 4096, one vector 2 / 3 tiles 7.3 / 7.8, 128256 x 4096, sixteen 53.0 / 66.4.)
-template <int MODE, int NM, int NS, int NW, int XI>
-static hipError_t launch_q4_bf16(const Q4Mats<NM>& m, unsigned blocks, hipStream_t s) {
-    constexpr int DEPTH = NS == 1 && XI < 4 ? 4 : 2, RING = NW * DEPTH * q4_stage_bytes<NS, XI>(), SUMS = Q4_NORM_NB * NW * (int)sizeof(float),
-                  MOST = RING + (XI ? 0 : Q4_NORM_SLABS * 1024 + SUMS);
+// 12288 x 4096, one vector 2 / 3 tiles 7.3 / 7.8, 128256 x 4096, sixteen 53.0 / 66.4; one strip of eight fp32 vectors, 4096 x 14336, 18.8 / 19.3.)
+template <typename T, int MODE, int NM, int NS, int NW, int XI>
+static hipError_t launch_q4_matvec_x(const Q4Mats<NM>& m, unsigned blocks, hipStream_t s) {
+    constexpr bool F32 = sizeof(T) == 4;
+    constexpr int DEPTH = NS == 1 && XI < (F32 ? 2 : 4) ? 4 : 2, SUMS = Q4_NORM_NB * NW * (int)sizeof(float);
+    constexpr int RING = NW * DEPTH * q4_stage_bytes<T, NS, XI>() + (F32 && XI <= 2 ? NW * Q4_APART : 0), MOST = RING + (XI ? 0 : Q4_NORM_SLABS * 1024 + SUMS);
+    static_assert(MOST <= 160 * 1024, "LDS of a CU");
     const int lds = XI ? RING : RING + (m.nb + 1) * (int)q4_slabs(m.K) * 1024 + SUMS;
-    const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(&q4_matvec_kernel<MODE, NM, NS, NW, XI, DEPTH>), MOST);
+    const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(&q4_matvec_kernel<T, MODE, NM, NS, NW, XI, DEPTH>), MOST);
     if (e != hipSuccess) return e;
-    q4_matvec_kernel<MODE, NM, NS, NW, XI, DEPTH><<<dim3(blocks), dim3(NW * 64), lds, s>>>(m);
+    q4_matvec_kernel<T, MODE, NM, NS, NW, XI, DEPTH><<<dim3(blocks), dim3(NW * 64), lds, s>>>(m);
     return hipGetLastError();
 }
 
@@ -370,18 +361,15 @@ static hipError_t launch_q4_matvec_n(const Q4Args& a, hipStream_t s) {
     m.x = a.x; m.K = (int32_t)a.K; m.nb = a.nb;
     if (blocks == 0) return hipSuccess;
     const unsigned g = (unsigned)blocks;
-    if constexpr (sizeof(T) == 4) {
-        q4_matvec_f32_kernel<MODE, NM, NS, NW><<<dim3(g), dim3(NW * 64), 0, s>>>(m);
-        return hipGetLastError();
-    } else {
-        if constexpr (NM > 1) {
-            if (a.gamma) {
-                m.gamma = a.gamma; m.eps = a.eps;
-                return launch_q4_bf16<MODE, NM, NS, NW, 0>(m, g, s);
-            }
+    if constexpr (NM > 1 && sizeof(T) == 2) {
+        if (a.gamma) {
+            m.gamma = a.gamma; m.eps = a.eps;
+            return launch_q4_matvec_x<T, MODE, NM, NS, NW, 0>(m, g, s);
         }
-        return a.nb <= 4 ? launch_q4_bf16<MODE, NM, NS, NW, 1>(m, g, s) : a.nb <= 8 ? launch_q4_bf16<MODE, NM, NS, NW, 2>(m, g, s) : launch_q4_bf16<MODE, NM, NS, NW, 4>(m, g, s);
     }
+    return a.nb <= 4   ? launch_q4_matvec_x<T, MODE, NM, NS, NW, 1>(m, g, s)
+           : a.nb <= 8 ? launch_q4_matvec_x<T, MODE, NM, NS, NW, 2>(m, g, s)
+                       : launch_q4_matvec_x<T, MODE, NM, NS, NW, 4>(m, g, s);
 }
 
 template <typename T, int NS, int NW>
@@ -390,7 +378,7 @@ static hipError_t launch_q4_matvec_m(const Q4Args& a, hipStream_t s) {
         case Q4_STORE: return launch_q4_matvec_n<T, Q4_STORE, 1, NS, NW>(a, s);
         case Q4_F32: return a.rows[1] || a.rows[2] ? launch_q4_matvec_n<T, Q4_F32, 3, NS, NW>(a, s) : launch_q4_matvec_n<T, Q4_F32, 1, NS, NW>(a, s);
         case Q4_RESID: return launch_q4_matvec_n<T, Q4_RESID, 1, NS, NW>(a, s);
-        case Q4_SILU: return launch_q4_matvec_n<T, Q4_SILU, 2, (NS < 2 ? 2 : NS), NW>(a, s);
+        case Q4_SILU: return launch_q4_matvec_n<T, Q4_SILU, 2, (NS < 2 ? 2 : NS), (NS < 2 && sizeof(T) == 4 ? NW / 2 : NW)>(a, s);
         default: return hipErrorInvalidValue;
     }
 }
@@ -400,14 +388,14 @@ static hipError_t launch_q4_matvec_m(const Q4Args& a, hipStream_t s) {
 // 1 / 2 strips with 8 / 4 strips with 4 wavefronts (2 with 4, 4 with 8): 4096 x 14336, one vector 7.2 / 9.0 / 15.8 (12.8, 13.8), sixteen 12.0 / 14.4 / 19.2; 6144 x
 // 4096 5.1 / 4.6 / 6.4 and 8.1 / 5.9 / 7.5; 8192 x 8192 9.6 / 7.6 / 10.7 and 13.9 / 9.8 / 12.5; 12288 x 4096 7.4 / 6.7 / 6.9 (6.5, 6.8) and 12.1 / 10.2 / 7.9 (9.3, 8.2);
 // 28672 x 4096 14.6 / 12.6 / 12.3 (12.4, 13.5) and 26.6 / 19.4 / 14.0 (16.1, 15.4); 128256 x 4096 56.1 / 42.2 / 43.2 (42.4, 49.9) and 117 / 76.2 / 49.5 (59.9, 59.4).
-// fp32, 28672 x 4096: 35.5 / 33.7 / 24.1 (28.6) and 55.9 / 43.4 / 28.2 (38.6).  It goes by the matrices alone, and with it the order of a sum.
+// fp32, 28672 x 4096, 1 strip with 8 / 2 with 4 / 4 with 4 wavefronts: 29.1 / 15.9 / 13.7 and 55.9 / 39.5 / 26.4.  It goes by the matrices alone, and with it the order of a sum.
 template <typename T>
 static hipError_t launch_q4_matvec_t(const Q4Args& a, hipStream_t s) {
     int64_t strips = 0;
     for (int i = 0; i < 3; ++i) strips += (a.rows[i] + 15) / 16;
     if (a.mode == Q4_SILU) strips = 2 * ((a.rows[0] + 15) / 16);
     if (strips <= 256) return launch_q4_matvec_m<T, 1, 8>(a, s);
-    if (strips <= 512) return launch_q4_matvec_m<T, 2, 8>(a, s);
+    if (strips <= 512) return launch_q4_matvec_m<T, 2, (sizeof(T) == 4 ? 4 : 8)>(a, s);   // (eight rings of 16 fp32 vectors do not fit a CU)
     return launch_q4_matvec_m<T, 4, 4>(a, s);
 }
 

@@ -91,4 +91,12 @@ __device__ inline void bf16_parts(const float* v, u32x4 (&out)[N]) {
         }
 }
 
+// the same for eight values in two registers of four: all 24 bits, infinities as they are
+__device__ inline void bf16_parts3(u32x4 lo, u32x4 hi, u32x4 (&out)[3]) {
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) { v[j] = __uint_as_float(lo[j]); v[4 + j] = __uint_as_float(hi[j]); }
+    bf16_parts<3, true>(v, out);
+}
+
 }  // namespace spts
