@@ -31,7 +31,7 @@ constexpr int LT = 1024;
 template <typename T, int LW, int NB, bool ONE>
 __global__ void __launch_bounds__(LT) process_logits_kernel(const float* in, int V, Rules<NB> r, float* out, Best* __restrict__ part, int32_t* __restrict__ token,
                                                             const T* __restrict__ table, int D, T* __restrict__ x_next) {
-    __shared__ uint32_t cnt[ONE ? 1 : LT * LW];
+    __shared__ uint32_t cnt[ONE ? 1 : LT * LW + LT];   // and a place for each thread that takes the ids of other words
     __shared__ Best sb[LT / 64];
     const int b = blockIdx.y, rb = NB > 1 ? b : 0, tid = threadIdx.x, v0 = (int)blockIdx.x * (LT * LW);
     const int n = V - v0 < LT * LW ? V - v0 : LT * LW;
@@ -48,37 +48,49 @@ __global__ void __launch_bounds__(LT) process_logits_kernel(const float* in, int
         __syncthreads();
         const int32_t* const ids = r.history + b * r.history_stride;
         const int len = r.len[rb], prompt = r.prompt[rb];
-        auto count = [&](int32_t id, int at) {
-            const uint32_t w = (uint32_t)id - (uint32_t)v0;
-            if (w < (uint32_t)n) {
-                if (at < prompt) atomicOr(&cnt[w], IN_PROMPT);
-                else atomicAdd(&cnt[w], 1u);
-            }
+        // Every id is an operation on LDS without a branch, ids of other words in the thread's own place; a wavefront's 256 ids of a load are as a rule all of the
+        // prompt or all of the answer.  (A branch on whether the word is the workgroup's, and then on the part of the row: one sequence of 131072 ids 16.5 us, this way 14.7.)
+        auto place = [&](uint32_t id) {
+            const uint32_t w = id - (uint32_t)v0;
+            return &cnt[w < (uint32_t)n ? w : (uint32_t)(LT * LW + tid)];
         };
+        auto said = [&](uint32_t id) { atomicAdd(place(id), 1u); };
+        auto given = [&](uint32_t id) { atomicOr(place(id), IN_PROMPT); };
         // whole 16-byte pieces of the row, and what is before and behind them one by one
         int head = (int)((4 - (reinterpret_cast<uintptr_t>(ids) / 4 & 3)) & 3);
         head = head < len ? head : len;
-        const int quads = (len - head) / 4;
-        if (tid < head) count(ids[tid], tid);
-        if (tid < len - head - 4 * quads) count(ids[head + 4 * quads + tid], head + 4 * quads + tid);
+        const int quads = (len - head) / 4, tail = head + 4 * quads;
+        if (tid < head) { if (tid < prompt) given((uint32_t)ids[tid]); else said((uint32_t)ids[tid]); }
+        if (tid < len - tail) { if (tail + tid < prompt) given((uint32_t)ids[tail + tid]); else said((uint32_t)ids[tail + tid]); }
         const u32x4* const q = reinterpret_cast<const u32x4*>(ids + head);
         for (int i0 = tid; i0 < quads; i0 += 4 * LT) {
             u32x4 w[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u) w[u] = i0 + u * LT < quads ? q[i0 + u * LT] : u32x4{~0u, ~0u, ~0u, ~0u};
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
+            for (int u = 0; u < 4; ++u) {
+                if (i0 + u * LT >= quads) break;
+                const int at = head + 4 * (i0 + u * LT), lo = __builtin_amdgcn_readfirstlane(at);
+                if (lo >= prompt) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) count((int32_t)w[u][e], head + 4 * (i0 + u * LT) + e);
+                    for (int e = 0; e < 4; ++e) said(w[u][e]);
+                } else if (lo + 256 <= prompt) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) given(w[u][e]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) { if (at + e < prompt) given(w[u][e]); else said(w[u][e]); }
+                }
+            }
         }
         __syncthreads();
         const float rep = r.repetition[rb], freq = r.frequency[rb], pres = r.presence[rb];
 #pragma unroll
         for (int j = 0; j < LW; ++j) {
-            const uint32_t c = cnt[tid + j * LT], said = c & ~IN_PROMPT;
+            const uint32_t c = cnt[tid + j * LT], times = c & ~IN_PROMPT;
             if (c) x[j] = x[j] > 0.f ? x[j] / rep : x[j] * rep;
-            if (said) {
-                x[j] = x[j] - freq * (float)said;
+            if (times) {
+                x[j] = x[j] - freq * (float)times;
                 x[j] = x[j] - pres;
             }
         }
@@ -143,7 +155,7 @@ __global__ void __launch_bounds__(1024) pick_token_kernel(const Best* __restrict
 
 // Words of a thread: without a history 32 where that makes one workgroup per sequence and saves the second launch (us for one sequence of 4000 / 32000 words 7.7 -> 6.7,
 // 7.8 -> 7.2; with a history of 500 ids 8.1 -> 11.0, of 32768 9.7 -> 15.9), otherwise 4, so that the words are spread over the chip (16 sequences of
-// 128256 words, histories of up to 32768 ids: 2 / 4 / 8 / 16 words 16.9 / 13.4 / 13.1 / 14.8; one sequence 8.4 / 8.9 / 9.8 / 12.0)
+// 128256 words, histories of up to 32768 ids: 2 / 4 / 8 / 16 words 15.5 / 12.7 / 12.6 / 14.2; one sequence of 32768 ids 7.8 / 8.3 / 9.2 / 11.5)
 constexpr int LW_ONE = 32, LW_MANY = 4;
 
 size_t logits_scratch_bytes(int V, int nrows) { return (size_t)((V + LT * LW_MANY - 1) / (LT * LW_MANY)) * nrows * sizeof(Best); }
