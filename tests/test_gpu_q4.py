@@ -51,7 +51,7 @@ def rounded(a, dtype):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("rows,K,nb", [(1, 8, 1), (16, 32, 2), (17, 40, 3), (15, 512, 16), (64, 520, 5), (33, 688, 7), (100, 1032, 4), (48, 2048, 8),
                                        (16, 4096, 1), (1003, 688, 16), (5, 18944, 9),
-                                       (4090, 520, 3), (4100, 1032, 1), (8200, 520, 2), (8216, 1544, 3)])
+                                       (4090, 520, 3), (4100, 1032, 1), (8200, 520, 2), (8216, 1544, 3), (4100, 264, 6), (8190, 136, 16), (8216, 648, 8), (8200, 392, 13)])
 def test_product_of_whole_numbers_is_exact(torch, dtype, rows, K, nb):
     """Grid values times small whole numbers: every sum is a multiple of 1/2 below 2^23 whatever its order, so each output has one
     right bit pattern, and a missed, doubled or misplaced term shows."""
@@ -461,7 +461,7 @@ LAYERS = [(256, 4, 2, 64, 688), (64, 64, 16, 128, 8704), (4224, 4, 2, 32, 64), (
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("nseq,dims", [(1, 0), (2, 0), (5, 0), (16, 0), (1, 1), (3, 1), (1, 2), (2, 2), (1, 3), (2, 3), (3, 3),
-                                       (1, 4), (4, 4), (1, 5)])
+                                       (1, 4), (4, 4), (1, 5), (7, 1), (16, 1)])
 def test_decode_layer_lockstep(torch, dtype, nseq, dims):
     """Caches of different lengths filled from random pairs, three steps of the layer: the appended pair against the oracle's (to the
     element type's rounding, then one of 4 bits), the state against the oracle's over the pairs as stored."""
