@@ -492,9 +492,9 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) kv4_attn_kernel(cons
 // The splits of one query head meet: blockIdx.x = head, blockIdx.y = sequence, blockIdx.z = W of its dimensions; 512 / W groups of threads walk the splits.
 constexpr int KV4_MAX_SPLITS = 256;
 template <int NB> struct Kv4Ends { int32_t end[NB]; };
-template <typename T, int D, int W, int NB>
+template <typename T, int D, int NB>
 __global__ void __launch_bounds__(512) kv4_merge_kernel(const float* __restrict__ part, Kv4Ends<NB> sp, int H, int Hkv, T* __restrict__ out) {
-    constexpr int GROUPS = 512 / W, AHEAD = 4;
+    constexpr int W = 32, GROUPS = 512 / W, AHEAD = 4;
     __shared__ float sa[KV4_MAX_SPLITS], red[2][8], so[512];
     const int h = blockIdx.x, b = blockIdx.y, grp = H / Hkv, g = h / grp, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, e = blockIdx.z * W + tid % W;
     const int first = NB > 1 && b > 0 ? sp.end[NB > 1 ? b - 1 : 0] : 0, ns = sp.end[NB > 1 ? b : 0] - first;
@@ -532,6 +532,36 @@ __global__ void __launch_bounds__(512) kv4_merge_kernel(const float* __restrict_
     out[((int64_t)b * H + h) * D + e] = from_f32<T>(L == 0.f ? 0.f : t / L);
 }
 
+// Of up to KV4_FEW splits: a thread has a dimension and takes all of them at once, one round trip without a barrier.
+constexpr int KV4_FEW = 16;
+template <typename T, int D, int NB>
+__global__ void __launch_bounds__(D) kv4_merge_few_kernel(const float* __restrict__ part, Kv4Ends<NB> sp, int H, int Hkv, T* __restrict__ out) {
+    const int h = blockIdx.x, b = blockIdx.y, grp = H / Hkv, g = h / grp, e = threadIdx.x;
+    const int first = NB > 1 && b > 0 ? sp.end[NB > 1 ? b - 1 : 0] : 0, ns = sp.end[NB > 1 ? b : 0] - first;
+    if (ns == 1) return;
+    const float* base = part + (((int64_t)first * Hkv + g) * grp + h % grp) * (D + 2);
+    const int64_t stride = (int64_t)H * (D + 2);
+    float m[KV4_FEW], l[KV4_FEW], o[KV4_FEW], mx = -INFINITY;
+#pragma unroll
+    for (int s = 0; s < KV4_FEW; ++s) {
+        const float* const at = base + (s < ns ? s : 0) * stride;
+        m[s] = s < ns ? at[0] : -INFINITY;
+        l[s] = at[1];
+        o[s] = at[2 + e];
+    }
+#pragma unroll
+    for (int s = 0; s < KV4_FEW; ++s) mx = fmaxf(mx, m[s]);
+    const float mu = mx == -INFINITY ? 0.f : mx;
+    float L = 0.f, t = 0.f;
+#pragma unroll
+    for (int s = 0; s < KV4_FEW; ++s) {
+        const float a = __builtin_amdgcn_exp2f(m[s] - mu);
+        L += s < ns ? l[s] * a : 0.f;
+        t += s < ns ? o[s] * a : 0.f;
+    }
+    out[((int64_t)b * H + h) * D + e] = from_f32<T>(L == 0.f ? 0.f : t / L);
+}
+
 template <typename T, int D, int NW, int NB>
 static hipError_t launch_kv4_attn_n(const T* q, const Kv4Batch& kb, int64_t per, int H, int Hkv, float* part, T* out, hipStream_t s) {
     Kv4Caches<NB> c{};
@@ -548,12 +578,12 @@ static hipError_t launch_kv4_attn_n(const T* q, const Kv4Batch& kb, int64_t per,
     if (e != hipSuccess) return e;
     kv4_attn_kernel<T, D, NW, NB><<<dim3((unsigned)splits, (unsigned)Hkv), dim3(NW * 64), lds, s>>>(q, c, H, Hkv, 1.4426950408889634f / sqrtf((float)D), part, out);
     if (splits > kb.n) {
-        // Many shares are spread over four workgroups a head, of few one has all (us for 5000 / 13107 / 131072 keys of 32 heads, 40 or 64 shares, 32 or 128 dimensions a
-        // workgroup 8.2 / 9.2 / 27.4 and 9.2 / 10.9 / 28.3; 16 sequences of up to 3000 / 13107 keys, 12 shares 13.4 / 20.4 and 11.0 / 18.0)
+        // us by four workgroups a head / in one round trip: 16 sequences of up to 3000 / 13107 keys of 28 heads, 12 shares, 13.4 / 20.4 and 10.7 / 17.7; one sequence of 2000 keys, 16
+        // shares, 7.5 and 7.5; many shares by four workgroups a head / by one: 5000 / 13107 / 131072 keys of 32 heads, 40 or 64 shares, 8.2 / 9.2 / 27.4 and 9.2 / 10.9 / 28.3
         int most = 1;
         for (int b = 0; b < kb.n; ++b) most = std::max(most, ends.end[b] - (b > 0 ? ends.end[b - 1] : 0));
-        if (most > 16) kv4_merge_kernel<T, D, 32, NB><<<dim3((unsigned)H, (unsigned)kb.n, D / 32), dim3(512), 0, s>>>(part, ends, H, Hkv, out);
-        else kv4_merge_kernel<T, D, D, NB><<<dim3((unsigned)H, (unsigned)kb.n), dim3(512), 0, s>>>(part, ends, H, Hkv, out);
+        if (most > KV4_FEW) kv4_merge_kernel<T, D, NB><<<dim3((unsigned)H, (unsigned)kb.n, D / 32), dim3(512), 0, s>>>(part, ends, H, Hkv, out);
+        else kv4_merge_few_kernel<T, D, NB><<<dim3((unsigned)H, (unsigned)kb.n), dim3(D), 0, s>>>(part, ends, H, Hkv, out);
     }
     return hipGetLastError();
 }

@@ -5,7 +5,7 @@ from tests.test_kernel_resources import _named, kernels  # noqa: F401  (the fixt
 
 
 @pytest.mark.parametrize("part", ["q4_pack_kernel", "q4_matvec_kernel", "kv4_append_kernel", "kv4_read_kernel", "kv4_rope_append_kernel", "kv4_attn_kernel",
-                                  "kv4_merge_kernel", "process_logits_kernel", "pick_token_kernel"])
+                                  "kv4_merge_kernel", "kv4_merge_few_kernel", "process_logits_kernel", "pick_token_kernel"])
 def test_nothing_in_scratch(kernels, part):  # noqa: F811
     for name, k in _named(kernels, part).items():
         assert k[".private_segment_fixed_size"] == 0 and k[".vgpr_spill_count"] == 0, name
