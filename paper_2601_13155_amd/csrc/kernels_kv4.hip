@@ -601,14 +601,17 @@ static hipError_t launch_kv4_attn_t(const T* q, const Kv4Batch& kb, int H, int H
                          : launch_kv4_attn_n<T, D, WIDE, DECODE_MAX_BATCH>(q, kb, SHORT, H, Hkv, part, out, s);
     }
     // Shares of equal length over all sequences, none below 128 keys, the shortest with which no CU gets a third workgroup: 131072 keys of 8 heads in 64 shares
-    // 27.9 us, in 60 30.4, in 120 32.4; 16 sequences of 1048 .. 13107 keys, 4 heads, 480 / 536 / 960 workgroups 18.7 / 21.9 / 21.0 us.
-    int64_t per = (total * Hkv + KV4_WORKGROUPS - 1) / KV4_WORKGROUPS;
+    // 27.9 us, in 60 30.4, in 120 32.4; 16 sequences of 1048 .. 13107 keys, 4 heads, 480 / 536 / 960 workgroups 18.7 / 21.9 / 21.0 us.  Sequences and heads that are many on their own
+    // have room for four shares a sequence nevertheless, else the longest one's workgroups stay behind: the same sequences, 32 heads, 1 / 2 / 4 / 8 shares a sequence on average 116.8 /
+    // 95.7 / 86.8 / 85.1 us; 16 of 120 .. 1500 keys in fp32, 32 heads of 64, 15.2 / 15.4 / 16.0 / 19.2.
+    const int64_t most = std::max<int64_t>(KV4_WORKGROUPS, 4 * (int64_t)kb.n * Hkv);
+    int64_t per = (total * Hkv + most - 1) / most;
     per = per < 128 ? 128 : per > (1 << 30) ? (1 << 30) : (per + 31) / 32 * 32;
     const int64_t room = (int64_t)(part_floats / ((size_t)H * (D + 2)));
     for (;; per += (per / 64 + 31) / 32 * 32) {
         int64_t splits = 0;
         for (int b = 0; b < kb.n; ++b) splits += kb.count[b] > per ? (kb.count[b] + per - 1) / per : 1;
-        if (longest <= per * KV4_MAX_SPLITS && (splits == kb.n || (splits <= room && splits * Hkv <= KV4_WORKGROUPS))) break;
+        if (longest <= per * KV4_MAX_SPLITS && (splits == kb.n || (splits <= room && splits * Hkv <= most))) break;
     }
     return kb.n == 1 ? launch_kv4_attn_n<T, D, 4, 1>(q, kb, per, H, Hkv, part, out, s)
                      : launch_kv4_attn_n<T, D, 4, DECODE_MAX_BATCH>(q, kb, per, H, Hkv, part, out, s);
