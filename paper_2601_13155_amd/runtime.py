@@ -217,7 +217,10 @@ class Q4Matrix:
         self.codes = torch.empty(cb, dtype=torch.uint8, device=W.device)
         self.scales = torch.empty(sb, dtype=torch.uint8, device=W.device)
         self.struct = binding.spts_q4(self.codes.data_ptr(), self.scales.data_ptr(), rows, K)
-        ctx.spts_q4_pack(W.contiguous(), self.struct)
+        Wc = W.contiguous()
+        ctx.spts_q4_pack(Wc, self.struct)
+        if Wc is not W:
+            Wc.record_stream(ctx.stream)      # a copy of this call's own: not to be reused before it is packed
 
 
 def pack_layer_q4(ctx: binding.Context, w: binding.spts_layer_weights) -> binding.spts_layer_q4:
@@ -269,6 +272,7 @@ class KV4Batch:
         k = torch.empty((max(n, 1), shape.Hkv, shape.d), dtype=torch.bfloat16 if shape.dtype == "bf16" else torch.float32, device="cuda")
         v = torch.empty_like(k)
         ctx.spts_kv4_read([self.structs[b]], [0, n], k, v)
+        ctx.stream.synchronize()
         return to_host(k[:n]).astype(np.float64), to_host(v[:n]).astype(np.float64), self.tensors[b][4][:n].cpu().numpy()
 
 

@@ -376,6 +376,39 @@ def test_attention_in_place_and_on_two_streams(torch, dtype):
     assert all(torch.equal(m[2], m[3]) for m in made)
 
 
+@pytest.mark.parametrize("n", [200, 2500])
+def test_one_cache_for_several_queries(torch, n):
+    """The same buffers given to several queries, with counts of their own; a repeated query's result is the same bits, rows behind the last are left."""
+    ctx, shape = ctx_for("bf16", H=8, Hkv=2, d=128)
+    rng = np.random.default_rng(n)
+    caches = runtime.KV4Batch(shape, [n])
+    k, v = make_pairs(rng, n, 2, 128, "bf16")
+    append(torch, ctx, caches, [(k, v, np.arange(n))], "bf16")
+    counts = [n, n // 2, n, 0, 1]
+    many = (binding.spts_kv4 * 5)(*[caches.structs[0]] * 5)
+    for s, c in zip(many, counts):
+        s.count = c
+    q = rounded(rng.standard_normal((5, 8, 128)), "bf16")
+    q[2] = q[0]
+    qd = runtime.to_device(q, "bf16")
+    out = torch.full_like(qd, 9.0)
+    behind = torch.full((2, 8, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    both = torch.cat([out, behind])
+    ctx.spts_kv4_attn(qd, many, both)
+    torch.cuda.synchronize()
+    assert torch.equal(both[5:], behind)                # rows behind the last query
+    assert torch.equal(both[0], both[2]) and not both[3].any()
+    got = runtime.to_host(both).astype(np.float64)
+    for b, c in enumerate(counts):
+        if c == 0:
+            continue
+        kq, vq = fp4.fp4_round(k[:c]), fp4.fp4_round(v[:c])
+        ref = fp4.attend(q[b].astype(np.float64), kq, vq)
+        for h in range(8):
+            tol = attend_tol(q[b, h].astype(np.float64), kq[:, h // 4], vq[:, h // 4], "bf16")
+            assert np.all(np.abs(got[b, h] - ref[h]) <= tol), (b, h)
+
+
 # -------------------------------------------------------------------------------------------------------------- rules
 def words(allowed):
     """Bit masks [n, ceil(V / 32)] int32 of truth values [n, V]."""
