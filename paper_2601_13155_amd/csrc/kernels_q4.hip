@@ -271,7 +271,7 @@ __global__ void __launch_bounds__(NW * 64) q4_matvec_kernel(Q4Mats<NM> a) {
             c[s] = *reinterpret_cast<const u32x4*>(slot + s * 1024 + lane * 16);
             sc[s] = *reinterpret_cast<const uint32_t*>(slot + NS * 1024 + s * 64 + l16 * 4);
         }
-        const int xr = l16 & (4 * XI - 1);         // (with room for 4 or 8 vectors the columns behind repeat them, with one alone all do)
+        const int xr = l16 & (4 * XI - 1);         // (with room for 4 or 8 vectors the columns behind repeat them)
         const int k0 = (wave + NW * n) * 128;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {

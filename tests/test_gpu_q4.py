@@ -160,6 +160,30 @@ def test_product_with_infinities_and_the_largest_numbers(torch, dtype):
     assert np.array_equal(got[5], ref[5])               # whole numbers and quarters
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_product_of_the_longest_rows(torch, dtype):
+    """16 vectors of 2^26 values (fp32: 4 GB, byte offsets just below 2^32) that are zero but for a few whole numbers at either end."""
+    ctx, _ = ctx_for(dtype)
+    K = 1 << 26
+    tdt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    W = torch.ones((1, K), dtype=tdt, device="cuda")
+    W[0, 1::2] = -1.0
+    m = runtime.Q4Matrix(ctx, W)
+    del W
+    x = torch.zeros((16, K), dtype=tdt, device="cuda")
+    want = []
+    for b in range(16):
+        at = [b, K // 2 + 33 * b + 1, K - 1, K - 1 - 7 * b - 2]
+        vals = [1.0, 4.0, 16.0, 64.0]
+        for i, v in zip(at, vals):
+            x[b, i] = v
+        want.append(sum(v * (-1.0 if i % 2 else 1.0) for i, v in zip(at, vals)))
+    y = torch.empty((16, 1), dtype=torch.float32, device="cuda")
+    ctx.spts_matvec_q4(m.struct, x, 16, y, 1)
+    torch.cuda.synchronize()
+    assert y[:, 0].tolist() == want
+
+
 # ------------------------------------------------------------------------------------------------------------- caches
 def make_pairs(rng, n, Hkv, d, dtype):
     k = rounded(rng.standard_normal((n, Hkv, d)) * np.exp(rng.standard_normal((1, Hkv, d))), dtype)
