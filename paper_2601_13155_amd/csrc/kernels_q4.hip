@@ -55,8 +55,11 @@ template <int NM> struct Q4Mats { const u32x4* codes[NM]; const uint32_t* scales
 // loads, which a load behind them would have to wait for), takes the sums of squares and leaves the normalised vectors, rounded as rmsnorm_kernel does it,
 // in their place (zeros up to whole slabs).  Piece c (16 bytes) of vector b lies at slot c ^ 4 b, which spreads the vectors of an operand over the banks.
 // A wavefront reads only what it has loaded itself until the sums meet.
+// Where that is done: up to four vectors, in 40 KB of LDS with gamma, beside which two workgroups' rings fit a CU.  us of a decode layer over 1000 pairs, inside / with two
+// launches: hidden size 4096, 1 / 2 / 4 vectors 40.3 / 42.7 / 46.1 and 46.9 / 49.4 / 50.3; 2048 28.9 / 31.1 / 34.1 and 33.6 / 35.6 / 36.8; beyond, 8192, two vectors in 48 KB
+// 105.1 and 103.2, four in 80 KB 117.0 and 103.9; 4096, eight vectors inside Q/K/V alone 54.8 and 53.4.
 constexpr int Q4_NORM_NB = 4;
-constexpr int Q4_NORM_SLABS = 40;   // KB of LDS: the vectors and gamma
+constexpr int Q4_NORM_SLABS = 40;
 template <int NW>
 __device__ inline void norm_load(const bf16_t* x, const bf16_t* gamma, int K, int slabs, int nb, uint32_t at) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
