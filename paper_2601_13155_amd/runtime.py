@@ -242,15 +242,26 @@ class KV4Batch:
         torch = _torch()
         m = binding.model_desc(shape)
         self.structs = (binding.spts_kv4 * len(capacities))()
-        self.tensors = []
+        self._parts, at = [], 0               # (offset, bytes) of a sequence's k, v, k_scale, v_scale, pos in one allocation
         for s, cap in zip(self.structs, capacities):
-            cap = max(8, (int(cap) + 7) // 8 * 8)
+            s.capacity = cap = max(8, (int(cap) + 7) // 8 * 8)
             cb, sb = binding.spts_kv4_bytes(m, cap)
-            t = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in (cb, cb, sb, sb)] + [torch.empty(cap, dtype=torch.int32, device="cuda")]
-            self.tensors.append(t)
-            s.k, s.v, s.k_scale, s.v_scale, s.pos = (x.data_ptr() for x in t)
-            s.capacity = cap
+            parts = []
+            for n in (cb, cb, sb, sb, 4 * cap):
+                parts.append((at, n))
+                at += (n + 255) // 256 * 256
+            self._parts.append(parts)
+        self._buffer = torch.empty(at, dtype=torch.uint8, device="cuda")
+        base = self._buffer.data_ptr()
+        for s, parts in zip(self.structs, self._parts):
+            s.k, s.v, s.k_scale, s.v_scale, s.pos = (base + p for p, _ in parts)
         self._empty = bytes(self.structs)
+
+    @property
+    def tensors(self):
+        """Per sequence the buffers as tensors: codes of k and v and their scales (uint8), positions (int32)."""
+        view = [[self._buffer[p:p + n] for p, n in parts] for parts in self._parts]
+        return [t[:4] + [t[4].view(_torch().int32)] for t in view]
 
     @property
     def counts(self) -> List[int]:
