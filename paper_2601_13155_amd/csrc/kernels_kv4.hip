@@ -312,15 +312,20 @@ template <int D> struct Kv4Step {
 //     a lane, which is how the values are stored (piece n of eight keys: D / 16 dimensions): decoding gives pairs of dimensions, two byte permutes pairs of keys.
 //   In both results a column, i.e. lane % 16, is a query head, so the running maximum, the sum and the rescaling are the lane's own.
 // The maximum moves only when a score is 2^8 times above it (the sums stand that easily), so most steps have no rescaling.
-template <typename T, int D, int NW, int NB>
+// The weights of a bf16 output go into the matrix instructions as two bf16 parts (off by 2^-15 of a weight at most; one part, off by 2^-8, is as much again as the output's own rounding),
+// those of an fp32 output as three, all of their 24 bits.  With up to eight query heads the two parts are columns of one instruction (PAIRED: column c is head c % 8, the
+// upper eight columns have the second part; the scores are computed in both), added where the wavefronts meet, otherwise an instruction each.
+template <typename T, int D, int NW, int NB, bool PAIRED>
 __global__ void __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) kv4_attn_kernel(const T* q, Kv4Caches<NB> kb, int H, int Hkv, float scale_log2e, float* __restrict__ part,
                                                                           T* out) {   // (may be q: a workgroup has read its heads' queries before it writes them)
     constexpr bool F32 = sizeof(T) == 4;
-    constexpr int NP = F32 ? 3 : 1;                       // bf16 parts of a query or weight
+    constexpr int NP = F32 ? 3 : 1;                       // bf16 parts of a query
+    constexpr int WP = F32 ? 3 : PAIRED ? 1 : 2;          // instructions for the parts of a weight
+    static_assert(!(F32 && PAIRED), "three parts");
     constexpr int KW = D / 32, VM = D / 16, LD = D + 4;
     extern __shared__ __attribute__((aligned(16))) float lds[];   // [NW][group][LD] weighted values, then [NW][16][2] maximum and sum
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, kg = lane >> 4;
-    const int g = blockIdx.y, grp = H / Hkv;
+    const int g = blockIdx.y, grp = H / Hkv, head = PAIRED ? l16 & 7 : l16;   // the head of the lane's column
     float* const sml = lds + NW * grp * LD;
     int first;
     const int b = sequence_of(kb.end, (int)blockIdx.x, &first);
@@ -330,19 +335,19 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) kv4_attn_kernel(cons
     // the queries, columns beyond the group zero
     u32x4 qf[NP][KW];
     {
-        const T* qh = q + ((int64_t)b * H + g * grp + (l16 < grp ? l16 : 0)) * D + kg * (D / 4);
+        const T* qh = q + ((int64_t)b * H + g * grp + (head < grp ? head : 0)) * D + kg * (D / 4);
 #pragma unroll
         for (int i = 0; i < KW; ++i) {
             if constexpr (F32) {
                 float v[8];
                 u32x4 parts[NP];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = l16 < grp ? qh[8 * i + j] : 0.f;
+                for (int j = 0; j < 8; ++j) v[j] = head < grp ? qh[8 * i + j] : 0.f;
                 bf16_parts<NP>(v, parts);
 #pragma unroll
                 for (int p = 0; p < NP; ++p) qf[p][i] = parts[p];
             } else {
-                qf[0][i] = l16 < grp ? *reinterpret_cast<const u32x4*>(qh + 8 * i) : u32x4{0, 0, 0, 0};
+                qf[0][i] = head < grp ? *reinterpret_cast<const u32x4*>(qh + 8 * i) : u32x4{0, 0, 0, 0};
             }
         }
     }
@@ -378,6 +383,7 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) kv4_attn_kernel(cons
         load_words<2>((const char*)vsp + (uint32_t)((grp8 * (D / 32) + vblk) * 8), s.vs);
     };
 
+    const float less = PAIRED && l16 >= 8 ? -1.f : 0.f;
     float m = -INFINITY, l = 0.f;
     mfma_f32x4 acc[VM];
 #pragma unroll
@@ -429,8 +435,17 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) kv4_attn_kernel(cons
 #pragma unroll
         for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j / 4][j % 4], scale_log2e, -m));
         l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-        u32x4 pf[NP];
-        bf16_parts<NP>(p, pf);   // bf16 output: weights are rounded to bf16 for the matrix core; fp32: three parts are all of a weight's 24 bits
+        u32x4 pf[WP];
+        if constexpr (PAIRED) {
+            // the lower columns have the rounded weight, the upper columns what that leaves
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t h = cvt_pk_bf16(p[2 * j], p[2 * j + 1]);
+                pf[0][j] = cvt_pk_bf16(__builtin_fmaf(__uint_as_float(h << 16), less, p[2 * j]), __builtin_fmaf(__uint_as_float(h & 0xffff0000u), less, p[2 * j + 1]));
+            }
+        } else {
+            bf16_parts<WP>(p, pf);
+        }
         float vsc[8];
         vsc[0] = fp4_scale_of<0>(cur.vs[0]); vsc[1] = fp4_scale_of<1>(cur.vs[0]); vsc[2] = fp4_scale_of<2>(cur.vs[0]); vsc[3] = fp4_scale_of<3>(cur.vs[0]);
         vsc[4] = fp4_scale_of<0>(cur.vs[1]); vsc[5] = fp4_scale_of<1>(cur.vs[1]); vsc[6] = fp4_scale_of<2>(cur.vs[1]); vsc[7] = fp4_scale_of<3>(cur.vs[1]);
@@ -445,7 +460,7 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) kv4_attn_kernel(cons
                 hi[j] = __builtin_amdgcn_perm(d[2 * j + 1], d[2 * j], 0x07060302);
             }
 #pragma unroll
-            for (int p2 = NP - 1; p2 >= 0; --p2) {
+            for (int p2 = WP - 1; p2 >= 0; --p2) {
                 acc[2 * I] = mfma16(lo, pf[p2], acc[2 * I]);
                 acc[2 * I + 1] = mfma16(hi, pf[p2], acc[2 * I + 1]);
             }
@@ -456,6 +471,12 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) kv4_attn_kernel(cons
     }
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
+    if constexpr (PAIRED) {
+#pragma unroll
+        for (int i = 0; i < VM; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[i][r] += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(acc[i][r]), 0x128, 0xF, 0xF, true));   // row_ror 8
+    }
     // the wavefronts meet.  acc[i][r]: head l16, dimension (4 kg + r) D / 16 + i
     if (l16 < grp) {
         float* const to = lds + (wave * grp + l16) * LD + 4 * kg * VM;
@@ -562,8 +583,8 @@ __global__ void __launch_bounds__(D) kv4_merge_few_kernel(const float* __restric
     out[((int64_t)b * H + h) * D + e] = from_f32<T>(L == 0.f ? 0.f : t / L);
 }
 
-template <typename T, int D, int NW, int NB>
-static hipError_t launch_kv4_attn_n(const T* q, const Kv4Batch& kb, int64_t per, int H, int Hkv, float* part, T* out, hipStream_t s) {
+template <typename T, int D, int NW, int NB, bool PAIRED>
+static hipError_t launch_kv4_attn_p(const T* q, const Kv4Batch& kb, int64_t per, int H, int Hkv, float* part, T* out, hipStream_t s) {
     Kv4Caches<NB> c{};
     Kv4Ends<NB> ends{};
     for (int b = 0; b < NB; ++b) {
@@ -574,9 +595,9 @@ static hipError_t launch_kv4_attn_n(const T* q, const Kv4Batch& kb, int64_t per,
     }
     c.per = (uint32_t)per;
     const int splits = c.end[NB - 1], lds = (NW * (H / Hkv) * (D + 4) + NW * 32) * (int)sizeof(float);
-    const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(&kv4_attn_kernel<T, D, NW, NB>), (NW * KV4_MAX_GROUP * (D + 4) + NW * 32) * (int)sizeof(float));
+    const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(&kv4_attn_kernel<T, D, NW, NB, PAIRED>), (NW * KV4_MAX_GROUP * (D + 4) + NW * 32) * (int)sizeof(float));
     if (e != hipSuccess) return e;
-    kv4_attn_kernel<T, D, NW, NB><<<dim3((unsigned)splits, (unsigned)Hkv), dim3(NW * 64), lds, s>>>(q, c, H, Hkv, 1.4426950408889634f / sqrtf((float)D), part, out);
+    kv4_attn_kernel<T, D, NW, NB, PAIRED><<<dim3((unsigned)splits, (unsigned)Hkv), dim3(NW * 64), lds, s>>>(q, c, H, Hkv, 1.4426950408889634f / sqrtf((float)D), part, out);
     if (splits > kb.n) {
         // us by four workgroups a head / in one round trip: 16 sequences of up to 3000 / 13107 keys of 28 heads, 12 shares, 13.4 / 20.4 and 10.7 / 17.7; one sequence of 2000 keys, 16
         // shares, 7.5 and 7.5; many shares by four workgroups a head / by one: 5000 / 13107 / 131072 keys of 32 heads, 40 or 64 shares, 8.2 / 9.2 / 27.4 and 9.2 / 10.9 / 28.3
@@ -586,6 +607,17 @@ static hipError_t launch_kv4_attn_n(const T* q, const Kv4Batch& kb, int64_t per,
         else kv4_merge_few_kernel<T, D, NB><<<dim3((unsigned)H, (unsigned)kb.n), dim3(D), 0, s>>>(part, ends, H, Hkv, out);
     }
     return hipGetLastError();
+}
+
+// Pairing saves every step half of the value product's instructions and costs an addition of all sums at the end, so short caches (a step or two a wavefront) go without.
+// us with one part of a weight / two, an instruction each / two, paired: 517 keys of 32 / 8 heads 6.0 / 6.2 / 6.5, 13107 keys 9.2 / 9.45 / 9.45, 131072 keys 27.4 / 27.9 / 27.6,
+// 16 sequences of 1048 .. 13107 keys of 28 / 4 heads 17.6 / 18.5 / 18.1 (three parts, an instruction each: 6.6, 9.7, 30.4, 20.0).
+template <typename T, int D, int NW, int NB>
+static hipError_t launch_kv4_attn_n(const T* q, const Kv4Batch& kb, int64_t per, int H, int Hkv, float* part, T* out, hipStream_t s) {
+    if constexpr (sizeof(T) == 2) {
+        if (NW == 4 && H / Hkv <= 8) return launch_kv4_attn_p<T, D, NW, NB, true>(q, kb, per, H, Hkv, part, out, s);
+    }
+    return launch_kv4_attn_p<T, D, NW, NB, false>(q, kb, per, H, Hkv, part, out, s);
 }
 
 constexpr int KV4_WORKGROUPS = 512;   // two per CU
