@@ -298,6 +298,8 @@ template <int D, int J, int I> __device__ inline uint32_t value_pair(const uint3
     return fp4_pair_bf16<byte % 4>(w[byte / 4], scale);
 }
 
+constexpr float KV4_LOWEST = -3.402823466e38f;
+
 // what one lane needs of 32 keys
 template <int D> struct Kv4Step {
     uint32_t k[2][D / 32], v[D / 16], vs[2];
@@ -311,7 +313,8 @@ template <int D> struct Kv4Step {
 //   O^T = V^T P^T: these eight scores are already the second operand's eight values of the lane, no exchange needed; the first needs eight keys of one dimension in
 //     a lane, which is how the values are stored (piece n of eight keys: D / 16 dimensions): decoding gives pairs of dimensions, two byte permutes pairs of keys.
 //   In both results a column, i.e. lane % 16, is a query head, so the running maximum, the sum and the rescaling are the lane's own.
-// The maximum moves only when a score is 2^8 times above it (the sums stand that easily), so most steps have no rescaling.
+// The maximum moves only when a score is 2^8 times above it (the sums stand that easily), so most steps have no rescaling.  It begins at the lowest finite number, below
+// every finite score, so that scores that are -inf in fp32 weigh nothing even where a wavefront has met no other yet.
 // The weights of a bf16 output go into the matrix instructions as two bf16 parts (off by 2^-15 of a weight at most; one part, off by 2^-8, is as much again as the output's own rounding),
 // those of an fp32 output as three, all of their 24 bits.  With up to eight query heads the two parts are columns of one instruction (PAIRED: column c is head c % 8, the
 // upper eight columns have the second part; the scores are computed in both), added where the wavefronts meet, otherwise an instruction each.
@@ -384,7 +387,7 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) kv4_attn_kernel(cons
     };
 
     const float less = PAIRED && l16 >= 8 ? -1.f : 0.f;
-    float m = -INFINITY, l = 0.f;
+    float m = KV4_LOWEST, l = 0.f;
     mfma_f32x4 acc[VM];
 #pragma unroll
     for (int i = 0; i < VM; ++i) acc[i] = mfma_f32x4{0.f, 0.f, 0.f, 0.f};
@@ -489,19 +492,18 @@ __global__ void __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) kv4_attn_kernel(cons
     __syncthreads();
     for (int t = tid; t < grp * D; t += NW * 64) {
         const int hg = t / D, e = t % D;
-        float mn = -INFINITY;
+        float mn = KV4_LOWEST;
 #pragma unroll
         for (int w = 0; w < NW; ++w) mn = fmaxf(mn, sml[(w * 16 + hg) * 2]);
-        const float mu = mn == -INFINITY ? 0.f : mn;
         float ls = 0.f, o = 0.f;
 #pragma unroll 4
         for (int w = 0; w < NW; ++w) {
-            const float a = __builtin_amdgcn_exp2f(sml[(w * 16 + hg) * 2] - mu);
+            const float a = __builtin_amdgcn_exp2f(sml[(w * 16 + hg) * 2] - mn);
             ls += sml[(w * 16 + hg) * 2 + 1] * a;
             o += lds[(w * grp + hg) * LD + e] * a;
         }
         if (ns == 1) {
-            out[((int64_t)b * H + g * grp + hg) * D + e] = from_f32<T>(ls == 0.f ? 0.f : o / ls);
+            out[((int64_t)b * H + g * grp + hg) * D + e] = from_f32<T>(n == 0 ? 0.f : o / ls);
         } else {
             float* dst = part + (((int64_t)blockIdx.x * Hkv + g) * grp + hg) * (D + 2);
             if (e == 0) { dst[0] = mn; dst[1] = ls; }
@@ -531,7 +533,7 @@ __global__ void __launch_bounds__(512) kv4_merge_kernel(const float* __restrict_
     if (lane == 0) red[0][wave] = mx;
     __syncthreads();
     mx = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
-    const float mu = mx == -INFINITY ? 0.f : mx, a = __builtin_amdgcn_exp2f(m - mu);
+    const float a = __builtin_amdgcn_exp2f(m - mx);
     if (tid < KV4_MAX_SPLITS) sa[tid] = a;
     float ls = l * a;
     for (int off = 32; off > 0; off >>= 1) ls += __shfl_xor(ls, off);
@@ -550,7 +552,7 @@ __global__ void __launch_bounds__(512) kv4_merge_kernel(const float* __restrict_
     float t = 0.f;
 #pragma unroll
     for (int k = 0; k < GROUPS; ++k) t += so[k * W + tid];
-    out[((int64_t)b * H + h) * D + e] = from_f32<T>(L == 0.f ? 0.f : t / L);
+    out[((int64_t)b * H + h) * D + e] = from_f32<T>(t / L);
 }
 
 // Of up to KV4_FEW splits: a thread has a dimension and takes all of them at once, one round trip without a barrier.
@@ -572,15 +574,14 @@ __global__ void __launch_bounds__(D) kv4_merge_few_kernel(const float* __restric
     }
 #pragma unroll
     for (int s = 0; s < KV4_FEW; ++s) mx = fmaxf(mx, m[s]);
-    const float mu = mx == -INFINITY ? 0.f : mx;
     float L = 0.f, t = 0.f;
 #pragma unroll
     for (int s = 0; s < KV4_FEW; ++s) {
-        const float a = __builtin_amdgcn_exp2f(m[s] - mu);
+        const float a = __builtin_amdgcn_exp2f(m[s] - mx);
         L += s < ns ? l[s] * a : 0.f;
         t += s < ns ? o[s] * a : 0.f;
     }
-    out[((int64_t)b * H + h) * D + e] = from_f32<T>(L == 0.f ? 0.f : t / L);
+    out[((int64_t)b * H + h) * D + e] = from_f32<T>(t / L);
 }
 
 template <typename T, int D, int NW, int NB, bool PAIRED>

@@ -47,3 +47,35 @@ def test_attention_weights_are_not_rounded_to_bf16(torch, dtype, grp, Hkv, d, n)
             tol = (2 * (ds + 2.0 ** -22) + SUM(n) + weight + 3 * 2.0 ** -23 + HALF[dtype]) * np.abs(ref[h])
             err = np.abs(got[b, h] - ref[h])
             assert np.all(err <= tol), (b, h, float((err / np.maximum(tol, 1e-300)).max()))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("grp,d", [(4, 32), (8, 128), (12, 64)])
+@pytest.mark.parametrize("n,low", [(33, [32]), (70, list(range(32))), (700, list(range(0, 64)) + [699]), (1500, list(range(256)) + [1499]),
+                                   (9000, list(range(128, 512)) + [8999])])
+def test_attention_scores_below_all_of_fp32(torch, dtype, grp, d, n, low):  # noqa: F811
+    """Keys whose score is -inf in fp32 (d products of -2^190) weigh nothing, also where a wavefront, a share or the end of the cache has no others; the
+    remaining scores are small multiples of 2^-4 over sqrt(d), exact sums in fp32, so the bound is that of the exponentials and the weighted sum alone."""
+    ctx, shape = ctx_for(dtype, H=2 * grp, Hkv=2, d=d)
+    rng = np.random.default_rng(n)
+    k = 2.0 ** -95 * rng.choice([-2.0, -1.0, -0.5, 0.5, 1.0, 2.0], (n, 2, d))
+    k[low] = -2.0 ** 95
+    v = rounded(rng.standard_normal((n, 2, d)), dtype)
+    v[low] = 1000.0
+    q = 2.0 ** 95 * rng.choice([0.125, 0.25], (1, 2 * grp, d))
+    caches = runtime.KV4Batch(shape, [n])
+    append(torch, ctx, caches, [(k.astype(np.float32), v, np.arange(n))], dtype)
+    out = torch.empty(q.shape, dtype=torch.bfloat16 if dtype == "bf16" else torch.float32, device="cuda")
+    ctx.spts_kv4_attn(runtime.to_device(q.astype(np.float32), dtype), caches.structs, out)
+    torch.cuda.synchronize()
+    got = runtime.to_host(out).astype(np.float64)[0]
+    kq, vq = fp4.fp4_round(k), fp4.fp4_round(v)
+    assert np.array_equal(kq, k)
+    ref = fp4.attend(q[0], kq, vq)
+    keep = np.setdiff1d(np.arange(n), low)
+    for h in range(2 * grp):
+        s = kq[keep, h // grp] @ q[0, h] / math.sqrt(d)
+        p = np.exp(s - s.max())
+        mag = p @ np.abs(vq[keep, h // grp]) / p.sum()
+        tol = (2 * (2.0 ** -22 * np.abs(s).max() + 2.0 ** -22 + SUM(n)) + 2.0 ** -15 + 3 * 2.0 ** -23) * mag + HALF[dtype] * np.abs(ref[h])
+        assert np.all(np.abs(got[h] - ref[h]) <= tol), (h, got[h][:4], ref[h][:4])
