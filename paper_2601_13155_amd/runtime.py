@@ -4,6 +4,7 @@ Marshalling and sequencing only: every arithmetic step of the path runs inside l
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 from typing import Dict, List, Optional
 
@@ -206,6 +207,23 @@ class BatchedDecodeRunner:
             self.x.copy_(self.x_next)
 
 
+@contextlib.contextmanager
+def _on_stream_of(ctx: binding.Context):
+    """The body's work, torch's and the library's, goes to the context's stream: behind what the current stream has been given, and
+    ahead of what it is given afterwards (so that what the current stream's pool gets back is no longer in use)."""
+    torch = _torch()
+    current = torch.cuda.current_stream(ctx.stream.device)
+    if current == ctx.stream:
+        yield
+        return
+    ctx.stream.wait_stream(current)
+    try:
+        with torch.cuda.stream(ctx.stream):
+            yield
+    finally:
+        current.wait_stream(ctx.stream)
+
+
 # ------------------------------------------------------------------------------------------- decode in 4 bits
 class Q4Matrix:
     """A matrix [rows, K] packed into 4 bits (spts_q4_pack); W: device tensor of the context's element type."""
@@ -217,10 +235,8 @@ class Q4Matrix:
         self.codes = torch.empty(cb, dtype=torch.uint8, device=W.device)
         self.scales = torch.empty(sb, dtype=torch.uint8, device=W.device)
         self.struct = binding.spts_q4(self.codes.data_ptr(), self.scales.data_ptr(), rows, K)
-        Wc = W.contiguous()
-        ctx.spts_q4_pack(Wc, self.struct)
-        if Wc is not W:
-            Wc.record_stream(ctx.stream)      # a copy of this call's own: not to be reused before it is packed
+        with _on_stream_of(ctx):
+            ctx.spts_q4_pack(W.contiguous(), self.struct)
 
 
 def pack_layer_q4(ctx: binding.Context, w: binding.spts_layer_weights) -> binding.spts_layer_q4:
@@ -273,7 +289,8 @@ class KV4Batch:
     def append_cache(self, ctx: binding.Context, b: int, cache: "KVCache"):
         """Appends every pair of a prefill's cache to sequence b's."""
         one = [self.structs[b]]
-        ctx.spts_kv4_append(cache.k, cache.v, cache.pos, [0, cache.count], one)
+        with _on_stream_of(ctx):
+            ctx.spts_kv4_append(cache.k, cache.v, cache.pos, [0, cache.count], one)
         self.structs[b].count = one[0].count
 
     def host(self, ctx: binding.Context, shape, b: int):
@@ -282,8 +299,8 @@ class KV4Batch:
         n = self.counts[b]
         k = torch.empty((max(n, 1), shape.Hkv, shape.d), dtype=torch.bfloat16 if shape.dtype == "bf16" else torch.float32, device="cuda")
         v = torch.empty_like(k)
-        ctx.spts_kv4_read([self.structs[b]], [0, n], k, v)
-        ctx.stream.synchronize()
+        with _on_stream_of(ctx):
+            ctx.spts_kv4_read([self.structs[b]], [0, n], k, v)
         return to_host(k[:n]).astype(np.float64), to_host(v[:n]).astype(np.float64), self.tensors[b][4][:n].cpu().numpy()
 
 
@@ -332,7 +349,8 @@ class LogitsRules:
 
 class Q4DecodeRunner:
     """Decode phase with weights and caches in 4 bits for a batch of sequences: per step one spts_decode_layer_q4 per layer,
-    the final norm, the head's 4-bit matrix and spts_process_logits.  Only enqueues work; tokens stay on the device.
+    the final norm, the head's 4-bit matrix and spts_process_logits.  Only enqueues work; tokens stay on the device.  All of it goes to the
+    context's stream, between what torch's current stream has been given before and is given later.
 
     caches: one KV4Batch per layer; table [V, D]: the embedding (element type); head: its 4-bit form or another
     output matrix's; rules: LogitsRules, whose history the runner extends by the tokens it decodes (None = plain argmax)."""
@@ -362,15 +380,17 @@ class Q4DecodeRunner:
 
     def step(self, pos):
         """Runs self.x (in place) through every layer as the tokens at the host positions pos."""
-        for w, c in zip(self.layers, self.caches):
-            self.ctx.spts_decode_layer_q4(self.x, pos, w, c.structs)
+        with _on_stream_of(self.ctx):
+            for w, c in zip(self.layers, self.caches):
+                self.ctx.spts_decode_layer_q4(self.x, pos, w, c.structs)
 
     def next_token(self):
         """self.tokens and self.x_next from self.x: final norm, logits, rules, argmax, table row."""
         V = int(self.table.shape[0])
-        self.ctx.spts_rmsnorm(self.x, self.gamma_f, self.batch, self.xn)
-        self.ctx.spts_matvec_q4(self.head.struct, self.xn, self.batch, self.logits, 1)
-        self.ctx.spts_process_logits(self.logits, V, self.batch, self.rules.struct, self.logits, self.tokens, self.table, self.x_next)
+        with _on_stream_of(self.ctx):
+            self.ctx.spts_rmsnorm(self.x, self.gamma_f, self.batch, self.xn)
+            self.ctx.spts_matvec_q4(self.head.struct, self.xn, self.batch, self.logits, 1)
+            self.ctx.spts_process_logits(self.logits, V, self.batch, self.rules.struct, self.logits, self.tokens, self.table, self.x_next)
 
     def generate(self, pos0: List[int], steps: int, tokens_out=None):
         """steps decode steps from self.x at positions pos0; tokens_out [batch, steps] int32 device.  With a history in the
@@ -380,16 +400,17 @@ class Q4DecodeRunner:
             raise ValueError(f"the history's rows of {hist.shape[1]} ids have no room for {steps} more")
         if any(s.count + steps > s.capacity for c in self.caches for s in c.structs):
             raise ValueError(f"a cache has no room for {steps} more pairs")
-        for t in range(steps):
-            self.step([p + t for p in pos0])
-            self.next_token()
-            if hist is not None:
-                for b in range(self.batch):
-                    hist[b, lens[b]:lens[b] + 1].copy_(self.tokens[b:b + 1])
-                    lens[b] += 1
-            if tokens_out is not None:
-                tokens_out[:, t].copy_(self.tokens)
-            self.x.copy_(self.x_next)
+        with _on_stream_of(self.ctx):
+            for t in range(steps):
+                self.step([p + t for p in pos0])
+                self.next_token()
+                if hist is not None:
+                    for b in range(self.batch):
+                        hist[b, lens[b]:lens[b] + 1].copy_(self.tokens[b:b + 1])
+                        lens[b] += 1
+                if tokens_out is not None:
+                    tokens_out[:, t].copy_(self.tokens)
+                self.x.copy_(self.x_next)
 
 
 class StackRunner:

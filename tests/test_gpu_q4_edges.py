@@ -5,8 +5,8 @@ import numpy as np
 import pytest
 
 from oracle import fp4_oracle as fp4
-from tests.test_gpu_q4 import HALF, SUM, append, ctx_for, make_pairs, rounded, torch  # noqa: F401  (torch: the fixture)
-from paper_2601_13155_amd import runtime
+from paper_2601_13155_amd import binding, runtime, synth
+from tests.test_gpu_q4 import HALF, SUM, append, ctx_for, layer_for, make_pairs, rounded, torch  # noqa: F401  (torch: the fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -79,3 +79,117 @@ def test_attention_scores_below_all_of_fp32(torch, dtype, grp, d, n, low):  # no
         mag = p @ np.abs(vq[keep, h // grp]) / p.sum()
         tol = (2 * (2.0 ** -22 * np.abs(s).max() + 2.0 ** -22 + SUM(n)) + 2.0 ** -15 + 3 * 2.0 ** -23) * mag + HALF[dtype] * np.abs(ref[h])
         assert np.all(np.abs(got[h] - ref[h]) <= tol), (h, got[h][:4], ref[h][:4])
+
+
+# -------------------------------------------------------------------------------------------------------------- streams
+_BUSY = {}
+
+
+def keep_busy(torch, stream):  # noqa: F811
+    """Some 20 ms of products on a stream: what it is given next is late."""
+    if not _BUSY:
+        _BUSY["a"] = torch.ones((4096, 4096), device="cuda")
+        _BUSY["c"] = torch.empty_like(_BUSY["a"])
+        torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        for _ in range(20):
+            torch.matmul(_BUSY["a"], _BUSY["a"], out=_BUSY["c"])
+
+
+@pytest.fixture
+def side(torch):  # noqa: F811
+    """A context on a stream of its own, over the shape of ctx_for("bf16"); the tests call from the default stream."""
+    _, shape = ctx_for("bf16")
+    st = torch.cuda.Stream()
+    with torch.cuda.stream(st):
+        ctx = binding.Context(shape, 256, 1, 1, shape.Dff, stream=st)
+    torch.cuda.synchronize()
+    assert torch.cuda.current_stream() != st
+    return ctx
+
+
+@pytest.mark.parametrize("view", ["transposed", "columns", "rows"])
+def test_a_copied_matrix_is_packed_after_it_is_copied(torch, side, view):  # noqa: F811
+    """The copy of a strided matrix is made behind a busy current stream and packed on an idle one."""
+    base = torch.randn((640, 640), device="cuda").to(torch.bfloat16)
+    W = {"transposed": base.t(), "columns": base[:, 64:], "rows": base[::2]}[view]
+    alone = W.contiguous()
+    want = runtime.Q4Matrix(ctx_for("bf16")[0], alone)
+    torch.cuda.synchronize()
+    del alone
+    junk = torch.full(W.shape, 7.0, dtype=torch.bfloat16, device="cuda")
+    torch.cuda.synchronize()
+    del junk
+    keep_busy(torch, torch.cuda.current_stream())
+    got = runtime.Q4Matrix(side, W)
+    torch.cuda.synchronize()
+    assert torch.equal(got.codes, want.codes) and torch.equal(got.scales, want.scales)
+
+
+def test_a_cache_is_read_back_after_earlier_work(torch, side):  # noqa: F811
+    """A prefill's cache converted and read back while the current stream is still writing the pairs, and then what lies where the rows are read to."""
+    _, shape = ctx_for("bf16")
+    rng = np.random.default_rng(5)
+    k, v = make_pairs(rng, 100, shape.Hkv, shape.d, "bf16")
+    kd, vd = runtime.to_device(k, "bf16"), runtime.to_device(v, "bf16")
+    kept, caches = runtime.KVCache(shape, 100), runtime.KV4Batch(shape, [100])
+    torch.cuda.synchronize()
+    keep_busy(torch, torch.cuda.current_stream())
+    kept.k.copy_(kd)
+    kept.v.copy_(vd)
+    kept.pos.copy_(torch.arange(100, device="cuda"))
+    kept.struct.count = 100
+    caches.append_cache(side, 0, kept)
+    late = [torch.full((100, shape.Hkv, shape.d), 5.0, dtype=torch.bfloat16, device="cuda") for _ in range(4)]
+    del late
+    gk, gv, gp = caches.host(side, shape, 0)
+    assert np.array_equal(gk, fp4.fp4_round(k)) and np.array_equal(gv, fp4.fp4_round(v)) and np.array_equal(gp, np.arange(100))
+
+
+def make_runner(torch, ctx, nseq, history):  # noqa: F811
+    """A runner over two layers and caches of its own, everything made from fixed seeds; (runner, history tensor)."""
+    shape, main = ctx.shape, ctx_for("bf16")[0]
+    rng, V = np.random.default_rng(70), 416
+    layers = [layer_for(torch, main, shape, 71 + l)[0] for l in range(2)]
+    lens = [40, 7, 25][:nseq]
+    caches = [runtime.KV4Batch(shape, [n + 16 for n in lens]) for _ in layers]
+    for c in caches:
+        append(torch, main, c, [make_pairs(rng, n, shape.Hkv, shape.d, "bf16") + (np.arange(n),) for n in lens], "bf16")
+    table = runtime.to_device(rounded(rng.standard_normal((V, shape.D)), "bf16"), "bf16")
+    gamma = runtime.to_device(rounded(1.0 + 0.1 * rng.standard_normal(shape.D), "bf16"), "bf16")
+    hist = torch.from_numpy(rng.integers(0, V, (nseq, 20)).astype(np.int32)).cuda() if history else None
+    rules = runtime.LogitsRules(nseq, history=hist, history_len=[5, 3, 9][:nseq], prompt_len=[5, 3, 9][:nseq], repetition=[1.3] * nseq, frequency=[0.8] * nseq) if history else None
+    run = runtime.Q4DecodeRunner(ctx, shape, layers, caches, gamma, table, runtime.Q4Matrix(main, table), rules)
+    return run, hist, table[3:3 + nseq].clone(), lens
+
+
+@pytest.mark.parametrize("history", [False, True])
+@pytest.mark.parametrize("nseq", [1, 3])
+def test_generate_on_a_side_stream(torch, side, nseq, history):  # noqa: F811
+    """The first state is written by a busy current stream, the context's stream is busy as well: tokens, history, states and logits of five steps are
+    those of a run on one stream; and the same for a step and a token of their own."""
+    res = []
+    for ctx in (ctx_for("bf16")[0], side):
+        run, hist, x0, lens = make_runner(torch, ctx, nseq, history)
+        toks = torch.full((nseq, 5), -5, dtype=torch.int32, device="cuda")
+        torch.cuda.synchronize()
+        if ctx is side:
+            keep_busy(torch, torch.cuda.current_stream())
+        run.x.copy_(x0)
+        if ctx is side:
+            keep_busy(torch, ctx.stream)
+        run.generate(lens, 5, toks)
+        got = [t.clone() for t in [toks, run.x, run.logits, run.tokens] + ([hist] if history else [])]
+        if ctx is side:
+            keep_busy(torch, torch.cuda.current_stream())
+        run.x.copy_(x0)
+        if ctx is side:
+            keep_busy(torch, ctx.stream)
+        run.step([n + 5 for n in lens])
+        got.append(run.x.clone())
+        run.next_token()
+        got += [run.logits.clone(), run.tokens.clone(), run.x_next.clone()]
+        torch.cuda.synchronize()
+        res.append([t.cpu() for t in got] + [torch.tensor(c.counts) for c in run.caches])
+    assert all(torch.equal(a, b) for a, b in zip(*res)), [torch.equal(a, b) for a, b in zip(*res)]
+    assert (res[0][0] >= 0).all()
