@@ -36,6 +36,23 @@ def make_context(shape, max_tokens: int, max_probe: int, max_r: int, max_dlow: i
     return binding.Context(shape, max_tokens, max_probe, max_r, max_dlow)
 
 
+@contextlib.contextmanager
+def _on_stream_of(ctx: binding.Context):
+    """The body's work, torch's and the library's, goes to the context's stream: behind what the current stream has been given, and
+    ahead of what it is given afterwards (so that what the current stream's pool gets back is no longer in use)."""
+    torch = _torch()
+    current = torch.cuda.current_stream(ctx.stream.device)
+    if current == ctx.stream:
+        yield
+        return
+    ctx.stream.wait_stream(current)
+    try:
+        with torch.cuda.stream(ctx.stream):
+            yield
+    finally:
+        current.wait_stream(ctx.stream)
+
+
 SLAB_PACKED = ("Wq", "Wk", "Wv", "Wo", "Wgate", "Wup", "Wdown", "Vg", "Vu", "Vd", "Ug", "Uu")
 
 
@@ -97,7 +114,8 @@ def run_layer(ctx: binding.Context, x: np.ndarray, pos: np.ndarray, dw: binding.
         vv = torch.zeros_like(kk)
         pp = torch.zeros(max(cap, 1), dtype=torch.int32, device="cuda")
         kv = binding.spts_kv_out(kk.data_ptr(), vv.data_ptr(), pp.data_ptr(), cap, 0)
-    ctx.spts_layer_prefill(xd, posd, N, dw, cfg, kv, s, ia, iff)
+    with _on_stream_of(ctx):
+        ctx.spts_layer_prefill(xd, posd, N, dw, cfg, kv, s, ia, iff)
     torch.cuda.synchronize()
     out = dict(x=to_host(xd).astype(np.float64), s_mha=s[:N].cpu().numpy(), idx_attn=ia[:Ma].cpu().numpy(),
                idx_ffn=iff[:Mf].cpu().numpy())
@@ -116,9 +134,11 @@ def select_proxy_channels(ctx: binding.Context, dw: binding.spts_layer_weights, 
     torch = _torch()
     T = int(x_cal.shape[0])
     imp = torch.zeros(shape.Dff, dtype=torch.float32, device="cuda")
-    ctx.spts_channel_importance(to_device(x_cal, shape.dtype), T, dw, int(k), imp)
     sel = torch.empty(dlow, dtype=torch.int32, device="cuda")
-    ctx.spts_select_topk(imp, shape.Dff, dlow, 0, sel)
+    xd = to_device(x_cal, shape.dtype)
+    with _on_stream_of(ctx):
+        ctx.spts_channel_importance(xd, T, dw, int(k), imp)
+        ctx.spts_select_topk(imp, shape.Dff, dlow, 0, sel)
     torch.cuda.synchronize()
     return sel.cpu().numpy(), imp.cpu().numpy()
 
@@ -161,22 +181,25 @@ class DecodeRunner:
 
     def step(self, pos: int):
         """Runs self.x (in place) through every layer as the token at absolute position pos."""
-        for w, c in zip(self.layers, self.caches):
-            self.ctx.spts_decode_layer(self.x, pos, w, c.struct)
+        with _on_stream_of(self.ctx):
+            for w, c in zip(self.layers, self.caches):
+                self.ctx.spts_decode_layer(self.x, pos, w, c.struct)
 
     def greedy(self):
         """token = argmax over the table of the final-normed self.x; self.x_next = table[token]."""
-        self.ctx.spts_greedy_token(self.x, self.gamma_f, self.table, int(self.table.shape[0]), self.token, self.logits,
-                                   self.x_next)
+        with _on_stream_of(self.ctx):
+            self.ctx.spts_greedy_token(self.x, self.gamma_f, self.table, int(self.table.shape[0]), self.token, self.logits,
+                                       self.x_next)
 
     def generate(self, pos0: int, steps: int, tokens_out=None):
         """steps greedy decode steps starting from self.x at position pos0; tokens_out [steps] int32 device."""
-        for t in range(steps):
-            self.step(pos0 + t)
-            self.greedy()
-            if tokens_out is not None:
-                tokens_out[t:t + 1].copy_(self.token[:1])
-            self.x.copy_(self.x_next)
+        with _on_stream_of(self.ctx):
+            for t in range(steps):
+                self.step(pos0 + t)
+                self.greedy()
+                if tokens_out is not None:
+                    tokens_out[t:t + 1].copy_(self.token[:1])
+                self.x.copy_(self.x_next)
 
 
 class BatchedDecodeRunner:
@@ -196,32 +219,17 @@ class BatchedDecodeRunner:
         self.logits = torch.zeros((self.batch, table.shape[0]), dtype=torch.float32, device="cuda")
 
     def step(self, pos: List[int]):
-        for l, w in enumerate(self.layers):
-            self.ctx.spts_decode_layer_batched(self.x, pos, w, [seq[l].struct for seq in self.caches])
+        with _on_stream_of(self.ctx):
+            for l, w in enumerate(self.layers):
+                self.ctx.spts_decode_layer_batched(self.x, pos, w, [seq[l].struct for seq in self.caches])
 
     def generate(self, pos0: List[int], steps: int):
-        for t in range(steps):
-            self.step([p + t for p in pos0])
-            self.ctx.spts_greedy_token_batched(self.x, self.gamma_f, self.table, int(self.table.shape[0]), self.batch,
-                                               self.tokens, self.logits, self.x_next)
-            self.x.copy_(self.x_next)
-
-
-@contextlib.contextmanager
-def _on_stream_of(ctx: binding.Context):
-    """The body's work, torch's and the library's, goes to the context's stream: behind what the current stream has been given, and
-    ahead of what it is given afterwards (so that what the current stream's pool gets back is no longer in use)."""
-    torch = _torch()
-    current = torch.cuda.current_stream(ctx.stream.device)
-    if current == ctx.stream:
-        yield
-        return
-    ctx.stream.wait_stream(current)
-    try:
-        with torch.cuda.stream(ctx.stream):
-            yield
-    finally:
-        current.wait_stream(ctx.stream)
+        with _on_stream_of(self.ctx):
+            for t in range(steps):
+                self.step([p + t for p in pos0])
+                self.ctx.spts_greedy_token_batched(self.x, self.gamma_f, self.table, int(self.table.shape[0]), self.batch,
+                                                   self.tokens, self.logits, self.x_next)
+                self.x.copy_(self.x_next)
 
 
 # ------------------------------------------------------------------------------------------- decode in 4 bits
@@ -443,33 +451,34 @@ class StackRunner:
         """x0 [N0, D] device tensor (copied, not modified), pos0 [N0] int32 device tensor.
         Returns (x, pos, N_final) as views into the runner's buffers."""
         torch = _torch()
-        xa, xb, pa, pb = self.xa, self.xb, self.posa, self.posb
-        N = self.plan[0]["N"]
-        xa[:N].copy_(x0)
-        pa[:N].copy_(pos0)
-        self.trace = []
-        for li, (w, item, cfg) in enumerate(zip(self.layers, self.plan, self.cfgs)):
-            tr = None
-            if self.keep_trace:
-                tr = dict(N=N, x_in=xa[:N].clone(), pos_in=pa[:N].clone(),
-                          idx_attn=torch.empty(max(min(N, item["m_attn"]), 1), dtype=torch.int32, device="cuda"),
-                          idx_ffn=torch.empty(max(min(N, item["m_ffn"]), 1), dtype=torch.int32, device="cuda"))
-            self.ctx.spts_layer_prefill(xa, pa, N, w, cfg, self.caches[li].struct if self.caches else None, self.s,
-                                        tr["idx_attn"] if tr else None, tr["idx_ffn"] if tr else None)
-            if tr is not None:
-                tr["x_out"] = xa[:N].clone()
-                tr["s_mha"] = self.s[:N].clone()
-            if cfg.skip and item.get("N_next") is not None:
-                n_next = min(N, item["N_next"])
-                self.ctx.spts_msdp_compact(xa, pa, self.s, N, n_next, self.protect_last, xb, pb, self.new2old, None)
+        with _on_stream_of(self.ctx):
+            xa, xb, pa, pb = self.xa, self.xb, self.posa, self.posb
+            N = self.plan[0]["N"]
+            xa[:N].copy_(x0)
+            pa[:N].copy_(pos0)
+            self.trace = []
+            for li, (w, item, cfg) in enumerate(zip(self.layers, self.plan, self.cfgs)):
+                tr = None
+                if self.keep_trace:
+                    tr = dict(N=N, x_in=xa[:N].clone(), pos_in=pa[:N].clone(),
+                              idx_attn=torch.empty(max(min(N, item["m_attn"]), 1), dtype=torch.int32, device="cuda"),
+                              idx_ffn=torch.empty(max(min(N, item["m_ffn"]), 1), dtype=torch.int32, device="cuda"))
+                self.ctx.spts_layer_prefill(xa, pa, N, w, cfg, self.caches[li].struct if self.caches else None, self.s,
+                                            tr["idx_attn"] if tr else None, tr["idx_ffn"] if tr else None)
                 if tr is not None:
-                    tr["map_new2old"] = self.new2old[:n_next].clone()
-                xa, xb = xb, xa
-                pa, pb = pb, pa
-                N = n_next
-            if tr is not None:
-                self.trace.append(tr)
-        return xa[:N], pa[:N], N
+                    tr["x_out"] = xa[:N].clone()
+                    tr["s_mha"] = self.s[:N].clone()
+                if cfg.skip and item.get("N_next") is not None:
+                    n_next = min(N, item["N_next"])
+                    self.ctx.spts_msdp_compact(xa, pa, self.s, N, n_next, self.protect_last, xb, pb, self.new2old, None)
+                    if tr is not None:
+                        tr["map_new2old"] = self.new2old[:n_next].clone()
+                    xa, xb = xb, xa
+                    pa, pb = pb, pa
+                    N = n_next
+                if tr is not None:
+                    self.trace.append(tr)
+            return xa[:N], pa[:N], N
 
 
 class BatchedStackRunner:
@@ -493,22 +502,23 @@ class BatchedStackRunner:
 
     def run(self, x0, pos0):
         """x0 [sum N0_b, D], pos0 [sum N0_b]: the sequences back to back.  Returns (x, pos, offsets)."""
-        xa, xb, pa, pb = self.xa, self.xb, self.posa, self.posb
-        offs = [0]
-        for p in self.plans:
-            offs.append(offs[-1] + p[0]["N"])
-        xa[:offs[-1]].copy_(x0)
-        pa[:offs[-1]].copy_(pos0)
-        for li, w in enumerate(self.layers):
-            items = [p[li] for p in self.plans]
-            skip_l = int(items[0].get("skip", 1))
-            assert all(int(it.get("skip", 1)) == skip_l for it in items), "a layer is dense or skipped for the whole batch"
-            self.ctx.spts_layer_prefill_batched(xa, pa, offs, w, self.probe_len, [it["m_attn"] for it in items],
-                                                [it["m_ffn"] for it in items], self.protect_last, None, self.s, skip=skip_l)
-            if skip_l and items[0].get("N_next") is not None:
-                offs = self.ctx.spts_msdp_compact_batched(xa, pa, self.s, offs, [it["N_next"] for it in items],
-                                                          self.protect_last, xb, pb, self.new2old)
-                xa, xb = xb, xa
-                pa, pb = pb, pa
-        return xa[:offs[-1]], pa[:offs[-1]], offs
+        with _on_stream_of(self.ctx):
+            xa, xb, pa, pb = self.xa, self.xb, self.posa, self.posb
+            offs = [0]
+            for p in self.plans:
+                offs.append(offs[-1] + p[0]["N"])
+            xa[:offs[-1]].copy_(x0)
+            pa[:offs[-1]].copy_(pos0)
+            for li, w in enumerate(self.layers):
+                items = [p[li] for p in self.plans]
+                skip_l = int(items[0].get("skip", 1))
+                assert all(int(it.get("skip", 1)) == skip_l for it in items), "a layer is dense or skipped for the whole batch"
+                self.ctx.spts_layer_prefill_batched(xa, pa, offs, w, self.probe_len, [it["m_attn"] for it in items],
+                                                    [it["m_ffn"] for it in items], self.protect_last, None, self.s, skip=skip_l)
+                if skip_l and items[0].get("N_next") is not None:
+                    offs = self.ctx.spts_msdp_compact_batched(xa, pa, self.s, offs, [it["N_next"] for it in items],
+                                                              self.protect_last, xb, pb, self.new2old)
+                    xa, xb = xb, xa
+                    pa, pb = pb, pa
+            return xa[:offs[-1]], pa[:offs[-1]], offs
 
