@@ -14,10 +14,10 @@ SHAPE = synth.ModelShape(D=256, H=4, Hkv=2, d=64, Dff=688, dtype="bf16")
 
 def contexts(torch):  # noqa: F811
     """On the default stream, then on one of its own."""
-    yield runtime.make_context(SHAPE, 512, 16, 16, SHAPE.Dff)
+    yield runtime.make_context(SHAPE, 1024, 16, 16, SHAPE.Dff)
     st = torch.cuda.Stream()
     with torch.cuda.stream(st):
-        ctx = binding.Context(SHAPE, 512, 16, 16, SHAPE.Dff, stream=st)
+        ctx = binding.Context(SHAPE, 1024, 16, 16, SHAPE.Dff, stream=st)
     torch.cuda.synchronize()
     yield ctx
 
