@@ -6,6 +6,7 @@ import pytest
 
 from oracle import fp4_oracle as fp4
 from paper_2601_13155_amd import binding, runtime, synth
+from tests import test_gpu_q4 as q4_tests
 from tests.test_gpu_q4 import HALF, SUM, append, ctx_for, layer_for, make_pairs, rounded, torch  # noqa: F401  (torch: the fixture)
 
 pytestmark = pytest.mark.gpu
@@ -193,3 +194,111 @@ def test_generate_on_a_side_stream(torch, side, nseq, history):  # noqa: F811
         res.append([t.cpu() for t in got] + [torch.tensor(c.counts) for c in run.caches])
     assert all(torch.equal(a, b) for a, b in zip(*res)), [torch.equal(a, b) for a, b in zip(*res)]
     assert (res[0][0] >= 0).all()
+
+
+# --------------------------------------------------------------------------------------------- the layer's stored pairs
+def pairs_of_every_kind(rng, n, dtype):
+    """n values (a multiple of 32) whose blocks have sizes of their own over 2^-20 .. 2^20: random ones, ties between codes, zeros, one value alone, the edges of an
+    exponent."""
+    out = np.empty((n // 32, 32))
+    for i in range(n // 32):
+        kind, a = i % 6, rng.standard_normal(32)
+        if kind == 1:
+            a = np.resize([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0], 32) * rng.choice([-1.0, 1.0], 32)
+        elif kind == 2:
+            a = np.where(np.arange(32) == rng.integers(32), 1.0, 0.0)
+        elif kind == 3:
+            a = a / np.abs(a).max() * (6.0 if i % 4 else 6.03125)      # the largest that an exponent holds, and the next bf16
+        elif kind == 4 and i % 12 == 4:
+            a = np.zeros(32)
+        out[i] = a * 2.0 ** rng.integers(-20, 21)
+    return rounded(out.reshape(-1), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Hkv,d", [(5, 32), (3, 64), (1, 64), (2, 128), (8, 128)])
+@pytest.mark.parametrize("nseq", [1, 3, 16])
+def test_the_layer_stores_the_nearest_4_bit_values(torch, dtype, Hkv, d, nseq):  # noqa: F811
+    """States of +-1 have a norm of exactly 1 (an epsilon of 2^-100 vanishes beside it), so a projection row with a single 1 gives the gain of its column with the state's sign, exactly;
+    at position 0 the rotation is the identity.  Keys and values of the new pair are then known to the bit, and so is what 4 bits make of them."""
+    n = Hkv * d
+    D = 2 * n
+    ctx, shape = ctx_for(dtype, H=Hkv, Hkv=Hkv, d=d, D=D, Dff=1024, rms_eps=2.0 ** -100)
+    rng = np.random.default_rng(n + nseq)
+    gains = np.concatenate([pairs_of_every_kind(rng, n, dtype), pairs_of_every_kind(rng, n, dtype)])
+    eye = np.eye(D, dtype=np.float32)
+    w = {"Wq": np.zeros((n, D)), "Wk": eye[:n], "Wv": eye[n:], "Wo": np.zeros((D, n)), "Wgate": np.zeros((1024, D)), "Wup": np.zeros((1024, D)), "Wdown": np.zeros((D, 1024))}
+    t = {k: runtime.to_device(np.asarray(a, dtype=np.float32), dtype) for k, a in w.items()}
+    t["gamma1"], t["gamma2"] = runtime.to_device(gains.astype(np.float32), dtype), runtime.to_device(np.ones(D, dtype=np.float32), dtype)
+    q4 = runtime.pack_layer_q4(ctx, binding.layer_weights(t))
+    held = [int(c) for c in rng.integers(0, 40, nseq)]
+    caches = runtime.KV4Batch(shape, [c + 2 for c in held])
+    append(torch, ctx, caches, [make_pairs(rng, c, Hkv, d, dtype) + (np.arange(c),) for c in held], dtype)
+    before = [caches.host(ctx, shape, b) for b in range(nseq)]
+    for _ in range(2):
+        sign = rng.choice([-1.0, 1.0], (nseq, D)).astype(np.float32)
+        x = runtime.to_device(sign.copy(), dtype)
+        ctx.spts_decode_layer_q4(x, [0] * nseq, q4, caches.structs)
+        torch.cuda.synchronize()
+        assert np.array_equal(runtime.to_host(x), sign)                # nothing is added to the state
+        for b in range(nseq):
+            k, v, p = caches.host(ctx, shape, b)
+            assert len(k) == len(before[b][0]) + 1 and p[-1] == 0
+            assert np.array_equal(k[:-1], before[b][0]) and np.array_equal(v[:-1], before[b][1])
+            new = gains * sign[b].astype(np.float64)
+            assert np.array_equal(k[-1], fp4.fp4_round(new[:n].reshape(Hkv, d))), b
+            assert np.array_equal(v[-1], fp4.fp4_round(new[n:].reshape(Hkv, d))), b
+            before[b] = (k, v, p)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nseq,D", [(1, 4096), (2, 2568), (3, 2568), (4, 2568), (3, 4096), (4, 4096), (3, 4616), (4, 4104)])
+def test_decode_layer_of_several_slabs(torch, monkeypatch, dtype, nseq, D):  # noqa: F811
+    """The layer in lockstep with the oracle where the norm of one to four vectors inside the products goes over several slabs of 512, whole and partial
+    last ones, up to the most that LDS is kept for, and just beyond."""
+    monkeypatch.setattr(q4_tests, "LAYERS", [(D, 4, 2, 32, 64)])
+    q4_tests.test_decode_layer_lockstep(torch, dtype, nseq, 0)
+
+
+def test_append_and_read_of_more_rows_than_a_launch(torch):  # noqa: F811
+    """2^24 + 1000 rows of two sequences: rows on both sides of where the second launch begins, the ends, and some between."""
+    Hkv, d, n = 1, 32, (1 << 24) + 1000
+    ctx, shape = ctx_for("bf16", H=1, Hkv=Hkv, d=d)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    lens = [n - 700, 700]
+    k = torch.randn((n, Hkv, d), generator=g, device="cuda").to(torch.bfloat16)
+    v = torch.randn((n, Hkv, d), generator=g, device="cuda").to(torch.bfloat16)
+    pos = torch.arange(n, dtype=torch.int32, device="cuda") * 3
+    caches = runtime.KV4Batch(shape, lens)
+    for t in caches.tensors:
+        for x in t[:4]:
+            x.fill_(0xFF)
+        t[4].fill_(-1)
+    offs = [0, lens[0], n]
+    ctx.spts_kv4_append(k, v, pos, offs, caches.structs)
+    torch.cuda.synchronize()
+    assert caches.counts == lens
+    assert torch.equal(caches.tensors[0][4][:lens[0]], pos[:lens[0]]) and torch.equal(caches.tensors[1][4][:700], pos[lens[0]:])
+    kb, vb = torch.empty_like(k), torch.empty_like(v)
+    ctx.spts_kv4_read(caches.structs, offs, kb, vb)
+    torch.cuda.synchronize()
+    rows = np.unique(np.concatenate([np.arange(64), np.arange((1 << 24) - 64, n), np.random.default_rng(3).integers(0, n, 2000)]))
+    at = torch.from_numpy(rows).cuda()
+    for src, back in ((k, kb), (v, vb)):
+        assert np.array_equal(runtime.to_host(back[at]), fp4.fp4_round(runtime.to_host(src[at])))
+    # the same bytes as from calls that stay below a launch's rows
+    again = runtime.KV4Batch(shape, lens)
+    half = 1 << 23
+    for lo in range(0, n, half):
+        hi = min(lo + half, n)
+        cut = [0, max(0, min(hi, lens[0]) - lo), hi - lo]
+        ctx.spts_kv4_append(k[lo:hi], v[lo:hi], pos[lo:hi], cut, again.structs)
+    torch.cuda.synchronize()
+    k2, v2 = torch.empty_like(k), torch.empty_like(v)
+    for lo in range(0, lens[0], half):
+        c = min(half, lens[0] - lo)
+        ctx.spts_kv4_read([again.structs[0]], [0, c], k2[lo:lo + c], v2[lo:lo + c], first=[lo])
+    ctx.spts_kv4_read([again.structs[1]], [0, 700], k2[lens[0]:], v2[lens[0]:])
+    torch.cuda.synchronize()
+    assert torch.equal(k2, kb) and torch.equal(v2, vb)
