@@ -1485,9 +1485,9 @@ int spts_decode_layer_q4(spts_ctx* c, void* x, const int32_t* pos, int32_t batch
     SPTS_TRY(kv4_distinct(caches, batch));
     for (int b = 0; b < batch; ++b)
         if (pos[b] < 0 || kb.count[b] >= kb.cap[b]) return SPTS_EINVAL;
-    // the projections' fp32 sums, in the FFN's hidden buffer (free until gate/up)
-    if ((size_t)batch * (QD + 2 * KV) * sizeof(float) > c->off.misc - c->off.big) return SPTS_EWORKSPACE;
-    float* q32 = c->p<float>(c->off.big);
+    // the projections' fp32 sums lie where the attention leaves its shares after they are read: 1 KB at least for each of the H * d query
+    // dimensions, of which sixteen sequences' sums are at most 192 bytes (Hkv <= H)
+    float* q32 = c->p<float>(c->off.tmp32);
     float* k32 = q32 + batch * QD;
     float* v32 = k32 + batch * KV;
     void* xn = c->p<void>(c->off.xn);

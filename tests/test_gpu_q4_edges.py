@@ -302,3 +302,11 @@ def test_append_and_read_of_more_rows_than_a_launch(torch):  # noqa: F811
     ctx.spts_kv4_read([again.structs[1]], [0, 700], k2[lens[0]:], v2[lens[0]:])
     torch.cuda.synchronize()
     assert torch.equal(k2, kb) and torch.equal(v2, vb)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads,Hkv,d", [(16, 8, 64), (9, 9, 128)])
+def test_decode_layer_with_more_head_dimensions_than_hidden_ones(torch, monkeypatch, dtype, heads, Hkv, d):  # noqa: F811
+    """Sixteen sequences' projections are larger than everything that the feed-forward block of this model needs."""
+    monkeypatch.setattr(q4_tests, "LAYERS", [(64, heads, Hkv, d, 8)])
+    q4_tests.test_decode_layer_lockstep(torch, dtype, 16, 0)
