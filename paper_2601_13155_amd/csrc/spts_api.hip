@@ -750,8 +750,9 @@ int spts_decode_layer_batched(spts_ctx* c, void* x, const int32_t* pos, int32_t 
     void* hbuf = c->p<void>(c->off.big);
     float* part = c->p<float>(c->off.tmp32);
     const size_t part_floats = (c->off.qp - c->off.tmp32) / sizeof(float);
-    // the projections leave fp32 sums (in the FFN's hidden buffer, free until gate/up); the rotary kernel rounds once
-    float* q32 = c->p<float>(c->off.big);
+    // the projections leave fp32 sums (where the attention leaves its partial results after they are read: at least 1 KB for each of the H * d query
+    // dimensions, of which sixteen sequences' sums are at most 192 bytes); the rotary kernel rounds once
+    float* q32 = part;
     float* k32 = q32 + (size_t)batch * QD;
     float* v32 = k32 + (size_t)batch * KV;
     GemvArgs qkv{}; qkv.mode = GEMV_F32; qkv.x = xn; qkv.K = m.D;
