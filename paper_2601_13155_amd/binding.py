@@ -70,11 +70,16 @@ class spts_logits_rules(C.Structure):
                 ("mask_stride", C.c_int64)]
 
 
+def _host(values, typ, least: int, what: str):
+    """A host array of `typ`, of `least` entries at least: the C calls read that many."""
+    if len(values) < least:
+        raise ValueError(f"{what}: {least} values needed, got {len(values)}")
+    return values if isinstance(values, C.Array) else (typ * max(len(values), 1))(*[int(v) for v in values])
+
+
 def host_i64(values):
     """A host int64 array as the C calls take it (to be built once and passed to several calls); such an array is returned as it is."""
-    if isinstance(values, C.Array):
-        return values
-    return (C.c_int64 * max(len(values), 1))(*[int(v) for v in values])
+    return _host(values, C.c_int64, 0, "")
 
 
 def kv4_array(caches):
@@ -369,7 +374,7 @@ class Context:
     def spts_kv4_append(self, k, v, pos, offsets, caches):
         """offsets [batch+1]: host integers or binding.host_i64; caches: a list of spts_kv4 (count fields updated in place)
         or a ctypes array of them."""
-        off = host_i64(offsets)
+        off = _host(offsets, C.c_int64, len(caches) + 1, "offsets")
         arr, copied = kv4_array(caches)
         _check(load().spts_kv4_append(self.handle, _ptr(k), _ptr(v), _ptr(pos), off, len(caches), arr), "spts_kv4_append")
         if copied:
@@ -378,8 +383,9 @@ class Context:
 
     def spts_kv4_read(self, caches, offsets, k_out, v_out, first=None):
         arr, _ = kv4_array(caches)
-        _check(load().spts_kv4_read(self.handle, arr, None if first is None else host_i64(first), host_i64(offsets), len(caches),
-                                    _ptr(k_out), _ptr(v_out)), "spts_kv4_read")
+        at = None if first is None else _host(first, C.c_int64, len(caches), "first")
+        off = _host(offsets, C.c_int64, len(caches) + 1, "offsets")
+        _check(load().spts_kv4_read(self.handle, arr, at, off, len(caches), _ptr(k_out), _ptr(v_out)), "spts_kv4_read")
 
     def spts_kv4_attn(self, q, caches, out):
         arr, _ = kv4_array(caches)
@@ -388,7 +394,7 @@ class Context:
     def spts_decode_layer_q4(self, x, pos, w: spts_layer_q4, caches):
         """x [batch, D] device tensor; pos: host integers; caches as in spts_kv4_append."""
         arr, copied = kv4_array(caches)
-        pa = pos if isinstance(pos, C.Array) else (C.c_int32 * max(len(pos), 1))(*[int(v) for v in pos])
+        pa = _host(pos, C.c_int32, len(caches), "pos")
         _check(load().spts_decode_layer_q4(self.handle, _ptr(x), pa, len(caches), C.byref(w), arr), "spts_decode_layer_q4")
         if copied:
             for dst, src in zip(caches, arr):

@@ -234,10 +234,13 @@ class BatchedDecodeRunner:
 
 # ------------------------------------------------------------------------------------------- decode in 4 bits
 class Q4Matrix:
-    """A matrix [rows, K] packed into 4 bits (spts_q4_pack); W: device tensor of the context's element type."""
+    """A matrix [rows, K] packed into 4 bits (spts_q4_pack); W: device tensor of the context's element type (ValueError otherwise)."""
 
     def __init__(self, ctx: binding.Context, W):
         torch = _torch()
+        want = torch.bfloat16 if ctx.shape.dtype == "bf16" else torch.float32
+        if W.dim() != 2 or W.dtype != want or not W.is_cuda:
+            raise ValueError(f"a device matrix of {want}, not {W.dtype} {list(W.shape)} on {W.device}")
         rows, K = (int(n) for n in W.shape)
         cb, sb = binding.spts_q4_bytes(rows, K)
         self.codes = torch.empty(cb, dtype=torch.uint8, device=W.device)
@@ -381,6 +384,12 @@ class Q4DecodeRunner:
         if (bias is not None and bias.shape[-1] < V) or (mask is not None and mask.shape[-1] < (V + 31) // 32):
             raise ValueError(f"bias and mask: rows of {V} words")
         tdt = torch.bfloat16 if shape.dtype == "bf16" else torch.float32
+        if table.dtype != tdt or not table.is_contiguous():
+            raise ValueError(f"table: a contiguous tensor of {tdt}")
+        if gamma_f is not None and (gamma_f.dtype != tdt or not gamma_f.is_contiguous() or gamma_f.numel() != shape.D):
+            raise ValueError(f"gamma_f: {shape.D} values of {tdt}")
+        if any(t is not None and t.device != table.device for t in (*self.rules._keepalive, gamma_f)):
+            raise ValueError(f"history, bias, mask and gamma_f: on {table.device} as the table is")
         self.x = torch.zeros((self.batch, shape.D), dtype=tdt, device="cuda")
         self.x_next, self.xn = torch.zeros_like(self.x), torch.zeros_like(self.x)
         self.tokens = torch.zeros(self.batch, dtype=torch.int32, device="cuda")
@@ -402,7 +411,12 @@ class Q4DecodeRunner:
 
     def generate(self, pos0: List[int], steps: int, tokens_out=None):
         """steps decode steps from self.x at positions pos0; tokens_out [batch, steps] int32 device.  With a history in the
-        rules every token joins it: ValueError, before any step, if its rows or the caches have no room for that many."""
+        rules every token joins it: ValueError, before any step, if its rows, the caches or tokens_out have no room for that many, or
+        positions are missing."""
+        if len(pos0) != self.batch:
+            raise ValueError(f"pos0: one position for each of {self.batch} sequences, got {len(pos0)}")
+        if tokens_out is not None and (tokens_out.dim() != 2 or tokens_out.shape[0] != self.batch or tokens_out.shape[1] < steps):
+            raise ValueError(f"tokens_out: [{self.batch}, {steps}]")
         hist, lens = self.rules._keepalive[0], self.rules.history_len
         if hist is not None and any(n + steps > hist.shape[1] for n in lens):
             raise ValueError(f"the history's rows of {hist.shape[1]} ids have no room for {steps} more")
