@@ -13,8 +13,9 @@ __device__ inline int64_t key_scale_at(int g, int64_t cap, int64_t key, int blk,
 __device__ inline int64_t value_at(int g, int64_t cap, int64_t key, int n, int d) { return ((((int64_t)g * cap + key) >> 3) * 16 + n) * (d / 4) + (key & 7) * (d / 32); }
 __device__ inline int64_t value_scale_at(int g, int64_t cap, int64_t key, int blk, int d) { return ((((int64_t)g * cap + key) >> 3) * (d / 32) + blk) * 8 + (key & 7); }
 
-// A kernel's view of up to NB caches.  Arguments beyond some 100 bytes cost every launch 0.6 us, beyond 800 another 0.5 (measured with empty kernels:
-// 2.65 / 3.3 / 3.8 us a launch), so a single sequence has a descriptor of its own and sixteen fit 800 bytes.
+// A kernel's view of up to NB caches: one, or sixteen (the launches' arguments are then 752 bytes for the attention, 860 for reading, 868 for appending, 952 for the rotation with the
+// append; 84 to 120 for one).  What it costs is finding the sequence and its pointers, not the arguments' bytes (an empty kernel takes 2.4 us with 24 bytes and with 1288): one sequence
+// by the descriptor of one / of sixteen, 517 keys 6.3 / 7.0 us, 13107 keys (two launches) 9.6 / 10.7, a pair appended and read back 9.0 / 10.3.
 template <int NB> struct Kv4Rows {
     char *k[NB], *v[NB];
     uint8_t *ks[NB], *vs[NB];
