@@ -100,7 +100,10 @@ __global__ void __launch_bounds__(LT) process_logits_kernel(const float* in, int
 #pragma unroll
         for (int j = 0; j < LW; ++j) x[j] = x[j] + (tid + j * LT < n ? bias[tid + j * LT] : 0.f);
     }
-    uint32_t word[LW];   // (all ones without a mask: a condition `!mask || bit` came out wrong in the select below when the words beside it diverged)
+    // Words of a mask that is not there are all ones, so that whether a word is allowed is one divergent condition.  Written as `!mask || bit`, a uniform branch around a divergent one,
+    // it goes wrong in this compiler (AMD clang 22.0.0git, roc-7.2.0 26014): where both meet, the result of `allowed ? x : -inf` is copied on the uniform branch's way only, and
+    // allowed words of a given mask get -inf.  The LLVM IR is right, the copy is missing in the machine code; no other kernel here selects a value by such a condition.
+    uint32_t word[LW];
 #pragma unroll
     for (int j = 0; j < LW; ++j) word[j] = ~0u;
     if (r.mask) {
