@@ -404,6 +404,10 @@ class Context:
         _check(load().spts_rmsnorm(self.handle, _ptr(x), _ptr(gamma), batch, _ptr(xn)), "spts_rmsnorm")
 
     def spts_process_logits(self, logits, V: int, batch: int, rules: spts_logits_rules, logits_out, token_out=None, table=None, x_next=None):
+        """rules: with what a runtime.LogitsRules knows of its arrays, ValueError where they are shorter than the call needs."""
+        for name, have, need in zip(("sequences", "words of bias", "words of mask"), getattr(rules, "_room", ()), (batch, V, (V + 31) // 32)):
+            if have is not None and have < need:
+                raise ValueError(f"rules for {have} {name}, {need} needed")
         _check(load().spts_process_logits(self.handle, _ptr(logits), V, batch, C.byref(rules), _ptr(logits_out), _ptr(token_out),
                                           _ptr(table), _ptr(x_next)), "spts_process_logits")
 

@@ -246,6 +246,7 @@ class Q4Matrix:
         self.codes = torch.empty(cb, dtype=torch.uint8, device=W.device)
         self.scales = torch.empty(sb, dtype=torch.uint8, device=W.device)
         self.struct = binding.spts_q4(self.codes.data_ptr(), self.scales.data_ptr(), rows, K)
+        self.struct._keepalive = (self.codes, self.scales)
         with _on_stream_of(ctx):
             ctx.spts_q4_pack(W.contiguous(), self.struct)
 
@@ -279,6 +280,7 @@ class KV4Batch:
                 at += (n + 255) // 256 * 256
             self._parts.append(parts)
         self._buffer = torch.empty(at, dtype=torch.uint8, device="cuda")
+        self.structs._keepalive = self._buffer
         base = self._buffer.data_ptr()
         for s, parts in zip(self.structs, self._parts):
             s.k, s.v, s.k_scale, s.v_scale, s.pos = (base + p for p, _ in parts)
@@ -356,6 +358,9 @@ class LogitsRules:
             s.bias, s.bias_stride = rows(bias)
         if mask is not None:
             s.mask, s.mask_stride = rows(mask)
+        s._keepalive = self._keepalive
+        each = history is not None or s.bias_stride or s.mask_stride or any(v is not None for v in (self.repetition, self.frequency, self.presence))
+        s._room = (batch if each else None, None if bias is None else bias.shape[-1], None if mask is None else mask.shape[-1])
 
 
 class Q4DecodeRunner:

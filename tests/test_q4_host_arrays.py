@@ -1,7 +1,9 @@
 """What the Python side of the 4-bit decode refuses because the C side could not see it: host arrays that are too short, tensors of another type
 (no GPU: nothing is launched)."""
 import ctypes as C
+import gc
 import types
+import weakref
 
 import pytest
 import torch
@@ -52,3 +54,46 @@ def test_runner_of_another_type(monkeypatch):
                 lambda: run.generate([0, 0], 3, torch.zeros(6, dtype=torch.int32))):
         with pytest.raises(ValueError):
             bad()
+
+
+def test_structs_keep_their_tensors():
+    """What a call is given is the struct; the tensors that it points into live as long."""
+    hist, bias, mask = torch.zeros((2, 4), dtype=torch.int32), torch.zeros(64), torch.zeros(2, dtype=torch.int32)
+    s = runtime.LogitsRules(2, history=hist, history_len=[1, 2], bias=bias, mask=mask, repetition=[1.5, 2.5]).struct
+    refs = [weakref.ref(t) for t in (hist, bias, mask)]
+    del hist, bias, mask
+    gc.collect()
+    assert all(r() is not None for r in refs) and list(s.repetition[:2]) == [1.5, 2.5] and list(s.history_len[:2]) == [1, 2]
+
+
+def test_caches_and_matrices_keep_their_buffers(monkeypatch):
+    """The same of packed matrices and caches (host tensors in the place of device ones, nothing is launched)."""
+    import contextlib
+    monkeypatch.setattr(torch, "empty", lambda *a, device=None, _empty=torch.empty, **kw: _empty(*a, **kw))
+    monkeypatch.setattr(runtime, "_on_stream_of", lambda ctx: contextlib.nullcontext())
+    shape = synth.ModelShape(D=64, H=4, Hkv=2, d=32, Dff=64, dtype="f32")
+    structs = runtime.KV4Batch(shape, [9, 1]).structs
+    gc.collect()
+    buf = structs._keepalive
+    assert structs[0].k == buf.data_ptr() and structs[1].pos + 4 * 8 <= buf.data_ptr() + buf.numel()
+
+    class Matrix(torch.Tensor):
+        is_cuda = True
+
+    me = types.SimpleNamespace(shape=shape, spts_q4_pack=lambda W, s: None)
+    s = runtime.Q4Matrix(me, torch.zeros((16, 64)).as_subclass(Matrix)).struct
+    gc.collect()
+    assert [t.data_ptr() for t in s._keepalive] == [s.codes, s.scales]
+
+
+def test_rules_shorter_than_the_call(ctx):  # noqa: F811
+    me = types.SimpleNamespace(handle=ctx())
+    call = lambda V, n, **kw: binding.Context.spts_process_logits(me, A, V, n, runtime.LogitsRules(2, **kw).struct, None)  # noqa: E731
+    for V, n, kw in ((64, 3, dict(repetition=[1.0, 1.0])), (65, 2, dict(bias=torch.zeros(64))), (65, 1, dict(bias=torch.zeros((2, 64)))), (64, 3, dict(bias=torch.zeros((2, 64)))),
+                     (64, 3, dict(history=torch.zeros((2, 4), dtype=torch.int32), history_len=[1, 2])),
+                     (65, 2, dict(mask=torch.zeros(2, dtype=torch.int32)))):
+        with pytest.raises(ValueError):
+            call(V, n, **kw)
+    for V, n, kw in ((64, 2, dict(bias=torch.zeros(64), mask=torch.zeros(2, dtype=torch.int32))), (64, 1, {}), (64, 16, {}), (64, 5, dict(bias=torch.zeros(64))), (33, 2, dict(bias=torch.zeros((2, 80))))):
+        with pytest.raises(binding.SptsError):           # these come to the library, which refuses the missing result
+            call(V, n, **kw)
