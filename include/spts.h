@@ -296,7 +296,7 @@ int spts_msdp_compact_batched(spts_ctx *ctx, const void *x_in, const int32_t *po
  * row of a matrix, or along the head dimension of a cached key or value, share the smallest power of two 2^e,
  * -126 <= e <= 125, with max|v| <= 6 * 2^e; a value is stored as the nearest of +-{0, 1/2, 1, 3/2, 2, 3, 4, 6} * 2^e, ties to
  * the even code, larger magnitudes (above 6 * 2^125) as 6 * 2^125.  A block that holds a NaN reads as NaN.  17/32 of a
- * byte per value; a stored value is exact in bf16 and fp32, so products with it are those of the rounded matrix. */
+ * byte per stored value (of a matrix as stored: rows up to a multiple of 16, K up to one of 512, which spts_q4_bytes counts); a stored value is exact in bf16 and fp32, so products with it are those of the rounded matrix. */
 
 /* One matrix [rows, K] (y = x * W^T, as all matrices here) in 4 bits: two caller-owned device buffers of the sizes that
  * spts_q4_bytes gives, in a layout of this library (strips of 16 rows by slabs of 512 columns).  K % 8 == 0. */

@@ -601,8 +601,8 @@ static hipError_t launch_kv4_attn_p(const T* q, const Kv4Batch& kb, int64_t per,
     if (e != hipSuccess) return e;
     kv4_attn_kernel<T, D, NW, NB, PAIRED><<<dim3((unsigned)splits, (unsigned)Hkv), dim3(NW * 64), lds, s>>>(q, c, H, Hkv, 1.4426950408889634f / sqrtf((float)D), part, out);
     if (splits > kb.n) {
-        // us by four workgroups a head / in one round trip: 16 sequences of up to 3000 / 13107 keys of 28 heads, 12 shares, 13.4 / 20.4 and 10.7 / 17.7; one sequence of 2000 keys, 16
-        // shares, 7.5 and 7.5; many shares by four workgroups a head / by one: 5000 / 13107 / 131072 keys of 32 heads, 40 or 64 shares, 8.2 / 9.2 / 27.4 and 9.2 / 10.9 / 28.3
+        // us by four workgroups a head / in one round trip: 16 sequences of up to 3000 / 13107 keys of 28 heads, 12 shares, 13.5 / 21.0 and 10.9 / 18.4; one sequence of 2000 keys, 16
+        // shares, 7.5 and 7.5; many shares, 5000 / 13107 / 131072 keys of 32 heads, 40 or 64 shares, by four workgroups a head 8.3 / 9.5 / 27.9, by one a head 1.0 / 1.7 / 0.9 more
         int most = 1;
         for (int b = 0; b < kb.n; ++b) most = std::max(most, ends.end[b] - (b > 0 ? ends.end[b - 1] : 0));
         if (most > KV4_FEW) kv4_merge_kernel<T, D, NB><<<dim3((unsigned)H, (unsigned)kb.n, D / 32), dim3(512), 0, s>>>(part, ends, H, Hkv, out);
@@ -634,10 +634,10 @@ static hipError_t launch_kv4_attn_t(const T* q, const Kv4Batch& kb, int H, int H
         return kb.n == 1 ? launch_kv4_attn_n<T, D, WIDE, 1>(q, kb, SHORT, H, Hkv, part, out, s)
                          : launch_kv4_attn_n<T, D, WIDE, DECODE_MAX_BATCH>(q, kb, SHORT, H, Hkv, part, out, s);
     }
-    // Shares of equal length over all sequences, none below 128 keys, the shortest with which no CU gets a third workgroup: 131072 keys of 8 heads in 64 shares
-    // 27.9 us, in 60 30.4, in 120 32.4; 16 sequences of 1048 .. 13107 keys, 4 heads, 480 / 536 / 960 workgroups 18.7 / 21.9 / 21.0 us.  Sequences and heads that are many on their own
-    // have room for four shares a sequence nevertheless, else the longest one's workgroups stay behind: the same sequences, 32 heads, 1 / 2 / 4 / 8 shares a sequence on average 116.8 /
-    // 95.7 / 86.8 / 85.1 us; 16 of 120 .. 1500 keys in fp32, 32 heads of 64, 15.2 / 15.4 / 16.0 / 19.2.
+    // Shares of equal length over all sequences, none below 128 keys, the shortest with which no CU gets a third workgroup: 131072 keys of 8 heads in 64 / 60 /
+    // 70 / 128 shares 27.9 / 28.9 / 35.0 / 29.7 us; 16 sequences of 1048 .. 13107 keys, 4 heads, room for 480 / 512 / 560 / 1024 workgroups 18.3 / 18.4 / 21.4 / 22.8 us.  Sequences and heads that are many on their own
+    // have room for four shares a sequence nevertheless, else the longest one's workgroups stay behind: the same sequences, 32 heads, 1 / 2 / 4 / 8 shares a sequence on average 118.5 /
+    // 96.7 / 87.9 / 85.9 us; 16 of 120 .. 1500 keys in fp32, 32 heads of 64, 15.1 / 15.4 / 15.9 / 19.2.
     const int64_t most = std::max<int64_t>(KV4_WORKGROUPS, 4 * (int64_t)kb.n * Hkv);
     int64_t per = (total * Hkv + most - 1) / most;
     per = per < 128 ? 128 : per > (1 << 30) ? (1 << 30) : (per + 31) / 32 * 32;

@@ -4,7 +4,8 @@
 
 namespace spts {
 
-// One thread per piece and slab: eight values of sixteen blocks of one row; the other values of a block are 16, 32 and 48 lanes away.
+// One thread per piece and slab: eight values of sixteen blocks of one row; the other values of a block are 16, 32 and 48 lanes away.  Done once for a matrix: 28672 x 4096 in bf16
+// 87.9 us, 3.4 TB/s read and written (a copy's rate would be 60.0; a wavefront's load is 16 rows of 64 bytes), 4096 x 4096 15.8 (8.6).
 template <typename T>
 __global__ void __launch_bounds__(256) q4_pack_kernel(const T* __restrict__ W, int64_t rows, int64_t K, int64_t slabs, int64_t pieces,
                                                       u32x4* __restrict__ codes, uint32_t* __restrict__ scales) {
