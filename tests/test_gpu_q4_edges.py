@@ -310,3 +310,35 @@ def test_decode_layer_with_more_head_dimensions_than_hidden_ones(torch, monkeypa
     """Sixteen sequences' projections are larger than everything that the feed-forward block of this model needs."""
     monkeypatch.setattr(q4_tests, "LAYERS", [(64, heads, Hkv, d, 8)])
     q4_tests.test_decode_layer_lockstep(torch, dtype, 16, 0)
+
+
+@pytest.mark.parametrize("own_stream", [False, True])
+def test_generate_captured_and_replayed(torch, side, own_stream):  # noqa: F811
+    """One step of generate with a history under a graph, captured on the context's stream or on another that the context's joins; replayed between eager runs of another
+    runner over the same context, after which every buffer is what the eager step leaves."""
+    want, (run, hist, x0, lens) = [], make_runner(torch, side, 3, True)
+    eager, hist_e, _, _ = make_runner(torch, side, 3, True)
+    toks, toks_e = (torch.full((3, 1), -5, dtype=torch.int32, device="cuda") for _ in range(2))
+    eager.x.copy_(x0)
+    eager.generate(lens, 1, toks_e)                     # the first use of every kernel, and the result
+    want = [t.clone() for t in (toks_e, eager.x, eager.logits, hist_e)]
+    start = hist.clone()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side.stream if own_stream else torch.cuda.Stream()):
+        run.x.copy_(x0)
+        run.generate(lens, 1, toks)
+    for t in range(4):
+        for b in (run.x, run.logits, run.x_next, toks):
+            b.zero_()
+        hist.copy_(start)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((toks, run.x, run.logits, hist), want)), t
+        eager.generate([n + 1 + t for n in lens], 1, toks_e)
+        torch.cuda.synchronize()
+    assert [c.counts for c in run.caches] == [[n + 1 for n in lens]] * 2
+    for a, b in zip(run.caches, eager.caches):
+        for s, n in enumerate(lens):
+            assert all(np.array_equal(p, q[:n + 1]) for p, q in zip(a.host(side, side.shape, s), b.host(side, side.shape, s)))
