@@ -380,6 +380,70 @@ typedef struct {
 int spts_process_logits(spts_ctx *ctx, const float *logits, int32_t V, int32_t batch, const spts_logits_rules *rules,
                         float *logits_out, int32_t *token_out, const void *table, void *x_next);
 
+/* ---- caches in pages --------------------------------------------------------------------------
+ * Follow-up turns over caches that exist: the rows of many sequences share one pool of pages for a layer, a chunk of new tokens
+ * (one when decoding, a turn after a prompt) attends to the rows before it and to its own, and a cache that has outgrown its
+ * budget is cut down to the rows that got the most attention (the choice that Eq. (mha_importance) makes in a prefill, from
+ * weights that were added up while serving). */
+
+/* One layer's pool: k, v [pages, Hkv, page, d] of the context's element type (device, 16-byte aligned), post-rotary keys; page: rows of
+ * a page, 16, 32, 64, 128 or 256. */
+typedef struct {
+    void *k, *v;
+    int64_t pages;
+    int32_t page;
+} spts_kv_pool;
+/* One sequence's cache in the pool: row i is row i % page of page table[i / page].  table [capacity / page], pos [capacity] int32 and
+ * weight [capacity] fp32 (NULL = no account of attention is kept) are device arrays, 16-byte aligned; capacity is a multiple of page
+ * below 2^31.  count lives on the host, as in spts_kv_out.  The table's entries for the rows in use are pages of the pool; an entry outside
+ * [0, pages) is a caller's mistake: its rows are read as the same rows of page 0 and never written.  Sequences may share pages that
+ * are only read (a common prompt); the pages that a call appends to or evicts in belong to one sequence.  What lies behind the first
+ * count rows is never read as a value: pages need no initialisation. */
+typedef struct {
+    const int32_t *table;
+    int32_t *pos;
+    float *weight;
+    int64_t capacity;
+    int64_t count;
+} spts_kvp;
+/* Appends rows to the caches of `batch` sequences (<= SPTS_MAX_DECODE_BATCH, distinct tables, positions and weights): rows
+ * [offsets[b], offsets[b+1]) of k, v [rows, Hkv, d] (element type) and pos [rows] (all device) go behind caches[b]'s count, which is
+ * increased; their weights become 0.  offsets [batch+1] is a HOST array, offsets[0] = 0, ascending.  A prefill's spts_kv_out is
+ * taken over with batch = 1 and offsets {0, count}.  d = 32, 64 or 128 (SPTS_ESHAPE otherwise, as for the calls below); SPTS_EINVAL where a capacity
+ * is exceeded. */
+int spts_kvp_append(spts_ctx *ctx, const spts_kv_pool *pool, const void *k, const void *v, const int32_t *pos, const int64_t *offsets,
+                    int32_t batch, spts_kvp *caches);
+/* Attention of new tokens over their sequences' caches: rows [offsets[b], offsets[b+1]) of q, out [rows, H, d] (element type) are the queries
+ * of the last rows of caches[b], which have been appended: with n of them, query i of sequence b sees rows 0 .. count - n + i, and
+ * out = softmax(q K^T / sqrt(d)) V over these, query head h reading key/value head h / (H / Hkv).  A sequence may have no queries; more queries than
+ * rows are SPTS_EINVAL, more in all than the context's max_tokens SPTS_EWORKSPACE.  Rows that a query does not see do not matter, whatever
+ * they hold; a query all of whose scores are -inf gives zeros.  Probabilities of chunks are rounded to the element type
+ * before they meet the values, of single tokens (at most 16 queries and heads of a key/value head) they keep 16 bits or more.
+ * add_weights != 0: for every sequence with queries, weight[j] = decay * weight[j] + the softmax weight of row j summed over the
+ * call's queries and all heads, for its count rows (0 <= decay <= 1; with decay = 0 the old weights are not read); all caches of such sequences need
+ * a weight, and no two the same one.  out may be q itself, and must not overlap it otherwise.  Uses the context's workspace. */
+int spts_kvp_attn(spts_ctx *ctx, const spts_kv_pool *pool, const void *q, const int64_t *offsets, int32_t batch, const spts_kvp *caches,
+                  void *out, int32_t add_weights, float decay);
+/* Cuts caches[b] down to min(count, keep[b]) rows, those with the largest weight, ties to the lower row; rows at positions below
+ * keep_below[b] (the beginning) or from keep_from[b] on (the latest) come before all others, by weight among themselves.  Kept rows below keep[b] stay where they
+ * are; those from keep[b] on go, in ascending order, to the places of rows that left, in ascending order (keys carry their
+ * rotation, so their order does not matter), with positions and weights; count becomes the rows kept.  Negative weights count as 0, a NaN as more than any
+ * number.  keep, keep_below and keep_from are HOST arrays [batch] (NULL for either of the last two = no such rows); old_out (device int32, NULL = not
+ * wanted) [sum of rows kept]: for each row of each sequence the row that it was.  What is behind the rows kept stays as it was.
+ * Distinct tables, positions and weights; SPTS_EWORKSPACE where 8 bytes for each row that may move do not fit the workspace. */
+int spts_kvp_evict(spts_ctx *ctx, const spts_kv_pool *pool, const int64_t *keep, const int32_t *keep_below, const int32_t *keep_from,
+                   int32_t batch, spts_kvp *caches, int32_t *old_out);
+
+/* Log probabilities of given words: logits [rows, V] of type dtype (spts_dtype; row i at element i * stride, stride >= V), tokens [rows]:
+ * logprob[i] = logits[i, tokens[i]] - log sum exp logits[i] (NaN for a token outside [0, V)); entropy[i] = -sum p log p in nats; and the n_top
+ * (<= SPTS_MAX_TOP_LOGPROBS) words with the largest logits, ties to the lower id: top_ids, top_logprobs [rows, n_top].  logprob goes with
+ * tokens, top_ids with top_logprobs and n_top > 0; entropy and each of these pairs may be NULL.  Words at -inf have no part in it: where fewer than n_top are
+ * above -inf the rest is -1 and -inf; a row without any has entropy 0 and log probabilities of -inf.  A NaN or +inf makes the row's log probabilities and
+ * entropy NaN; a NaN is never among the top.  V <= 2^28, rows < 2^31.  spts_process_logits' logits_out are such logits. */
+#define SPTS_MAX_TOP_LOGPROBS 32
+int spts_token_logprobs(spts_ctx *ctx, const void *logits, int32_t dtype, int64_t stride, int32_t V, int64_t rows, const int32_t *tokens,
+                        float *logprob, float *entropy, int32_t n_top, int32_t *top_ids, float *top_logprobs);
+
 /* Per-phase timing for benchmarks.  Between spts_profile_begin and spts_profile_end every phase of
  * every call on this context (k_proj, probe_attn, topk, attention, ffn_gate_up, ...) is bracketed
  * by two HIP events on the context's stream.  Products that share a launch are one phase (qv_proj:

@@ -25,6 +25,7 @@ EXPORTS = (
     "spts_pack_slab32",
     "spts_q4_bytes", "spts_q4_pack", "spts_matvec_q4", "spts_kv4_bytes", "spts_kv4_append", "spts_kv4_read", "spts_kv4_attn",
     "spts_decode_layer_q4", "spts_rmsnorm", "spts_process_logits",
+    "spts_kvp_append", "spts_kvp_attn", "spts_kvp_evict", "spts_token_logprobs",
     "spts_profile_begin", "spts_profile_end", "spts_profile_count", "spts_profile_get",
 )
 
@@ -70,6 +71,14 @@ class spts_logits_rules(C.Structure):
                 ("mask_stride", C.c_int64)]
 
 
+class spts_kv_pool(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("pages", C.c_int64), ("page", C.c_int32)]
+
+
+class spts_kvp(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("pos", C.c_void_p), ("weight", C.c_void_p), ("capacity", C.c_int64), ("count", C.c_int64)]
+
+
 def _host(values, typ, least: int, what: str):
     """A host array of `typ`, of `least` entries at least: the C calls read that many."""
     if len(values) < least:
@@ -84,9 +93,13 @@ def host_i64(values):
 
 def kv4_array(caches):
     """(array of spts_kv4, whether it is a copy): a ctypes array is passed on and its counts change in place, a list is copied."""
+    return _caches(caches, spts_kv4)
+
+
+def _caches(caches, typ):
     if isinstance(caches, C.Array):
         return caches, False
-    return (spts_kv4 * max(len(caches), 1))(*caches), True
+    return (typ * max(len(caches), 1))(*caches), True
 
 
 _lib = None
@@ -168,6 +181,14 @@ def load() -> C.CDLL:
     lib.spts_rmsnorm.argtypes = [vp, vp, vp, i32, vp]
     lib.spts_process_logits.restype = C.c_int
     lib.spts_process_logits.argtypes = [vp, vp, i32, i32, C.POINTER(spts_logits_rules), vp, vp, vp, vp]
+    lib.spts_kvp_append.restype = C.c_int
+    lib.spts_kvp_append.argtypes = [vp, C.POINTER(spts_kv_pool), vp, vp, vp, C.POINTER(i64), i32, C.POINTER(spts_kvp)]
+    lib.spts_kvp_attn.restype = C.c_int
+    lib.spts_kvp_attn.argtypes = [vp, C.POINTER(spts_kv_pool), vp, C.POINTER(i64), i32, C.POINTER(spts_kvp), vp, i32, C.c_float]
+    lib.spts_kvp_evict.restype = C.c_int
+    lib.spts_kvp_evict.argtypes = [vp, C.POINTER(spts_kv_pool), C.POINTER(i64), C.POINTER(i32), C.POINTER(i32), i32, C.POINTER(spts_kvp), vp]
+    lib.spts_token_logprobs.restype = C.c_int
+    lib.spts_token_logprobs.argtypes = [vp, vp, i32, i64, i32, i64, vp, vp, vp, i32, vp, vp]
     lib.spts_profile_begin.restype = C.c_int
     lib.spts_profile_begin.argtypes = [vp]
     lib.spts_profile_end.restype = C.c_int
@@ -410,6 +431,45 @@ class Context:
                 raise ValueError(f"rules for {have} {name}, {need} needed")
         _check(load().spts_process_logits(self.handle, _ptr(logits), V, batch, C.byref(rules), _ptr(logits_out), _ptr(token_out),
                                           _ptr(table), _ptr(x_next)), "spts_process_logits")
+
+    # ---- caches in pages
+    def spts_kvp_append(self, pool: spts_kv_pool, k, v, pos, offsets, caches):
+        """offsets [batch+1]: host integers or binding.host_i64; caches: a list of spts_kvp (count fields updated in place) or a
+        ctypes array of them."""
+        off = _host(offsets, C.c_int64, len(caches) + 1, "offsets")
+        arr, copied = _caches(caches, spts_kvp)
+        _check(load().spts_kvp_append(self.handle, C.byref(pool), _ptr(k), _ptr(v), _ptr(pos), off, len(caches), arr), "spts_kvp_append")
+        if copied:
+            for dst, src in zip(caches, arr):
+                dst.count = src.count
+
+    def spts_kvp_attn(self, pool: spts_kv_pool, q, offsets, caches, out, add_weights: int = 0, decay: float = 1.0):
+        arr, _ = _caches(caches, spts_kvp)
+        off = _host(offsets, C.c_int64, len(caches) + 1, "offsets")
+        _check(load().spts_kvp_attn(self.handle, C.byref(pool), _ptr(q), off, len(caches), arr, _ptr(out), add_weights, decay), "spts_kvp_attn")
+
+    def spts_kvp_evict(self, pool: spts_kv_pool, keep, caches, keep_below=None, keep_from=None, old_out=None):
+        """keep, keep_below, keep_from [batch]: host integers; caches as in spts_kvp_append."""
+        n = len(caches)
+        arr, copied = _caches(caches, spts_kvp)
+        first = None if keep_below is None else _host(keep_below, C.c_int32, n, "keep_below")
+        late = None if keep_from is None else _host(keep_from, C.c_int32, n, "keep_from")
+        _check(load().spts_kvp_evict(self.handle, C.byref(pool), _host(keep, C.c_int64, n, "keep"), first, late, n, arr, _ptr(old_out)), "spts_kvp_evict")
+        if copied:
+            for dst, src in zip(caches, arr):
+                dst.count = src.count
+
+    def spts_token_logprobs(self, logits, V: int, rows: int, tokens=None, logprob=None, entropy=None, n_top: int = 0, top_ids=None, top_logprobs=None,
+                            stride: Optional[int] = None):
+        """logits: fp32 or bf16 device tensor, the type is taken from it (ValueError otherwise); stride: elements from a row to the next (None = that of a
+        tensor of two dimensions, V otherwise)."""
+        import torch
+        if logits.dtype not in (torch.float32, torch.bfloat16) or (logits.dim() > 0 and logits.stride(-1) != 1):
+            raise ValueError(f"logits: rows of float32 or bfloat16, not {logits.dtype} with strides {tuple(logits.stride())}")
+        if stride is None:
+            stride = logits.stride(0) if logits.dim() == 2 and rows > 1 else V
+        _check(load().spts_token_logprobs(self.handle, _ptr(logits), SPTS_BF16 if logits.dtype == torch.bfloat16 else SPTS_F32, stride, V, rows, _ptr(tokens), _ptr(logprob),
+                                          _ptr(entropy), n_top, _ptr(top_ids), _ptr(top_logprobs)), "spts_token_logprobs")
 
     def spts_msdp_compact(self, x_in, pos_in, s_mha, N, N_next, protect_last, x_out, pos_out, map_new2old,
                           map_old2new=None):

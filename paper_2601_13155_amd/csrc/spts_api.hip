@@ -109,6 +109,7 @@ enum PhaseId {
     PH_COMPACT, PH_DEC_NORM, PH_DEC_QKV, PH_DEC_ROPE_APPEND, PH_DEC_ATTN, PH_DEC_O, PH_DEC_GATE_UP, PH_DEC_DOWN, PH_DEC_HEAD,
     PH_BUILD_SALIENCY, PH_BUILD_TOPMEAN, PH_QV_PROJ, PH_KQV_PROJ,
     PH_Q4_PACK, PH_Q4_MATVEC, PH_KV4_APPEND, PH_KV4_READ, PH_KV4_ATTN, PH_LOGITS_RULES,
+    PH_KVP_APPEND, PH_KVP_ATTN, PH_KVP_EVICT, PH_LOGPROBS,
     PH_COUNT
 };
 static const char* const kPhaseNames[PH_COUNT] = {
@@ -116,7 +117,8 @@ static const char* const kPhaseNames[PH_COUNT] = {
     "attention", "o_proj", "proxy_in", "proxy_mid", "proxy_z", "proxy_out", "ffn_gate_up", "ffn_down", "compact",
     "dec_rmsnorm", "dec_qkv", "dec_rope_append", "dec_attention", "dec_o_proj", "dec_gate_up", "dec_down", "dec_head",
     "build_saliency", "build_topmean", "qv_proj", "kqv_proj",
-    "q4_pack", "q4_matvec", "kv4_append", "kv4_read", "kv4_attn", "logits_rules"};
+    "q4_pack", "q4_matvec", "kv4_append", "kv4_read", "kv4_attn", "logits_rules",
+    "kvp_append", "kvp_attn", "kvp_evict", "logprobs"};
 
 // Brackets the launches issued during its lifetime with two events when profiling is on.
 struct PhaseScope {
@@ -1563,6 +1565,152 @@ int spts_process_logits(spts_ctx* c, const float* logits, int32_t V, int32_t bat
     if (token_out && logits_scratch_bytes(V, batch) > c->off.qp - c->off.tmp32) return SPTS_EWORKSPACE;
     PHASE(c, PH_LOGITS_RULES);
     SPTS_HIP(c, launch_process_logits(logits, V, batch, r, logits_out, token_out, table, c->m.D, x_next, c->bf16, c->p<void>(c->off.tmp32), c->stream));
+    return SPTS_OK;
+}
+
+// ---- caches in pages ----------------------------------------------------------------------------
+static_assert(SPTS_MAX_TOP_LOGPROBS == LOGPROBS_MAX_TOP, "the documented maximum is the kernels'");
+namespace {
+
+int kvp_pool(const spts_ctx* c, const spts_kv_pool* p, PagedPool* pool) {
+    if (!kv4_shape_ok(c->m)) return SPTS_ESHAPE;
+    if (!p || !p->k || !p->v || p->k == p->v || p->pages < 1) return SPTS_EINVAL;
+    if (!aligned16(p->k) || !aligned16(p->v)) return SPTS_EALIGN;
+    int shift = KVP_MIN_SHIFT;
+    while (shift <= KVP_MAX_SHIFT && (1 << shift) != p->page) ++shift;
+    if (shift > KVP_MAX_SHIFT || p->pages > INT32_MAX) return SPTS_ESHAPE;
+    *pool = PagedPool{p->k, p->v, p->pages, shift};
+    return SPTS_OK;
+}
+
+int kvp_batch(const spts_kvp* caches, int32_t batch, const PagedPool& pool, PagedBatch* pb) {
+    pb->n = batch;
+    for (int b = 0; b < batch; ++b) {
+        const spts_kvp& k = caches[b];
+        if (!k.table || !k.pos || k.capacity < 1 || k.count < 0 || k.count > k.capacity) return SPTS_EINVAL;
+        if (!aligned16(k.table) || !aligned16(k.pos) || !aligned16(k.weight)) return SPTS_EALIGN;
+        if (k.capacity % (1 << pool.shift) != 0 || k.capacity > INT32_MAX) return SPTS_ESHAPE;
+        pb->table[b] = k.table; pb->pos[b] = k.pos; pb->weight[b] = k.weight; pb->count[b] = k.count;
+    }
+    return SPTS_OK;
+}
+
+int kvp_distinct(const spts_kvp* caches, int32_t batch) {
+    for (int b = 0; b < batch; ++b)
+        for (int o = 0; o < b; ++o)
+            if (caches[o].table == caches[b].table || caches[o].pos == caches[b].pos || (caches[b].weight && caches[o].weight == caches[b].weight)) return SPTS_EINVAL;
+    return SPTS_OK;
+}
+
+int kvp_offsets(const int64_t* offsets, int32_t batch, PagedBatch* pb) {
+    if (!offsets || offsets[0] != 0) return SPTS_EINVAL;
+    for (int b = 0; b < batch; ++b)
+        if (offsets[b + 1] < offsets[b]) return SPTS_EINVAL;
+    if (offsets[batch] > INT32_MAX) return SPTS_ESHAPE;
+    for (int b = 0; b <= batch; ++b) pb->off[b] = offsets[b];
+    return SPTS_OK;
+}
+
+}  // namespace
+
+int spts_kvp_append(spts_ctx* c, const spts_kv_pool* p, const void* k, const void* v, const int32_t* pos, const int64_t* offsets, int32_t batch, spts_kvp* caches) {
+    if (!c || batch < 0 || batch > SPTS_MAX_DECODE_BATCH) return SPTS_EINVAL;
+    PagedPool pool{};
+    SPTS_TRY(kvp_pool(c, p, &pool));
+    if (batch == 0) return SPTS_OK;
+    if (!caches) return SPTS_EINVAL;
+    PagedBatch pb{};
+    SPTS_TRY(kvp_batch(caches, batch, pool, &pb));
+    SPTS_TRY(kvp_offsets(offsets, batch, &pb));
+    SPTS_TRY(kvp_distinct(caches, batch));
+    for (int b = 0; b < batch; ++b)
+        if (offsets[b + 1] - offsets[b] > caches[b].capacity - caches[b].count) return SPTS_EINVAL;
+    if (offsets[batch] == 0) return SPTS_OK;
+    if (!k || !v || !pos) return SPTS_EINVAL;
+    if (!aligned16(k) || !aligned16(v) || !aligned16(pos)) return SPTS_EALIGN;
+    PHASE(c, PH_KVP_APPEND);
+    SPTS_HIP(c, launch_kvp_append(k, v, pos, pool, pb, c->m.Hkv, c->m.d, c->bf16, c->stream));
+    for (int b = 0; b < batch; ++b) caches[b].count += offsets[b + 1] - offsets[b];
+    return SPTS_OK;
+}
+
+int spts_kvp_attn(spts_ctx* c, const spts_kv_pool* p, const void* q, const int64_t* offsets, int32_t batch, const spts_kvp* caches, void* out, int32_t add_weights, float decay) {
+    if (!c || batch < 0 || batch > SPTS_MAX_DECODE_BATCH) return SPTS_EINVAL;
+    PagedPool pool{};
+    SPTS_TRY(kvp_pool(c, p, &pool));
+    if (add_weights && !(decay >= 0.f && decay <= 1.f)) return SPTS_EINVAL;
+    if (batch == 0) return SPTS_OK;
+    if (!caches) return SPTS_EINVAL;
+    PagedBatch pb{};
+    SPTS_TRY(kvp_batch(caches, batch, pool, &pb));
+    SPTS_TRY(kvp_offsets(offsets, batch, &pb));
+    for (int b = 0; b < batch; ++b) {
+        const int64_t nq = offsets[b + 1] - offsets[b];
+        if (nq > pb.count[b]) return SPTS_EINVAL;
+        if (!add_weights || nq == 0) continue;
+        if (!pb.weight[b]) return SPTS_EINVAL;
+        for (int o = 0; o < b; ++o)
+            if (pb.weight[o] == pb.weight[b] && offsets[o + 1] > offsets[o]) return SPTS_EINVAL;
+    }
+    if (offsets[batch] == 0) return SPTS_OK;
+    if (!q || !out) return SPTS_EINVAL;
+    if (!aligned16(q) || !aligned16(out)) return SPTS_EALIGN;
+    const auto& m = c->m;
+    const int64_t bytes = offsets[batch] * m.H * m.d * elem_bytes(c);
+    if ((out != q || add_weights) && overlap(q, bytes, out, bytes)) return SPTS_EINVAL;
+    if (offsets[batch] > c->lim.max_tokens) return SPTS_EWORKSPACE;
+    PHASE(c, PH_KVP_ATTN);
+    SPTS_HIP(c, launch_kvp_attn(q, pool, pb, m.H, m.Hkv, m.d, c->p<float>(c->off.tmp32), (c->off.qp - c->off.tmp32) / sizeof(float), out, add_weights != 0, decay, c->bf16,
+                                c->stream));
+    return SPTS_OK;
+}
+
+int spts_kvp_evict(spts_ctx* c, const spts_kv_pool* p, const int64_t* keep, const int32_t* keep_below, const int32_t* keep_from, int32_t batch, spts_kvp* caches,
+                   int32_t* old_out) {
+    if (!c || batch < 0 || batch > SPTS_MAX_DECODE_BATCH) return SPTS_EINVAL;
+    PagedPool pool{};
+    SPTS_TRY(kvp_pool(c, p, &pool));
+    if (batch == 0) return SPTS_OK;
+    if (!caches || !keep) return SPTS_EINVAL;
+    PagedBatch pb{};
+    SPTS_TRY(kvp_batch(caches, batch, pool, &pb));
+    SPTS_TRY(kvp_distinct(caches, batch));
+    PagedEvict ev{};
+    int64_t kept = 0, moving = 0;
+    for (int b = 0; b < batch; ++b) {
+        if (keep[b] < 0 || !pb.weight[b]) return SPTS_EINVAL;
+        ev.keep[b] = keep[b];
+        ev.below[b] = keep_below ? keep_below[b] : INT32_MIN;
+        ev.above[b] = !keep_from ? INT32_MAX : keep_from[b] > INT32_MIN ? keep_from[b] - 1 : INT32_MAX;   // (before INT32_MIN: all rows alike, as with none)
+        if (keep_from && keep_from[b] == INT32_MIN) ev.below[b] = INT32_MIN;
+        kept += std::min(keep[b], pb.count[b]);
+        moving += pb.count[b] > keep[b];
+    }
+    if (kept > INT32_MAX) return SPTS_ESHAPE;
+    if (old_out && !aligned16(old_out)) return SPTS_EALIGN;
+    if (kvp_evict_scratch(pb, ev) > c->off.qp - c->off.tmp32) return SPTS_EWORKSPACE;
+    if (kept > 0 && (moving > 0 || old_out)) {
+        PHASE(c, PH_KVP_EVICT);
+        SPTS_HIP(c, launch_kvp_evict(pool, pb, ev, old_out, c->m.Hkv, c->m.d, c->bf16, c->p<void>(c->off.tmp32), c->stream));
+    }
+    for (int b = 0; b < batch; ++b) caches[b].count = std::min(keep[b], pb.count[b]);
+    return SPTS_OK;
+}
+
+int spts_token_logprobs(spts_ctx* c, const void* logits, int32_t dtype, int64_t stride, int32_t V, int64_t rows, const int32_t* tokens, float* logprob, float* entropy,
+                        int32_t n_top, int32_t* top_ids, float* top_logprobs) {
+    if (!c || V < 1 || rows < 0 || n_top < 0) return SPTS_EINVAL;
+    if (dtype != SPTS_F32 && dtype != SPTS_BF16) return SPTS_EDTYPE;
+    if (V > LOGITS_MAX_WORDS || n_top > SPTS_MAX_TOP_LOGPROBS || rows > INT32_MAX) return SPTS_ESHAPE;
+    if (stride < V || (logprob != nullptr) != (tokens != nullptr) || (top_ids != nullptr) != (n_top > 0) || (top_logprobs != nullptr) != (n_top > 0)) return SPTS_EINVAL;
+    if (rows == 0) return SPTS_OK;
+    if (!logits) return SPTS_EINVAL;
+    const void* ps[] = {logits, tokens, logprob, entropy, top_ids, top_logprobs};
+    for (const void* p : ps) if (!aligned16(p)) return SPTS_EALIGN;
+    if (logprobs_scratch_bytes(rows, V, n_top) > c->off.qp - c->off.tmp32) return SPTS_EWORKSPACE;
+    PHASE(c, PH_LOGPROBS);
+    SPTS_HIP(c, launch_token_logprobs(LogprobArgs{logits, stride, V, rows, tokens, logprob, entropy, n_top, top_ids, top_logprobs}, dtype == SPTS_BF16,
+                                      c->p<void>(c->off.tmp32), c->stream));
     return SPTS_OK;
 }
 

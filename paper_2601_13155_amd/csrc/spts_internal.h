@@ -394,4 +394,37 @@ size_t logits_scratch_bytes(int V, int nrows);
 hipError_t launch_process_logits(const float* in, int V, int nrows, const LogitsRules& r, float* out, int32_t* token, const void* table, int D,
                                  void* x_next, bool bf16, void* scratch, hipStream_t s);
 
+// ------------------------------------------------------------------ caches in pages
+// Pool: k, v [pages, Hkv, page, d], page = 1 << shift (16 .. 256).  Row i of a sequence lies in row i % page of the pool's page table[i / page]; an entry outside
+// [0, pages) is read as page 0 and not written.  Of each sequence: positions and accumulated attention by row.
+constexpr int KVP_MIN_SHIFT = 4, KVP_MAX_SHIFT = 8;
+struct PagedPool { void* k; void* v; int64_t pages; int32_t shift; };
+struct PagedBatch {
+    const int32_t* table[DECODE_MAX_BATCH]; int32_t* pos[DECODE_MAX_BATCH]; float* weight[DECODE_MAX_BATCH];   // weight may be null
+    int64_t count[DECODE_MAX_BATCH]; int64_t off[DECODE_MAX_BATCH + 1]; int32_t n;
+};
+// rows off[b] .. off[b + 1] of k, v [.., Hkv, d] and pos into rows count[b] .. of cache b, weights 0
+hipError_t launch_kvp_append(const void* k, const void* v, const int32_t* pos, const PagedPool& pool, const PagedBatch& pb, int Hkv, int d, bool bf16, hipStream_t s);
+// out [off[n], H, d]: the queries off[b] .. off[b + 1] belong to the last of sequence b's count[b] rows and see the rows up to their own; a query all of whose scores are
+// -inf gives zeros.  part: fp32 scratch of at least kvp_attn_min_floats.  add: weight[b][j] = decay * weight[b][j] + sum over b's queries and heads of row j's softmax weight (decay 0: the
+// old ones are not read; sequences without queries keep theirs).
+size_t kvp_attn_min_floats(int64_t rows, int H);
+hipError_t launch_kvp_attn(const void* q, const PagedPool& pool, const PagedBatch& pb, int H, int Hkv, int d, float* part, size_t part_floats, void* out, bool add, float decay,
+                           bool bf16, hipStream_t s);
+// keep[b] < count[b] rows of each sequence stay: of the largest (pos < below[b] or pos > above[b], weight, lower row); kept rows from keep[b] on go to the free places below it, both
+// ascending.  old [sum of min(count, keep)] (may be null): the row that each was.  scratch: kvp_evict_scratch bytes.
+struct PagedEvict { int64_t keep[DECODE_MAX_BATCH]; int32_t below[DECODE_MAX_BATCH]; int32_t above[DECODE_MAX_BATCH]; };
+size_t kvp_evict_scratch(const PagedBatch& pb, const PagedEvict& ev);
+hipError_t launch_kvp_evict(const PagedPool& pool, const PagedBatch& pb, const PagedEvict& ev, int32_t* old, int Hkv, int d, bool bf16, void* scratch, hipStream_t s);
+
+// ------------------------------------------------------------------ log probabilities
+// Of rows of V logits (stride apart): logprob[i] of word tokens[i] (NaN outside [0, V)), entropy[i], and the `top` words with the largest logits, ties to the lower word
+// (ids -1 and -inf where fewer are above -inf).  tokens with logprob, entropy, ids and top_lp may be null.  scratch: logprobs_scratch_bytes.
+constexpr int LOGPROBS_MAX_TOP = 32;
+struct LogprobArgs {
+    const void* logits; int64_t stride; int32_t V; int64_t rows; const int32_t* tokens; float* logprob; float* entropy; int32_t top; int32_t* ids; float* top_lp;
+};
+size_t logprobs_scratch_bytes(int64_t rows, int32_t V, int32_t top);
+hipError_t launch_token_logprobs(const LogprobArgs& a, bool bf16, void* scratch, hipStream_t s);
+
 }  // namespace spts

@@ -440,6 +440,83 @@ class Q4DecodeRunner:
                 self.x.copy_(self.x_next)
 
 
+# ------------------------------------------------------------------------------------------- caches in pages
+class PagedKV:
+    """One layer's caches of several sequences in pages of a pool that they share.  `pool` and `structs` are what the calls take (structs: a ctypes array of
+    spts_kvp, its counts kept up to date by them); k, v [pages, Hkv, page, d], table [sequences, capacity / page], pos and weight
+    [sequences, capacity] are the tensors behind them.  The host hands out the pages: reserve before appending, release after an eviction.
+
+    capacity: rows that a sequence may grow to (rounded up to whole pages); free: the order in which pages are handed out (None = 0, 1, 2, ..)."""
+
+    def __init__(self, shape, pages: int, page: int, sequences: int, capacity: int, weights: bool = True, free=None):
+        torch = _torch()
+        tdt = torch.bfloat16 if shape.dtype == "bf16" else torch.float32
+        per = max(1, -(-int(capacity) // page))
+        stride = (per + 3) // 4 * 4                     # rows of the table begin at multiples of 16 bytes
+        self.page, self.shape = page, shape
+        self.k = torch.empty((pages, shape.Hkv, page, shape.d), dtype=tdt, device="cuda")
+        self.v = torch.empty_like(self.k)
+        self._table = torch.full((sequences, stride), -1, dtype=torch.int32, device="cuda")
+        self.table = self._table[:, :per]
+        self.pos = torch.zeros((sequences, per * page), dtype=torch.int32, device="cuda")
+        self.weight = torch.zeros((sequences, per * page), dtype=torch.float32, device="cuda") if weights else None
+        self.pool = binding.spts_kv_pool(self.k.data_ptr(), self.v.data_ptr(), pages, page)
+        self.pool._keepalive = (self.k, self.v)
+        self.structs = (binding.spts_kvp * sequences)()
+        self.structs._keepalive = (self._table, self.pos, self.weight)
+        for b, s in enumerate(self.structs):
+            s.table, s.pos = self._table[b].data_ptr(), self.pos[b].data_ptr()
+            s.weight = self.weight[b].data_ptr() if weights else None
+            s.capacity = per * page
+        self._free = list(range(pages) if free is None else free)[::-1]
+        if sorted(self._free) != list(range(pages)):
+            raise ValueError(f"free: each of {pages} pages once")
+        self.pages = [[] for _ in range(sequences)]     # the pages of each sequence, as its table has them
+
+    @property
+    def counts(self) -> List[int]:
+        return [int(s.count) for s in self.structs]
+
+    @property
+    def free_pages(self) -> int:
+        return len(self._free)
+
+    def reserve(self, b: int, rows: int):
+        """Pages for the first `rows` rows of sequence b; ValueError where its capacity or the pool has no room.  Writes the table from the
+        host, in order with what the current stream is given."""
+        torch = _torch()
+        have, need = len(self.pages[b]), -(-int(rows) // self.page)
+        if need * self.page > self.structs[b].capacity:
+            raise ValueError(f"sequence {b}: {rows} rows exceed its capacity of {self.structs[b].capacity}")
+        if need - have > len(self._free):
+            raise ValueError(f"{need - have} pages needed, {len(self._free)} free")
+        if need > have:
+            new = [self._free.pop() for _ in range(need - have)]
+            self.pages[b] += new
+            self.table[b, have:need].copy_(torch.tensor(new, dtype=torch.int32))
+
+    def release(self, b: int):
+        """Hands back the pages behind sequence b's count rows (all of them where it is 0).  Call it when the work on them is in the stream that
+        their next owner uses too."""
+        need = -(-int(self.structs[b].count) // self.page)
+        while len(self.pages[b]) > need:
+            self._free.append(self.pages[b].pop())
+
+    def append_cache(self, ctx: binding.Context, b: int, cache: "KVCache"):
+        """Takes over every pair of a prefill's cache behind sequence b's rows (their weights 0)."""
+        one = [self.structs[b]]
+        with _on_stream_of(ctx):
+            self.reserve(b, self.structs[b].count + cache.count)
+            ctx.spts_kvp_append(self.pool, cache.k, cache.v, cache.pos, [0, cache.count], one)
+        self.structs[b].count = one[0].count
+
+    def host(self, b: int):
+        """(k, v, pos) of sequence b's filled rows, as host arrays (fp64 / int32)."""
+        n = self.counts[b]
+        k, v = (to_host(t[self.table[b].clamp(min=0).long()].transpose(1, 2).flatten(0, 1)[:n]).astype(np.float64) for t in (self.k, self.v))
+        return k, v, self.pos[b, :n].cpu().numpy()
+
+
 class StackRunner:
     """Runs Alg. 1's outer loop on the GPU: per layer one spts_layer_prefill, at stage ends one
     spts_msdp_compact.  Buffers are allocated once; run() only enqueues work (no host sync)."""
