@@ -5,49 +5,15 @@
 //
 // The queries of a key/value head are columns: column n of sequence b is query n / G, head n % G of the G heads that read it, so that any group and any chunk
 // fill blocks of 32 columns and a key that is loaded serves them all.
-#include "spts_lanes.h"
+#include "spts_paged.h"
 
 #include <algorithm>
 
 namespace spts {
 
 namespace {
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-constexpr float LOG2E = 1.4426950408889634f;
-constexpr float LOWEST = -3.402823466e38f;   // a running maximum starts here: below every finite score, and a score of -inf then weighs 2^-inf = 0
-
-// A kernel's view of up to NB sequences
-template <int NB> struct PagedSeqs {
-    const int32_t* table[NB];
-    float* weight[NB];
-    int32_t count[NB], first[NB], nq[NB];   // rows, the call's first query row, queries
-    int32_t end[NB];                        // work items of the sequences up to here
-    int32_t at[NB];                         // first row of sequence b in arrays over all sequences' rows (weights) / first partial result (attention)
-};
-struct Pool { const char* k; const char* v; uint32_t pages; int32_t shift; };
-
-template <int NB> __device__ inline int seq_of(const int32_t (&end)[NB], int i, int* first) {
-    int b = 0;
-    *first = 0;
-#pragma unroll
-    for (int j = 0; j + 1 < NB; ++j)
-        if (i >= end[j]) { b = j + 1; *first = end[j]; }
-    return b;
-}
-// element offset of the first row of a page's half of 16 rows that holds `row` (a multiple of 16)
-__device__ inline int64_t page_at(const Pool& pool, const int32_t* table, int64_t row, int g, int Hkv, int D) {
-    uint32_t id = (uint32_t)table[row >> pool.shift];
-    id = id < pool.pages ? id : 0;
-    return (((int64_t)id * Hkv + g) << pool.shift) * D + (row & ((1 << pool.shift) - 1)) * D;
-}
-
+typedef paged_f32x16 f32x16;
 __device__ inline f32x16 mfma_f32(float a, float b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
-__device__ inline f32x16 zero16() {
-    f32x16 z;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) z[r] = 0.f;
-    return z;
-}
 // N consecutive elements as fp32 (16-byte aligned)
 template <int N> __device__ inline void load_row(const float* p, float (&v)[N]) {
 #pragma unroll
@@ -74,8 +40,8 @@ template <int N> __device__ inline void load_row(const bf16_t* p, float (&v)[N])
 // count those that a column does see and put the infinity or NaN where it belongs.
 constexpr int AW = 4;
 template <typename T, int D, int NB>
-__global__ void __launch_bounds__(AW * 64) kvp_attn_kernel(const T* q, Pool pool, PagedSeqs<NB> sq, int H, int Hkv, int64_t per, float c, float* __restrict__ part,
-                                                           float2* __restrict__ stats, T* out) {
+__global__ void __launch_bounds__(AW * 64) kvp_attn_kernel(const T* q, PoolView pool, PagedSeqs<NB> sq, int H, int Hkv, float c, Shares sh, float2* __restrict__ stats,
+                                                           T* out) {   // (out may be q: a workgroup has read its columns before it writes them)
     constexpr int DB = D / 32, LD = D + 4;
     __shared__ float so[AW][32][LD];
     __shared__ float sm[AW][32], sl[AW][32];
@@ -85,19 +51,19 @@ __global__ void __launch_bounds__(AW * 64) kvp_attn_kernel(const T* q, Pool pool
     const int b = seq_of(sq.end, (int)(blockIdx.x / Hkv), &first);
     const int item = (int)(blockIdx.x / Hkv) - first;
     const int n = sq.count[b], nq = sq.nq[b], cols = nq * G, blocks = (cols + 31) / 32;
-    const int splits = (int)((n + per - 1) / per), split = item % splits, blk = blocks - 1 - item / splits;
+    const int splits = sq.splits[b], split = item % splits, blk = blocks - 1 - item / splits;
     const int32_t* const table = sq.table[b];
     const int col = blk * 32 + l32, cc = col < cols ? col : cols - 1, last = blk * 32 + 31 < cols ? blk * 32 + 31 : cols - 1;
     const int seen = n - nq + cc / G + 1;                                   // keys that the lane's column sees
     const int seen_all = n - nq + blk * 32 / G + 1, seen_any = n - nq + last / G + 1;
-    const int64_t k0 = split * per, k1 = k0 + per < seen_any ? k0 + per : seen_any;
+    const int64_t k0 = (int64_t)split * sq.per[b], k1 = k0 + sq.per[b] < seen_any ? k0 + sq.per[b] : seen_any;
 
     float qf[D / 2];
     load_row(q + ((int64_t)(sq.first[b] + cc / G) * H + g * G + cc % G) * D + lh * (D / 2), qf);
     f32x16 o[DB];
 #pragma unroll
     for (int i = 0; i < DB; ++i) o[i] = zero16();
-    float m = LOWEST, l = 0.f;
+    float m = PAGED_LOWEST, l = 0.f;
     for (int64_t key0 = k0 + wave * 32; key0 < k1; key0 += AW * 32) {
         const int left = (int)(n - key0 < 32 ? n - key0 : 32);
         const int64_t p0 = page_at(pool, table, key0, g, Hkv, D), p1 = left > 16 ? page_at(pool, table, key0 + 16, g, Hkv, D) - 16 * D : p0;
@@ -110,7 +76,7 @@ __global__ void __launch_bounds__(AW * 64) kvp_attn_kernel(const T* q, Pool pool
             for (int i = 0; i < D / 2; ++i) s = mfma_f32(kf[i], qf[i], s);
         }
         const bool masked = key0 + 32 > seen_all;
-        float mx = LOWEST;
+        float mx = PAGED_LOWEST;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             const int64_t key = key0 + 8 * (r >> 2) + 4 * lh + (r & 3);
@@ -168,7 +134,7 @@ __global__ void __launch_bounds__(AW * 64) kvp_attn_kernel(const T* q, Pool pool
     for (int i = tid; i < 32 * (D / 4); i += AW * 64) {
         const int cl = i / (D / 4), e = i % (D / 4) * 4, cn = blk * 32 + cl;
         if (cn >= cols) continue;
-        float M = LOWEST, L = 0.f;
+        float M = PAGED_LOWEST, L = 0.f;
         f32x4 t = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < AW; ++w) M = fmaxf(M, sm[w][cl]);
@@ -180,12 +146,11 @@ __global__ void __launch_bounds__(AW * 64) kvp_attn_kernel(const T* q, Pool pool
             for (int j = 0; j < 4; ++j) t[j] += so[w][cl][e + j] * a;
         }
         if (splits > 1) {
-            float* const to = part + ((int64_t)sq.at[b] + ((int64_t)split * Hkv + g) * cols + cn) * (D + 2);
-            if (e == 0) { to[0] = M; to[1] = L; }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) to[2 + e + j] = t[j];
+            const int64_t to = (int64_t)sq.at[b] + ((int64_t)split * Hkv + g) * cols + cn;
+            if (e == 0) sh.ml[to] = make_float2(M, L);
+            *reinterpret_cast<f32x4*>(sh.o + to * D + e) = t;
         } else {
-            const float inv = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;
+            const float inv = inverse_sum(L);
             const int64_t head = (int64_t)(sq.first[b] + cn / G) * H + g * G + cn % G;
 #pragma unroll
             for (int j = 0; j < 4; ++j) out[head * D + e + j] = from_f32<T>(t[j] * inv);
@@ -194,42 +159,56 @@ __global__ void __launch_bounds__(AW * 64) kvp_attn_kernel(const T* q, Pool pool
     }
 }
 
-// The shares of a head's keys, one workgroup of D threads per query and head
-template <typename T, int NB>
-__global__ void kvp_merge_kernel(const float* __restrict__ part, PagedSeqs<NB> sq, int H, int Hkv, int64_t per, float2* __restrict__ stats, T* __restrict__ out) {
-    const int h = blockIdx.x % H, G = H / Hkv, D = blockDim.x, e = threadIdx.x;
-    const int64_t row = blockIdx.x / H;
-    int b = 0;
+// The shares of a head's keys: one workgroup per query and head.  Every wavefront finds the column's maximum and sum (a lane a share), then groups of D / 4 threads take shares in turn.
+constexpr int MERGE_T = 256;
+template <typename T, int D, int NB>
+__global__ void __launch_bounds__(MERGE_T) kvp_merge_kernel(Shares sh, PagedSeqs<NB> sq, int H, int Hkv, float2* __restrict__ stats, T* __restrict__ out) {
+    constexpr int TG = D / 4, GROUPS = MERGE_T / TG;
+    __shared__ float so[GROUPS][D];
+    const int h = blockIdx.x % H, G = H / Hkv, tid = threadIdx.x, lane = tid & 63, grp = tid / TG, e = tid % TG * 4;
+    int first;
+    const int b = seq_of(sq.end, (int)(blockIdx.x / H), &first);   // (of sequences in shares)
+    const int qi = (int)(blockIdx.x / H) - first, splits = sq.splits[b], cols = sq.nq[b] * G;
+    const int64_t base = (int64_t)sq.at[b] + (int64_t)(h / G) * cols + qi * G + h % G, step = (int64_t)Hkv * cols;
+    float M = PAGED_LOWEST, L = 0.f;
+    for (int s = lane; s < splits; s += 64) M = fmaxf(M, sh.ml[base + s * step].x);
 #pragma unroll
-    for (int j = 1; j < NB; ++j)
-        if (sq.nq[j] > 0 && row >= sq.first[j]) b = j;
-    const int splits = (int)((sq.count[b] + per - 1) / per), cols = sq.nq[b] * G;
-    if (splits <= 1) return;
-    const int cn = (int)(row - sq.first[b]) * G + h % G;
-    const float* const base = part + ((int64_t)sq.at[b] + (int64_t)(h / G) * cols + cn) * (D + 2);
-    const int64_t stride = (int64_t)Hkv * cols * (D + 2);
-    float M = LOWEST, L = 0.f, t = 0.f;
-    for (int s = 0; s < splits; ++s) M = fmaxf(M, base[s * stride]);
-    for (int s = 0; s < splits; ++s) {
-        const float a = __builtin_amdgcn_exp2f(base[s * stride] - M);
-        L += base[s * stride + 1] * a;
-        t += base[s * stride + 2 + e] * a;
+    for (int off = 32; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor(M, off));
+    for (int s = lane; s < splits; s += 64) {
+        const float2 w = sh.ml[base + s * step];
+        L += w.y * __builtin_amdgcn_exp2f(w.x - M);
     }
-    const float inv = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;
-    out[(row * H + h) * D + e] = from_f32<T>(t * inv);
-    if (stats && e == 0) stats[row * H + h] = make_float2(M, inv);
+    L = wave_sum(L);
+    f32x4 t = {0.f, 0.f, 0.f, 0.f};
+    for (int s = grp; s < splits; s += GROUPS) {
+        const float a = __builtin_amdgcn_exp2f(sh.ml[base + s * step].x - M);
+        const f32x4 o = *reinterpret_cast<const f32x4*>(sh.o + (base + s * step) * D + e);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) t[j] += o[j] * a;
+    }
+    *reinterpret_cast<f32x4*>(&so[grp][e]) = t;
+    __syncthreads();
+    const float inv = inverse_sum(L);
+    const int64_t head = (int64_t)(sq.first[b] + qi) * H + h;
+    if (tid < D) {
+        float v = 0.f;
+#pragma unroll
+        for (int i = 0; i < GROUPS; ++i) v += so[i][tid];
+        out[head * D + tid] = from_f32<T>(v * inv);
+    }
+    if (stats && tid == 0) stats[head] = make_float2(M, inv);
 }
 
 // Column sums of the probabilities: a wavefront holds the keys of 32 rows and goes over the blocks of columns of its part of all heads, the scores anew (storing them would be
 // more bytes than the products cost, but for a few columns); stats has each column's maximum and 1 / sum.
 template <typename T, int D, int NB>
-__global__ void __launch_bounds__(AW * 64) kvp_weights_kernel(const T* __restrict__ q, Pool pool, PagedSeqs<NB> sq, int H, int Hkv, int parts, int64_t rows, float c,
+__global__ void __launch_bounds__(AW * 64) kvp_weights_kernel(const T* __restrict__ q, PoolView pool, PagedSeqs<NB> sq, int H, int Hkv, int parts, int64_t rows, float c,
                                                               const float2* __restrict__ stats, float* __restrict__ wpart, float decay) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, lh = lane >> 5, G = H / Hkv;
     const int p = (int)(blockIdx.x % parts);
     int first;
     const int b = seq_of(sq.end, (int)(blockIdx.x / parts), &first);
-    const int n = sq.count[b], nq = sq.nq[b], cols = nq * G, blocks = (cols + 31) / 32;
+    const int n = sq.count[b], nq = sq.nq[b], cols = nq * G, blocks = (cols + 31) / 32;   // (nq > 0: others have no tiles)
     const int64_t key0 = ((int64_t)(blockIdx.x / parts) - first) * (AW * 32) + wave * 32;
     if (key0 >= n) return;
     const int left = (int)(n - key0 < 32 ? n - key0 : 32), row = l32 < left ? l32 : left - 1;
@@ -289,56 +268,110 @@ __global__ void __launch_bounds__(256) kvp_add_weights_kernel(const float* __res
 
 size_t kvp_attn_min_floats(int64_t rows, int H) { return ((size_t)rows * H * 2 + 63) / 64 * 64; }   // the statistics of every column
 
+// How the keys of each sequence are shared out
+struct Plan {
+    int64_t cols_wg;      // columns of a workgroup
+    int64_t wgs;          // workgroups that fill the chip
+    int64_t least;        // keys of a share at least
+};
+static int64_t columns(const PagedBatch& pb, int b, int G) { return (pb.off[b + 1] - pb.off[b]) * G; }
+
+// per[b], splits[b] of the sequences that `mine` picks: shares of about equal length, as many as fill the chip where blocks of columns and heads are few
+template <int NB, typename F>
+static void share_keys(PagedSeqs<NB>& sq, const PagedBatch& pb, int Hkv, int G, const Plan& plan, F mine) {
+    int64_t total = 0;    // keys times blocks of columns
+    for (int b = 0; b < pb.n; ++b)
+        if (mine(b)) total += (columns(pb, b, G) + plan.cols_wg - 1) / plan.cols_wg * pb.count[b];
+    int64_t per = (total * Hkv + plan.wgs - 1) / plan.wgs;
+    per = per < plan.least ? plan.least : (per + 127) / 128 * 128;
+    for (int b = 0; b < pb.n; ++b)
+        if (mine(b)) {
+            const int64_t n = (pb.count[b] + per - 1) / per, even = ((pb.count[b] + n - 1) / n + 127) / 128 * 128;   // (equal shares)
+            sq.per[b] = (int32_t)std::min<int64_t>(even, 1 << 30);
+            sq.splits[b] = (int32_t)((pb.count[b] + sq.per[b] - 1) / sq.per[b]);
+        }
+}
+
 constexpr int64_t ATT_WORKGROUPS = 1024;
 template <typename T, int D, int NB>
 static hipError_t launch_kvp_attn_t(const T* q, const PagedPool& pool, const PagedBatch& pb, int H, int Hkv, float* part, size_t part_floats, T* out, bool add, float decay,
                                     hipStream_t s) {
+    constexpr bool BF16 = sizeof(T) == 2;
     const int G = H / Hkv;
     const int64_t rows = pb.off[pb.n];
-    const float c = LOG2E / sqrtf((float)D);
-    const Pool pl{(const char*)pool.k, (const char*)pool.v, (uint32_t)pool.pages, pool.shift};
+    const float c = PAGED_LOG2E / sqrtf((float)D);
+    const PoolView pl{(const char*)pool.k, (const char*)pool.v, (uint32_t)pool.pages, pool.shift};
     float2* const stats = add ? (float2*)part : nullptr;
     const size_t used = add ? kvp_attn_min_floats(rows, H) : 0;
     float* const rest = part + used;
     const size_t room = part_floats - used;
-    int64_t total = 0, blocks = 0;   // keys times blocks of columns
-    for (int b = 0; b < pb.n; ++b) {
-        const int64_t nb = ((pb.off[b + 1] - pb.off[b]) * G + 31) / 32;
-        total += nb * pb.count[b];
-        blocks += nb;
-    }
-    // keys of a share: the chip's workgroups where blocks of columns and heads are few
-    int64_t per = (total * Hkv + ATT_WORKGROUPS - 1) / ATT_WORKGROUPS;
-    per = per < 256 ? 256 : (per + 127) / 128 * 128;
-    auto splits_of = [&](int b) { return (pb.count[b] + per - 1) / per; };
-    for (;; per *= 2) {
-        int64_t floats = 0, split = 0;
-        for (int b = 0; b < pb.n; ++b)
-            if (splits_of(b) > 1) { floats += splits_of(b) * (pb.off[b + 1] - pb.off[b]) * H * (D + 2); split += pb.off[b + 1] - pb.off[b]; }
-        if (split == 0 || ((size_t)floats <= room && floats <= 0x7fffffff)) break;
-    }
     PagedSeqs<NB> sq{};
-    int64_t items = 0, parts_at = 0, most = 1;
-    for (int b = 0; b < NB; ++b) {
-        if (b < pb.n) {
-            const int64_t nq = pb.off[b + 1] - pb.off[b], sp = splits_of(b);
-            sq.table[b] = pb.table[b]; sq.weight[b] = pb.weight[b];
-            sq.count[b] = (int32_t)pb.count[b]; sq.first[b] = (int32_t)pb.off[b]; sq.nq[b] = (int32_t)nq; sq.at[b] = (int32_t)parts_at;
-            items += (nq * G + 31) / 32 * sp;
-            if (nq > 0 && sp > 1) { parts_at += sp * nq * H; most = std::max(most, sp); }
-        }
-        sq.end[b] = (int32_t)items;
+    int64_t big = 0;
+    for (int b = 0; b < pb.n; ++b) {
+        sq.table[b] = pb.table[b]; sq.weight[b] = pb.weight[b];
+        sq.count[b] = (int32_t)pb.count[b]; sq.first[b] = (int32_t)pb.off[b]; sq.nq[b] = (int32_t)(pb.off[b + 1] - pb.off[b]);
+        sq.per[b] = 1 << 30; sq.splits[b] = sq.nq[b] > 0 ? 1 : 0;
+        big += columns(pb, b, G) > KVP_FEW_COLS ? (columns(pb, b, G) + 127) / 128 : 0;
     }
-    if (items * Hkv > 0x7fffffff) return hipErrorInvalidValue;
-    kvp_attn_kernel<T, D, NB><<<dim3((unsigned)(items * Hkv)), dim3(AW * 64), 0, s>>>(q, pl, sq, H, Hkv, per, c, rest, stats, out);
-    if (most > 1) kvp_merge_kernel<T, NB><<<dim3((unsigned)(rows * H)), dim3(D), 0, s>>>(rest, sq, H, Hkv, per, stats, out);
+    auto few = [&](int b) { return sq.nq[b] > 0 && columns(pb, b, G) <= KVP_FEW_COLS; };
+    auto many = [&](int b) { return sq.nq[b] > 0 && columns(pb, b, G) > KVP_FEW_COLS; };
+    auto any = [&](int b) { return sq.nq[b] > 0; };
+    const int waves = D == 32 || big * Hkv < 512 ? 4 : 8;
+    int64_t shares = 0;
+    for (int64_t least = 256, scale = 1;; least *= 2, scale *= 2) {   // (fewer and longer shares where they would not fit the scratch)
+        if constexpr (BF16) {
+            share_keys(sq, pb, Hkv, G, Plan{KVP_FEW_COLS, std::max<int64_t>(1, 256 / scale), least}, few);
+            share_keys(sq, pb, Hkv, G, Plan{waves * 32, std::max<int64_t>(1, (waves == 8 ? 256 : 512) / scale), least}, many);
+        } else {
+            share_keys(sq, pb, Hkv, G, Plan{32, std::max<int64_t>(1, ATT_WORKGROUPS / scale), least}, any);
+        }
+        shares = 0;
+        for (int b = 0; b < pb.n; ++b)
+            if (sq.splits[b] > 1) { sq.at[b] = (int32_t)std::min<int64_t>(shares, 0x7fffffff); shares += (int64_t)sq.splits[b] * sq.nq[b] * H; }
+        if (shares == 0 || (shares <= 0x7fffffff && (size_t)shares * (D + 2) + 64 <= room)) break;
+    }
+    const Shares sh{(float2*)rest, rest + (2 * shares + 63) / 64 * 64};
+    // work items of the sequences that `mine` picks, in blocks of w columns
+    auto items_of = [&](auto mine, int64_t w) {
+        int64_t n = 0;
+        for (int b = 0; b < NB; ++b) {
+            if (b < pb.n && mine(b)) n += (columns(pb, b, G) + w - 1) / w * sq.splits[b];
+            sq.end[b] = (int32_t)std::min<int64_t>(n, 0x7fffffff);
+        }
+        return n;
+    };
+    hipError_t e = hipSuccess;
+    if constexpr (BF16) {
+        const int64_t nm = items_of(many, waves * 32);
+        if (nm * Hkv > 0x7fffffff) return hipErrorInvalidValue;
+        if (nm > 0) e = launch_kvp_attn_many<NB>(q, pl, sq, (int)nm, waves, H, Hkv, D, sh, stats, out, s);
+        if (e != hipSuccess) return e;
+        const int64_t nf = items_of(few, KVP_FEW_COLS);
+        if (nf > 0) e = launch_kvp_attn_few<NB>(q, pl, sq, (int)nf, H, Hkv, D, sh, stats, out, s);
+    } else {
+        const int64_t n = items_of(any, 32);
+        if (n * Hkv > 0x7fffffff) return hipErrorInvalidValue;
+        kvp_attn_kernel<T, D, NB><<<dim3((unsigned)(n * Hkv)), dim3(AW * 64), 0, s>>>(q, pl, sq, H, Hkv, c, sh, stats, out);
+        e = hipGetLastError();
+    }
+    if (e != hipSuccess) return e;
+    if (shares > 0) {
+        int64_t n = 0;
+        for (int b = 0; b < NB; ++b) {
+            if (b < pb.n && sq.splits[b] > 1) n += sq.nq[b];
+            sq.end[b] = (int32_t)n;
+        }
+        if (n * H > 0x7fffffff) return hipErrorInvalidValue;
+        kvp_merge_kernel<T, D, NB><<<dim3((unsigned)(n * H)), dim3(MERGE_T), 0, s>>>(sh, sq, H, Hkv, stats, out);
+    }
     if (add) {
-        int64_t tiles = 0, keys = 0;
+        int64_t tiles = 0, keys = 0, blocks = 0;
         for (int b = 0; b < NB; ++b) {
             if (b < pb.n && sq.nq[b] > 0) {
                 sq.at[b] = (int32_t)keys;
                 keys += pb.count[b];
                 tiles += (pb.count[b] + AW * 32 - 1) / (AW * 32);
+                blocks += (columns(pb, b, G) + 31) / 32;
             }
             sq.end[b] = (int32_t)tiles;
         }

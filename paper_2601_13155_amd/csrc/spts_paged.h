@@ -1,0 +1,60 @@
+// What the attention kernels over caches in pages share: a kernel's view of the sequences, where rows lie, how scores and values that are not finite are kept out.
+#pragma once
+#include "spts_lanes.h"
+
+namespace spts {
+typedef float paged_f32x16 __attribute__((ext_vector_type(16)));
+constexpr float PAGED_LOG2E = 1.4426950408889634f;
+constexpr float PAGED_LOWEST = -3.402823466e38f;   // a running maximum starts here: below every finite score, and a score of -inf then weighs 2^-inf = 0
+
+// A kernel's view of up to NB sequences
+template <int NB> struct PagedSeqs {
+    const int32_t* table[NB];
+    float* weight[NB];
+    int32_t count[NB], first[NB], nq[NB];   // rows, the call's first query row, queries
+    int32_t per[NB], splits[NB];            // keys of a share (a multiple of 128), shares
+    int32_t end[NB];                        // work items of the sequences up to here
+    int32_t at[NB];                         // first row of sequence b in arrays over all sequences' rows (weights) / first partial result (attention)
+};
+struct PoolView { const char* k; const char* v; uint32_t pages; int32_t shift; };
+// Shares of a column's keys, each with its maximum and sum (ml) and its unnormalised output (o [D]); column n of head g in share s is at at[b] + (s * Hkv + g) * columns + n
+struct Shares { float2* ml; float* o; };
+
+template <int NB> __device__ inline int seq_of(const int32_t (&end)[NB], int i, int* first) {
+    int b = 0;
+    *first = 0;
+#pragma unroll
+    for (int j = 0; j + 1 < NB; ++j)
+        if (i >= end[j]) { b = j + 1; *first = end[j]; }
+    return b;
+}
+// the pool's page of a row; the table does not change while kernels read it
+__device__ inline uint32_t page_id(const PoolView& pool, const int32_t* table, int64_t row) {
+    typedef const __attribute__((address_space(4))) int32_t* constant_i32;
+    const uint32_t id = (uint32_t)((constant_i32)(uintptr_t)table)[row >> pool.shift];
+    return id < pool.pages ? id : 0;
+}
+// element offset of a row (a multiple of 16) of kv head g on a page
+__device__ inline int64_t row_at(const PoolView& pool, uint32_t id, int64_t row, int g, int Hkv, int D) {
+    return (((int64_t)id * Hkv + g) << pool.shift) * D + (row & ((1 << pool.shift) - 1)) * D;
+}
+__device__ inline int64_t page_at(const PoolView& pool, const int32_t* table, int64_t row, int g, int Hkv, int D) {
+    return row_at(pool, page_id(pool, table, row), row, g, Hkv, D);
+}
+
+__device__ inline paged_f32x16 zero16() {
+    paged_f32x16 z;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) z[r] = 0.f;
+    return z;
+}
+// 1 / sum of a column's probabilities: 0 where all scores are -inf
+__device__ inline float inverse_sum(float L) { return L > 0.f ? 1.f / L : L == 0.f ? 0.f : L; }
+
+// kernels_paged_mfma.hip: bf16 on the bf16 matrix instructions.  `few`: sequences whose columns fit 16, `many`: the others (items of either may be none)
+template <int NB> hipError_t launch_kvp_attn_few(const bf16_t* q, const PoolView& pool, const PagedSeqs<NB>& sq, int items, int H, int Hkv, int d, const Shares& sh, float2* stats,
+                                                 bf16_t* out, hipStream_t s);
+template <int NB> hipError_t launch_kvp_attn_many(const bf16_t* q, const PoolView& pool, const PagedSeqs<NB>& sq, int items, int waves, int H, int Hkv, int d, const Shares& sh,
+                                                  float2* stats, bf16_t* out, hipStream_t s);
+constexpr int KVP_FEW_COLS = 16;
+}  // namespace spts
