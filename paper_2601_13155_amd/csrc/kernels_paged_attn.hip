@@ -199,17 +199,17 @@ __global__ void __launch_bounds__(MERGE_T) kvp_merge_kernel(Shares sh, PagedSeqs
     if (stats && tid == 0) stats[head] = make_float2(M, inv);
 }
 
-// Column sums of the probabilities: a wavefront holds the keys of 32 rows and goes over the blocks of columns of its part of all heads, the scores anew (storing them would be
-// more bytes than the products cost, but for a few columns); stats has each column's maximum and 1 / sum.
+// Column sums of the probabilities in fp32: a wavefront holds 32 keys and goes over the blocks of columns of its part of all heads, the scores anew; stats has each column's maximum
+// and 1 / sum.
 template <typename T, int D, int NB>
-__global__ void __launch_bounds__(AW * 64) kvp_weights_kernel(const T* __restrict__ q, PoolView pool, PagedSeqs<NB> sq, int H, int Hkv, int parts, int64_t rows, float c,
-                                                              const float2* __restrict__ stats, float* __restrict__ wpart, float decay) {
+__global__ void __launch_bounds__(AW * 64) kvp_weights_kernel(const T* __restrict__ q, PoolView pool, PagedSeqs<NB> sq, int H, int Hkv, float c, const float2* __restrict__ stats,
+                                                              float* __restrict__ sums, float decay) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, lh = lane >> 5, G = H / Hkv;
-    const int p = (int)(blockIdx.x % parts);
     int first;
-    const int b = seq_of(sq.end, (int)(blockIdx.x / parts), &first);
+    const int b = seq_of(sq.end, (int)blockIdx.x, &first);
+    const int parts = sq.parts[b], p = ((int)blockIdx.x - first) % parts;
     const int n = sq.count[b], nq = sq.nq[b], cols = nq * G, blocks = (cols + 31) / 32;   // (nq > 0: others have no tiles)
-    const int64_t key0 = ((int64_t)(blockIdx.x / parts) - first) * (AW * 32) + wave * 32;
+    const int64_t key0 = (int64_t)(((int)blockIdx.x - first) / parts) * (AW * 32) + wave * 32;
     if (key0 >= n) return;
     const int left = (int)(n - key0 < 32 ? n - key0 : 32), row = l32 < left ? l32 : left - 1;
     const int64_t total = (int64_t)blocks * Hkv;
@@ -247,23 +247,42 @@ __global__ void __launch_bounds__(AW * 64) kvp_weights_kernel(const T* __restric
         const float w = group_sum<32>(acc[r]);
         const int64_t key = key0 + 8 * (r >> 2) + 4 * lh + (r & 3);
         if (l32 != 0 || key >= n) continue;
-        if (parts > 1) wpart[p * rows + sq.at[b] + key] = w;
+        if (parts > 1) sums[(int64_t)sq.at[b] + (int64_t)p * n + key] = w;
         else sq.weight[b][key] = decay == 0.f ? w : decay * sq.weight[b][key] + w;
     }
 }
 
+// Accounts from kept scores (few columns): a thread has a key and goes over all heads' columns
 template <int NB>
-__global__ void __launch_bounds__(256) kvp_add_weights_kernel(const float* __restrict__ wpart, PagedSeqs<NB> sq, int parts, int64_t rows, float decay) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= rows) return;
-    int b = 0;
-#pragma unroll
-    for (int j = 1; j < NB; ++j)
-        if (sq.nq[j] > 0 && i >= sq.at[j]) b = j;
+__global__ void __launch_bounds__(256) kvp_scores_weights_kernel(const float* __restrict__ scores, PagedSeqs<NB> sq, int H, int Hkv, const float2* __restrict__ stats, float decay) {
+    int first;
+    const int b = seq_of(sq.end, (int)blockIdx.x, &first);
+    const int key = ((int)blockIdx.x - first) * 256 + threadIdx.x, n = sq.count[b], G = H / Hkv, cols = sq.nq[b] * G, stride = (n + 31) / 32 * 32;
+    if (key >= n) return;
+    const float* const at = scores + (int64_t)sq.scores[b] * 32 + key;
     float w = 0.f;
-    for (int p = 0; p < parts; ++p) w += wpart[p * rows + i];
-    float* const at = sq.weight[b] + (i - sq.at[b]);
-    *at = decay == 0.f ? w : decay * *at + w;
+    for (int g = 0; g < Hkv; ++g) {
+        const float2* const st = stats + (int64_t)sq.first[b] * H + g * G;
+#pragma unroll 4
+        for (int cn = 0; cn < cols; ++cn) {
+            const float2 z = st[(int64_t)(cn / G) * H + cn % G];
+            w = fmaf(__builtin_amdgcn_exp2f(at[(int64_t)(g * cols + cn) * stride] - z.x), z.y, w);
+        }
+    }
+    sq.weight[b][key] = decay == 0.f ? w : decay * sq.weight[b][key] + w;
+}
+
+// The parts' sums of a key, in their order
+template <int NB>
+__global__ void __launch_bounds__(256) kvp_add_weights_kernel(const float* __restrict__ sums, PagedSeqs<NB> sq, float decay) {
+    int first;
+    const int b = seq_of(sq.end, (int)blockIdx.x, &first);
+    const int key = ((int)blockIdx.x - first) * 256 + threadIdx.x, n = sq.count[b], parts = sq.parts[b];
+    if (key >= n) return;
+    float w = 0.f;
+#pragma unroll 4
+    for (int p = 0; p < parts; ++p) w += sums[(int64_t)sq.at[b] + (int64_t)p * n + key];
+    sq.weight[b][key] = decay == 0.f ? w : decay * sq.weight[b][key] + w;
 }
 
 size_t kvp_attn_min_floats(int64_t rows, int H) { return ((size_t)rows * H * 2 + 63) / 64 * 64; }   // the statistics of every column
@@ -310,7 +329,7 @@ static hipError_t launch_kvp_attn_t(const T* q, const PagedPool& pool, const Pag
     for (int b = 0; b < pb.n; ++b) {
         sq.table[b] = pb.table[b]; sq.weight[b] = pb.weight[b];
         sq.count[b] = (int32_t)pb.count[b]; sq.first[b] = (int32_t)pb.off[b]; sq.nq[b] = (int32_t)(pb.off[b + 1] - pb.off[b]);
-        sq.per[b] = 1 << 30; sq.splits[b] = sq.nq[b] > 0 ? 1 : 0;
+        sq.per[b] = 1 << 30; sq.splits[b] = sq.nq[b] > 0 ? 1 : 0; sq.scores[b] = -1;
         big += columns(pb, b, G) > KVP_FEW_COLS ? (columns(pb, b, G) + 127) / 128 : 0;
     }
     auto few = [&](int b) { return sq.nq[b] > 0 && columns(pb, b, G) <= KVP_FEW_COLS; };
@@ -331,6 +350,18 @@ static hipError_t launch_kvp_attn_t(const T* q, const PagedPool& pool, const Pag
         if (shares == 0 || (shares <= 0x7fffffff && (size_t)shares * (D + 2) + 64 <= room)) break;
     }
     const Shares sh{(float2*)rest, rest + (2 * shares + 63) / 64 * 64};
+    size_t taken = shares > 0 ? (2 * shares + 63) / 64 * 64 + (size_t)shares * D : 0;
+    // scores of few columns are kept for the accounts where there is room: rows of whole blocks of 32 keys
+    float* const scores = rest + taken;
+    if (BF16 && add) {
+        int64_t at = 0;
+        for (int b = 0; b < pb.n; ++b) {
+            const int64_t need = (pb.count[b] + 31) / 32 * columns(pb, b, G) * Hkv;
+            if (!few(b) || (size_t)(at + need) * 32 > room - taken || at + need > 0x7fffffff) continue;
+            sq.scores[b] = (int32_t)at;
+            at += need;
+        }
+    }
     // work items of the sequences that `mine` picks, in blocks of w columns
     auto items_of = [&](auto mine, int64_t w) {
         int64_t n = 0;
@@ -347,7 +378,7 @@ static hipError_t launch_kvp_attn_t(const T* q, const PagedPool& pool, const Pag
         if (nm > 0) e = launch_kvp_attn_many<NB>(q, pl, sq, (int)nm, waves, H, Hkv, D, sh, stats, out, s);
         if (e != hipSuccess) return e;
         const int64_t nf = items_of(few, KVP_FEW_COLS);
-        if (nf > 0) e = launch_kvp_attn_few<NB>(q, pl, sq, (int)nf, H, Hkv, D, sh, stats, out, s);
+        if (nf > 0) e = launch_kvp_attn_few<NB>(q, pl, sq, (int)nf, H, Hkv, D, sh, stats, scores, out, s);
     } else {
         const int64_t n = items_of(any, 32);
         if (n * Hkv > 0x7fffffff) return hipErrorInvalidValue;
@@ -365,20 +396,52 @@ static hipError_t launch_kvp_attn_t(const T* q, const PagedPool& pool, const Pag
         kvp_merge_kernel<T, D, NB><<<dim3((unsigned)(n * H)), dim3(MERGE_T), 0, s>>>(sh, sq, H, Hkv, stats, out);
     }
     if (add) {
-        int64_t tiles = 0, keys = 0, blocks = 0;
-        for (int b = 0; b < NB; ++b) {
-            if (b < pb.n && sq.nq[b] > 0) {
-                sq.at[b] = (int32_t)keys;
-                keys += pb.count[b];
-                tiles += (pb.count[b] + AW * 32 - 1) / (AW * 32);
-                blocks += (columns(pb, b, G) + 31) / 32;
+        auto kept = [&](int b) { return sq.scores[b] >= 0; };
+        auto anew = [&](int b) { return sq.nq[b] > 0 && sq.scores[b] < 0; };
+        // workgroups of `keys` rows of the sequences that `mine` picks, each `parts` times
+        auto tiles_of = [&](auto mine, int64_t keys, bool in_parts) {
+            int64_t t = 0;
+            for (int b = 0; b < NB; ++b) {
+                if (b < pb.n && mine(b)) t += (pb.count[b] + keys - 1) / keys * (in_parts ? sq.parts[b] : 1);
+                sq.end[b] = (int32_t)std::min<int64_t>(t, 0x7fffffff);
             }
-            sq.end[b] = (int32_t)tiles;
+            return t;
+        };
+        const int64_t ns = tiles_of(kept, 256, false);
+        if (ns > 0) kvp_scores_weights_kernel<NB><<<dim3((unsigned)ns), dim3(256), 0, s>>>(scores, sq, H, Hkv, stats, decay);
+        // parts of the heads and blocks of columns of each sequence, so that all workgroups have about the same number of blocks (the shares' and scores' room is free again, but for what
+        // the kept scores' kernel still reads: it is ahead in the stream)
+        constexpr int64_t KEYS = BF16 ? KVP_WEIGHT_KEYS : AW * 32;
+        int64_t work = 0;
+        for (int b = 0; b < pb.n; ++b)
+            if (anew(b)) work += (pb.count[b] + KEYS - 1) / KEYS * ((columns(pb, b, G) + 31) / 32) * Hkv;
+        bool joined = false;
+        for (int64_t target = std::max<int64_t>(1, work / ATT_WORKGROUPS); work > 0; target *= 2) {
+            int64_t at = 0;
+            joined = false;
+            for (int b = 0; b < pb.n; ++b) {
+                if (!anew(b)) continue;
+                const int64_t all = (columns(pb, b, G) + 31) / 32 * Hkv;
+                sq.parts[b] = (int32_t)std::max<int64_t>(1, std::min<int64_t>(256, all / target));
+                sq.at[b] = (int32_t)std::min<int64_t>(at, 0x7fffffff);
+                if (sq.parts[b] > 1) { at += sq.parts[b] * pb.count[b]; joined = true; }
+            }
+            if (!joined || ((size_t)at <= room && at <= 0x7fffffff)) break;
         }
-        int64_t parts = std::max<int64_t>(1, std::min<int64_t>({ATT_WORKGROUPS / std::max<int64_t>(1, tiles), blocks * Hkv, (int64_t)(room / (size_t)keys)}));
-        if (tiles * parts > 0x7fffffff) return hipErrorInvalidValue;
-        kvp_weights_kernel<T, D, NB><<<dim3((unsigned)(tiles * parts)), dim3(AW * 64), 0, s>>>(q, pl, sq, H, Hkv, (int)parts, keys, c, stats, rest, decay);
-        if (parts > 1) kvp_add_weights_kernel<NB><<<dim3((unsigned)((keys + 255) / 256)), dim3(256), 0, s>>>(rest, sq, (int)parts, keys, decay);
+        const int64_t nt = tiles_of(anew, KEYS, true);
+        if (nt > 0x7fffffff) return hipErrorInvalidValue;
+        if (nt > 0) {
+            if constexpr (BF16) {
+                e = launch_kvp_weights_many<NB>(q, pl, sq, (int)nt, H, Hkv, D, stats, rest, decay, s);
+                if (e != hipSuccess) return e;
+            } else {
+                kvp_weights_kernel<T, D, NB><<<dim3((unsigned)nt), dim3(AW * 64), 0, s>>>(q, pl, sq, H, Hkv, c, stats, rest, decay);
+            }
+        }
+        if (joined) {
+            const int64_t na = tiles_of([&](int b) { return anew(b) && sq.parts[b] > 1; }, 256, false);
+            kvp_add_weights_kernel<NB><<<dim3((unsigned)na), dim3(256), 0, s>>>(rest, sq, decay);
+        }
     }
     return hipGetLastError();
 }

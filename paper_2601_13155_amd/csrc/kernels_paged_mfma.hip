@@ -362,7 +362,8 @@ __global__ void __launch_bounds__(NW * 64, NW == 8 ? 2 : 1) kvp_many_kernel(cons
 // has the scores of keys 8 kg .. 8 kg + 7, which is the operand of O^T = V^T P^T as it stands.  Probabilities go in as two bf16 parts (off by 2^-17 of each at most), which costs
 // nothing here.  The maximum moves only when a score is 2^8 above it.
 template <int D, int NW, int NB>
-__global__ void __launch_bounds__(NW * 64, NW / 4) kvp_few_kernel(const bf16_t* q, PoolView pool, PagedSeqs<NB> sq, int H, int Hkv, float c, Shares sh, float2* __restrict__ stats, bf16_t* out) {
+__global__ void __launch_bounds__(NW * 64, NW / 4) kvp_few_kernel(const bf16_t* q, PoolView pool, PagedSeqs<NB> sq, int H, int Hkv, float c, Shares sh, float2* __restrict__ stats,
+                                                                 float* __restrict__ scores, bf16_t* out) {
     using L = Tile<D>;
     constexpr int KI = D / 32, VM = D / 16, BLOCK = 32 * L::ROW, LOADS = BLOCK / 1024, LD = D + 4;
     extern __shared__ __attribute__((aligned(1024))) char smem[];   // [NW][2][BLOCK] values; then [NW][16][LD] outputs and [NW][16][2] maxima and sums
@@ -406,6 +407,7 @@ __global__ void __launch_bounds__(NW * 64, NW / 4) kvp_few_kernel(const bf16_t* 
     };
     // the lane's place among value rows 8 kg + (lane % 16) / 4 (and 4 on), dimensions 4 (lane % 4) of 16
     const int vr = 8 * kg + (l16 >> 2), vc = (l16 & 3) >> 1;
+    float* const to_scores = scores && sq.scores[b] >= 0 ? scores + ((int64_t)sq.scores[b] + (int64_t)(g * cols + col) * ((n + 31) / 32)) * 32 + 8 * kg : nullptr;
     f32x4 o[VM];
 #pragma unroll
     for (int i = 0; i < VM; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -438,6 +440,10 @@ __global__ void __launch_bounds__(NW * 64, NW / 4) kvp_few_kernel(const bf16_t* 
             if (masked) x = key0 + 8 * kg + j < seen ? x : -INFINITY;
             s[j >> 2][j & 3] = x;
             mx = fmaxf(mx, x);
+        }
+        if (to_scores && l16 < cols) {   // rows of whole blocks of 32 keys
+            *reinterpret_cast<f32x4*>(to_scores + key0) = s[0];
+            *reinterpret_cast<f32x4*>(to_scores + key0 + 4) = s[1];
         }
         if (__ballot(mx > m + TAU) != 0) {
             mx = fmaxf(mx, __shfl_xor(mx, 16));
@@ -520,6 +526,130 @@ __global__ void __launch_bounds__(NW * 64, NW / 4) kvp_few_kernel(const bf16_t* 
     }
 }
 
+// ------------------------------------------------------------------ accounts of many columns
+// Column sums of the probabilities, the scores anew: storing them would be more bytes than the products cost.  A workgroup has 256 keys, a wavefront 64 of them in registers, and
+// goes over the blocks of 32 columns of its part of (head, block); the queries of a block and the columns' maxima and 1 / sums come into LDS by direct loads, two blocks ahead in a ring of four.
+// While the scores of one half of a wavefront's keys are on the matrix core, the lane takes the exponentials of the other half: an exponential, a multiplication and two additions a
+// score bound the kernel.
+constexpr int WW = 4, WST = 4;
+template <int D, int NB>
+__global__ void __launch_bounds__(WW * 64, 2) kvp_weights_mfma_kernel(const bf16_t* __restrict__ q, PoolView pool, PagedSeqs<NB> sq, int H, int Hkv, DivG dg, float c,
+                                                                      const float2* __restrict__ stats, float* __restrict__ sums, float decay) {
+    using L = Tile<D>;
+    constexpr int KS = D / 16, BLOCK = 32 * L::ROW, LOADS = BLOCK / 1024, STAGE = BLOCK + 256;
+    __shared__ __attribute__((aligned(1024))) char ring[WST * BLOCK];
+    __shared__ __attribute__((aligned(256))) float2 col_stats[WST][32];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, lh = lane >> 5, G = dg.G;
+    int first;
+    const int b = seq_of(sq.end, (int)blockIdx.x, &first);
+    const int parts = sq.parts[b], item = (int)blockIdx.x - first, part = item % parts;
+    const int n = sq.count[b], nq = sq.nq[b], cols = nq * G, blocks = (cols + 31) / 32;
+    const int tile0 = item / parts * (WW * 64), key0 = tile0 + wave * 64;
+    // blocks that see nothing of the tile come first: a column sees row n - nq + col / G at last
+    const int skip = tile0 > n - nq ? (int)((int64_t)(tile0 - (n - nq)) * G / 32) : 0;
+    const int each = blocks - skip;
+    const int64_t total = (int64_t)each * Hkv;
+    const int64_t i0 = total * part / parts, i1 = total * (part + 1) / parts;
+    const int steps = (int)(i1 - i0);
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)ring;
+    const uint32_t st0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float2*)&col_stats[0][0];
+    const int lrow = lane / L::CPR, lchunk = lane % L::CPR;
+    // head and block of the next block to load
+    int lg = (int)(i0 / each), lblk = skip + (int)(i0 % each);
+    auto issue = [&](int i) __attribute__((always_inline)) {
+        const int st = i % WST;
+        auto head_of = [&](int cn) {
+            cn = cn < cols ? cn : cols - 1;
+            const uint32_t qi = div_g((uint32_t)cn, dg);
+            return (int64_t)(sq.first[b] + (int)qi) * H + lg * G + (cn - (int)qi * G);
+        };
+#pragma unroll
+        for (int j = 0; j < LOADS; j += WW) {
+            const int ld = j + wave;
+            if (LOADS % WW == 0 || ld < LOADS) {
+                const int row = ld * L::ROWS_PER_LOAD + lrow;
+                dma16(q + head_of(lblk * 32 + row) * D + ((lchunk ^ L::kswz(row)) << 3), lds0 + (uint32_t)(st * BLOCK + ld * 1024));
+            }
+        }
+        if (wave == WW - 1) dma4_nt((const float*)(stats + head_of(lblk * 32 + (lane >> 1))) + (lane & 1), st0 + (uint32_t)(st * 256));
+        if (++lblk == blocks) { lblk = skip; ++lg; }
+    };
+    constexpr int MINE = (LOADS + WW - 1) / WW;   // loads of a wavefront a block, at most (and one more of the last)
+
+    f32x16 acc[2] = {zero16(), zero16()};
+    bf16x8 kf[2][KS];
+    const uint32_t kplace = (uint32_t)L::k_at(l32, lh);
+    int64_t krow[2];    // element offsets of the lane's two keys on head 0's page
+    {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int r = key0 + 32 * h + l32 < n ? key0 + 32 * h + l32 : n - 1;
+            krow[h] = page_at(pool, sq.table[b], r & ~15, 0, Hkv, D) + (r & 15) * D + 8 * lh;
+        }
+    }
+    const int64_t head_step = (int64_t)D << pool.shift;
+    auto load_keys = [&](int g) __attribute__((always_inline)) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) kf[h][ks] = *reinterpret_cast<const bf16x8*>((const bf16_t*)pool.k + krow[h] + g * head_step + 16 * ks);
+    };
+    auto frag = [&](uint32_t at, int ks) { return *(const __attribute__((address_space(3))) bf16x8*)(uintptr_t)(at ^ (uint32_t)(ks << 5)); };
+    // scores of half h of the keys with the block at `at` into SN, while the exponentials of the other half's scores SC are added to its account
+    auto half_step = [&](int h, uint32_t at, f32x16& SN, f32x16& SC, f32x16& a, float2 st, int first_key, int seen, bool masked) __attribute__((always_inline)) {
+        constexpr int EPS = 16 / KS;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            SN = mfma32(kf[h][ks], frag(at, ks), ks == 0 ? zero16() : SN);
+#pragma unroll
+            for (int e = ks * EPS; e < (ks + 1) * EPS; ++e) {
+                const float p = __builtin_amdgcn_exp2f(fmaf(SC[e], c, -st.x)) * st.y;
+                a[e] += !masked || first_key + 8 * (e >> 2) + 4 * lh + (e & 3) < seen ? p : 0.f;
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    auto stats_of = [&](int i) { return col_stats[i % WST][l32]; };
+    if (steps > 0) {
+        for (int i = 0; i < 2 && i < steps; ++i) issue(i);
+        int g = (int)(i0 / each), blk = skip + (int)(i0 % each);
+        load_keys(g);
+        SPTS_WAIT_VMCNT(0);
+        __syncthreads();
+        f32x16 S0 = zero16(), S1;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) S0 = mfma32(kf[0][ks], frag(lds0 + kplace, ks), ks == 0 ? zero16() : S0);
+        for (int i = 0; i < steps; ++i) {
+            // block i + 1 has landed for everyone, and block i - 2's place is free
+            if (i > 0) {
+                SPTS_WAIT_VMCNT(0);
+                __syncthreads();
+            }
+            if (i + 2 < steps) issue(i + 2);
+            const float2 st = stats_of(i);
+            const int col = blk * 32 + l32;
+            const int seen = col < cols ? n - nq + (int)div_g((uint32_t)col, dg) + 1 : 0;
+            const bool masked = blk * 32 + 32 > cols || n - nq + (int)div_g((uint32_t)(blk * 32), dg) + 1 < key0 + 64;
+            const uint32_t here = lds0 + (uint32_t)(i % WST * BLOCK) + kplace, ahead = lds0 + (uint32_t)((i + 1) % WST * BLOCK) + kplace;
+            if (masked) half_step(1, here, S1, S0, acc[0], st, key0, seen, true);
+            else half_step(1, here, S1, S0, acc[0], st, key0, seen, false);
+            if (++blk == blocks) { blk = skip; if (++g < Hkv && i + 1 < steps) load_keys(g); }
+            if (masked) half_step(0, ahead, S0, S1, acc[1], st, key0 + 32, seen, true);
+            else half_step(0, ahead, S0, S1, acc[1], st, key0 + 32, seen, false);
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const float w = group_sum<32>(acc[h][r]);
+            const int key = key0 + 32 * h + 8 * (r >> 2) + 4 * lh + (r & 3);
+            if (l32 != 0 || key >= n) continue;
+            if (parts > 1) sums[(int64_t)sq.at[b] + (int64_t)part * n + key] = w;
+            else sq.weight[b][key] = decay == 0.f ? w : decay * sq.weight[b][key] + w;
+        }
+}
+
 // ------------------------------------------------------------------ launches
 template <int D, int NW, int NB>
 static hipError_t launch_many(const bf16_t* q, const PoolView& pool, const PagedSeqs<NB>& sq, int items, int H, int Hkv, const Shares& sh, float2* stats, bf16_t* out, hipStream_t s) {
@@ -542,23 +672,43 @@ template hipError_t launch_kvp_attn_many<DECODE_MAX_BATCH>(const bf16_t*, const 
                                                            hipStream_t);
 
 template <int D, int NB>
-static hipError_t launch_few(const bf16_t* q, const PoolView& pool, const PagedSeqs<NB>& sq, int items, int H, int Hkv, const Shares& sh, float2* stats, bf16_t* out, hipStream_t s) {
+static hipError_t launch_few(const bf16_t* q, const PoolView& pool, const PagedSeqs<NB>& sq, int items, int H, int Hkv, const Shares& sh, float2* stats, float* scores, bf16_t* out,
+                             hipStream_t s) {
     constexpr int NW = 8, RING = NW * 2 * 32 * Tile<D>::ROW, MEET = NW * 16 * (D + 4 + 2) * 4, LDS = RING > MEET ? RING : MEET;
     const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(&kvp_few_kernel<D, NW, NB>), LDS);
     if (e != hipSuccess) return e;
-    kvp_few_kernel<D, NW, NB><<<dim3((unsigned)(items * Hkv)), dim3(NW * 64), LDS, s>>>(q, pool, sq, H, Hkv, PAGED_LOG2E / sqrtf((float)D), sh, stats, out);
+    kvp_few_kernel<D, NW, NB><<<dim3((unsigned)(items * Hkv)), dim3(NW * 64), LDS, s>>>(q, pool, sq, H, Hkv, PAGED_LOG2E / sqrtf((float)D), sh, stats, scores, out);
     return hipGetLastError();
 }
 
 template <int NB>
-hipError_t launch_kvp_attn_few(const bf16_t* q, const PoolView& pool, const PagedSeqs<NB>& sq, int items, int H, int Hkv, int d, const Shares& sh, float2* stats, bf16_t* out,
+hipError_t launch_kvp_attn_few(const bf16_t* q, const PoolView& pool, const PagedSeqs<NB>& sq, int items, int H, int Hkv, int d, const Shares& sh, float2* stats, float* scores, bf16_t* out,
                                hipStream_t s) {
     if ((int64_t)items * Hkv > 0x7fffffff) return hipErrorInvalidValue;
-    return d == 128 ? launch_few<128, NB>(q, pool, sq, items, H, Hkv, sh, stats, out, s)
-         : d == 64 ? launch_few<64, NB>(q, pool, sq, items, H, Hkv, sh, stats, out, s) : launch_few<32, NB>(q, pool, sq, items, H, Hkv, sh, stats, out, s);
+    return d == 128 ? launch_few<128, NB>(q, pool, sq, items, H, Hkv, sh, stats, scores, out, s)
+         : d == 64 ? launch_few<64, NB>(q, pool, sq, items, H, Hkv, sh, stats, scores, out, s)
+                    : launch_few<32, NB>(q, pool, sq, items, H, Hkv, sh, stats, scores, out, s);
 }
-template hipError_t launch_kvp_attn_few<1>(const bf16_t*, const PoolView&, const PagedSeqs<1>&, int, int, int, int, const Shares&, float2*, bf16_t*, hipStream_t);
-template hipError_t launch_kvp_attn_few<DECODE_MAX_BATCH>(const bf16_t*, const PoolView&, const PagedSeqs<DECODE_MAX_BATCH>&, int, int, int, int, const Shares&, float2*, bf16_t*,
+template hipError_t launch_kvp_attn_few<1>(const bf16_t*, const PoolView&, const PagedSeqs<1>&, int, int, int, int, const Shares&, float2*, float*, bf16_t*, hipStream_t);
+template hipError_t launch_kvp_attn_few<DECODE_MAX_BATCH>(const bf16_t*, const PoolView&, const PagedSeqs<DECODE_MAX_BATCH>&, int, int, int, int, const Shares&, float2*, float*, bf16_t*,
                                                           hipStream_t);
+
+template <int D, int NB>
+static hipError_t launch_weights(const bf16_t* q, const PoolView& pool, const PagedSeqs<NB>& sq, int items, int H, int Hkv, const float2* stats, float* sums, float decay, hipStream_t s) {
+    const int G = H / Hkv;
+    const DivG dg{(uint32_t)((((uint64_t)1 << 32) + G - 1) / G), G};
+    kvp_weights_mfma_kernel<D, NB><<<dim3((unsigned)items), dim3(WW * 64), 0, s>>>(q, pool, sq, H, Hkv, dg, PAGED_LOG2E / sqrtf((float)D), stats, sums, decay);
+    return hipGetLastError();
+}
+
+template <int NB>
+hipError_t launch_kvp_weights_many(const bf16_t* q, const PoolView& pool, const PagedSeqs<NB>& sq, int items, int H, int Hkv, int d, const float2* stats, float* sums, float decay,
+                                   hipStream_t s) {
+    return d == 128 ? launch_weights<128, NB>(q, pool, sq, items, H, Hkv, stats, sums, decay, s)
+         : d == 64 ? launch_weights<64, NB>(q, pool, sq, items, H, Hkv, stats, sums, decay, s) : launch_weights<32, NB>(q, pool, sq, items, H, Hkv, stats, sums, decay, s);
+}
+template hipError_t launch_kvp_weights_many<1>(const bf16_t*, const PoolView&, const PagedSeqs<1>&, int, int, int, int, const float2*, float*, float, hipStream_t);
+template hipError_t launch_kvp_weights_many<DECODE_MAX_BATCH>(const bf16_t*, const PoolView&, const PagedSeqs<DECODE_MAX_BATCH>&, int, int, int, int, const float2*, float*, float,
+                                                              hipStream_t);
 
 }  // namespace spts

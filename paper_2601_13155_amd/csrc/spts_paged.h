@@ -14,11 +14,16 @@ template <int NB> struct PagedSeqs {
     int32_t count[NB], first[NB], nq[NB];   // rows, the call's first query row, queries
     int32_t per[NB], splits[NB];            // keys of a share (a multiple of 128), shares
     int32_t end[NB];                        // work items of the sequences up to here
-    int32_t at[NB];                         // first row of sequence b in arrays over all sequences' rows (weights) / first partial result (attention)
+    int32_t at[NB];                         // first share of sequence b (attention) / first of its partial sums (accounts)
+    int32_t scores[NB];                     // where the scores of sequence b begin, in rows of 32 (-1: not kept)
+    int32_t parts[NB];                      // accounts: parts of its heads and columns
 };
 struct PoolView { const char* k; const char* v; uint32_t pages; int32_t shift; };
 // Shares of a column's keys, each with its maximum and sum (ml) and its unnormalised output (o [D]); column n of head g in share s is at at[b] + (s * Hkv + g) * columns + n
 struct Shares { float2* ml; float* o; };
+// x / G for x below 2^32 / G: the upper half of x times ceil(2^32 / G)
+struct DivG { uint32_t m; int32_t G; };
+__device__ inline uint32_t div_g(uint32_t x, DivG g) { return g.G == 1 ? x : __umulhi(x, g.m); }
 
 template <int NB> __device__ inline int seq_of(const int32_t (&end)[NB], int i, int* first) {
     int b = 0;
@@ -53,8 +58,11 @@ __device__ inline float inverse_sum(float L) { return L > 0.f ? 1.f / L : L == 0
 
 // kernels_paged_mfma.hip: bf16 on the bf16 matrix instructions.  `few`: sequences whose columns fit 16, `many`: the others (items of either may be none)
 template <int NB> hipError_t launch_kvp_attn_few(const bf16_t* q, const PoolView& pool, const PagedSeqs<NB>& sq, int items, int H, int Hkv, int d, const Shares& sh, float2* stats,
-                                                 bf16_t* out, hipStream_t s);
+                                                 float* scores, bf16_t* out, hipStream_t s);
 template <int NB> hipError_t launch_kvp_attn_many(const bf16_t* q, const PoolView& pool, const PagedSeqs<NB>& sq, int items, int waves, int H, int Hkv, int d, const Shares& sh,
                                                   float2* stats, bf16_t* out, hipStream_t s);
-constexpr int KVP_FEW_COLS = 16;
+// accounts of the sequences that have parts, over tiles of KVP_WEIGHT_KEYS keys; sums: partial sums of sequences in more than one part
+template <int NB> hipError_t launch_kvp_weights_many(const bf16_t* q, const PoolView& pool, const PagedSeqs<NB>& sq, int items, int H, int Hkv, int d, const float2* stats, float* sums,
+                                                     float decay, hipStream_t s);
+constexpr int KVP_FEW_COLS = 16, KVP_WEIGHT_KEYS = 256;
 }  // namespace spts
