@@ -31,6 +31,8 @@ template <int N> __device__ inline void load_row(const bf16_t* p, float (&v)[N])
         for (int e = 0; e < 8; ++e) v[i + e] = chunk_elem(w, e, bf16_t{});
     }
 }
+__device__ inline void store4(float* p, f32x4 v, float f) { *reinterpret_cast<f32x4*>(p) = f32x4{v[0] * f, v[1] * f, v[2] * f, v[3] * f}; }
+__device__ inline void store4(bf16_t* p, f32x4 v, float f) { *reinterpret_cast<u32x2*>(p) = u32x2{cvt_pk_bf16(v[0] * f, v[1] * f), cvt_pk_bf16(v[2] * f, v[3] * f)}; }
 }  // namespace
 
 // On the fp32 matrix instruction 32x32x2.  S^T = K Q^T: operand rows are keys, columns queries; of the two halves of a wavefront one multiplies the first, one the second half of the
@@ -159,8 +161,44 @@ __global__ void __launch_bounds__(AW * 64) kvp_attn_kernel(const T* q, PoolView 
     }
 }
 
-// The shares of a head's keys: one workgroup per query and head.  Every wavefront finds the column's maximum and sum (a lane a share), then groups of D / 4 threads take shares in turn.
+// The shares of a column's keys, up to MOST: D / 4 threads a column, which ask for everything at once
 constexpr int MERGE_T = 256;
+template <typename T, int D, int NB, int MOST>
+__global__ void __launch_bounds__(MERGE_T) kvp_merge_few_kernel(Shares sh, PagedSeqs<NB> sq, uint32_t total, int H, int Hkv, float2* __restrict__ stats, T* __restrict__ out) {
+    constexpr uint32_t TG = D / 4;
+    const uint32_t item = blockIdx.x * (MERGE_T / TG) + threadIdx.x / TG;   // query and head among those of sequences in shares
+    if (item >= total) return;
+    const int e = (int)(threadIdx.x % TG) * 4, row = (int)(item / (uint32_t)H), h = (int)item - row * H, G = H / Hkv, g = h / G;
+    int first;
+    const int b = seq_of(sq.end, row, &first);
+    const int qi = row - first, splits = sq.splits[b], cols = sq.nq[b] * G;
+    const int64_t base = (int64_t)sq.at[b] + g * cols + qi * G + (h - g * G), step = (int64_t)Hkv * cols;
+    float2 ml[MOST];
+    f32x4 o[MOST];
+#pragma unroll
+    for (int s = 0; s < MOST; ++s) {   // (all at once; those that are not there weigh nothing)
+        const int64_t at = base + (s < splits ? s : 0) * step;
+        ml[s] = sh.ml[at];
+        o[s] = *reinterpret_cast<const f32x4*>(sh.o + at * D + e);
+    }
+    float M = PAGED_LOWEST, L = 0.f;
+#pragma unroll
+    for (int s = 0; s < MOST; ++s) M = fmaxf(M, s < splits ? ml[s].x : PAGED_LOWEST);
+    f32x4 t = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < MOST; ++s) {
+        const float a = __builtin_amdgcn_exp2f(ml[s].x - M);
+        L += s < splits ? ml[s].y * a : 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) t[j] += s < splits ? o[s][j] * a : 0.f;
+    }
+    const float inv = inverse_sum(L);
+    const int64_t head = (int64_t)(sq.first[b] + qi) * H + h;
+    store4(out + head * D + e, t, inv);
+    if (stats && e == 0) stats[head] = make_float2(M, inv);
+}
+
+// ... and many: a workgroup a column.  Every wavefront finds the column's maximum and sum (a lane a share), then groups of D / 4 threads take shares in turn.
 template <typename T, int D, int NB>
 __global__ void __launch_bounds__(MERGE_T) kvp_merge_kernel(Shares sh, PagedSeqs<NB> sq, int H, int Hkv, float2* __restrict__ stats, T* __restrict__ out) {
     constexpr int TG = D / 4, GROUPS = MERGE_T / TG;
@@ -287,28 +325,53 @@ __global__ void __launch_bounds__(256) kvp_add_weights_kernel(const float* __res
 
 size_t kvp_attn_min_floats(int64_t rows, int H) { return ((size_t)rows * H * 2 + 63) / 64 * 64; }   // the statistics of every column
 
-// How the keys of each sequence are shared out
-struct Plan {
-    int64_t cols_wg;      // columns of a workgroup
-    int64_t wgs;          // workgroups that fill the chip
-    int64_t least;        // keys of a share at least
-};
 static int64_t columns(const PagedBatch& pb, int b, int G) { return (pb.off[b + 1] - pb.off[b]) * G; }
 
-// per[b], splits[b] of the sequences that `mine` picks: shares of about equal length, as many as fill the chip where blocks of columns and heads are few
+// per[b], splits[b] of the sequences that `mine` picks: shares of about equal length (none below `least` keys), so many that blocks of `cols_wg` columns, heads and shares make
+// about `wgs` workgroups.  Returns the workgroups; *longest: keys of the longest share.
 template <int NB, typename F>
-static void share_keys(PagedSeqs<NB>& sq, const PagedBatch& pb, int Hkv, int G, const Plan& plan, F mine) {
-    int64_t total = 0;    // keys times blocks of columns
+static int64_t share_keys(PagedSeqs<NB>& sq, const PagedBatch& pb, int Hkv, int G, int64_t cols_wg, int64_t wgs, int64_t least, F mine, int64_t* longest = nullptr) {
+    int64_t total = 0, n_wgs = 0, most = 0;    // keys times blocks of columns
     for (int b = 0; b < pb.n; ++b)
-        if (mine(b)) total += (columns(pb, b, G) + plan.cols_wg - 1) / plan.cols_wg * pb.count[b];
-    int64_t per = (total * Hkv + plan.wgs - 1) / plan.wgs;
-    per = per < plan.least ? plan.least : (per + 127) / 128 * 128;
+        if (mine(b)) total += (columns(pb, b, G) + cols_wg - 1) / cols_wg * pb.count[b];
+    int64_t per = (total * Hkv + wgs - 1) / wgs;
+    per = per < least ? least : (per + 127) / 128 * 128;
     for (int b = 0; b < pb.n; ++b)
         if (mine(b)) {
-            const int64_t n = (pb.count[b] + per - 1) / per, even = ((pb.count[b] + n - 1) / n + 127) / 128 * 128;   // (equal shares)
+            const int64_t n = (pb.count[b] + per - 1) / per, even = ((pb.count[b] + n - 1) / n + 127) / 128 * 128;
             sq.per[b] = (int32_t)std::min<int64_t>(even, 1 << 30);
             sq.splits[b] = (int32_t)((pb.count[b] + sq.per[b] - 1) / sq.per[b]);
+            n_wgs += (columns(pb, b, G) + cols_wg - 1) / cols_wg * Hkv * sq.splits[b];
+            most = std::max<int64_t>(most, std::min<int64_t>(sq.per[b], pb.count[b]));
         }
+    if (longest) *longest = most;
+    return n_wgs;
+}
+
+// Workgroups of many columns, one a CU: a share costs about 12 us and 1.6 us for 64 keys of 128 dimensions (1.35 with a quarter of the chip at work, 1.87 with all of it), shares are
+// merged at about 4 us and 4 TB/s.  The number of them for which that sum is least (us for all keys in one share / this choice: 64 tokens after 4096, 8 heads of 4, 36.6 / 24; 256 after
+// 4096 110 / 39; 1024 tokens alone 33 / 33, in two shares 28 and a merge of 8).
+template <int NB, typename F>
+static int64_t pick_workgroups(PagedSeqs<NB>& sq, const PagedBatch& pb, int H, int Hkv, int D, int64_t cols_wg, int64_t least, F mine) {
+    const double tile = D == 128 ? 1.6 : D == 64 ? 1.0 : 0.6;
+    double best = 0.0;
+    int64_t choice = 1;
+    for (const int64_t wgs : {1, 32, 64, 96, 128, 192, 256, 384, 512, 768, 1024}) {
+        int64_t longest;
+        const int64_t n = share_keys(sq, pb, Hkv, H / Hkv, cols_wg, wgs, least, mine, &longest);
+        const double unit = 12.0 + tile * ((longest + 63) / 64);
+        double all = 0.0, bytes = 0.0;
+        for (int b = 0; b < pb.n; ++b) {
+            if (!mine(b)) continue;
+            all += (double)((columns(pb, b, H / Hkv) + cols_wg - 1) / cols_wg * Hkv * sq.splits[b]) * (12.0 + tile * (sq.per[b] < pb.count[b] ? sq.per[b] : pb.count[b]) / 64);
+            if (sq.splits[b] > 1) bytes += (double)sq.splits[b] * (pb.off[b + 1] - pb.off[b]) * H * D * 8;
+        }
+        const double rounds = (double)((n + 255) / 256) * unit, spread = n <= 256 ? unit : std::min(rounds, all / 256 + 0.5 * unit);
+        const double t = spread + (bytes > 0 ? 4.0 + bytes / 4e6 : 0.0);
+        if (choice == 1 && best == 0.0) { best = t; continue; }
+        if (t < best) { best = t; choice = wgs; }
+    }
+    return choice;
 }
 
 constexpr int64_t ATT_WORKGROUPS = 1024;
@@ -325,24 +388,35 @@ static hipError_t launch_kvp_attn_t(const T* q, const PagedPool& pool, const Pag
     float* const rest = part + used;
     const size_t room = part_floats - used;
     PagedSeqs<NB> sq{};
-    int64_t big = 0;
     for (int b = 0; b < pb.n; ++b) {
         sq.table[b] = pb.table[b]; sq.weight[b] = pb.weight[b];
         sq.count[b] = (int32_t)pb.count[b]; sq.first[b] = (int32_t)pb.off[b]; sq.nq[b] = (int32_t)(pb.off[b + 1] - pb.off[b]);
         sq.per[b] = 1 << 30; sq.splits[b] = sq.nq[b] > 0 ? 1 : 0; sq.scores[b] = -1;
-        big += columns(pb, b, G) > KVP_FEW_COLS ? (columns(pb, b, G) + 127) / 128 : 0;
     }
     auto few = [&](int b) { return sq.nq[b] > 0 && columns(pb, b, G) <= KVP_FEW_COLS; };
     auto many = [&](int b) { return sq.nq[b] > 0 && columns(pb, b, G) > KVP_FEW_COLS; };
     auto any = [&](int b) { return sq.nq[b] > 0; };
-    const int waves = D == 32 || big * Hkv < 512 ? 4 : 8;
+    constexpr int64_t COLS = kvp_many_waves(D) * 32;
+    int64_t want = ATT_WORKGROUPS, want_few = 256, least_few = 256;
+    if constexpr (BF16) {
+        want = pick_workgroups(sq, pb, H, Hkv, D, COLS, 256, many);
+        // Few columns: two workgroups fit a CU.  A single sequence's shares are all alike, one a CU; those of several are not, and more of them even out (us at 256 / 384 / 512 / 1024
+        // workgroups: 131072 rows of 8 heads 95 / 105 / 98 / 102, 30000 24.3 / 26.7 / 25.9 / 29.7; 16 sequences of 1048 .. 13107 rows, 4 heads, 53 / 44 / 47 / 43, of 480 .. 6000 rows,
+        // 8 heads, 46 / 38 / 39 / 40).  Short caches in one share, without a merge: 301 rows 7.7 for 9.1, 16 of up to 501 10.4 for 11.8; two shares of 517 rows 9.2, one 9.9.
+        int n = 0;
+        int64_t longest = 0;
+        for (int b = 0; b < pb.n; ++b)
+            if (few(b)) { ++n; longest = std::max(longest, pb.count[b]); }
+        if (n > 1) want_few = 384;
+        if (longest <= 512) least_few = 512;
+    }
     int64_t shares = 0;
-    for (int64_t least = 256, scale = 1;; least *= 2, scale *= 2) {   // (fewer and longer shares where they would not fit the scratch)
+    for (int64_t scale = 1;; scale *= 2) {   // (fewer and longer shares where they would not fit the scratch)
         if constexpr (BF16) {
-            share_keys(sq, pb, Hkv, G, Plan{KVP_FEW_COLS, std::max<int64_t>(1, 256 / scale), least}, few);
-            share_keys(sq, pb, Hkv, G, Plan{waves * 32, std::max<int64_t>(1, (waves == 8 ? 256 : 512) / scale), least}, many);
+            share_keys(sq, pb, Hkv, G, KVP_FEW_COLS, std::max<int64_t>(1, want_few / scale), least_few * scale, few);
+            share_keys(sq, pb, Hkv, G, COLS, std::max<int64_t>(1, want / scale), 256 * scale, many);
         } else {
-            share_keys(sq, pb, Hkv, G, Plan{32, std::max<int64_t>(1, ATT_WORKGROUPS / scale), least}, any);
+            share_keys(sq, pb, Hkv, G, 32, std::max<int64_t>(1, want / scale), 256 * scale, any);
         }
         shares = 0;
         for (int b = 0; b < pb.n; ++b)
@@ -373,9 +447,9 @@ static hipError_t launch_kvp_attn_t(const T* q, const PagedPool& pool, const Pag
     };
     hipError_t e = hipSuccess;
     if constexpr (BF16) {
-        const int64_t nm = items_of(many, waves * 32);
+        const int64_t nm = items_of(many, COLS);
         if (nm * Hkv > 0x7fffffff) return hipErrorInvalidValue;
-        if (nm > 0) e = launch_kvp_attn_many<NB>(q, pl, sq, (int)nm, waves, H, Hkv, D, sh, stats, out, s);
+        if (nm > 0) e = launch_kvp_attn_many<NB>(q, pl, sq, (int)nm, H, Hkv, D, sh, stats, out, s);
         if (e != hipSuccess) return e;
         const int64_t nf = items_of(few, KVP_FEW_COLS);
         if (nf > 0) e = launch_kvp_attn_few<NB>(q, pl, sq, (int)nf, H, Hkv, D, sh, stats, scores, out, s);
@@ -393,7 +467,13 @@ static hipError_t launch_kvp_attn_t(const T* q, const PagedPool& pool, const Pag
             sq.end[b] = (int32_t)n;
         }
         if (n * H > 0x7fffffff) return hipErrorInvalidValue;
-        kvp_merge_kernel<T, D, NB><<<dim3((unsigned)(n * H)), dim3(MERGE_T), 0, s>>>(sh, sq, H, Hkv, stats, out);
+        int most = 1;
+        for (int b = 0; b < pb.n; ++b) most = std::max(most, sq.splits[b]);
+        const dim3 grid((unsigned)((n * H + MERGE_T / (D / 4) - 1) / (MERGE_T / (D / 4))));
+        if (most <= 2) kvp_merge_few_kernel<T, D, NB, 2><<<grid, dim3(MERGE_T), 0, s>>>(sh, sq, (uint32_t)(n * H), H, Hkv, stats, out);
+        else if (most <= 4) kvp_merge_few_kernel<T, D, NB, 4><<<grid, dim3(MERGE_T), 0, s>>>(sh, sq, (uint32_t)(n * H), H, Hkv, stats, out);
+        else if (most <= 8) kvp_merge_few_kernel<T, D, NB, 8><<<grid, dim3(MERGE_T), 0, s>>>(sh, sq, (uint32_t)(n * H), H, Hkv, stats, out);
+        else kvp_merge_kernel<T, D, NB><<<dim3((unsigned)(n * H)), dim3(MERGE_T), 0, s>>>(sh, sq, H, Hkv, stats, out);
     }
     if (add) {
         auto kept = [&](int b) { return sq.scores[b] >= 0; };

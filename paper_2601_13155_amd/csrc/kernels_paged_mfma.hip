@@ -362,7 +362,7 @@ __global__ void __launch_bounds__(NW * 64, NW == 8 ? 2 : 1) kvp_many_kernel(cons
 // has the scores of keys 8 kg .. 8 kg + 7, which is the operand of O^T = V^T P^T as it stands.  Probabilities go in as two bf16 parts (off by 2^-17 of each at most), which costs
 // nothing here.  The maximum moves only when a score is 2^8 above it.
 template <int D, int NW, int NB>
-__global__ void __launch_bounds__(NW * 64, NW / 4) kvp_few_kernel(const bf16_t* q, PoolView pool, PagedSeqs<NB> sq, int H, int Hkv, float c, Shares sh, float2* __restrict__ stats,
+__global__ void __launch_bounds__(NW * 64, 2) kvp_few_kernel(const bf16_t* q, PoolView pool, PagedSeqs<NB> sq, int H, int Hkv, float c, Shares sh, float2* __restrict__ stats,
                                                                  float* __restrict__ scores, bf16_t* out) {
     using L = Tile<D>;
     constexpr int KI = D / 32, VM = D / 16, BLOCK = 32 * L::ROW, LOADS = BLOCK / 1024, LD = D + 4;
@@ -661,20 +661,20 @@ static hipError_t launch_many(const bf16_t* q, const PoolView& pool, const Paged
 }
 
 template <int NB>
-hipError_t launch_kvp_attn_many(const bf16_t* q, const PoolView& pool, const PagedSeqs<NB>& sq, int items, int waves, int H, int Hkv, int d, const Shares& sh, float2* stats, bf16_t* out,
+hipError_t launch_kvp_attn_many(const bf16_t* q, const PoolView& pool, const PagedSeqs<NB>& sq, int items, int H, int Hkv, int d, const Shares& sh, float2* stats, bf16_t* out,
                                 hipStream_t s) {
-    if (d == 128) return waves == 8 ? launch_many<128, 8, NB>(q, pool, sq, items, H, Hkv, sh, stats, out, s) : launch_many<128, 4, NB>(q, pool, sq, items, H, Hkv, sh, stats, out, s);
-    if (d == 64) return waves == 8 ? launch_many<64, 8, NB>(q, pool, sq, items, H, Hkv, sh, stats, out, s) : launch_many<64, 4, NB>(q, pool, sq, items, H, Hkv, sh, stats, out, s);
-    return waves == 4 ? launch_many<32, 4, NB>(q, pool, sq, items, H, Hkv, sh, stats, out, s) : hipErrorInvalidValue;
+    return d == 128 ? launch_many<128, kvp_many_waves(128), NB>(q, pool, sq, items, H, Hkv, sh, stats, out, s)
+         : d == 64 ? launch_many<64, kvp_many_waves(64), NB>(q, pool, sq, items, H, Hkv, sh, stats, out, s)
+                   : launch_many<32, kvp_many_waves(32), NB>(q, pool, sq, items, H, Hkv, sh, stats, out, s);
 }
-template hipError_t launch_kvp_attn_many<1>(const bf16_t*, const PoolView&, const PagedSeqs<1>&, int, int, int, int, int, const Shares&, float2*, bf16_t*, hipStream_t);
-template hipError_t launch_kvp_attn_many<DECODE_MAX_BATCH>(const bf16_t*, const PoolView&, const PagedSeqs<DECODE_MAX_BATCH>&, int, int, int, int, int, const Shares&, float2*, bf16_t*,
+template hipError_t launch_kvp_attn_many<1>(const bf16_t*, const PoolView&, const PagedSeqs<1>&, int, int, int, int, const Shares&, float2*, bf16_t*, hipStream_t);
+template hipError_t launch_kvp_attn_many<DECODE_MAX_BATCH>(const bf16_t*, const PoolView&, const PagedSeqs<DECODE_MAX_BATCH>&, int, int, int, int, const Shares&, float2*, bf16_t*,
                                                            hipStream_t);
 
 template <int D, int NB>
 static hipError_t launch_few(const bf16_t* q, const PoolView& pool, const PagedSeqs<NB>& sq, int items, int H, int Hkv, const Shares& sh, float2* stats, float* scores, bf16_t* out,
                              hipStream_t s) {
-    constexpr int NW = 8, RING = NW * 2 * 32 * Tile<D>::ROW, MEET = NW * 16 * (D + 4 + 2) * 4, LDS = RING > MEET ? RING : MEET;
+    constexpr int NW = 4, RING = NW * 2 * 32 * Tile<D>::ROW, MEET = NW * 16 * (D + 4 + 2) * 4, LDS = RING > MEET ? RING : MEET;
     const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(&kvp_few_kernel<D, NW, NB>), LDS);
     if (e != hipSuccess) return e;
     kvp_few_kernel<D, NW, NB><<<dim3((unsigned)(items * Hkv)), dim3(NW * 64), LDS, s>>>(q, pool, sq, H, Hkv, PAGED_LOG2E / sqrtf((float)D), sh, stats, scores, out);

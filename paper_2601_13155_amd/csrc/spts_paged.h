@@ -59,10 +59,11 @@ __device__ inline float inverse_sum(float L) { return L > 0.f ? 1.f / L : L == 0
 // kernels_paged_mfma.hip: bf16 on the bf16 matrix instructions.  `few`: sequences whose columns fit 16, `many`: the others (items of either may be none)
 template <int NB> hipError_t launch_kvp_attn_few(const bf16_t* q, const PoolView& pool, const PagedSeqs<NB>& sq, int items, int H, int Hkv, int d, const Shares& sh, float2* stats,
                                                  float* scores, bf16_t* out, hipStream_t s);
-template <int NB> hipError_t launch_kvp_attn_many(const bf16_t* q, const PoolView& pool, const PagedSeqs<NB>& sq, int items, int waves, int H, int Hkv, int d, const Shares& sh,
+template <int NB> hipError_t launch_kvp_attn_many(const bf16_t* q, const PoolView& pool, const PagedSeqs<NB>& sq, int items, int H, int Hkv, int d, const Shares& sh,
                                                   float2* stats, bf16_t* out, hipStream_t s);
 // accounts of the sequences that have parts, over tiles of KVP_WEIGHT_KEYS keys; sums: partial sums of sequences in more than one part
 template <int NB> hipError_t launch_kvp_weights_many(const bf16_t* q, const PoolView& pool, const PagedSeqs<NB>& sq, int items, int H, int Hkv, int d, const float2* stats, float* sums,
                                                      float decay, hipStream_t s);
 constexpr int KVP_FEW_COLS = 16, KVP_WEIGHT_KEYS = 256;
+constexpr int kvp_many_waves(int d) { return d == 32 ? 4 : 8; }   // of a workgroup, 32 columns each (a tile of 64 keys of 32 dimensions is four loads)
 }  // namespace spts
