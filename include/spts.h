@@ -394,8 +394,8 @@ typedef struct {
     int32_t page;
 } spts_kv_pool;
 /* One sequence's cache in the pool: row i is row i % page of page table[i / page].  table [capacity / page], pos [capacity] int32 and
- * weight [capacity] fp32 (NULL = no account of attention is kept) are device arrays, 16-byte aligned; capacity is a multiple of page
- * below 2^31.  count lives on the host, as in spts_kv_out.  The table's entries for the rows in use are pages of the pool; an entry outside
+ * weight [capacity] fp32 (NULL = no account of attention is kept) are device arrays, 16-byte aligned; capacity is a multiple of page,
+ * 2^30 at most.  count lives on the host, as in spts_kv_out.  The table's entries for the rows in use are pages of the pool; an entry outside
  * [0, pages) is a caller's mistake: its rows are read as the same rows of page 0 and never written.  Sequences may share pages that
  * are only read (a common prompt); the pages that a call appends to or evicts in belong to one sequence.  What lies behind the first
  * count rows is never read as a value: pages need no initialisation. */
@@ -430,7 +430,8 @@ int spts_kvp_attn(spts_ctx *ctx, const spts_kv_pool *pool, const void *q, const 
  * rotation, so their order does not matter), with positions and weights; count becomes the rows kept.  Negative weights count as 0, a NaN as more than any
  * number.  keep, keep_below and keep_from are HOST arrays [batch] (NULL for either of the last two = no such rows); old_out (device int32, NULL = not
  * wanted) [sum of rows kept]: for each row of each sequence the row that it was.  What is behind the rows kept stays as it was.
- * Distinct tables, positions and weights; SPTS_EWORKSPACE where 8 bytes for each row that may move do not fit the workspace. */
+ * Distinct tables, positions and weights; SPTS_EWORKSPACE where the workspace has no room for 8 bytes for each
+ * row that may move (and, if a sequence has more than 16384 rows, for 25 KB for each 4096 of the longest's, up to 3.3 MB, for every sequence). */
 int spts_kvp_evict(spts_ctx *ctx, const spts_kv_pool *pool, const int64_t *keep, const int32_t *keep_below, const int32_t *keep_from,
                    int32_t batch, spts_kvp *caches, int32_t *old_out);
 

@@ -1589,7 +1589,7 @@ int kvp_batch(const spts_kvp* caches, int32_t batch, const PagedPool& pool, Page
         const spts_kvp& k = caches[b];
         if (!k.table || !k.pos || k.capacity < 1 || k.count < 0 || k.count > k.capacity) return SPTS_EINVAL;
         if (!aligned16(k.table) || !aligned16(k.pos) || !aligned16(k.weight)) return SPTS_EALIGN;
-        if (k.capacity % (1 << pool.shift) != 0 || k.capacity > INT32_MAX) return SPTS_ESHAPE;
+        if (k.capacity % (1 << pool.shift) != 0 || k.capacity > KVP_MAX_ROWS) return SPTS_ESHAPE;
         pb->table[b] = k.table; pb->pos[b] = k.pos; pb->weight[b] = k.weight; pb->count[b] = k.count;
     }
     return SPTS_OK;
@@ -1688,7 +1688,7 @@ int spts_kvp_evict(spts_ctx* c, const spts_kv_pool* p, const int64_t* keep, cons
     }
     if (kept > INT32_MAX) return SPTS_ESHAPE;
     if (old_out && !aligned16(old_out)) return SPTS_EALIGN;
-    if (kvp_evict_scratch(pb, ev) > c->off.qp - c->off.tmp32) return SPTS_EWORKSPACE;
+    if (kvp_evict_scratch(pb, ev) > c->off.total - c->off.tmp32) return SPTS_EWORKSPACE;   // (all that lies behind is scratch of other calls)
     if (kept > 0 && (moving > 0 || old_out)) {
         PHASE(c, PH_KVP_EVICT);
         SPTS_HIP(c, launch_kvp_evict(pool, pb, ev, old_out, c->m.Hkv, c->m.d, c->bf16, c->p<void>(c->off.tmp32), c->stream));

@@ -398,6 +398,7 @@ hipError_t launch_process_logits(const float* in, int V, int nrows, const Logits
 // Pool: k, v [pages, Hkv, page, d], page = 1 << shift (16 .. 256).  Row i of a sequence lies in row i % page of the pool's page table[i / page]; an entry outside
 // [0, pages) is read as page 0 and not written.  Of each sequence: positions and accumulated attention by row.
 constexpr int KVP_MIN_SHIFT = 4, KVP_MAX_SHIFT = 8;
+constexpr int64_t KVP_MAX_ROWS = 1 << 30;   // of a sequence: rows and what tiles and chunks add to them are 32-bit numbers
 struct PagedPool { void* k; void* v; int64_t pages; int32_t shift; };
 struct PagedBatch {
     const int32_t* table[DECODE_MAX_BATCH]; int32_t* pos[DECODE_MAX_BATCH]; float* weight[DECODE_MAX_BATCH];   // weight may be null

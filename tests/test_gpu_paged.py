@@ -292,8 +292,8 @@ def test_append_without_accounts_and_from_a_prefill():
 
 
 # ------------------------------------------------------------------------------------------------------------ eviction
-def run_evict(shape, rows, keep, below=None, start=None, weights="random", page=16, seed=0, want_old=True):
-    ctx = context(shape)
+def run_evict(shape, rows, keep, below=None, start=None, weights="random", page=16, seed=0, want_old=True, tokens=256):
+    ctx = context(shape, tokens)
     kv, host = filled(shape, page, rows, seed=seed)
     r = np.random.default_rng(seed)
     w = [np.zeros(n, np.float32) for n in rows]
@@ -342,9 +342,15 @@ def test_evict(dtype, weights):
     run_evict(shape, rows, keep, below=[4] * 13, start=[2 * n - 20 for n in rows], weights=weights, seed=2, page=64)
 
 
-@pytest.mark.parametrize("rows,keep", [(5000, 4096), (20000, 311), (16384, 16383), (40000, 20000)])
-def test_evict_long_rows(rows, keep):
-    run_evict(shape_of(1, 1, 32, "bf16"), [rows], [keep], below=[10], start=[2 * rows - 500], weights="few", seed=rows, page=128)
+@pytest.mark.parametrize("weights", ["few", "random", "zero", "odd"])
+@pytest.mark.parametrize("rows,keep", [(5000, 4096), (8192, 4000), (8193, 4096), (20000, 311), (16384, 16383), (16384, 1), (16385, 16384), (40000, 20000)])
+def test_evict_long_rows(rows, keep, weights):
+    run_evict(shape_of(1, 1, 32, "bf16"), [rows], [keep], below=[10], start=[2 * rows - 500], weights=weights, seed=rows, page=128)
+
+
+def test_evict_long_and_short_rows_together():
+    run_evict(shape_of(1, 1, 32, "f32"), [9000, 20, 700, 30000, 12288, 5, 8192], [4097, 30, 0, 4096, 8192, 2, 8191], weights="few", seed=6, tokens=8192)
+    run_evict(shape_of(1, 1, 32, "bf16"), [530000], [270001], weights="few", seed=7, page=256, want_old=False)     # chunks of 8192 rows
 
 
 def test_evict_where_more_rows_go_before_others_than_stay():

@@ -64,7 +64,7 @@ def i32(*v):
 BAD_POOLS = [(dict(k=None), INVAL), (dict(v=None), INVAL), (dict(k=A, v=A), INVAL), (dict(pages=0), INVAL), (dict(pages=1 << 31), SHAPE), (dict(k=A + 8), ALIGN), (dict(v=A + 2), ALIGN),
              (dict(page=8), SHAPE), (dict(page=0), SHAPE), (dict(page=48), SHAPE), (dict(page=512), SHAPE), (dict(page=-16), SHAPE)]
 BAD_CACHES = [(dict(table=None), INVAL), (dict(pos=None), INVAL), (dict(capacity=0), INVAL), (dict(count=-1), INVAL), (dict(count=65), INVAL), (dict(table=3 * A + 4), ALIGN),
-              (dict(pos=3 * A + 8), ALIGN), (dict(weight=3 * A + 4), ALIGN), (dict(capacity=72), SHAPE), (dict(capacity=1 << 31), SHAPE)]
+              (dict(pos=3 * A + 8), ALIGN), (dict(weight=3 * A + 4), ALIGN), (dict(capacity=72), SHAPE), (dict(capacity=1 << 31), SHAPE), (dict(capacity=(1 << 30) + 16), SHAPE)]
 
 
 def test_every_call_refuses_bad_pools_and_caches(lib, ctx):
@@ -93,7 +93,7 @@ def test_append(lib, ctx):
     h = ctx()
     call = lambda off, caches, k=A, v=A, p=A: lib.spts_kvp_append(h, pool(), k, v, p, off, len(caches), caches)
     assert call(None, kvp()) == INVAL and call(i64(1, 2), kvp()) == INVAL and call(i64(0, 2, 1), kvp(2)) == INVAL
-    assert call(i64(0, 1 << 31), kvp(capacity=(1 << 31) - 16)) == SHAPE
+    assert call(i64(0, 1 << 31), kvp(capacity=1 << 30)) == SHAPE
     assert call(i64(0, 65), kvp()) == INVAL and call(i64(0, 2), kvp(count=63)) == INVAL
     for name in ("table", "pos", "weight"):
         two = kvp(2)
