@@ -2,24 +2,33 @@
 //
 // One pass over a row with a running maximum m: s = sum e^(x - m), t = sum e^(x - m) (x - m).  Then log p(w) = (x_w - m) - log s and the entropy
 // is log s - t / s; neither term is below zero, so nothing cancels.
-// The row is bound by its bytes, so the largest words come out of the same pass: after the first tile of the row a bound is known that `top` words reach (the top-th largest of
-// the maxima of 64 groups of the tile), and words above it are put into a list in LDS, some 200 of 128256 for top = 20.  Where a row (ascending logits, say) fills the list, it is cut down in
-// the same way, by a bound from its own groups; at the end the words that are left are ranked.  Words are ordered by (logit, lower id), so that equals cannot fill the list either.
+// The row is bound by its bytes, so the largest words come out of the same pass, and every wavefront keeps a list of its own in LDS, without a barrier: after its first 1024 words it has
+// a bound that `top` of them reach (the top-th largest of its lanes' maxima), and puts words above it into the list.  A list that gets long is cut by a bound from its own
+// words, which is a better one, and so is a list that a row (ascending logits, say) fills.  At the end the lists' words are ranked together.  Words are ordered by
+// (logit, lower id), so that equals cannot fill a list either.
 #include "spts_lanes.h"
 
 namespace spts {
 
 namespace {
 constexpr int PT = 256, PWV = PT / 64;      // threads
-constexpr int PCAP = 2048, PCUT = 512;      // places of the list; it is cut beyond PCUT words, for the better bound
-constexpr int PGROUPS = 64;                 // of PT / 64 threads
+constexpr int PCAP = 512, PCUT = 256;       // places of a wavefront's list; beyond PCUT it is cut
 constexpr float LOWEST = -3.402823466e38f;
 constexpr float L2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-constexpr int NOWORD = 0x7fffffff;
 
-struct Word { float x; int id; };
-__device__ inline bool before(Word a, Word b) { return a.x > b.x || (a.x == b.x && a.id < b.id); }
-__device__ inline Word first_of(Word a, Word b) { return before(b, a) ? b : a; }
+// A word as one number: its logit's bits in ascending order above its id's complement, so that the larger number is the word that comes first (-0 counts as 0)
+typedef uint64_t Word;
+constexpr Word NOTHING = 0;   // (below every word: the bits of -inf are 0x007fffff)
+__device__ inline Word word_of(float x, int id) {
+    const uint32_t u = __float_as_uint(x + 0.f);
+    return (Word)(u & 0x80000000u ? ~u : u | 0x80000000u) << 32 | (uint32_t)~id;
+}
+__device__ inline float logit_of(Word w) {
+    const uint32_t u = (uint32_t)(w >> 32);
+    return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u);
+}
+__device__ inline int id_of_word(Word w) { return (int)~(uint32_t)w; }
+__device__ inline Word first_of(Word a, Word b) { return a > b ? a : b; }
 
 struct Sums { float m, s, t; };
 // e^d for d <= 0
@@ -53,76 +62,81 @@ __device__ inline void finish_row(const PartArgs& a, int64_t row, Sums z, float 
 
 template <typename T> __device__ inline float word_at(const T* row, int64_t i) { return to_f32(row[i]); }
 
-// What a workgroup shares
-struct ListLds {
-    Word list[PCAP];
-    Word gmax[PGROUPS];
-    Word bound;
-    int count;
-    Sums sums[PWV];
-};
-static_assert(LOGPROBS_MAX_TOP <= PGROUPS && LOGPROBS_MAX_TOP * (PCAP / PGROUPS) + LOGPROBS_MAX_TOP * (4 * PT / PGROUPS) <= PCAP, "a list that was cut takes four words of every thread");
+static_assert(LOGPROBS_MAX_TOP <= 64 && LOGPROBS_MAX_TOP * (PCAP / 64) <= PCAP - 64, "a list that was cut has room for a word of every lane");
 
-// The bound from the largest word of every thread: the top-th of the 64 groups' (groups are neighbouring threads), which `top` words of those that the threads have reach
-__device__ inline void bound_of(ListLds& l, Word mx, int top, int tid) {
-    constexpr int PER = PT / PGROUPS;
-#pragma unroll
-    for (int off = 1; off < PER; off <<= 1) mx = first_of(mx, Word{__shfl_xor(mx.x, off), __shfl_xor(mx.id, off)});
-    if (tid % PER == 0) l.gmax[tid / PER] = mx;
-    __syncthreads();
-    if (tid < PGROUPS) {
-        const Word w = l.gmax[tid];
-        int rank = 0;
-#pragma unroll 8
-        for (int i = 0; i < PGROUPS; ++i) rank += before(l.gmax[i], w) ? 1 : 0;
-        if (rank == top - 1) l.bound = first_of(l.bound, w);
-    }
-    __syncthreads();
+// A wavefront's list: n and bound are the same in all lanes
+struct List { Word* at; int n; Word bound; };
+
+__device__ inline Word lane_word(Word w, int lane) {
+    return (Word)(uint32_t)__builtin_amdgcn_readlane((int)(w >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)w, lane);
 }
-
-// The list without the words below a bound that `top` of its own reach: at most top * PCAP / PGROUPS words stay
-__device__ inline void cut_list(ListLds& l, int top, int tid) {
-    __syncthreads();
-    const int n = l.count;
-    constexpr int PER = PCAP / PT;
-    Word w[PER], mx{-INFINITY, NOWORD - tid};   // (groups without a word differ from each other)
+// A bound from the largest word of every lane (NOTHING: none): the top-th of them, which `top` words of those that the lanes have reach; none where fewer lanes have words
+__device__ inline void raise_bound(List& l, Word mx, int top) {
+    int rank = 0;
+#pragma unroll 8
+    for (int i = 0; i < 64; ++i) rank += lane_word(mx, i) > mx ? 1 : 0;
+    const uint64_t m = __ballot(rank == top - 1 && mx != NOTHING);   // (words differ, so do ranks)
+    if (m) l.bound = first_of(l.bound, lane_word(mx, __builtin_ctzll(m)));
+}
+__device__ inline int lanes_below(uint64_t m) { return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u)); }
+__device__ inline void push(List& l, Word w, bool yes) {
+    const uint64_t m = __ballot(yes);
+    if (yes) l.at[l.n + lanes_below(m)] = w;
+    l.n += (int)__popcll(m);
+}
+// Without the words below a bound that `top` of its own reach: at most top * PCAP / 64 stay
+__device__ inline void cut(List& l, int top, int lane) {
+    constexpr int PER = PCAP / 64;
+    Word w[PER], mx = NOTHING;
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
-        const int i = tid + j * PT;
-        w[j] = i < n ? l.list[i] : Word{-INFINITY, NOWORD};
-        if (i < n) mx = first_of(mx, w[j]);
+        const int i = lane + 64 * j;
+        w[j] = l.at[i];   // (whole lists are read; what is behind their ends does not count)
+        w[j] = i < l.n ? w[j] : NOTHING;
+        mx = first_of(mx, w[j]);
     }
-    bound_of(l, mx, top, tid);
-    if (tid == 0) l.count = 0;
-    __syncthreads();
-    const Word bd = l.bound;
+    raise_bound(l, mx, top);
+    const int n = l.n;
+    l.n = 0;
 #pragma unroll
-    for (int j = 0; j < PER; ++j)
-        if (tid + j * PT < n && !before(bd, w[j])) l.list[atomicAdd(&l.count, 1)] = w[j];
-    __syncthreads();
+    for (int j = 0; j < PER; ++j) push(l, w[j], lane + 64 * j < n && w[j] >= l.bound);
 }
 
-// Ranks the words of the list: put(rank, word) for the best `top`, and for the places without a word
-template <typename F> __device__ inline void rank_list(ListLds& l, int top, int tid, F put) {
-    if (l.count > PGROUPS) cut_list(l, top, tid);
-    const int n = l.count;
-    for (int i = tid; i < n || i < top; i += PT) {
-        if (i >= n) { put(i, Word{-INFINITY, NOWORD}); continue; }
-        const Word w = l.list[i];
+// What a workgroup shares
+struct ListLds {
+    Word list[PWV][PCAP];
+    int n[PWV];
+    Sums sums[PWV];
+};
+// Ranks the words of all lists: put(rank, word) for the best `top`, and for the places without a word
+template <typename F> __device__ inline void rank_lists(ListLds& s, List& l, int top, int tid, F put) {
+    const int lane = tid & 63, wave = tid >> 6;
+    if (l.n > 64) cut(l, top, lane);
+    if (lane == 0) s.n[wave] = l.n;
+    __syncthreads();
+    int total = 0;
+#pragma unroll
+    for (int w = 0; w < PWV; ++w) total += s.n[w];
+    for (int i = lane; i < l.n; i += 64) {
+        const Word me = l.at[i];
         int rank = 0;
+        for (int w = 0; w < PWV; ++w) {
+            const int n = s.n[w];
 #pragma unroll 4
-        for (int o = 0; o < n; ++o) rank += before(l.list[o], w) ? 1 : 0;
-        if (rank < top) put(rank, w);
+            for (int o = 0; o < n; ++o) rank += s.list[w][o] > me ? 1 : 0;
+        }
+        if (rank < top) put(rank, me);
     }
+    for (int i = total + tid; i < top; i += PT) put(i, NOTHING);
 }
 
 // Words [part * span, ..) of a row, a tile of PT * EPT at a time: pieces of up to 16 bytes at multiples of their size, of which the first begins at or before the part
 template <typename T, int EPT>
-__global__ void __launch_bounds__(PT) logprobs_kernel(PartArgs a) {
+__global__ void __launch_bounds__(PT, 4) logprobs_kernel(PartArgs a) {
     constexpr int C = EPT < 16 / (int)sizeof(T) ? EPT : 16 / (int)sizeof(T), U = EPT / C;
     typedef uint32_t piece __attribute__((ext_vector_type(C * sizeof(T) / 4)));
-    __shared__ ListLds l;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, top = a.top;
+    __shared__ ListLds s;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), top = a.top;
     const uint32_t row = blockIdx.x / (uint32_t)a.parts;
     const int part = (int)(blockIdx.x - row * (uint32_t)a.parts);
     const T* const x = (const T*)a.logits + row * a.stride;
@@ -146,8 +160,7 @@ __global__ void __launch_bounds__(PT) logprobs_kernel(PartArgs a) {
         }
     };
     Sums z{LOWEST, 0.f, 0.f};
-    if (tid == 0) { l.count = 0; l.bound = Word{-INFINITY, NOWORD}; }
-    __syncthreads();
+    List l{s.list[wave], 0, NOTHING};
     piece next[U];
     load(start, next);
     for (int base = start; base < v1; base += PT * EPT) {
@@ -157,14 +170,18 @@ __global__ void __launch_bounds__(PT) logprobs_kernel(PartArgs a) {
             union { piece p; T e[C]; } w;
             w.p = next[u];
 #pragma unroll
-            for (int e = 0; e < C; ++e) v[u * C + e] = base + (u * PT + tid) * C + e >= v0 ? to_f32(w.e[e]) : -INFINITY;
+            for (int e = 0; e < C; ++e) v[u * C + e] = to_f32(w.e[e]);
+        }
+        if (base < v0) {   // words before the part
+#pragma unroll
+            for (int e = 0; e < C; ++e) v[e] = base + tid * C + e >= v0 ? v[e] : -INFINITY;
         }
         if (base + PT * EPT < v1) load(base + PT * EPT, next);
         auto id_of = [&](int j) { return base + ((j / C) * PT + tid) * C + j % C; };
-        float m = z.m, big = -INFINITY;
+        float big = -INFINITY;
 #pragma unroll
         for (int j = 0; j < EPT; ++j) big = fmaxf(big, v[j]);
-        m = fmaxf(m, big);
+        const float m = fmaxf(z.m, big);
         if (m > z.m) z = moved(z, m);
 #pragma unroll
         for (int j = 0; j < EPT; ++j) {
@@ -173,50 +190,32 @@ __global__ void __launch_bounds__(PT) logprobs_kernel(PartArgs a) {
             z.t = fmaf(e, fmaxf(d, -1000.f), z.t);
         }
         if (top == 0) continue;
-        auto largest = [&](int j0, int n) {
-            Word mx{-INFINITY, NOWORD - tid};
+        if (base == start) {
+            Word mx = NOTHING;
 #pragma unroll
-            for (int j = 0; j < EPT; ++j)
-                if (j >= j0 && j < j0 + n) mx = first_of(mx, Word{v[j], id_of(j)});
-            return mx;
-        };
-        auto push = [&](int j0, int n) {
-            const Word bd = l.bound;
-            if (big >= bd.x) {
-#pragma unroll
-                for (int j = 0; j < EPT; ++j) {
-                    const Word w{v[j], id_of(j)};
-                    if (j >= j0 && j < j0 + n && w.x > -INFINITY && !before(bd, w)) {
-                        const int at = atomicAdd(&l.count, 1);
-                        if (at < PCAP) l.list[at] = w;
-                    }
-                }
-            }
-            __syncthreads();
-        };
-        if (base == start) bound_of(l, largest(0, EPT), top, tid);
-        const int had = l.count;
-        __syncthreads();
-        push(0, EPT);
-        if (l.count > PCAP) {   // more than the list holds: it is as before this tile again, and takes four words of every thread at a time, cut before by bounds from them and from itself
-            __syncthreads();
-            if (tid == 0) l.count = had;
-            for (int j0 = 0; j0 < EPT; j0 += 4) {
-                Word mx = largest(j0, 4);
-                bound_of(l, mx, top, tid);
-                cut_list(l, top, tid);
-                push(j0, 4);
-            }
-        } else if (l.count > PCUT) {
-            cut_list(l, top, tid);
+            for (int j = 0; j < EPT; ++j) mx = first_of(mx, v[j] > -INFINITY ? word_of(v[j], id_of(j)) : NOTHING);
+            raise_bound(l, mx, top);
         }
+        float least = l.bound == NOTHING ? -INFINITY : logit_of(l.bound);   // what a word's logit has to reach
+        if (__ballot(big >= least) == 0) continue;
+#pragma unroll
+        for (int j = 0; j < EPT; ++j) {
+            if (__ballot(v[j] >= least) == 0) continue;
+            const Word w = word_of(v[j], id_of(j));
+            if (l.n > PCAP - 64) {
+                cut(l, top, lane);
+                least = logit_of(l.bound);
+            }
+            push(l, w, v[j] > -INFINITY && w >= l.bound);
+        }
+        if (l.n > PCUT) cut(l, top, lane);
     }
     // the sums of the workgroup
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) z = joined(z, Sums{__shfl_xor(z.m, off), __shfl_xor(z.s, off), __shfl_xor(z.t, off)});
-    if (lane == 0) l.sums[wave] = z;
+    if (lane == 0) s.sums[wave] = z;
     __syncthreads();
-    z = l.sums[lane % PWV];
+    z = s.sums[lane % PWV];
 #pragma unroll
     for (int off = PWV / 2; off > 0; off >>= 1) z = joined(z, Sums{__shfl_xor(z.m, off), __shfl_xor(z.s, off), __shfl_xor(z.t, off)});
     if (tid == 0) {
@@ -228,45 +227,47 @@ __global__ void __launch_bounds__(PT) logprobs_kernel(PartArgs a) {
     }
     if (top == 0) return;
     const float ls = lse_of(z);
-    rank_list(l, top, tid, [&](int rank, Word w) {
+    rank_lists(s, l, top, tid, [&](int rank, Word w) {
         if (a.parts > 1) a.pword[(int64_t)blockIdx.x * top + rank] = w;
         else {
-            a.ids[(int64_t)row * top + rank] = w.id == NOWORD ? -1 : w.id;
-            a.top_lp[(int64_t)row * top + rank] = w.id == NOWORD ? -INFINITY : (w.x - z.m) - ls;
+            a.ids[(int64_t)row * top + rank] = w == NOTHING ? -1 : id_of_word(w);
+            a.top_lp[(int64_t)row * top + rank] = w == NOTHING ? -INFINITY : (logit_of(w) - z.m) - ls;
         }
     });
 }
 
-// The parts of a row: a lane has a part's sums, and the parts' words are a list
+// The parts of a row: a lane has a part's sums, and the wavefronts share the parts' words
 constexpr int PPARTS = 64;
-static_assert(PPARTS * LOGPROBS_MAX_TOP <= PCAP, "the words of all parts fit the list");
+static_assert(PPARTS * LOGPROBS_MAX_TOP <= PWV * PCAP, "the words of all parts fit the lists");
 template <typename T>
 __global__ void __launch_bounds__(PT) logprobs_join_kernel(PartArgs a) {
-    __shared__ ListLds l;
-    const int tid = threadIdx.x, lane = tid & 63, top = a.top, n = a.parts * top;
+    __shared__ ListLds s;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), top = a.top, n = a.parts * top;
     const int64_t row = blockIdx.x;
     Sums z = lane < a.parts ? a.psum[row * a.parts + lane] : Sums{LOWEST, 0.f, 0.f};
+    List l{s.list[wave], 0, NOTHING};
+    Word w[PCAP / 64];
+#pragma unroll
+    for (int j = 0; j < PCAP / 64; ++j) {
+        const int i = tid + j * PT;
+        w[j] = top ? a.pword[row * n + (i < n ? i : n - 1)] : NOTHING;
+        w[j] = i < n ? w[j] : NOTHING;
+    }
     float xt = 0.f;
     if (tid == 0) {
         const int32_t t = a.tokens ? a.tokens[row] : -1;
         if (t >= 0 && t < a.V) xt = word_at((const T*)a.logits + row * a.stride, t);
-        l.count = 0;
-        l.bound = Word{-INFINITY, NOWORD};
-    }
-    __syncthreads();
-    for (int i = tid; i < n; i += PT) {
-        const Word w = a.pword[row * n + i];
-        if (w.id != NOWORD) l.list[atomicAdd(&l.count, 1)] = w;
     }
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) z = joined(z, Sums{__shfl_xor(z.m, off), __shfl_xor(z.s, off), __shfl_xor(z.t, off)});
     if (tid == 0) finish_row(a, row, z, xt);
     if (top == 0) return;
-    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < PCAP / 64; ++j) push(l, w[j], w[j] != NOTHING);
     const float ls = lse_of(z);
-    rank_list(l, top, tid, [&](int rank, Word w) {
-        a.ids[row * top + rank] = w.id == NOWORD ? -1 : w.id;
-        a.top_lp[row * top + rank] = w.id == NOWORD ? -INFINITY : (w.x - z.m) - ls;
+    rank_lists(s, l, top, tid, [&](int rank, Word best) {
+        a.ids[row * top + rank] = best == NOTHING ? -1 : id_of_word(best);
+        a.top_lp[row * top + rank] = best == NOTHING ? -INFINITY : (logit_of(best) - z.m) - ls;
     });
 }
 
