@@ -304,7 +304,8 @@ __global__ void __launch_bounds__(256) kvp_scores_weights_kernel(const float* __
 #pragma unroll 4
         for (int cn = 0; cn < cols; ++cn) {
             const float2 z = st[(int64_t)(cn / G) * H + cn % G];
-            w = fmaf(__builtin_amdgcn_exp2f(at[(int64_t)(g * cols + cn) * stride] - z.x), z.y, w);
+            const float x = at[(int64_t)(g * cols + cn) * stride];
+            w += x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x - z.x) * z.y;   // (unseen by the column, whose sum may be NaN)
         }
     }
     sq.weight[b][key] = decay == 0.f ? w : decay * sq.weight[b][key] + w;
@@ -318,7 +319,7 @@ __global__ void __launch_bounds__(256) kvp_add_weights_kernel(const float* __res
     const int key = ((int)blockIdx.x - first) * 256 + threadIdx.x, n = sq.count[b], parts = sq.parts[b];
     if (key >= n) return;
     float w = 0.f;
-#pragma unroll 4
+#pragma unroll 16
     for (int p = 0; p < parts; ++p) w += sums[(int64_t)sq.at[b] + (int64_t)p * n + key];
     sq.weight[b][key] = decay == 0.f ? w : decay * sq.weight[b][key] + w;
 }
@@ -473,6 +474,7 @@ static hipError_t launch_kvp_attn_t(const T* q, const PagedPool& pool, const Pag
         if (most <= 2) kvp_merge_few_kernel<T, D, NB, 2><<<grid, dim3(MERGE_T), 0, s>>>(sh, sq, (uint32_t)(n * H), H, Hkv, stats, out);
         else if (most <= 4) kvp_merge_few_kernel<T, D, NB, 4><<<grid, dim3(MERGE_T), 0, s>>>(sh, sq, (uint32_t)(n * H), H, Hkv, stats, out);
         else if (most <= 8) kvp_merge_few_kernel<T, D, NB, 8><<<grid, dim3(MERGE_T), 0, s>>>(sh, sq, (uint32_t)(n * H), H, Hkv, stats, out);
+        else if (most <= 16) kvp_merge_few_kernel<T, D, NB, 16><<<grid, dim3(MERGE_T), 0, s>>>(sh, sq, (uint32_t)(n * H), H, Hkv, stats, out);
         else kvp_merge_kernel<T, D, NB><<<dim3((unsigned)(n * H)), dim3(MERGE_T), 0, s>>>(sh, sq, H, Hkv, stats, out);
     }
     if (add) {
@@ -543,7 +545,7 @@ static hipError_t launch_kvp_attn_d(const T* q, const PagedPool& pool, const Pag
 
 hipError_t launch_kvp_attn(const void* q, const PagedPool& pool, const PagedBatch& pb, int H, int Hkv, int d, float* part, size_t part_floats, void* out, bool add, float decay,
                            bool bf16, hipStream_t s) {
-    if (pb.n < 1 || pb.n > DECODE_MAX_BATCH || pb.off[pb.n] < 1) return hipErrorInvalidValue;
+    if (pb.n < 1 || pb.n > DECODE_MAX_BATCH || pb.off[pb.n] < 1 || pb.off[pb.n] * H > 0x7fffffff) return hipErrorInvalidValue;
     return bf16 ? launch_kvp_attn_d<bf16_t>((const bf16_t*)q, pool, pb, H, Hkv, d, part, part_floats, (bf16_t*)out, add, decay, s)
                 : launch_kvp_attn_d<float>((const float*)q, pool, pb, H, Hkv, d, part, part_floats, (float*)out, add, decay, s);
 }

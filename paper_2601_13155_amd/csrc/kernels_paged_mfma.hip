@@ -528,9 +528,9 @@ __global__ void __launch_bounds__(NW * 64, 2) kvp_few_kernel(const bf16_t* q, Po
 
 // ------------------------------------------------------------------ accounts of many columns
 // Column sums of the probabilities, the scores anew: storing them would be more bytes than the products cost.  A workgroup has 256 keys, a wavefront 64 of them in registers, and
-// goes over the blocks of 32 columns of its part of (head, block); the queries of a block and the columns' maxima and 1 / sums come into LDS by direct loads, two blocks ahead in a ring of four.
-// While the scores of one half of a wavefront's keys are on the matrix core, the lane takes the exponentials of the other half: an exponential, a multiplication and two additions a
-// score bound the kernel.
+// goes over the blocks of 32 columns of its part of (head, block); the queries of a block and the columns' maxima and 1 / sums come into LDS by direct loads, three blocks ahead in a ring
+// of four.  While the scores of the next block are on the matrix core, the lane takes the exponentials of this one's; a step is one operand read ahead, two matrix instructions
+// and four exponentials (operands read where they are used instead: 792 us for 2048 tokens after 30720 rows, so 682).
 constexpr int WW = 4, WST = 4;
 template <int D, int NB>
 __global__ void __launch_bounds__(WW * 64, 2) kvp_weights_mfma_kernel(const bf16_t* __restrict__ q, PoolView pool, PagedSeqs<NB> sq, int H, int Hkv, DivG dg, float c,
@@ -556,25 +556,22 @@ __global__ void __launch_bounds__(WW * 64, 2) kvp_weights_mfma_kernel(const bf16
     const int lrow = lane / L::CPR, lchunk = lane % L::CPR;
     // head and block of the next block to load
     int lg = (int)(i0 / each), lblk = skip + (int)(i0 % each);
+    constexpr int EACH = (LOADS + WW - 1) / WW + 1;   // loads of every wavefront a block: its share of the queries and, each the same, the statistics
     auto issue = [&](int i) __attribute__((always_inline)) {
         const int st = i % WST;
         auto head_of = [&](int cn) {
             cn = cn < cols ? cn : cols - 1;
             const uint32_t qi = div_g((uint32_t)cn, dg);
-            return (int64_t)(sq.first[b] + (int)qi) * H + lg * G + (cn - (int)qi * G);
+            return (uint32_t)((sq.first[b] + (int)qi) * H + lg * G + (cn - (int)qi * G));   // (queries times heads stay below 2^31: checked on the host)
         };
 #pragma unroll
-        for (int j = 0; j < LOADS; j += WW) {
-            const int ld = j + wave;
-            if (LOADS % WW == 0 || ld < LOADS) {
-                const int row = ld * L::ROWS_PER_LOAD + lrow;
-                dma16(q + head_of(lblk * 32 + row) * D + ((lchunk ^ L::kswz(row)) << 3), lds0 + (uint32_t)(st * BLOCK + ld * 1024));
-            }
+        for (int j = 0; j < EACH - 1; ++j) {
+            const int ld = (j * WW + wave) % LOADS, row = ld * L::ROWS_PER_LOAD + lrow;
+            dma16(q + (int64_t)head_of(lblk * 32 + row) * D + ((lchunk ^ L::kswz(row)) << 3), lds0 + (uint32_t)(st * BLOCK + ld * 1024));
         }
-        if (wave == WW - 1) dma4_nt((const float*)(stats + head_of(lblk * 32 + (lane >> 1))) + (lane & 1), st0 + (uint32_t)(st * 256));
+        dma4_nt((const float*)(stats + head_of(lblk * 32 + (lane >> 1))) + (lane & 1), st0 + (uint32_t)(st * 256));
         if (++lblk == blocks) { lblk = skip; ++lg; }
     };
-    constexpr int MINE = (LOADS + WW - 1) / WW;   // loads of a wavefront a block, at most (and one more of the last)
 
     f32x16 acc[2] = {zero16(), zero16()};
     bf16x8 kf[2][KS];
@@ -595,47 +592,62 @@ __global__ void __launch_bounds__(WW * 64, 2) kvp_weights_mfma_kernel(const bf16
             for (int ks = 0; ks < KS; ++ks) kf[h][ks] = *reinterpret_cast<const bf16x8*>((const bf16_t*)pool.k + krow[h] + g * head_step + 16 * ks);
     };
     auto frag = [&](uint32_t at, int ks) { return *(const __attribute__((address_space(3))) bf16x8*)(uintptr_t)(at ^ (uint32_t)(ks << 5)); };
-    // scores of half h of the keys with the block at `at` into SN, while the exponentials of the other half's scores SC are added to its account
-    auto half_step = [&](int h, uint32_t at, f32x16& SN, f32x16& SC, f32x16& a, float2 st, int first_key, int seen, bool masked) __attribute__((always_inline)) {
-        constexpr int EPS = 16 / KS;
+    // scores of the block at `at` into N, while the exponentials of the block before it, C, are added to the accounts
+    constexpr int FD = KS > 2 ? 3 : 1, EPS = 16 / KS;
+    auto step = [&](uint32_t at, f32x16 (&N)[2], f32x16 (&C)[2], float2 st) __attribute__((always_inline)) {
+        bf16x8 fr[FD + 1];
+#pragma unroll
+        for (int ks = 0; ks < FD; ++ks) fr[ks] = frag(at, ks);
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-            SN = mfma32(kf[h][ks], frag(at, ks), ks == 0 ? zero16() : SN);
+            if (ks + FD < KS) fr[(ks + FD) % (FD + 1)] = frag(at, ks + FD);
 #pragma unroll
-            for (int e = ks * EPS; e < (ks + 1) * EPS; ++e) {
-                const float p = __builtin_amdgcn_exp2f(fmaf(SC[e], c, -st.x)) * st.y;
-                a[e] += !masked || first_key + 8 * (e >> 2) + 4 * lh + (e & 3) < seen ? p : 0.f;
+            for (int h = 0; h < 2; ++h) {
+                N[h] = mfma32(kf[h][ks], fr[ks % (FD + 1)], ks == 0 ? zero16() : N[h]);
+#pragma unroll
+                for (int e = ks * EPS; e < (ks + 1) * EPS; ++e) acc[h][e] = fmaf(__builtin_amdgcn_exp2f(fmaf(C[h][e], c, -st.x)), st.y, acc[h][e]);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    auto stats_of = [&](int i) { return col_stats[i % WST][l32]; };
     if (steps > 0) {
-        for (int i = 0; i < 2 && i < steps; ++i) issue(i);
+        for (int i = 0; i < 3 && i < steps; ++i) issue(i);
         int g = (int)(i0 / each), blk = skip + (int)(i0 % each);
         load_keys(g);
         SPTS_WAIT_VMCNT(0);
         __syncthreads();
-        f32x16 S0 = zero16(), S1;
+        f32x16 sa[2], sb[2];
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) S0 = mfma32(kf[0][ks], frag(lds0 + kplace, ks), ks == 0 ? zero16() : S0);
-        for (int i = 0; i < steps; ++i) {
-            // block i + 1 has landed for everyone, and block i - 2's place is free
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) sa[h] = mfma32(kf[h][ks], frag(lds0 + kplace, ks), ks == 0 ? zero16() : sa[h]);
+        auto block = [&](int i, f32x16 (&N)[2], f32x16 (&C)[2]) __attribute__((always_inline)) {
+            if (i >= steps) return;
+            // block i + 1 has landed for everyone, and block i - 1's place is free
             if (i > 0) {
-                SPTS_WAIT_VMCNT(0);
+                if (i + 2 < steps) { SPTS_WAIT_VMCNT(EACH); } else { SPTS_WAIT_VMCNT(0); }
                 __syncthreads();
             }
-            if (i + 2 < steps) issue(i + 2);
-            const float2 st = stats_of(i);
+            if (i + 3 < steps) issue(i + 3);
+            float2 st = col_stats[i % WST][l32];
             const int col = blk * 32 + l32;
-            const int seen = col < cols ? n - nq + (int)div_g((uint32_t)col, dg) + 1 : 0;
+            const int seen = (col < cols ? n - nq + (int)div_g((uint32_t)col, dg) + 1 : 0) - key0 - 4 * lh;   // of the lane's keys, from its first one
             const bool masked = blk * 32 + 32 > cols || n - nq + (int)div_g((uint32_t)(blk * 32), dg) + 1 < key0 + 64;
-            const uint32_t here = lds0 + (uint32_t)(i % WST * BLOCK) + kplace, ahead = lds0 + (uint32_t)((i + 1) % WST * BLOCK) + kplace;
-            if (masked) half_step(1, here, S1, S0, acc[0], st, key0, seen, true);
-            else half_step(1, here, S1, S0, acc[0], st, key0, seen, false);
             if (++blk == blocks) { blk = skip; if (++g < Hkv && i + 1 < steps) load_keys(g); }
-            if (masked) half_step(0, ahead, S0, S1, acc[1], st, key0 + 32, seen, true);
-            else half_step(0, ahead, S0, S1, acc[1], st, key0 + 32, seen, false);
+            const uint32_t at = lds0 + (uint32_t)((i + 1) % WST * BLOCK) + kplace;
+            if (masked) {   // unseen keys weigh nothing, not even of a column whose sum is NaN
+                const bool odd = !(st.y < INFINITY);
+                st.y = odd ? 1.f : st.y;
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) C[h][e] = 32 * h + 8 * (e >> 2) + (e & 3) < seen ? (odd ? NAN : C[h][e]) : -INFINITY;
+            }
+            step(at, N, C, st);
+        };
+        for (int i = 0; i < steps; i += 2) {
+            block(i, sb, sa);
+            block(i + 1, sa, sb);
         }
     }
 #pragma unroll

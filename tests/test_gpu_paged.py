@@ -105,6 +105,13 @@ def test_rows_that_a_query_does_not_see_do_not_matter(dtype, rows, new):
     err = (out[:good].cpu().double() - want).abs()
     assert bool((err <= attend_bound(want, spread, big, n, 64, dtype, True)).all())
     assert not torch.isfinite(out[-1]).all()
+    # a query that is NaN itself makes the accounts of the rows that it sees NaN, and only those
+    put(kv, 0, 0, *host[0])
+    q[m // 3, 3] = math.nan
+    run_attn(ctx, kv, q, new, 1, 0.0)
+    w = kv.weight[0].cpu()
+    sees = n - m + m // 3 + 1
+    assert torch.isnan(w[:sees]).all() and torch.isfinite(w[sees:n]).all()
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
