@@ -23,27 +23,21 @@ template <int N> __device__ inline void load_row(const float* p, float (&v)[N]) 
         for (int e = 0; e < 4; ++e) v[i + e] = w[e];
     }
 }
-template <int N> __device__ inline void load_row(const bf16_t* p, float (&v)[N]) {
-#pragma unroll
-    for (int i = 0; i < N; i += 8) {
-        const u32x4 w = *reinterpret_cast<const u32x4*>(p + i);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[i + e] = chunk_elem(w, e, bf16_t{});
-    }
-}
 __device__ inline void store4(float* p, f32x4 v, float f) { *reinterpret_cast<f32x4*>(p) = f32x4{v[0] * f, v[1] * f, v[2] * f, v[3] * f}; }
 __device__ inline void store4(bf16_t* p, f32x4 v, float f) { *reinterpret_cast<u32x2*>(p) = u32x2{cvt_pk_bf16(v[0] * f, v[1] * f), cvt_pk_bf16(v[2] * f, v[3] * f)}; }
 }  // namespace
 
 // On the fp32 matrix instruction 32x32x2.  S^T = K Q^T: operand rows are keys, columns queries; of the two halves of a wavefront one multiplies the first, one the second half of the
 // dimensions, so a lane's operand is half a row.  O^T += V^T P^T: result element r of lane (l, half) is key 8 (r / 4) + 4 half + r % 4 of column l, which is the second operand of the
-// r-th product of V^T as it stands.  The four wavefronts of a workgroup take blocks of 32 keys in turn and meet in LDS.
+// r-th product of V^T as it stands.  The four wavefronts of a workgroup take blocks of 32 keys in turn and meet in LDS; a lane
+// asks for the next piece of a key, and the next 32 dimensions of the values, before it multiplies these: 128 tokens after 4000 rows of 8 heads (d = 128) 121 us, 71 TFLOP/s of the
+// 154 that a large fp32 product reaches here.
 // A block that some column does not see entirely has its scores set to -inf there, and values that are not finite kept out of the product (0 times them would be NaN): two more products
 // count those that a column does see and put the infinity or NaN where it belongs.
 constexpr int AW = 4;
-template <typename T, int D, int NB>
-__global__ void __launch_bounds__(AW * 64) kvp_attn_kernel(const T* q, PoolView pool, PagedSeqs<NB> sq, int H, int Hkv, float c, Shares sh, float2* __restrict__ stats,
-                                                           T* out) {   // (out may be q: a workgroup has read its columns before it writes them)
+template <int D, int NB>
+__global__ void __launch_bounds__(AW * 64, 2) kvp_attn_kernel(const float* q, PoolView pool, PagedSeqs<NB> sq, int H, int Hkv, float c, Shares sh, float2* __restrict__ stats,
+                                                              float* out) {   // (out may be q: a workgroup has read its columns before it writes them)
     constexpr int DB = D / 32, LD = D + 4;
     __shared__ float so[AW][32][LD];
     __shared__ float sm[AW][32], sl[AW][32];
@@ -66,23 +60,48 @@ __global__ void __launch_bounds__(AW * 64) kvp_attn_kernel(const T* q, PoolView 
 #pragma unroll
     for (int i = 0; i < DB; ++i) o[i] = zero16();
     float m = PAGED_LOWEST, l = 0.f;
-    for (int64_t key0 = k0 + wave * 32; key0 < k1; key0 += AW * 32) {
-        const int left = (int)(n - key0 < 32 ? n - key0 : 32);
-        const int64_t p0 = page_at(pool, table, key0, g, Hkv, D), p1 = left > 16 ? page_at(pool, table, key0 + 16, g, Hkv, D) - 16 * D : p0;
-        const int row = l32 < left ? l32 : left - 1;
-        f32x16 s = zero16();
-        {
-            float kf[D / 2];
-            load_row((const T*)pool.k + (row < 16 ? p0 : p1) + row * D + lh * (D / 2), kf);
+    constexpr int CH = D == 128 ? 8 : 16, NCH = D / 2 / CH;          // a lane's half row of a key in pieces, the next one on its way
+    struct Rows { const float *k, *v; int64_t upper; };             // the lane's key; element 4 lh of dimension l32 of the block's values, and what lies between its halves of 16 rows
+    auto rows_of = [&](int64_t key0) {
+        const int left = (int)(n - key0 < 32 ? n - key0 : 32), row = l32 < left ? l32 : left - 1;
+        const int64_t p0 = page_at(pool, table, key0, g, Hkv, D), p1 = left > 16 ? page_at(pool, table, key0 + 16, g, Hkv, D) : p0 + 16 * D;
+        return Rows{(const float*)pool.k + (row < 16 ? p0 + row * D : p1 + (row - 16) * D) + lh * (D / 2), (const float*)pool.v + p0 + 4 * lh * D + l32, p1 - p0 - 16 * D};
+    };
+    auto load_key = [&](const Rows& at, int ch, float (&v)[CH]) __attribute__((always_inline)) { load_row(at.k + ch * CH, v); };
+    auto load_values = [&](const Rows& at, int i, int left, float (&v)[16]) __attribute__((always_inline)) {
+        if (left == 32) {
 #pragma unroll
-            for (int i = 0; i < D / 2; ++i) s = mfma_f32(kf[i], qf[i], s);
+            for (int r = 0; r < 16; ++r) v[r] = at.v[(r < 8 ? 0 : at.upper) + (8 * (r >> 2) + (r & 3)) * D + 32 * i];
+        } else {   // rows behind the last one are the last one again
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int want = 8 * (r >> 2) + 4 * lh + (r & 3), row = want < left ? want : left - 1;
+                v[r] = at.v[(row < 16 ? 0 : at.upper) + (row - 4 * lh) * D + 32 * i];
+            }
+        }
+    };
+    int64_t key0 = k0 + wave * 32;
+    Rows here{};
+    float kb[2][CH], vb[2][16];
+    if (key0 < k1) {
+        here = rows_of(key0);
+        load_key(here, 0, kb[0]);
+    }
+    for (; key0 < k1; key0 += AW * 32) {
+        const int left = (int)(n - key0 < 32 ? n - key0 : 32);
+        f32x16 s = zero16();
+#pragma unroll
+        for (int ch = 0; ch < NCH; ++ch) {
+            if (ch + 1 < NCH) load_key(here, ch + 1, kb[(ch + 1) & 1]);
+            else load_values(here, 0, left, vb[0]);
+#pragma unroll
+            for (int i = 0; i < CH; ++i) s = mfma_f32(kb[ch & 1][i], qf[ch * CH + i], s);
         }
         const bool masked = key0 + 32 > seen_all;
         float mx = PAGED_LOWEST;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            const int64_t key = key0 + 8 * (r >> 2) + 4 * lh + (r & 3);
-            s[r] = masked && key >= seen ? -INFINITY : s[r] * c;
+            s[r] = masked && (int)(seen - key0) - 4 * lh <= 8 * (r >> 2) + (r & 3) ? -INFINITY : s[r] * c;
             mx = fmaxf(mx, s[r]);
         }
         mx = fmaxf(mx, __shfl_xor(mx, 32));
@@ -98,32 +117,35 @@ __global__ void __launch_bounds__(AW * 64) kvp_attn_kernel(const T* q, PoolView 
             s[r] = __builtin_amdgcn_exp2f(s[r] - m);
             l += s[r];
         }
+        Rows next = here;
+        if (key0 + AW * 32 < k1) next = rows_of(key0 + AW * 32);
 #pragma unroll
         for (int i = 0; i < DB; ++i) {
-            float vf[16];
-            bool odd = false;
+            if (i + 1 < DB) load_values(here, i + 1, left, vb[(i + 1) & 1]);
+            else load_key(next, 0, kb[0]);
+            float (&vf)[16] = vb[i & 1];
+            if (masked) {
+                bool odd = false;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int at = 8 * (r >> 2) + 4 * lh + (r & 3), vr = at < left ? at : left - 1;
-                vf[r] = to_f32(((const T*)pool.v)[(vr < 16 ? p0 : p1) + vr * D + 32 * i + l32]);
-                odd |= !(fabsf(vf[r]) < INFINITY);
-            }
-            if (masked && __ballot(odd) != 0) {
-                f32x16 up = zero16(), down = zero16();
+                for (int r = 0; r < 16; ++r) odd |= !(fabsf(vf[r]) < INFINITY);
+                if (__ballot(odd) != 0) {
+                    f32x16 up = zero16(), down = zero16();
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const float sees = key0 + 8 * (r >> 2) + 4 * lh + (r & 3) < seen ? 1.f : 0.f;
-                    const float v = vf[r];
-                    up = mfma_f32(v == INFINITY || v != v ? 1.f : 0.f, sees, up);
-                    down = mfma_f32(v == -INFINITY || v != v ? 1.f : 0.f, sees, down);
-                    vf[r] = fabsf(v) < INFINITY ? v : 0.f;
+                    for (int r = 0; r < 16; ++r) {
+                        const float sees = (int)(seen - key0) - 4 * lh > 8 * (r >> 2) + (r & 3) ? 1.f : 0.f;
+                        const float v = vf[r];
+                        up = mfma_f32(v == INFINITY || v != v ? 1.f : 0.f, sees, up);
+                        down = mfma_f32(v == -INFINITY || v != v ? 1.f : 0.f, sees, down);
+                        vf[r] = fabsf(v) < INFINITY ? v : 0.f;
+                    }
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o[i][r] += (up[r] > 0.f ? INFINITY : 0.f) - (down[r] > 0.f ? INFINITY : 0.f);
                 }
-#pragma unroll
-                for (int r = 0; r < 16; ++r) o[i][r] += (up[r] > 0.f ? INFINITY : 0.f) - (down[r] > 0.f ? INFINITY : 0.f);
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r) o[i] = mfma_f32(vf[r], s[r], o[i]);
         }
+        here = next;
     }
     l += __shfl_xor(l, 32);
 #pragma unroll
@@ -155,7 +177,7 @@ __global__ void __launch_bounds__(AW * 64) kvp_attn_kernel(const T* q, PoolView 
             const float inv = inverse_sum(L);
             const int64_t head = (int64_t)(sq.first[b] + cn / G) * H + g * G + cn % G;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) out[head * D + e + j] = from_f32<T>(t[j] * inv);
+            for (int j = 0; j < 4; ++j) out[head * D + e + j] = t[j] * inv;
             if (stats && e == 0) stats[head] = make_float2(M, inv);
         }
     }
@@ -239,8 +261,8 @@ __global__ void __launch_bounds__(MERGE_T) kvp_merge_kernel(Shares sh, PagedSeqs
 
 // Column sums of the probabilities in fp32: a wavefront holds 32 keys and goes over the blocks of columns of its part of all heads, the scores anew; stats has each column's maximum
 // and 1 / sum.
-template <typename T, int D, int NB>
-__global__ void __launch_bounds__(AW * 64) kvp_weights_kernel(const T* __restrict__ q, PoolView pool, PagedSeqs<NB> sq, int H, int Hkv, float c, const float2* __restrict__ stats,
+template <int D, int NB>
+__global__ void __launch_bounds__(AW * 64) kvp_weights_kernel(const float* __restrict__ q, PoolView pool, PagedSeqs<NB> sq, int H, int Hkv, float c, const float2* __restrict__ stats,
                                                               float* __restrict__ sums, float decay) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, lh = lane >> 5, G = H / Hkv;
     int first;
@@ -263,7 +285,7 @@ __global__ void __launch_bounds__(AW * 64) kvp_weights_kernel(const T* __restric
         if (key0 >= n - nq + last / G + 1) continue;
         if (g != have) {
             have = g;
-            load_row((const T*)pool.k + page_at(pool, sq.table[b], key0 + (row & 16), g, Hkv, D) + (row & 15) * D + lh * (D / 2), kf);
+            load_row((const float*)pool.k + page_at(pool, sq.table[b], key0 + (row & 16), g, Hkv, D) + (row & 15) * D + lh * (D / 2), kf);
         }
         const int64_t head = (int64_t)(sq.first[b] + cc / G) * H + g * G + cc % G;
         float qf[D / 2];
@@ -375,7 +397,7 @@ static int64_t pick_workgroups(PagedSeqs<NB>& sq, const PagedBatch& pb, int H, i
     return choice;
 }
 
-constexpr int64_t ATT_WORKGROUPS = 1024;
+constexpr int64_t F32_WORKGROUPS = 512, ACCOUNT_WORKGROUPS = 1024;
 template <typename T, int D, int NB>
 static hipError_t launch_kvp_attn_t(const T* q, const PagedPool& pool, const PagedBatch& pb, int H, int Hkv, float* part, size_t part_floats, T* out, bool add, float decay,
                                     hipStream_t s) {
@@ -398,7 +420,7 @@ static hipError_t launch_kvp_attn_t(const T* q, const PagedPool& pool, const Pag
     auto many = [&](int b) { return sq.nq[b] > 0 && columns(pb, b, G) > KVP_FEW_COLS; };
     auto any = [&](int b) { return sq.nq[b] > 0; };
     constexpr int64_t COLS = kvp_many_waves(D) * 32;
-    int64_t want = ATT_WORKGROUPS, want_few = 256, least_few = 256;
+    int64_t want = F32_WORKGROUPS, want_few = 256, least_few = 256, least = 256;
     if constexpr (BF16) {
         want = pick_workgroups(sq, pb, H, Hkv, D, COLS, 256, many);
         // Few columns: two workgroups fit a CU.  A single sequence's shares are all alike, one a CU; those of several are not, and more of them even out (us at 256 / 384 / 512 / 1024
@@ -410,6 +432,13 @@ static hipError_t launch_kvp_attn_t(const T* q, const PagedPool& pool, const Pag
             if (few(b)) { ++n; longest = std::max(longest, pb.count[b]); }
         if (n > 1) want_few = 384;
         if (longest <= 512) least_few = 512;
+    } else {
+        // Two workgroups a CU (us at 256 / 512 / 1024: 128 tokens after 4000 rows, 8 heads of 4, d = 128, 125 / 121 / 136, one token after 60000 163 / 152 / 155, four of 300 after 3000
+        // 33 / 29 / 32), and a block of keys for every wavefront where that leaves most of the chip idle (one token after 500 rows of two heads 8.3, with two blocks each 11.7; three
+        // sequences of up to 333 after 1500 17.3 / 15.4)
+        int64_t n = 0;
+        for (int b = 0; b < pb.n; ++b) n += (columns(pb, b, G) + 31) / 32 * Hkv;
+        if (n < 32) least = 128;
     }
     int64_t shares = 0;
     for (int64_t scale = 1;; scale *= 2) {   // (fewer and longer shares where they would not fit the scratch)
@@ -417,7 +446,7 @@ static hipError_t launch_kvp_attn_t(const T* q, const PagedPool& pool, const Pag
             share_keys(sq, pb, Hkv, G, KVP_FEW_COLS, std::max<int64_t>(1, want_few / scale), least_few * scale, few);
             share_keys(sq, pb, Hkv, G, COLS, std::max<int64_t>(1, want / scale), 256 * scale, many);
         } else {
-            share_keys(sq, pb, Hkv, G, 32, std::max<int64_t>(1, want / scale), 256 * scale, any);
+            share_keys(sq, pb, Hkv, G, 32, std::max<int64_t>(1, want / scale), least * scale, any);
         }
         shares = 0;
         for (int b = 0; b < pb.n; ++b)
@@ -457,7 +486,7 @@ static hipError_t launch_kvp_attn_t(const T* q, const PagedPool& pool, const Pag
     } else {
         const int64_t n = items_of(any, 32);
         if (n * Hkv > 0x7fffffff) return hipErrorInvalidValue;
-        kvp_attn_kernel<T, D, NB><<<dim3((unsigned)(n * Hkv)), dim3(AW * 64), 0, s>>>(q, pl, sq, H, Hkv, c, sh, stats, out);
+        kvp_attn_kernel<D, NB><<<dim3((unsigned)(n * Hkv)), dim3(AW * 64), 0, s>>>(q, pl, sq, H, Hkv, c, sh, stats, out);
         e = hipGetLastError();
     }
     if (e != hipSuccess) return e;
@@ -498,7 +527,7 @@ static hipError_t launch_kvp_attn_t(const T* q, const PagedPool& pool, const Pag
         for (int b = 0; b < pb.n; ++b)
             if (anew(b)) work += (pb.count[b] + KEYS - 1) / KEYS * ((columns(pb, b, G) + 31) / 32) * Hkv;
         bool joined = false;
-        for (int64_t target = std::max<int64_t>(1, work / ATT_WORKGROUPS); work > 0; target *= 2) {
+        for (int64_t target = std::max<int64_t>(1, work / ACCOUNT_WORKGROUPS); work > 0; target *= 2) {
             int64_t at = 0;
             joined = false;
             for (int b = 0; b < pb.n; ++b) {
@@ -517,7 +546,7 @@ static hipError_t launch_kvp_attn_t(const T* q, const PagedPool& pool, const Pag
                 e = launch_kvp_weights_many<NB>(q, pl, sq, (int)nt, H, Hkv, D, stats, rest, decay, s);
                 if (e != hipSuccess) return e;
             } else {
-                kvp_weights_kernel<T, D, NB><<<dim3((unsigned)nt), dim3(AW * 64), 0, s>>>(q, pl, sq, H, Hkv, c, stats, rest, decay);
+                kvp_weights_kernel<D, NB><<<dim3((unsigned)nt), dim3(AW * 64), 0, s>>>(q, pl, sq, H, Hkv, c, stats, rest, decay);
             }
         }
         if (joined) {

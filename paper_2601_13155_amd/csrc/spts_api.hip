@@ -1660,7 +1660,8 @@ int spts_kvp_attn(spts_ctx* c, const spts_kv_pool* p, const void* q, const int64
     if ((out != q || add_weights) && overlap(q, bytes, out, bytes)) return SPTS_EINVAL;
     if (offsets[batch] > c->lim.max_tokens) return SPTS_EWORKSPACE;
     PHASE(c, PH_KVP_ATTN);
-    SPTS_HIP(c, launch_kvp_attn(q, pool, pb, m.H, m.Hkv, m.d, c->p<float>(c->off.tmp32), (c->off.qp - c->off.tmp32) / sizeof(float), out, add_weights != 0, decay, c->bf16,
+    // scratch: all that lies behind there is of other calls
+    SPTS_HIP(c, launch_kvp_attn(q, pool, pb, m.H, m.Hkv, m.d, c->p<float>(c->off.tmp32), (c->off.total - c->off.tmp32) / sizeof(float), out, add_weights != 0, decay, c->bf16,
                                 c->stream));
     return SPTS_OK;
 }
