@@ -220,6 +220,14 @@ def _check(status: int, where: str):
         raise SptsError(status, where)
 
 
+def _need(t, what: str, least: int, dtype):
+    """ValueError where a tensor is not a contiguous device tensor of dtype with at least `least` elements (addresses and None pass: the C call judges those)."""
+    if t is None or isinstance(t, int):
+        return
+    if t.dtype is not dtype or t.numel() < least or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{what}: {least} contiguous elements of {dtype} on the GPU needed, got {t.dtype} {list(t.shape)} on {t.device}")
+
+
 def model_desc(shape) -> spts_model_desc:
     """shape: any object with D, H, Hkv, d, Dff, rms_eps, rope_base, dtype ('f32' | 'bf16')."""
     return spts_model_desc(shape.D, shape.H, shape.Hkv, shape.d, shape.Dff, shape.rms_eps, shape.rope_base,
@@ -275,6 +283,8 @@ class Context:
         if not torch.cuda.is_available():
             raise RuntimeError("libspts needs a GPU: no device is visible (there is no CPU fallback)")
         self.shape = shape
+        self.f32, self.bf16, self.i32 = torch.float32, torch.bfloat16, torch.int32
+        self.elem = self.bf16 if shape.dtype == "bf16" else self.f32
         self.model = model_desc(shape)
         nbytes = spts_workspace_bytes(self.model, max_tokens, max_probe, max_r, max_dlow)
         if nbytes == 0:
@@ -432,11 +442,15 @@ class Context:
         _check(load().spts_process_logits(self.handle, _ptr(logits), V, batch, C.byref(rules), _ptr(logits_out), _ptr(token_out),
                                           _ptr(table), _ptr(x_next)), "spts_process_logits")
 
-    # ---- caches in pages
+    # ---- caches in pages.  Tensors of another type, of too few elements or with gaps are a ValueError.
     def spts_kvp_append(self, pool: spts_kv_pool, k, v, pos, offsets, caches):
         """offsets [batch+1]: host integers or binding.host_i64; caches: a list of spts_kvp (count fields updated in place) or a
         ctypes array of them."""
         off = _host(offsets, C.c_int64, len(caches) + 1, "offsets")
+        n = off[len(caches)]
+        _need(k, "k", n * self.shape.Hkv * self.shape.d, self.elem)
+        _need(v, "v", n * self.shape.Hkv * self.shape.d, self.elem)
+        _need(pos, "pos", n, self.i32)
         arr, copied = _caches(caches, spts_kvp)
         _check(load().spts_kvp_append(self.handle, C.byref(pool), _ptr(k), _ptr(v), _ptr(pos), off, len(caches), arr), "spts_kvp_append")
         if copied:
@@ -446,6 +460,9 @@ class Context:
     def spts_kvp_attn(self, pool: spts_kv_pool, q, offsets, caches, out, add_weights: int = 0, decay: float = 1.0):
         arr, _ = _caches(caches, spts_kvp)
         off = _host(offsets, C.c_int64, len(caches) + 1, "offsets")
+        n = off[len(caches)] * self.shape.H * self.shape.d
+        _need(q, "q", n, self.elem)
+        _need(out, "out", n, self.elem)
         _check(load().spts_kvp_attn(self.handle, C.byref(pool), _ptr(q), off, len(caches), arr, _ptr(out), add_weights, decay), "spts_kvp_attn")
 
     def spts_kvp_evict(self, pool: spts_kv_pool, keep, caches, keep_below=None, keep_from=None, old_out=None):
@@ -454,21 +471,29 @@ class Context:
         arr, copied = _caches(caches, spts_kvp)
         first = None if keep_below is None else _host(keep_below, C.c_int32, n, "keep_below")
         late = None if keep_from is None else _host(keep_from, C.c_int32, n, "keep_from")
-        _check(load().spts_kvp_evict(self.handle, C.byref(pool), _host(keep, C.c_int64, n, "keep"), first, late, n, arr, _ptr(old_out)), "spts_kvp_evict")
+        stay = _host(keep, C.c_int64, n, "keep")
+        if old_out is not None:
+            _need(old_out, "old_out", sum(min(int(arr[b].count), stay[b]) for b in range(n)), self.i32)
+        _check(load().spts_kvp_evict(self.handle, C.byref(pool), stay, first, late, n, arr, _ptr(old_out)), "spts_kvp_evict")
         if copied:
             for dst, src in zip(caches, arr):
                 dst.count = src.count
 
     def spts_token_logprobs(self, logits, V: int, rows: int, tokens=None, logprob=None, entropy=None, n_top: int = 0, top_ids=None, top_logprobs=None,
                             stride: Optional[int] = None):
-        """logits: fp32 or bf16 device tensor, the type is taken from it (ValueError otherwise); stride: elements from a row to the next (None = that of a
-        tensor of two dimensions, V otherwise)."""
-        import torch
-        if logits.dtype not in (torch.float32, torch.bfloat16) or (logits.dim() > 0 and logits.stride(-1) != 1):
-            raise ValueError(f"logits: rows of float32 or bfloat16, not {logits.dtype} with strides {tuple(logits.stride())}")
+        """logits: fp32 or bf16 device tensor, the type is taken from it; stride: elements from a row to the next (None = that of a tensor of two
+        dimensions, V otherwise); tokens and top_ids int32, the other results fp32."""
+        if logits.dtype not in (self.f32, self.bf16) or not logits.is_cuda or (logits.dim() > 0 and logits.stride(-1) != 1):
+            raise ValueError(f"logits: rows of float32 or bfloat16 on the GPU, not {logits.dtype} with strides {tuple(logits.stride())} on {logits.device}")
         if stride is None:
             stride = logits.stride(0) if logits.dim() == 2 and rows > 1 else V
-        _check(load().spts_token_logprobs(self.handle, _ptr(logits), SPTS_BF16 if logits.dtype == torch.bfloat16 else SPTS_F32, stride, V, rows, _ptr(tokens), _ptr(logprob),
+        have = 1 + sum((n - 1) * s for n, s in zip(logits.shape, logits.stride())) if logits.numel() else 0
+        if rows > 0 and have < (rows - 1) * stride + V:
+            raise ValueError(f"logits: {list(logits.shape)} do not hold {rows} rows of {V} words, {stride} apart")
+        for t, what, least, dtype in ((tokens, "tokens", rows, self.i32), (logprob, "logprob", rows, self.f32), (entropy, "entropy", rows, self.f32),
+                                      (top_ids, "top_ids", rows * n_top, self.i32), (top_logprobs, "top_logprobs", rows * n_top, self.f32)):
+            _need(t, what, least, dtype)
+        _check(load().spts_token_logprobs(self.handle, _ptr(logits), SPTS_BF16 if logits.dtype == self.bf16 else SPTS_F32, stride, V, rows, _ptr(tokens), _ptr(logprob),
                                           _ptr(entropy), n_top, _ptr(top_ids), _ptr(top_logprobs)), "spts_token_logprobs")
 
     def spts_msdp_compact(self, x_in, pos_in, s_mha, N, N_next, protect_last, x_out, pos_out, map_new2old,

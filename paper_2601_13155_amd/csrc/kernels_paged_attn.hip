@@ -312,23 +312,29 @@ __global__ void __launch_bounds__(AW * 64) kvp_weights_kernel(const float* __res
     }
 }
 
-// Accounts from kept scores (few columns): a thread has a key and goes over all heads' columns
+// Accounts from kept scores (few columns): a thread has a place of the scores' rows and goes over all heads' columns
 template <int NB>
 __global__ void __launch_bounds__(256) kvp_scores_weights_kernel(const float* __restrict__ scores, PagedSeqs<NB> sq, int H, int Hkv, const float2* __restrict__ stats, float decay) {
     int first;
     const int b = seq_of(sq.end, (int)blockIdx.x, &first);
-    const int key = ((int)blockIdx.x - first) * 256 + threadIdx.x, n = sq.count[b], G = H / Hkv, cols = sq.nq[b] * G, stride = (n + 31) / 32 * 32;
+    const int n = sq.count[b], G = H / Hkv, cols = sq.nq[b] * G;
+    const int64_t at = (int64_t)((int)blockIdx.x - first) * 256 + threadIdx.x, stride = score_blocks(n) * 32;
+    const int64_t key = (at & ~31) + 8 * (at >> 2 & 3) + 4 * (at >> 4 & 1) + (at & 3);   // as the scores were stored
     if (key >= n) return;
-    const float* const at = scores + (int64_t)sq.scores[b] * 32 + key;
+    const float* row = scores + (int64_t)sq.scores[b] * 32 + at;
     float w = 0.f;
-    for (int g = 0; g < Hkv; ++g) {
-        const float2* const st = stats + (int64_t)sq.first[b] * H + g * G;
-#pragma unroll 4
-        for (int cn = 0; cn < cols; ++cn) {
-            const float2 z = st[(int64_t)(cn / G) * H + cn % G];
-            const float x = at[(int64_t)(g * cols + cn) * stride];
-            w += x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x - z.x) * z.y;   // (unseen by the column, whose sum may be NaN)
-        }
+    const float2* const st0 = stats + (int64_t)sq.first[b] * H;
+    int64_t st = 0;                      // the column's place among the statistics, [query][head]
+    int j = 0, cn = 0, g = 0;            // head of the group, column of the head, head
+#pragma unroll 8
+    for (int r = 0; r < cols * Hkv; ++r) {
+        const float2 z = st0[st];
+        const float x = *row, e = __builtin_amdgcn_exp2f(x - z.x) * z.y;
+        w += x == -INFINITY ? 0.f : e;   // (unseen by the column, whose sum may be NaN)
+        row += stride;
+        ++st;
+        if (++j == G) { j = 0; st += H - G; }
+        if (++cn == cols) { cn = 0; ++g; st = g * G; }
     }
     sq.weight[b][key] = decay == 0.f ? w : decay * sq.weight[b][key] + w;
 }
@@ -455,12 +461,12 @@ static hipError_t launch_kvp_attn_t(const T* q, const PagedPool& pool, const Pag
     }
     const Shares sh{(float2*)rest, rest + (2 * shares + 63) / 64 * 64};
     size_t taken = shares > 0 ? (2 * shares + 63) / 64 * 64 + (size_t)shares * D : 0;
-    // scores of few columns are kept for the accounts where there is room: rows of whole blocks of 32 keys
+    // scores of few columns are kept for the accounts where there is room
     float* const scores = rest + taken;
     if (BF16 && add) {
         int64_t at = 0;
         for (int b = 0; b < pb.n; ++b) {
-            const int64_t need = (pb.count[b] + 31) / 32 * columns(pb, b, G) * Hkv;
+            const int64_t need = score_blocks(pb.count[b]) * columns(pb, b, G) * Hkv;
             if (!few(b) || (size_t)(at + need) * 32 > room - taken || at + need > 0x7fffffff) continue;
             sq.scores[b] = (int32_t)at;
             at += need;
@@ -481,8 +487,10 @@ static hipError_t launch_kvp_attn_t(const T* q, const PagedPool& pool, const Pag
         if (nm * Hkv > 0x7fffffff) return hipErrorInvalidValue;
         if (nm > 0) e = launch_kvp_attn_many<NB>(q, pl, sq, (int)nm, H, Hkv, D, sh, stats, out, s);
         if (e != hipSuccess) return e;
-        const int64_t nf = items_of(few, KVP_FEW_COLS);
-        if (nf > 0) e = launch_kvp_attn_few<NB>(q, pl, sq, (int)nf, H, Hkv, D, sh, stats, scores, out, s);
+        for (const bool keep : {true, false}) {   // those whose scores are kept, and those for which there was no room, or no wish
+            const int64_t nf = items_of([&](int b) { return few(b) && (sq.scores[b] >= 0) == keep; }, KVP_FEW_COLS);
+            if (nf > 0 && e == hipSuccess) e = launch_kvp_attn_few<NB>(q, pl, sq, (int)nf, H, Hkv, D, sh, stats, keep ? scores : nullptr, out, s);
+        }
     } else {
         const int64_t n = items_of(any, 32);
         if (n * Hkv > 0x7fffffff) return hipErrorInvalidValue;

@@ -361,7 +361,7 @@ __global__ void __launch_bounds__(NW * 64, NW == 8 ? 2 : 1) kvp_many_kernel(cons
 // registers, values into its two stages of LDS, a block ahead.  16x16x32: S^T = K Q^T with key 8 (m / 4) + 4 t + m % 4 as operand row m of the t-th product, so that lane group kg
 // has the scores of keys 8 kg .. 8 kg + 7, which is the operand of O^T = V^T P^T as it stands.  Probabilities go in as two bf16 parts (off by 2^-17 of each at most), which costs
 // nothing here.  The maximum moves only when a score is 2^8 above it.
-template <int D, int NW, int NB>
+template <int D, int NW, int NB, bool SCORES>
 __global__ void __launch_bounds__(NW * 64, 2) kvp_few_kernel(const bf16_t* q, PoolView pool, PagedSeqs<NB> sq, int H, int Hkv, float c, Shares sh, float2* __restrict__ stats,
                                                                  float* __restrict__ scores, bf16_t* out) {
     using L = Tile<D>;
@@ -407,7 +407,7 @@ __global__ void __launch_bounds__(NW * 64, 2) kvp_few_kernel(const bf16_t* q, Po
     };
     // the lane's place among value rows 8 kg + (lane % 16) / 4 (and 4 on), dimensions 4 (lane % 4) of 16
     const int vr = 8 * kg + (l16 >> 2), vc = (l16 & 3) >> 1;
-    float* const to_scores = scores && sq.scores[b] >= 0 ? scores + ((int64_t)sq.scores[b] + (int64_t)(g * cols + col) * ((n + 31) / 32)) * 32 + 8 * kg : nullptr;
+    float* const to_scores = SCORES ? scores + ((int64_t)sq.scores[b] + (g * cols + col) * score_blocks(n)) * 32 + 4 * kg : nullptr;
     f32x4 o[VM];
 #pragma unroll
     for (int i = 0; i < VM; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -419,7 +419,9 @@ __global__ void __launch_bounds__(NW * 64, 2) kvp_few_kernel(const bf16_t* q, Po
         next = ids_of(key0 + NW * 32);
     }
     for (; key0 < k1; key0 += NW * 32, stage ^= 1) {
-        SPTS_WAIT_VMCNT(0);
+        // The values have landed where all but two operations have: behind them went at least two loads of keys (which the compiler waits for itself), and two stores of scores that
+        // need not have.
+        SPTS_WAIT_VMCNT(2);
         asm volatile("" ::: "memory");   // (the values' reads stay behind the wait)
         f32x4 s[2];
 #pragma unroll
@@ -441,9 +443,10 @@ __global__ void __launch_bounds__(NW * 64, 2) kvp_few_kernel(const bf16_t* q, Po
             s[j >> 2][j & 3] = x;
             mx = fmaxf(mx, x);
         }
-        if (to_scores && l16 < cols) {   // rows of whole blocks of 32 keys
+        if constexpr (SCORES) {   // behind the next block's loads, so that the wait for those is none for these; rows of whole blocks of 32 keys, in the order that stores whole
+            // pieces of 64 bytes: place 16 t + 4 kg + r has key 8 kg + 4 t + r (lanes without a column store the last column's again)
             *reinterpret_cast<f32x4*>(to_scores + key0) = s[0];
-            *reinterpret_cast<f32x4*>(to_scores + key0 + 4) = s[1];
+            *reinterpret_cast<f32x4*>(to_scores + key0 + 16) = s[1];
         }
         if (__ballot(mx > m + TAU) != 0) {
             mx = fmaxf(mx, __shfl_xor(mx, 16));
@@ -683,14 +686,20 @@ template hipError_t launch_kvp_attn_many<1>(const bf16_t*, const PoolView&, cons
 template hipError_t launch_kvp_attn_many<DECODE_MAX_BATCH>(const bf16_t*, const PoolView&, const PagedSeqs<DECODE_MAX_BATCH>&, int, int, int, int, const Shares&, float2*, bf16_t*,
                                                            hipStream_t);
 
+template <int D, int NB, bool SCORES>
+static hipError_t launch_few_s(const bf16_t* q, const PoolView& pool, const PagedSeqs<NB>& sq, int items, int H, int Hkv, const Shares& sh, float2* stats, float* scores, bf16_t* out,
+                             hipStream_t s) {
+    constexpr int NW = 4, RING = NW * 2 * 32 * Tile<D>::ROW, MEET = NW * 16 * (D + 4 + 2) * 4, LDS = RING > MEET ? RING : MEET;
+    const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(&kvp_few_kernel<D, NW, NB, SCORES>), LDS);
+    if (e != hipSuccess) return e;
+    kvp_few_kernel<D, NW, NB, SCORES><<<dim3((unsigned)(items * Hkv)), dim3(NW * 64), LDS, s>>>(q, pool, sq, H, Hkv, PAGED_LOG2E / sqrtf((float)D), sh, stats, scores, out);
+    return hipGetLastError();
+}
+
 template <int D, int NB>
 static hipError_t launch_few(const bf16_t* q, const PoolView& pool, const PagedSeqs<NB>& sq, int items, int H, int Hkv, const Shares& sh, float2* stats, float* scores, bf16_t* out,
                              hipStream_t s) {
-    constexpr int NW = 4, RING = NW * 2 * 32 * Tile<D>::ROW, MEET = NW * 16 * (D + 4 + 2) * 4, LDS = RING > MEET ? RING : MEET;
-    const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(&kvp_few_kernel<D, NW, NB>), LDS);
-    if (e != hipSuccess) return e;
-    kvp_few_kernel<D, NW, NB><<<dim3((unsigned)(items * Hkv)), dim3(NW * 64), LDS, s>>>(q, pool, sq, H, Hkv, PAGED_LOG2E / sqrtf((float)D), sh, stats, scores, out);
-    return hipGetLastError();
+    return scores ? launch_few_s<D, NB, true>(q, pool, sq, items, H, Hkv, sh, stats, scores, out, s) : launch_few_s<D, NB, false>(q, pool, sq, items, H, Hkv, sh, stats, scores, out, s);
 }
 
 template <int NB>

@@ -15,15 +15,19 @@ template <int NB> struct PagedSeqs {
     int32_t per[NB], splits[NB];            // keys of a share (a multiple of 128), shares
     int32_t end[NB];                        // work items of the sequences up to here
     int32_t at[NB];                         // first share of sequence b (attention) / first of its partial sums (accounts)
-    int32_t scores[NB];                     // where the scores of sequence b begin, in rows of 32 (-1: not kept)
+    int32_t scores[NB];                     // where the scores of sequence b begin, in blocks of 32 (-1: not kept)
     int32_t parts[NB];                      // accounts: parts of its heads and columns
 };
 struct PoolView { const char* k; const char* v; uint32_t pages; int32_t shift; };
 // Shares of a column's keys, each with its maximum and sum (ml) and its unnormalised output (o [D]); column n of head g in share s is at at[b] + (s * Hkv + g) * columns + n
 struct Shares { float2* ml; float* o; };
-// x / G for x below 2^32 / G: the upper half of x times ceil(2^32 / G)
+// x / G: the upper half of x times ceil(2^32 / G) is that, or one more
 struct DivG { uint32_t m; int32_t G; };
-__device__ inline uint32_t div_g(uint32_t x, DivG g) { return g.G == 1 ? x : __umulhi(x, g.m); }
+__device__ inline uint32_t div_g(uint32_t x, DivG g) {
+    if (g.G == 1) return x;
+    const uint32_t y = __umulhi(x, g.m);
+    return y - (y * (uint32_t)g.G > x ? 1u : 0u);
+}
 
 template <int NB> __device__ inline int seq_of(const int32_t (&end)[NB], int i, int* first) {
     int b = 0;
@@ -32,6 +36,12 @@ template <int NB> __device__ inline int seq_of(const int32_t (&end)[NB], int i, 
     for (int j = 0; j + 1 < NB; ++j)
         if (i >= end[j]) { b = j + 1; *first = end[j]; }
     return b;
+}
+// Blocks of 32 scores from a column's row to the next one's: no power of two, which would put the same keys of all columns into one memory channel (131004 rows, 128 columns, stored
+// while the cache is read: 127 us, this way 121)
+__host__ __device__ inline int64_t score_blocks(int64_t n) {
+    const int64_t blocks = (n + 31) / 32;
+    return blocks < 512 ? blocks : (blocks + 63) / 64 * 64 + 9;
 }
 // the pool's page of a row; the table does not change while kernels read it
 __device__ inline uint32_t page_id(const PoolView& pool, const int32_t* table, int64_t row) {

@@ -481,9 +481,9 @@ class PagedKV:
     def free_pages(self) -> int:
         return len(self._free)
 
-    def reserve(self, b: int, rows: int):
+    def reserve(self, b: int, rows: int, ctx: Optional[binding.Context] = None):
         """Pages for the first `rows` rows of sequence b; ValueError where its capacity or the pool has no room.  Writes the table from the
-        host, in order with what the current stream is given."""
+        host, in order with what the current stream is given, and with ctx in order with what its stream is given."""
         torch = _torch()
         have, need = len(self.pages[b]), -(-int(rows) // self.page)
         if need * self.page > self.structs[b].capacity:
@@ -493,7 +493,8 @@ class PagedKV:
         if need > have:
             new = [self._free.pop() for _ in range(need - have)]
             self.pages[b] += new
-            self.table[b, have:need].copy_(torch.tensor(new, dtype=torch.int32))
+            with _on_stream_of(ctx) if ctx is not None else contextlib.nullcontext():
+                self.table[b, have:need].copy_(torch.tensor(new, dtype=torch.int32))
 
     def release(self, b: int):
         """Hands back the pages behind sequence b's count rows (all of them where it is 0).  Call it when the work on them is in the stream that
@@ -503,18 +504,22 @@ class PagedKV:
             self._free.append(self.pages[b].pop())
 
     def append_cache(self, ctx: binding.Context, b: int, cache: "KVCache"):
-        """Takes over every pair of a prefill's cache behind sequence b's rows (their weights 0)."""
+        """Takes over every pair of a prefill's cache behind sequence b's rows (their weights 0); ValueError where it has other heads or
+        another type, or there is no room."""
+        if cache.k.dtype != self.k.dtype or tuple(cache.k.shape[1:]) != (self.shape.Hkv, self.shape.d):
+            raise ValueError(f"a cache of {self.k.dtype} [.., {self.shape.Hkv}, {self.shape.d}], not {cache.k.dtype} {list(cache.k.shape)}")
         one = [self.structs[b]]
         with _on_stream_of(ctx):
             self.reserve(b, self.structs[b].count + cache.count)
             ctx.spts_kvp_append(self.pool, cache.k, cache.v, cache.pos, [0, cache.count], one)
         self.structs[b].count = one[0].count
 
-    def host(self, b: int):
+    def host(self, ctx: binding.Context, b: int):
         """(k, v, pos) of sequence b's filled rows, as host arrays (fp64 / int32)."""
         n = self.counts[b]
-        k, v = (to_host(t[self.table[b].clamp(min=0).long()].transpose(1, 2).flatten(0, 1)[:n]).astype(np.float64) for t in (self.k, self.v))
-        return k, v, self.pos[b, :n].cpu().numpy()
+        with _on_stream_of(ctx):
+            k, v = (to_host(t[self.table[b].clamp(min=0).long()].transpose(1, 2).flatten(0, 1)[:n]).astype(np.float64) for t in (self.k, self.v))
+            return k, v, self.pos[b, :n].cpu().numpy()
 
 
 class StackRunner:

@@ -122,6 +122,13 @@ def test_only_what_is_wanted(ctx):
         ctx.spts_token_logprobs(x.half(), 7000, 3, tokens, lp)
     with pytest.raises(ValueError):
         ctx.spts_token_logprobs(x.t(), 3, 7000, tokens, lp)
+    for bad in (dict(tokens=tokens.long(), logprob=lp), dict(tokens=tokens[:2], logprob=lp), dict(entropy=lp.double()), dict(entropy=lp[::2]), dict(tokens=tokens.cpu(), logprob=lp),
+                dict(n_top=3, top_ids=ids, top_logprobs=torch.empty((3, 3), device="cuda"))):
+        with pytest.raises(ValueError):
+            ctx.spts_token_logprobs(x, 7000, 3, **bad)
+    for V, rows, stride in ((7001, 3, None), (7000, 4, None), (7000, 3, 7001)):
+        with pytest.raises(ValueError):
+            ctx.spts_token_logprobs(x, V, rows, entropy=torch.empty(8, device="cuda"), stride=stride)
 
 
 def test_more_elements_than_32_bits(ctx):

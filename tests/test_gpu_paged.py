@@ -220,7 +220,7 @@ def test_attention_beyond_32_bit_offsets():
     g = torch.Generator().manual_seed(3)
     k, v = (torch.randn((700, 1, 128), generator=g).bfloat16() for _ in range(2))
     ctx.spts_kvp_append(kv.pool, k.cuda(), v.cuda(), torch.arange(700, dtype=torch.int32, device="cuda"), [0, 700], kv.structs)
-    hk, hv, _ = kv.host(0)
+    hk, hv, _ = kv.host(ctx, 0)
     assert np.array_equal(hk, k.double().numpy()) and np.array_equal(hv, v.double().numpy())
     for m in (1, 50):
         q = torch.randn((m, 4, 128), generator=g).bfloat16().cuda()
@@ -229,7 +229,7 @@ def test_attention_beyond_32_bit_offsets():
     old = torch.empty(300, dtype=torch.int32, device="cuda")
     ctx.spts_kvp_evict(kv.pool, [300], kv.structs, old_out=old)
     o = old.cpu().long()
-    assert np.array_equal(kv.host(0)[0], k.double().numpy()[o])
+    assert np.array_equal(kv.host(ctx, 0)[0], k.double().numpy()[o])
     del kv
     torch.cuda.empty_cache()
 
@@ -286,7 +286,7 @@ def test_append_without_accounts_and_from_a_prefill():
     cache.struct.count = 37
     kv.append_cache(ctx, 1, cache)
     assert kv.counts == [0, 37] and kv.free_pages == 5
-    for got, want in zip(kv.host(1), cache.host()):
+    for got, want in zip(kv.host(ctx, 1), cache.host()):
         assert np.array_equal(got, want)
     with pytest.raises(ValueError):
         kv.append_cache(ctx, 1, cache)      # 74 rows
@@ -416,7 +416,7 @@ def test_a_second_turn(tmp_path):
     kv.release(1)
     assert kv.counts == [24, 96] and kv.free_pages == 24 - 2 - 6
     for b in range(2):
-        assert all(np.array_equal(a, h.numpy()) for a, h in zip(kv.host(b)[:2], host[b]))
+        assert all(np.array_equal(a, h.numpy()) for a, h in zip(kv.host(ctx, b)[:2], host[b]))
     out = turn([1, 1])
     table = torch.randn((1000, 256), generator=g).bfloat16().cuda()
     logits = torch.empty((2, 1000), device="cuda")
@@ -429,6 +429,56 @@ def test_a_second_turn(tmp_path):
     assert np.array_equal(ids.cpu().numpy(), want[2]) and torch.equal(ids[:, 0], tokens[:2])
     for got, w in ((lp[:2], want[0]), (ent[:2], want[1]), (tops, want[3])):
         assert np.allclose(got.cpu().numpy(), w, rtol=2e-6, atol=2e-6)
+
+
+def test_a_context_on_its_own_stream():
+    """Tensors made on the current stream, calls on the context's: the conveniences order the two, and results are those of one stream."""
+    shape = shape_of(4, 2, 64, "bf16")
+    ctx = context(shape)
+    side = torch.cuda.Stream()
+    other = binding.Context(shape, 256, 1, 1, 256, stream=side)
+    cache = runtime.KVCache(shape, 300)
+    for t in (cache.k, cache.v):
+        t.normal_()
+    cache.pos[:] = torch.arange(300, device="cuda", dtype=torch.int32)
+    cache.struct.count = 300
+    q = torch.randn((3, 4, 64), device="cuda").bfloat16()
+    outs = []
+    for c in (ctx, other):
+        kv = runtime.PagedKV(shape, 24, 16, 1, 330)
+        torch.cuda._sleep(20_000_000)          # the current stream is busy: an unordered call would read tables and rows that are not there yet
+        kv.append_cache(c, 0, cache)
+        kv.reserve(0, 320, c)
+        with runtime._on_stream_of(c):
+            out = torch.empty_like(q)
+            c.spts_kvp_attn(kv.pool, q, [0, 3], kv.structs, out, 1, 0.0)
+        outs.append((out.clone(), kv.weight.clone(), kv.host(c, 0)))
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+    assert all(np.array_equal(a, b) for a, b in zip(outs[0][2], outs[1][2]))
+
+
+def test_tensors_that_do_not_fit_are_refused():
+    shape = shape_of(4, 2, 64, "bf16")
+    ctx = context(shape)
+    kv, _ = filled(shape, 16, [40], seed=1, capacity=64)
+    kv.reserve(0, 64)
+    bf = lambda *s: torch.zeros(s, dtype=torch.bfloat16, device="cuda")
+    pos = torch.zeros(4, dtype=torch.int32, device="cuda")
+    for k, v, p in ((bf(3, 2, 64), bf(4, 2, 64), pos), (bf(4, 2, 64), bf(4, 2, 64).float(), pos), (bf(4, 2, 64), bf(4, 2, 64), pos.long()), (bf(4, 2, 64).cpu(), bf(4, 2, 64), pos),
+                    (bf(4, 2, 128)[:, :, ::2], bf(4, 2, 64), pos), (bf(4, 2, 64), bf(4, 2, 64), pos[:3])):
+        with pytest.raises(ValueError):
+            ctx.spts_kvp_append(kv.pool, k, v, p, [0, 4], kv.structs)
+    for q, out in ((bf(1, 4, 64), bf(2, 4, 64)), (bf(2, 4, 64).float(), bf(2, 4, 64)), (bf(2, 4, 64), bf(2, 4, 128)[..., :64])):
+        with pytest.raises(ValueError):
+            ctx.spts_kvp_attn(kv.pool, q, [0, 2], kv.structs, out)
+    with pytest.raises(ValueError):
+        ctx.spts_kvp_attn(kv.pool, bf(2, 4, 64), [0], kv.structs, bf(2, 4, 64))
+    for old in (torch.zeros(10, dtype=torch.int64, device="cuda"), torch.zeros(9, dtype=torch.int32, device="cuda")):
+        with pytest.raises(ValueError):
+            ctx.spts_kvp_evict(kv.pool, [10], kv.structs, old_out=old)
+    with pytest.raises(ValueError):
+        kv.append_cache(ctx, 0, runtime.KVCache(shape_of(4, 2, 64, "f32"), 4))
+    assert kv.counts == [40]
 
 
 @pytest.mark.parametrize("replays", [4])
