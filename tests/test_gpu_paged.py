@@ -71,6 +71,64 @@ def test_attention_of_ragged_batches(dtype, H, Hkv, rows, new):
             assert not torch.isnan(kv.weight[0, :rows[0]]).any()
 
 
+@pytest.mark.parametrize("rows,new", [(600, 600), (700, 570), (1031, 517), (333, 300), (4000, 260)])
+@pytest.mark.parametrize("H,Hkv,d", [(2, 2, 128), (3, 3, 64), (2, 2, 32), (3, 1, 128), (64, 1, 64), (5, 1, 32)])
+def test_long_chunks(H, Hkv, d, rows, new):
+    """Workgroups whose columns end far apart (a head of its own for every key/value head), groups that divide no block of columns, keys in shares."""
+    shape = shape_of(H, Hkv, d, "bf16")
+    new = new if H < 64 else new // 8
+    ctx = context(shape, 1024)
+    kv, host = filled(shape, 32, [rows], seed=rows + d)
+    q = torch.randn((new, H, d), generator=torch.Generator().manual_seed(d)).bfloat16().cuda()
+    before = kv.weight.cpu().clone()
+    check_attn(shape, kv, host, q, [new], run_attn(ctx, kv, q, [new], 1, 0.5), 1, 0.5, before, chunk=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_sixteen_sequences(dtype):
+    shape = shape_of(8, 2, 64, dtype)
+    ctx = context(shape, 512)
+    rows = [1, 700, 64, 63, 65, 300, 128, 129, 5, 1000, 16, 17, 31, 32, 33, 250]
+    new = [1, 1, 64, 1, 3, 40, 0, 129, 5, 2, 16, 1, 31, 4, 5, 1]
+    kv, host = filled(shape, 16, rows, seed=16)
+    q = torch.randn((sum(new), 8, 64), generator=torch.Generator().manual_seed(1)).to(TD[dtype]).cuda()
+    before = kv.weight.cpu().clone()
+    check_attn(shape, kv, host, q, new, run_attn(ctx, kv, q, new, 1, 0.25), 1, 0.25, before)
+
+
+def test_results_do_not_depend_on_the_batch():
+    """A sequence alone and among others: the same accounts and results where its keys are in as many shares, and in any case within the tolerance."""
+    shape = shape_of(8, 2, 64, "bf16")
+    ctx = context(shape, 512)
+    kv, host = filled(shape, 16, [300, 900, 77], seed=13)
+    new = [40, 1, 3]
+    q = torch.randn((44, 8, 64), generator=torch.Generator().manual_seed(2)).bfloat16().cuda()
+    run_attn(ctx, kv, q, new, 1, 0.0)
+    w, at = kv.weight.clone(), 0
+    for b, m in enumerate(new):
+        one = (binding.spts_kvp * 1)(kv.structs[b])
+        out = torch.empty_like(q[at:at + m])
+        ctx.spts_kvp_attn(kv.pool, q[at:at + m].contiguous(), [0, m], one, out, 1, 0.0)
+        want, spread, big, _ = attend64(q[at:at + m], *host[b], 8, 2)
+        assert bool(((out.cpu().double() - want).abs() <= attend_bound(want, spread, big, 900, 64, "bf16", m * 4 > 16)).all())
+        assert torch.allclose(kv.weight[b, :kv.counts[b]], w[b, :kv.counts[b]], rtol=1e-5)
+        at += m
+
+
+def test_accounts_without_room_for_scores():
+    """300000 rows of 64 columns: their scores exceed a small context's scratch and are computed anew; and few shares of many columns in fp32."""
+    shape = shape_of(64, 4, 32, "bf16")
+    ctx = context(shape)
+    kv, host = filled(shape, 256, [300000], seed=3)
+    q = torch.randn((1, 64, 32), generator=torch.Generator().manual_seed(1)).bfloat16().cuda()
+    check_attn(shape, kv, host, q, [1], run_attn(ctx, kv, q, [1], 1, 0.0), 1, 0.0, kv.weight.cpu().clone())
+    shape = shape_of(2, 2, 128, "f32")
+    ctx = context(shape)
+    kv, host = filled(shape, 64, [20000], seed=4)
+    q = torch.randn((200, 2, 128), generator=torch.Generator().manual_seed(1)).cuda()
+    check_attn(shape, kv, host, q, [200], run_attn(ctx, kv, q, [200], 1, 0.0), 1, 0.0, kv.weight.cpu().clone())
+
+
 @pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
 @pytest.mark.parametrize("d", [32, 64, 128])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
