@@ -421,7 +421,7 @@ int spts_kvp_append(spts_ctx *ctx, const spts_kv_pool *pool, const void *k, cons
  * before they meet the values, of single tokens (at most 16 queries and heads of a key/value head) they keep 16 bits or more.
  * add_weights != 0: for every sequence with queries, weight[j] = decay * weight[j] + the softmax weight of row j summed over the
  * call's queries and all heads, for its count rows (0 <= decay <= 1; with decay = 0 the old weights are not read); all caches of such sequences need
- * a weight, and no two the same one.  out may be q itself, and must not overlap it otherwise.  Uses the context's workspace. */
+ * a weight, and no two the same one.  out may be q itself where no weights are added, and must not overlap it otherwise.  Uses the context's workspace. */
 int spts_kvp_attn(spts_ctx *ctx, const spts_kv_pool *pool, const void *q, const int64_t *offsets, int32_t batch, const spts_kvp *caches,
                   void *out, int32_t add_weights, float decay);
 /* Cuts caches[b] down to min(count, keep[b]) rows, those with the largest weight, ties to the lower row; rows at positions below
@@ -430,7 +430,7 @@ int spts_kvp_attn(spts_ctx *ctx, const spts_kv_pool *pool, const void *q, const 
  * rotation, so their order does not matter), with positions and weights; count becomes the rows kept.  Negative weights count as 0, a NaN as more than any
  * number.  keep, keep_below and keep_from are HOST arrays [batch] (NULL for either of the last two = no such rows); old_out (device int32, NULL = not
  * wanted) [sum of rows kept]: for each row of each sequence the row that it was.  What is behind the rows kept stays as it was.
- * Distinct tables, positions and weights; SPTS_EWORKSPACE where the workspace has no room for 8 bytes for each
+ * Distinct tables, positions and weights, which all of them have; SPTS_EWORKSPACE where the workspace has no room for 8 bytes for each
  * row that may move (and, if a sequence has more than 16384 rows, for 25 KB for each 4096 of the longest's, up to 3.3 MB, for every sequence). */
 int spts_kvp_evict(spts_ctx *ctx, const spts_kv_pool *pool, const int64_t *keep, const int32_t *keep_below, const int32_t *keep_from,
                    int32_t batch, spts_kvp *caches, int32_t *old_out);

@@ -290,7 +290,6 @@ size_t logprobs_scratch_bytes(int64_t rows, int32_t V, int32_t top) {
 
 template <typename T>
 static hipError_t launch_logprobs_t(const PartArgs& a, int64_t rows, hipStream_t s) {
-    if (rows * a.parts > 0x7fffffff) return hipErrorInvalidValue;
     const dim3 grid((unsigned)(rows * a.parts));
     if (a.span <= 8 * PT) logprobs_kernel<T, 8><<<grid, dim3(PT), 0, s>>>(a);
     else logprobs_kernel<T, 16><<<grid, dim3(PT), 0, s>>>(a);
@@ -304,7 +303,18 @@ hipError_t launch_token_logprobs(const LogprobArgs& g, bool bf16, void* scratch,
     a.parts = logprobs_parts(g.rows, g.V, &a.span);
     a.psum = (Sums*)scratch;
     a.pword = (Word*)((char*)scratch + ((size_t)g.rows * a.parts * sizeof(Sums) + 15) / 16 * 16);
-    return bf16 ? launch_logprobs_t<bf16_t>(a, g.rows, s) : launch_logprobs_t<float>(a, g.rows, s);
+    constexpr int64_t MOST = 1 << 23;   // rows of a launch, which has fewer than 2^32 threads (so many are in one part each)
+    for (int64_t r = 0; r < g.rows; r += MOST) {
+        PartArgs z = a;
+        z.logits = (const char*)a.logits + r * a.stride * (bf16 ? 2 : 4);
+        if (a.tokens) { z.tokens += r; z.logprob += r; }
+        if (a.entropy) z.entropy += r;
+        if (a.top > 0) { z.ids += r * a.top; z.top_lp += r * a.top; }
+        const int64_t n = g.rows - r < MOST ? g.rows - r : MOST;
+        const hipError_t e = bf16 ? launch_logprobs_t<bf16_t>(z, n, s) : launch_logprobs_t<float>(z, n, s);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace spts

@@ -22,6 +22,7 @@ template <int NB> struct EvictSeqs {
     int32_t old[NB];                                    // where its part of `old` begins
 };
 struct Move { int32_t src, dst; };
+constexpr int64_t MAX_GROUPS = (1 << 24) - 1;   // of 256 threads: a launch has fewer than 2^32
 }  // namespace
 
 // A thread copies 16 bytes of a key and of a value; the rows of a head lie next to each other in a page.
@@ -59,7 +60,7 @@ static hipError_t launch_kvp_append_n(const void* k, const void* v, const int32_
         sq.at[b] = (int32_t)pb.count[i]; sq.end[b] = (int32_t)pb.off[i + 1];
     }
     const int64_t total = pb.off[pb.n] * Hkv * chunks, groups = (total + 255) / 256;
-    if (groups > 0x7fffffff) return hipErrorInvalidValue;
+    if (groups > MAX_GROUPS) return hipErrorInvalidValue;
     kvp_append_kernel<NB><<<dim3((unsigned)groups), dim3(256), 0, s>>>((const u32x4*)k, (const u32x4*)v, pos, (u32x4*)pool.k, (u32x4*)pool.v, (uint32_t)pool.pages, pool.shift, sq,
                                                                        total, Hkv, chunks);
     return hipGetLastError();
@@ -447,31 +448,33 @@ __global__ void __launch_bounds__(ET) kvp_select_chip_kernel(EvictSeqs<NB> sq, C
     }
 }
 
-// One workgroup per row that may move: its keys and values of all heads, 16 bytes a thread, and its position and weight (sources lie from `keep` on, places below it, so that
-// no row is read after it was written)
+// One workgroup per row that may move, up to MOVE_GROUPS of them: its keys and values of all heads, 16 bytes a thread, and its position and weight (sources lie from `keep` on, places
+// below it, so that no row is read after it was written)
+constexpr int64_t MOVE_GROUPS = 1 << 20;
 template <int NB>
 __global__ void __launch_bounds__(256) kvp_move_kernel(u32x4* __restrict__ pk, u32x4* __restrict__ pv, uint32_t pages, int shift, EvictSeqs<NB> sq, const Move* __restrict__ moves,
                                                        const int32_t* __restrict__ n_moves, int32_t* __restrict__ old, int Hkv, int chunks) {
-    const int b = blockIdx.y;
-    if ((int)blockIdx.x >= n_moves[b]) return;
-    const Move mv = moves[sq.list[b] + blockIdx.x];
+    const int b = blockIdx.y, n = n_moves[b];
     const int mask = (1 << shift) - 1;
-    uint32_t from = (uint32_t)sq.table[b][mv.src >> shift];
-    const uint32_t to = (uint32_t)sq.table[b][mv.dst >> shift];
-    from = from < pages ? from : 0;
-    if (threadIdx.x == 0) {
-        sq.pos[b][mv.dst] = sq.pos[b][mv.src];
-        sq.weight[b][mv.dst] = sq.weight[b][mv.src];
-        if (old) old[sq.old[b] + mv.dst] = mv.src;
-    }
-    if (to >= pages) return;
-    for (int e = threadIdx.x; e < Hkv * chunks; e += 256) {
-        const int g = e / chunks, ch = e % chunks;
-        const int64_t f = ((((int64_t)from * Hkv + g) << shift) + (mv.src & mask)) * chunks + ch;
-        const int64_t t = ((((int64_t)to * Hkv + g) << shift) + (mv.dst & mask)) * chunks + ch;
-        const u32x4 kw = pk[f], vw = pv[f];
-        pk[t] = kw;
-        pv[t] = vw;
+    for (int i = blockIdx.x; i < n; i += gridDim.x) {
+        const Move mv = moves[(int64_t)sq.list[b] + i];
+        uint32_t from = (uint32_t)sq.table[b][mv.src >> shift];
+        const uint32_t to = (uint32_t)sq.table[b][mv.dst >> shift];
+        from = from < pages ? from : 0;
+        if (threadIdx.x == 0) {
+            sq.pos[b][mv.dst] = sq.pos[b][mv.src];
+            sq.weight[b][mv.dst] = sq.weight[b][mv.src];
+            if (old) old[(int64_t)sq.old[b] + mv.dst] = mv.src;
+        }
+        if (to >= pages) continue;
+        for (int e = threadIdx.x; e < Hkv * chunks; e += 256) {
+            const int g = e / chunks, ch = e % chunks;
+            const int64_t f = ((((int64_t)from * Hkv + g) << shift) + (mv.src & mask)) * chunks + ch;
+            const int64_t t = ((((int64_t)to * Hkv + g) << shift) + (mv.dst & mask)) * chunks + ch;
+            const u32x4 kw = pk[f], vw = pv[f];
+            pk[t] = kw;
+            pv[t] = vw;
+        }
     }
 }
 
@@ -533,7 +536,7 @@ static hipError_t launch_kvp_evict_n(const PagedPool& pool, const PagedBatch& pb
         kvp_select_chip_kernel<NB, 2><<<grid, dim3(ET), 0, s>>>(sq, cs, pb.n, moves, n_moves, old);
         kvp_select_chip_kernel<NB, 3><<<grid, dim3(ET), 0, s>>>(sq, cs, pb.n, moves, n_moves, old);
     }
-    if (most > 0) kvp_move_kernel<NB><<<dim3((unsigned)most, (unsigned)pb.n), dim3(256), 0, s>>>((u32x4*)pool.k, (u32x4*)pool.v, (uint32_t)pool.pages, pool.shift, sq, moves, n_moves,
+    if (most > 0) kvp_move_kernel<NB><<<dim3((unsigned)std::min(most, MOVE_GROUPS), (unsigned)pb.n), dim3(256), 0, s>>>((u32x4*)pool.k, (u32x4*)pool.v, (uint32_t)pool.pages, pool.shift, sq, moves, n_moves,
                                                                                                old, Hkv, chunks);
     return hipGetLastError();
 }

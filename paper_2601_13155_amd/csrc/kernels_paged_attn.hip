@@ -403,6 +403,7 @@ static int64_t pick_workgroups(PagedSeqs<NB>& sq, const PagedBatch& pb, int H, i
     return choice;
 }
 
+constexpr int64_t MAX_GROUPS = (1 << 24) - 1;   // of 256 threads: a launch has fewer than 2^32
 constexpr int64_t F32_WORKGROUPS = 512, ACCOUNT_WORKGROUPS = 1024;
 template <typename T, int D, int NB>
 static hipError_t launch_kvp_attn_t(const T* q, const PagedPool& pool, const PagedBatch& pb, int H, int Hkv, float* part, size_t part_floats, T* out, bool add, float decay,
@@ -484,7 +485,7 @@ static hipError_t launch_kvp_attn_t(const T* q, const PagedPool& pool, const Pag
     hipError_t e = hipSuccess;
     if constexpr (BF16) {
         const int64_t nm = items_of(many, COLS);
-        if (nm * Hkv > 0x7fffffff) return hipErrorInvalidValue;
+        if (nm * Hkv > MAX_GROUPS / 2) return hipErrorInvalidValue;
         if (nm > 0) e = launch_kvp_attn_many<NB>(q, pl, sq, (int)nm, H, Hkv, D, sh, stats, out, s);
         if (e != hipSuccess) return e;
         for (const bool keep : {true, false}) {   // those whose scores are kept, and those for which there was no room, or no wish
@@ -493,7 +494,7 @@ static hipError_t launch_kvp_attn_t(const T* q, const PagedPool& pool, const Pag
         }
     } else {
         const int64_t n = items_of(any, 32);
-        if (n * Hkv > 0x7fffffff) return hipErrorInvalidValue;
+        if (n * Hkv > MAX_GROUPS) return hipErrorInvalidValue;
         kvp_attn_kernel<D, NB><<<dim3((unsigned)(n * Hkv)), dim3(AW * 64), 0, s>>>(q, pl, sq, H, Hkv, c, sh, stats, out);
         e = hipGetLastError();
     }
@@ -504,7 +505,7 @@ static hipError_t launch_kvp_attn_t(const T* q, const PagedPool& pool, const Pag
             if (b < pb.n && sq.splits[b] > 1) n += sq.nq[b];
             sq.end[b] = (int32_t)n;
         }
-        if (n * H > 0x7fffffff) return hipErrorInvalidValue;
+        if (n * H > MAX_GROUPS) return hipErrorInvalidValue;
         int most = 1;
         for (int b = 0; b < pb.n; ++b) most = std::max(most, sq.splits[b]);
         const dim3 grid((unsigned)((n * H + MERGE_T / (D / 4) - 1) / (MERGE_T / (D / 4))));
@@ -548,7 +549,7 @@ static hipError_t launch_kvp_attn_t(const T* q, const PagedPool& pool, const Pag
             if (!joined || ((size_t)at <= room && at <= 0x7fffffff)) break;
         }
         const int64_t nt = tiles_of(anew, KEYS, true);
-        if (nt > 0x7fffffff) return hipErrorInvalidValue;
+        if (nt > MAX_GROUPS) return hipErrorInvalidValue;
         if (nt > 0) {
             if constexpr (BF16) {
                 e = launch_kvp_weights_many<NB>(q, pl, sq, (int)nt, H, Hkv, D, stats, rest, decay, s);

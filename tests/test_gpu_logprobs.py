@@ -144,3 +144,20 @@ def test_more_elements_than_32_bits(ctx):
     assert np.allclose(lp[at].cpu().numpy(), want[0], rtol=1e-5) and np.array_equal(ids[at].cpu().numpy(), want[2])
     del x
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_more_rows_than_a_launch_has(ctx, dtype):
+    """2^24 + 300 rows of two words, against torch in 64 bits."""
+    rows = (1 << 24) + 300
+    x = torch.randn((rows, 2), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(TD[dtype])
+    t = (torch.arange(rows, device="cuda") % 2).int()
+    lp, ent, tops = torch.zeros(rows, device="cuda"), torch.zeros(rows, device="cuda"), torch.zeros((rows, 1), device="cuda")
+    ids = torch.full((rows, 1), -5, dtype=torch.int32, device="cuda")
+    ctx.spts_token_logprobs(x, 2, rows, t, lp, ent, 1, ids, tops)
+    z = torch.log_softmax(x.double(), 1)
+    bound = (2 / 1024 + 64) * 2.0 ** -24 * 4 * (1 + float(z.abs().max()))     # as in check()
+    assert float((lp.double() - z.gather(1, t.long()[:, None])[:, 0]).abs().max()) <= bound
+    assert float((ent.double() + (z.exp() * z).sum(1)).abs().max()) <= bound
+    assert float((tops[:, 0].double() - z.max(1).values).abs().max()) <= bound
+    assert torch.equal(ids[:, 0].long(), (x[:, 1] > x[:, 0]).long())

@@ -418,6 +418,29 @@ def test_evict_long_and_short_rows_together():
     run_evict(shape_of(1, 1, 32, "bf16"), [530000], [270001], weights="few", seed=7, page=256, want_old=False)     # chunks of 8192 rows
 
 
+def test_evict_where_more_rows_move_than_workgroups_do_it():
+    """2 x 1049353 rows, the later half of them with the larger weights: all of it moves, in order."""
+    shape = shape_of(1, 1, 32, "bf16")
+    ctx = context(shape, 32768)
+    keep = (1 << 20) + 777
+    n = 2 * keep
+    kv = runtime.PagedKV(shape, -(-n // 256), 256, 1, n)
+    kv.reserve(0, n)
+    i = torch.arange(n, device="cuda")
+    fill = lambda shift: ((i[:, None] >> shift) & 255).to(torch.bfloat16).expand(-1, 32)     # (numbers that bf16 holds)
+    pages, at = i // 256, i % 256
+    kv.k[pages, 0, at], kv.v[pages, 0, at] = fill(0), fill(8)
+    kv.pos[0, :n] = (i + 7).int()
+    kv.weight[0, :n] = i.float()
+    kv.structs[0].count = n
+    old = torch.full((keep,), -1, dtype=torch.int32, device="cuda")
+    ctx.spts_kvp_evict(kv.pool, [keep], kv.structs, old_out=old)
+    torch.cuda.synchronize()
+    want = torch.arange(keep, n, device="cuda")
+    assert kv.counts == [keep] and torch.equal(old.long(), want) and torch.equal(kv.pos[0, :keep].long(), want + 7) and torch.equal(kv.weight[0, :keep], want.float())
+    assert torch.equal(kv.k[pages[:keep], 0, at[:keep]], fill(0)[keep:]) and torch.equal(kv.v[pages[:keep], 0, at[:keep]], fill(8)[keep:])
+
+
 def test_evict_where_more_rows_go_before_others_than_stay():
     run_evict(shape_of(2, 1, 32, "bf16"), [200, 90], [20, 40], below=[100, 0], start=[300, 0], seed=3)
     run_evict(shape_of(2, 1, 32, "bf16"), [200], [20], start=[-2 ** 31], seed=4, want_old=False)
