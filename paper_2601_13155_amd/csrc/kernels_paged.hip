@@ -471,7 +471,7 @@ __global__ void __launch_bounds__(256) kvp_move_kernel(u32x4* __restrict__ pk, u
             const int g = e / chunks, ch = e % chunks;
             const int64_t f = ((((int64_t)from * Hkv + g) << shift) + (mv.src & mask)) * chunks + ch;
             const int64_t t = ((((int64_t)to * Hkv + g) << shift) + (mv.dst & mask)) * chunks + ch;
-            const u32x4 kw = pk[f], vw = pv[f];
+            const u32x4 kw = __builtin_nontemporal_load(pk + f), vw = __builtin_nontemporal_load(pv + f);
             pk[t] = kw;
             pv[t] = vw;
         }

@@ -76,7 +76,9 @@ template <int D> struct Tile {
 constexpr int BKV = 64, NST = 5;
 constexpr float TAU = 8.0f, SUM_MAX = 4096.0f;
 
-template <int D, int NW, int NB>
+// ONCE: the sequences' columns fit a workgroup, so that nobody else reads their rows and the caches need not keep them (64 tokens after 30000 rows 59 us either way, behind a kernel that
+// wrote 1 GB 70 / 60).
+template <int D, int NW, int NB, bool ONCE>
 __global__ void __launch_bounds__(NW * 64, NW == 8 ? 2 : 1) kvp_many_kernel(const bf16_t* q, PoolView pool, PagedSeqs<NB> sq, int H, int Hkv, float c, Shares sh,
                                                                           float2* __restrict__ stats, bf16_t* out) {   // (out may be q: a workgroup has read its columns)
     using L = Tile<D>;
@@ -141,8 +143,13 @@ __global__ void __launch_bounds__(NW * 64, NW == 8 ? 2 : 1) kvp_many_kernel(cons
                 if (page - window > 63) { window = page; ids = entries(); }
                 const uint32_t id = (uint32_t)__builtin_amdgcn_readlane(ids, page - window);
                 const int64_t at = row_at(pool, id, row, g, Hkv, D) * 2;
-                dma16s(koff[i], pool.k + at, to + i * 1024);
-                dma16s(voff[i], pool.v + at, to + TILE + i * 1024);
+                if constexpr (ONCE) {
+                    dma16s_nt(koff[i], pool.k + at, to + i * 1024);
+                    dma16s_nt(voff[i], pool.v + at, to + TILE + i * 1024);
+                } else {
+                    dma16s(koff[i], pool.k + at, to + i * 1024);
+                    dma16s(voff[i], pool.v + at, to + TILE + i * 1024);
+                }
             } else {   // rows behind the last one are the last one again
                 const int r = row + lrow < n ? row + lrow : n - 1;
                 uint32_t kin = koff[i] - (uint32_t)(lrow * L::ROW), vin = voff[i] - (uint32_t)(lrow * L::ROW);
@@ -361,6 +368,9 @@ __global__ void __launch_bounds__(NW * 64, NW == 8 ? 2 : 1) kvp_many_kernel(cons
 // registers, values into its two stages of LDS, a block ahead.  16x16x32: S^T = K Q^T with key 8 (m / 4) + 4 t + m % 4 as operand row m of the t-th product, so that lane group kg
 // has the scores of keys 8 kg .. 8 kg + 7, which is the operand of O^T = V^T P^T as it stands.  Probabilities go in as two bf16 parts (off by 2^-17 of each at most), which costs
 // nothing here.  The maximum moves only when a score is 2^8 above it.
+// Rows are read once, by loads that do not leave them in the caches, where they would push out what other kernels wrote (us by plain loads / so: one token after 131071 rows with scores kept
+// 117 / 110, 16 of up to 13107 53 / 51; behind a kernel that wrote 1 GB 174 / 118 and 152 / 92.  Where it costs: all of 16 caches of 4000 rows in the last cache from the call before
+// 50 / 58, 16 sequences of 13106 rows on the same pages 58 / 63).
 template <int D, int NW, int NB, bool SCORES>
 __global__ void __launch_bounds__(NW * 64, 2) kvp_few_kernel(const bf16_t* q, PoolView pool, PagedSeqs<NB> sq, int H, int Hkv, float c, Shares sh, float2* __restrict__ stats,
                                                                  float* __restrict__ scores, bf16_t* out) {
@@ -395,14 +405,14 @@ __global__ void __launch_bounds__(NW * 64, 2) kvp_few_kernel(const bf16_t* q, Po
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int lr = i * L::ROWS_PER_LOAD + lrow, r = lr < left ? lr : left - 1;
-            dma16(pool.v + ((i * L::ROWS_PER_LOAD < 16 || r < 16 ? pa : pb) + r * D) * 2 + ((lchunk ^ L::vswz(lr)) << 4), lds0 + (uint32_t)(stage * BLOCK + i * 1024));
+            dma16_nt(pool.v + ((i * L::ROWS_PER_LOAD < 16 || r < 16 ? pa : pb) + r * D) * 2 + ((lchunk ^ L::vswz(lr)) << 4), lds0 + (uint32_t)(stage * BLOCK + i * 1024));
         }
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             const int lr = krow + 4 * t, r = lr < left ? lr : left - 1;
             const bf16_t* const kr = (const bf16_t*)pool.k + (r < 16 ? pa : pb) + r * D + 8 * kg;
 #pragma unroll
-            for (int i = 0; i < KI; ++i) kf[t][i] = *reinterpret_cast<const bf16x8*>(kr + 32 * i);
+            for (int i = 0; i < KI; ++i) kf[t][i] = __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(kr + 32 * i));
         }
     };
     // the lane's place among value rows 8 kg + (lane % 16) / 4 (and 4 on), dimensions 4 (lane % 4) of 16
@@ -666,21 +676,27 @@ __global__ void __launch_bounds__(WW * 64, 2) kvp_weights_mfma_kernel(const bf16
 }
 
 // ------------------------------------------------------------------ launches
-template <int D, int NW, int NB>
-static hipError_t launch_many(const bf16_t* q, const PoolView& pool, const PagedSeqs<NB>& sq, int items, int H, int Hkv, const Shares& sh, float2* stats, bf16_t* out, hipStream_t s) {
-    constexpr int LDS = NST * 2 * BKV * Tile<D>::ROW;
-    const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(&kvp_many_kernel<D, NW, NB>), LDS);
+template <int D, int NB, bool ONCE>
+static hipError_t launch_many_once(const bf16_t* q, const PoolView& pool, const PagedSeqs<NB>& sq, int items, int H, int Hkv, const Shares& sh, float2* stats, bf16_t* out, hipStream_t s) {
+    constexpr int LDS = NST * 2 * BKV * Tile<D>::ROW, NW = kvp_many_waves(D);
+    const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(&kvp_many_kernel<D, NW, NB, ONCE>), LDS);
     if (e != hipSuccess) return e;
-    kvp_many_kernel<D, NW, NB><<<dim3((unsigned)(items * Hkv)), dim3(NW * 64), LDS, s>>>(q, pool, sq, H, Hkv, PAGED_LOG2E / sqrtf((float)D), sh, stats, out);
+    kvp_many_kernel<D, NW, NB, ONCE><<<dim3((unsigned)(items * Hkv)), dim3(NW * 64), LDS, s>>>(q, pool, sq, H, Hkv, PAGED_LOG2E / sqrtf((float)D), sh, stats, out);
     return hipGetLastError();
+}
+
+template <int D, int NB>
+static hipError_t launch_many(const bf16_t* q, const PoolView& pool, const PagedSeqs<NB>& sq, int items, int H, int Hkv, const Shares& sh, float2* stats, bf16_t* out, hipStream_t s) {
+    bool once = true;
+    for (int b = 0; b < NB; ++b) once = once && (int64_t)sq.nq[b] * (H / Hkv) <= kvp_many_waves(D) * 32;
+    return once ? launch_many_once<D, NB, true>(q, pool, sq, items, H, Hkv, sh, stats, out, s) : launch_many_once<D, NB, false>(q, pool, sq, items, H, Hkv, sh, stats, out, s);
 }
 
 template <int NB>
 hipError_t launch_kvp_attn_many(const bf16_t* q, const PoolView& pool, const PagedSeqs<NB>& sq, int items, int H, int Hkv, int d, const Shares& sh, float2* stats, bf16_t* out,
                                 hipStream_t s) {
-    return d == 128 ? launch_many<128, kvp_many_waves(128), NB>(q, pool, sq, items, H, Hkv, sh, stats, out, s)
-         : d == 64 ? launch_many<64, kvp_many_waves(64), NB>(q, pool, sq, items, H, Hkv, sh, stats, out, s)
-                   : launch_many<32, kvp_many_waves(32), NB>(q, pool, sq, items, H, Hkv, sh, stats, out, s);
+    return d == 128 ? launch_many<128, NB>(q, pool, sq, items, H, Hkv, sh, stats, out, s)
+         : d == 64 ? launch_many<64, NB>(q, pool, sq, items, H, Hkv, sh, stats, out, s) : launch_many<32, NB>(q, pool, sq, items, H, Hkv, sh, stats, out, s);
 }
 template hipError_t launch_kvp_attn_many<1>(const bf16_t*, const PoolView&, const PagedSeqs<1>&, int, int, int, int, const Shares&, float2*, bf16_t*, hipStream_t);
 template hipError_t launch_kvp_attn_many<DECODE_MAX_BATCH>(const bf16_t*, const PoolView&, const PagedSeqs<DECODE_MAX_BATCH>&, int, int, int, int, const Shares&, float2*, bf16_t*,

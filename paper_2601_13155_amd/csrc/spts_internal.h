@@ -55,6 +55,9 @@ __device__ inline void dma16s(uint32_t voff, const void* sbase, uint32_t lds_bas
 __device__ inline void dma16s_nt(uint32_t voff, const void* sbase, uint32_t lds_base) {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt\n\t" ::"v"(voff), "s"(sbase), "s"(lds_base) : "memory");
 }
+__device__ inline void dma16_nt(const void* gptr, uint32_t lds_base) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt\n\t" ::"v"(gptr), "s"(lds_base) : "memory");
+}
 // One dword a lane (global_load_lds_dword) from the lane's own address, to lds_base + 4 * lane, of data that is read once
 __device__ inline void dma4_nt(const void* src, uint32_t lds_base) {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off nt\n\t" ::"v"(src), "s"(lds_base) : "memory");
