@@ -404,7 +404,7 @@ static int64_t pick_workgroups(PagedSeqs<NB>& sq, const PagedBatch& pb, int H, i
 }
 
 constexpr int64_t MAX_GROUPS = (1 << 24) - 1;   // of 256 threads: a launch has fewer than 2^32
-constexpr int64_t F32_WORKGROUPS = 512, ACCOUNT_WORKGROUPS = 1024;
+constexpr int64_t F32_WORKGROUPS = 512;
 template <typename T, int D, int NB>
 static hipError_t launch_kvp_attn_t(const T* q, const PagedPool& pool, const PagedBatch& pb, int H, int Hkv, float* part, size_t part_floats, T* out, bool add, float decay,
                                     hipStream_t s) {
@@ -535,8 +535,10 @@ static hipError_t launch_kvp_attn_t(const T* q, const PagedPool& pool, const Pag
         int64_t work = 0;
         for (int b = 0; b < pb.n; ++b)
             if (anew(b)) work += (pb.count[b] + KEYS - 1) / KEYS * ((columns(pb, b, G) + 31) / 32) * Hkv;
+        // Three workgroups for each of the 512 that are at work at a time, but no fewer than 10 blocks each as long as all 512 have one (us with 1024 workgroups / so, all kernels of the call: 300
+        // tokens after 3700 rows, 8 heads of 4, 83 / 75; six of 300 after 3700, 4 heads of 7, 216 / 208; six of 600 after 8400 871 / 824; 20 after 7980 47 / 45; 64 after 1936 42 / 42)
         bool joined = false;
-        for (int64_t target = std::max<int64_t>(1, work / ACCOUNT_WORKGROUPS); work > 0; target *= 2) {
+        for (int64_t target = std::max(std::max<int64_t>(1, work / 1536), std::min<int64_t>((work + 511) / 512, 10)); work > 0; target *= 2) {
             int64_t at = 0;
             joined = false;
             for (int b = 0; b < pb.n; ++b) {
