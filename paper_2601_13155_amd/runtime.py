@@ -465,11 +465,13 @@ class PagedKV:
         self.structs = (binding.spts_kvp * sequences)()
         self.structs._keepalive = (self._table, self.pos, self.weight)
         for b, s in enumerate(self.structs):
-            s.table, s.pos = self._table[b].data_ptr(), self.pos[b].data_ptr()
-            s.weight = self.weight[b].data_ptr() if weights else None
+            s.table, s.pos = self._table.data_ptr() + 4 * stride * b, self.pos.data_ptr() + 4 * per * page * b
+            s.weight = self.weight.data_ptr() + 4 * per * page * b if weights else None
             s.capacity = per * page
-        self._free = list(range(pages) if free is None else free)[::-1]
-        if sorted(self._free) != list(range(pages)):
+        every = np.arange(pages, dtype=np.int32)
+        self._free = (every if free is None else np.array(free, dtype=np.int32).reshape(-1))[::-1].copy()      # the first _left are free, the last of them is the next
+        self._left = pages
+        if not np.array_equal(np.sort(self._free), every):
             raise ValueError(f"free: each of {pages} pages once")
         self.pages = [[] for _ in range(sequences)]     # the pages of each sequence, as its table has them
 
@@ -479,7 +481,7 @@ class PagedKV:
 
     @property
     def free_pages(self) -> int:
-        return len(self._free)
+        return self._left
 
     def reserve(self, b: int, rows: int, ctx: Optional[binding.Context] = None):
         """Pages for the first `rows` rows of sequence b; ValueError where its capacity or the pool has no room.  Writes the table from the
@@ -488,20 +490,23 @@ class PagedKV:
         have, need = len(self.pages[b]), -(-int(rows) // self.page)
         if need * self.page > self.structs[b].capacity:
             raise ValueError(f"sequence {b}: {rows} rows exceed its capacity of {self.structs[b].capacity}")
-        if need - have > len(self._free):
-            raise ValueError(f"{need - have} pages needed, {len(self._free)} free")
+        if need - have > self._left:
+            raise ValueError(f"{need - have} pages needed, {self._left} free")
         if need > have:
-            new = [self._free.pop() for _ in range(need - have)]
-            self.pages[b] += new
+            left = self._left - (need - have)
+            new = self._free[left:self._left][::-1].copy()
+            self._left = left
+            self.pages[b] += new.tolist()
             with _on_stream_of(ctx) if ctx is not None else contextlib.nullcontext():
-                self.table[b, have:need].copy_(torch.tensor(new, dtype=torch.int32))
+                self.table[b, have:need].copy_(torch.from_numpy(new))
 
     def release(self, b: int):
         """Hands back the pages behind sequence b's count rows (all of them where it is 0).  Call it when the work on them is in the stream that
         their next owner uses too."""
         need = -(-int(self.structs[b].count) // self.page)
         while len(self.pages[b]) > need:
-            self._free.append(self.pages[b].pop())
+            self._free[self._left] = self.pages[b].pop()
+            self._left += 1
 
     def append_cache(self, ctx: binding.Context, b: int, cache: "KVCache"):
         """Takes over every pair of a prefill's cache behind sequence b's rows (their weights 0); ValueError where it has other heads or
