@@ -14,11 +14,11 @@ namespace spts {
 namespace {
 typedef paged_f32x16 f32x16;
 __device__ inline f32x16 mfma_f32(float a, float b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
-// N consecutive elements as fp32 (16-byte aligned)
-template <int N> __device__ inline void load_row(const float* p, float (&v)[N]) {
+// N of 2 N elements, every other four (16-byte aligned)
+template <int N> __device__ inline void load_quads(const float* p, float (&v)[N]) {
 #pragma unroll
     for (int i = 0; i < N; i += 4) {
-        const f32x4 w = *reinterpret_cast<const f32x4*>(p + i);
+        const f32x4 w = *reinterpret_cast<const f32x4*>(p + 2 * i);
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[i + e] = w[e];
     }
@@ -27,11 +27,12 @@ __device__ inline void store4(float* p, f32x4 v, float f) { *reinterpret_cast<f3
 __device__ inline void store4(bf16_t* p, f32x4 v, float f) { *reinterpret_cast<u32x2*>(p) = u32x2{cvt_pk_bf16(v[0] * f, v[1] * f), cvt_pk_bf16(v[2] * f, v[3] * f)}; }
 }  // namespace
 
-// On the fp32 matrix instruction 32x32x2.  S^T = K Q^T: operand rows are keys, columns queries; of the two halves of a wavefront one multiplies the first, one the second half of the
-// dimensions, so a lane's operand is half a row.  O^T += V^T P^T: result element r of lane (l, half) is key 8 (r / 4) + 4 half + r % 4 of column l, which is the second operand of the
-// r-th product of V^T as it stands.  The four wavefronts of a workgroup take blocks of 32 keys in turn and meet in LDS; a lane
-// asks for the next piece of a key, and the next 32 dimensions of the values, before it multiplies these: 128 tokens after 4000 rows of 8 heads (d = 128) 121 us, 71 TFLOP/s of the
-// 154 that a large fp32 product reaches here.
+// On the fp32 matrix instruction 32x32x2.  S^T = K Q^T: operand rows are keys, columns queries; the two halves of a wavefront multiply every other four of the dimensions, so a lane's
+// operand is half a row and a load takes 32 bytes of each key (halves that are 64 dimensions apart touch twice the lines a load, more than the first cache holds until the rest of them is
+// wanted: 128 tokens after 3872 rows 126 us for 115, one token after 60000 156 for 139, the accounts 57 for 45).  O^T += V^T P^T: result element r of lane (l, half) is key
+// 8 (r / 4) + 4 half + r % 4 of column l, which is the second operand of the r-th product of V^T as it stands.  The four wavefronts of a workgroup take blocks of 32 keys in turn and meet in
+// LDS; a lane asks for the next piece of a key, and the next 32 dimensions of the values, before it multiplies these: 128 tokens after 3872 rows of 8 heads of 4 (d = 128) 115 us, 72
+// TFLOP/s of the 154 that a large fp32 product reaches here.
 // A block that some column does not see entirely has its scores set to -inf there, and values that are not finite kept out of the product (0 times them would be NaN): two more products
 // count those that a column does see and put the infinity or NaN where it belongs.
 constexpr int AW = 4;
@@ -55,7 +56,7 @@ __global__ void __launch_bounds__(AW * 64, 2) kvp_attn_kernel(const float* q, Po
     const int64_t k0 = (int64_t)split * sq.per[b], k1 = k0 + sq.per[b] < seen_any ? k0 + sq.per[b] : seen_any;
 
     float qf[D / 2];
-    load_row(q + ((int64_t)(sq.first[b] + cc / G) * H + g * G + cc % G) * D + lh * (D / 2), qf);
+    load_quads(q + ((int64_t)(sq.first[b] + cc / G) * H + g * G + cc % G) * D + 4 * lh, qf);
     f32x16 o[DB];
 #pragma unroll
     for (int i = 0; i < DB; ++i) o[i] = zero16();
@@ -65,9 +66,9 @@ __global__ void __launch_bounds__(AW * 64, 2) kvp_attn_kernel(const float* q, Po
     auto rows_of = [&](int64_t key0) {
         const int left = (int)(n - key0 < 32 ? n - key0 : 32), row = l32 < left ? l32 : left - 1;
         const int64_t p0 = page_at(pool, table, key0, g, Hkv, D), p1 = left > 16 ? page_at(pool, table, key0 + 16, g, Hkv, D) : p0 + 16 * D;
-        return Rows{(const float*)pool.k + (row < 16 ? p0 + row * D : p1 + (row - 16) * D) + lh * (D / 2), (const float*)pool.v + p0 + 4 * lh * D + l32, p1 - p0 - 16 * D};
+        return Rows{(const float*)pool.k + (row < 16 ? p0 + row * D : p1 + (row - 16) * D) + 4 * lh, (const float*)pool.v + p0 + 4 * lh * D + l32, p1 - p0 - 16 * D};
     };
-    auto load_key = [&](const Rows& at, int ch, float (&v)[CH]) __attribute__((always_inline)) { load_row(at.k + ch * CH, v); };
+    auto load_key = [&](const Rows& at, int ch, float (&v)[CH]) __attribute__((always_inline)) { load_quads(at.k + 2 * ch * CH, v); };
     auto load_values = [&](const Rows& at, int i, int left, float (&v)[16]) __attribute__((always_inline)) {
         if (left == 32) {
 #pragma unroll
@@ -285,11 +286,11 @@ __global__ void __launch_bounds__(AW * 64) kvp_weights_kernel(const float* __res
         if (key0 >= n - nq + last / G + 1) continue;
         if (g != have) {
             have = g;
-            load_row((const float*)pool.k + page_at(pool, sq.table[b], key0 + (row & 16), g, Hkv, D) + (row & 15) * D + lh * (D / 2), kf);
+            load_quads((const float*)pool.k + page_at(pool, sq.table[b], key0 + (row & 16), g, Hkv, D) + (row & 15) * D + 4 * lh, kf);
         }
         const int64_t head = (int64_t)(sq.first[b] + cc / G) * H + g * G + cc % G;
         float qf[D / 2];
-        load_row(q + head * D + lh * (D / 2), qf);
+        load_quads(q + head * D + 4 * lh, qf);
         const float2 st = stats[head];
         const int seen = col < cols ? n - nq + cc / G + 1 : 0;
         f32x16 s = zero16();
