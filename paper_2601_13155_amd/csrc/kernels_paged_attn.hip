@@ -431,15 +431,22 @@ static hipError_t launch_kvp_attn_t(const T* q, const PagedPool& pool, const Pag
     int64_t want = F32_WORKGROUPS, want_few = 256, least_few = 256, least = 256;
     if constexpr (BF16) {
         want = pick_workgroups(sq, pb, H, Hkv, D, COLS, 256, many);
-        // Few columns: two workgroups fit a CU.  A single sequence's shares are all alike, one a CU; those of several are not, and more of them even out (us at 256 / 384 / 512 / 1024
-        // workgroups: 131072 rows of 8 heads 95 / 105 / 98 / 102, 30000 24.3 / 26.7 / 25.9 / 29.7; 16 sequences of 1048 .. 13107 rows, 4 heads, 53 / 44 / 47 / 43, of 480 .. 6000 rows,
-        // 8 heads, 46 / 38 / 39 / 40).  Short caches in one share, without a merge: 301 rows 7.7 for 9.1, 16 of up to 501 10.4 for 11.8; two shares of 517 rows 9.2, one 9.9.
+        // Few columns: a workgroup a CU where the shares come out alike (the longest times the CUs within 1.25 of all keys), with accounts such that their scores wait in LDS; otherwise, of several
+        // sequences, 384, two of which fit a CU, to even them out.  Us at 384 / so, behind reads of other data: 16 sequences of 1048 .. 13106 rows, 4 heads of 7, 59 / 53, with accounts 74 / 62;
+        // five of 1600 .. 20000, 8 heads, 55 / 48 and 64 / 54; two of up to 60000, 4 heads, 43 / 36 and 52 / 43; 16 of 640 .. 8000, 8 heads, where the least number of shares is uneven, 64 at
+        // 384, 85 at 224.  Short caches in one share, without a merge: 301 rows 7.7 for 9.1, 16 of up to 501 10.4 for 11.8; two shares of 517 rows 9.2, one 9.9.
         int n = 0;
-        int64_t longest = 0;
+        int64_t longest = 0, total = 0, cols = 0;
         for (int b = 0; b < pb.n; ++b)
-            if (few(b)) { ++n; longest = std::max(longest, pb.count[b]); }
+            if (few(b)) { ++n; longest = std::max(longest, pb.count[b]); total += pb.count[b] * Hkv; cols = std::max(cols, columns(pb, b, G)); }
         if (n > 1) want_few = 384;
         if (longest <= 512) least_few = 512;
+        for (int64_t w = CUS; n > 0 && w >= CUS * 5 / 8; w -= 8) {
+            int64_t share;
+            if (share_keys(sq, pb, Hkv, G, KVP_FEW_COLS, w, least_few, few, &share) > CUS) continue;
+            if ((!add || kvp_few_keeps(D, (int)cols, share)) && 4 * share * CUS <= 5 * total) want_few = w;
+            break;
+        }
     } else {
         // Two workgroups a CU (us at 256 / 512 / 1024: 128 tokens after 4000 rows, 8 heads of 4, d = 128, 125 / 121 / 136, one token after 60000 163 / 152 / 155, four of 300 after 3000
         // 33 / 29 / 32), and a block of keys for every wavefront where that leaves most of the chip idle (one token after 500 rows of two heads 8.3, with two blocks each 11.7; three

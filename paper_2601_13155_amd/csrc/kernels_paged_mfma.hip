@@ -4,6 +4,7 @@
 // columns that sixteen lanes address, each lane gets a column) gives them four at a time, so a cache needs no transposed copy and a row is written once.
 #include "spts_paged.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace spts {
@@ -368,15 +369,17 @@ __global__ void __launch_bounds__(NW * 64, NW == 8 ? 2 : 1) kvp_many_kernel(cons
 // registers, values into its two stages of LDS, a block ahead.  16x16x32: S^T = K Q^T with key 8 (m / 4) + 4 t + m % 4 as operand row m of the t-th product, so that lane group kg
 // has the scores of keys 8 kg .. 8 kg + 7, which is the operand of O^T = V^T P^T as it stands.  Probabilities go in as two bf16 parts (off by 2^-17 of each at most), which costs
 // nothing here.  The maximum moves only when a score is 2^8 above it.
+// Scores for the accounts wait in LDS for the end where a share's fit there and a workgroup has a CU to itself: stores among the reads cost more than their bytes (131071 rows 110 us by these
+// for 97, five of 1600 .. 20000 64 / 55; without accounts 87).
 // Rows are read once, by loads that do not leave them in the caches, where they would push out what other kernels wrote (us by plain loads / so: one token after 131071 rows with scores kept
 // 117 / 110, 16 of up to 13107 53 / 51; behind a kernel that wrote 1 GB 174 / 118 and 152 / 92.  Where it costs: all of 16 caches of 4000 rows in the last cache from the call before
 // 50 / 58, 16 sequences of 13106 rows on the same pages 58 / 63).
 template <int D, int NW, int NB, bool SCORES>
 __global__ void __launch_bounds__(NW * 64, 2) kvp_few_kernel(const bf16_t* q, PoolView pool, PagedSeqs<NB> sq, int H, int Hkv, float c, Shares sh, float2* __restrict__ stats,
-                                                                 float* __restrict__ scores, bf16_t* out) {
+                                                                 float* __restrict__ scores, int kept, bf16_t* out) {
     using L = Tile<D>;
     constexpr int KI = D / 32, VM = D / 16, BLOCK = 32 * L::ROW, LOADS = BLOCK / 1024, LD = D + 4;
-    extern __shared__ __attribute__((aligned(1024))) char smem[];   // [NW][2][BLOCK] values; then [NW][16][LD] outputs and [NW][16][2] maxima and sums
+    extern __shared__ __attribute__((aligned(1024))) char smem[];   // [NW][2][BLOCK] values; then [NW][16][LD] outputs and [NW][16][2] maxima and sums.  Behind these [cols][kept] scores
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, kg = lane >> 4;
     const int g = (int)(blockIdx.x % Hkv), G = H / Hkv;
     int first;
@@ -455,8 +458,16 @@ __global__ void __launch_bounds__(NW * 64, 2) kvp_few_kernel(const bf16_t* q, Po
         }
         if constexpr (SCORES) {   // behind the next block's loads, so that the wait for those is none for these; rows of whole blocks of 32 keys, in the order that stores whole
             // pieces of 64 bytes: place 16 t + 4 kg + r has key 8 kg + 4 t + r (lanes without a column store the last column's again)
-            *reinterpret_cast<f32x4*>(to_scores + key0) = s[0];
-            *reinterpret_cast<f32x4*>(to_scores + key0 + 16) = s[1];
+            if (kept > 0) {
+                float* const to = reinterpret_cast<float*>(smem + kvp_few_lds(D)) + l16 * kept + (key0 - k0) + 4 * kg;
+                if (l16 < cols) {
+                    *reinterpret_cast<f32x4*>(to) = s[0];
+                    *reinterpret_cast<f32x4*>(to + 16) = s[1];
+                }
+            } else {
+                *reinterpret_cast<f32x4*>(to_scores + key0) = s[0];
+                *reinterpret_cast<f32x4*>(to_scores + key0 + 16) = s[1];
+            }
         }
         if (__ballot(mx > m + TAU) != 0) {
             mx = fmaxf(mx, __shfl_xor(mx, 16));
@@ -511,6 +522,16 @@ __global__ void __launch_bounds__(NW * 64, 2) kvp_few_kernel(const bf16_t* q, Po
     for (int i = 0; i < VM; ++i) *reinterpret_cast<f32x4*>(so + (wave * 16 + l16) * LD + 16 * i + 4 * kg) = o[i];
     if (kg == 0) { sml[(wave * 16 + l16) * 2] = m; sml[(wave * 16 + l16) * 2 + 1] = l; }
     __syncthreads();
+    if constexpr (SCORES) {
+        if (kept > 0) {
+            const float* const from = reinterpret_cast<const float*>(smem + kvp_few_lds(D));
+            const int len = k1 > k0 ? (k1 - k0 + 31) / 32 * 32 : 0;
+            for (int cn = 0; cn < cols; ++cn) {
+                float* const to = scores + ((int64_t)sq.scores[b] + (g * cols + cn) * score_blocks(n)) * 32 + k0;
+                for (int i = 4 * tid; i < len; i += 4 * NW * 64) *reinterpret_cast<f32x4*>(to + i) = *reinterpret_cast<const f32x4*>(from + cn * kept + i);
+            }
+        }
+    }
     for (int i = tid; i < cols * (D / 4); i += NW * 64) {
         const int cn = i / (D / 4), e = i % (D / 4) * 4;
         float M = PAGED_LOWEST, sum = 0.f;
@@ -705,10 +726,25 @@ template hipError_t launch_kvp_attn_many<DECODE_MAX_BATCH>(const bf16_t*, const 
 template <int D, int NB, bool SCORES>
 static hipError_t launch_few_s(const bf16_t* q, const PoolView& pool, const PagedSeqs<NB>& sq, int items, int H, int Hkv, const Shares& sh, float2* stats, float* scores, bf16_t* out,
                              hipStream_t s) {
-    constexpr int NW = 4, RING = NW * 2 * 32 * Tile<D>::ROW, MEET = NW * 16 * (D + 4 + 2) * 4, LDS = RING > MEET ? RING : MEET;
-    const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(&kvp_few_kernel<D, NW, NB, SCORES>), LDS);
+    constexpr int NW = KVP_FEW_WAVES, LDS = kvp_few_lds(D);
+    static_assert(LDS % 16 == 0, "scores lie behind it");
+    const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(&kvp_few_kernel<D, NW, NB, SCORES>), SCORES ? KVP_LDS : LDS);
     if (e != hipSuccess) return e;
-    kvp_few_kernel<D, NW, NB, SCORES><<<dim3((unsigned)(items * Hkv)), dim3(NW * 64), LDS, s>>>(q, pool, sq, H, Hkv, PAGED_LOG2E / sqrtf((float)D), sh, stats, scores, out);
+    int kept = 0, bytes = 0;
+    if (SCORES && (int64_t)items * Hkv <= CUS) {
+        int cols = 0;
+        int64_t longest = 0;
+        for (int b = 0; b < NB; ++b) {
+            if (sq.scores[b] < 0) continue;
+            cols = std::max(cols, sq.nq[b] * (H / Hkv));
+            longest = std::max<int64_t>(longest, std::min(sq.per[b], sq.count[b]));
+        }
+        if (kvp_few_keeps(D, cols, longest)) {
+            kept = (int)kvp_kept_row(longest);
+            bytes = cols * kept * 4;
+        }
+    }
+    kvp_few_kernel<D, NW, NB, SCORES><<<dim3((unsigned)(items * Hkv)), dim3(NW * 64), LDS + bytes, s>>>(q, pool, sq, H, Hkv, PAGED_LOG2E / sqrtf((float)D), sh, stats, scores, kept, out);
     return hipGetLastError();
 }
 

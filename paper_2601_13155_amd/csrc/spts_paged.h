@@ -75,5 +75,11 @@ template <int NB> hipError_t launch_kvp_attn_many(const bf16_t* q, const PoolVie
 template <int NB> hipError_t launch_kvp_weights_many(const bf16_t* q, const PoolView& pool, const PagedSeqs<NB>& sq, int items, int H, int Hkv, int d, const float2* stats, float* sums,
                                                      float decay, hipStream_t s);
 constexpr int KVP_FEW_COLS = 16, KVP_WEIGHT_KEYS = 256;
+// Few columns: wavefronts of a workgroup, its LDS (two stages of 32 values each, then outputs, maxima and sums where they meet), and the scores of a share that are kept behind it: rows of
+// `longest` keys, whose 16 words more spread the columns over the banks.  They are kept where the call has no more workgroups than CUs.
+constexpr int KVP_FEW_WAVES = 4, KVP_LDS = 160 * 1024, CUS = 256;
+constexpr int kvp_few_lds(int d) { return KVP_FEW_WAVES * (2 * 32 * 2 * d > 16 * (d + 6) * 4 ? 2 * 32 * 2 * d : 16 * (d + 6) * 4); }
+constexpr int64_t kvp_kept_row(int64_t longest) { return (longest + 31) / 32 * 32 + 16; }
+constexpr bool kvp_few_keeps(int d, int cols, int64_t longest) { return cols * kvp_kept_row(longest) * 4 <= KVP_LDS - kvp_few_lds(d); }
 constexpr int kvp_many_waves(int d) { return d == 32 ? 4 : 8; }   // of a workgroup, 32 columns each (a tile of 64 keys of 32 dimensions is four loads)
 }  // namespace spts
