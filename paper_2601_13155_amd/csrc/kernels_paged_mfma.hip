@@ -371,9 +371,9 @@ __global__ void __launch_bounds__(NW * 64, NW == 8 ? 2 : 1) kvp_many_kernel(cons
 // nothing here.  The maximum moves only when a score is 2^8 above it.
 // Scores for the accounts wait in LDS for the end where a share's fit there and a workgroup has a CU to itself: stores among the reads cost more than their bytes (131071 rows 110 us by these
 // for 97, five of 1600 .. 20000 64 / 55; without accounts 87).
-// Rows are read once, by loads that do not leave them in the caches, where they would push out what other kernels wrote (us by plain loads / so: one token after 131071 rows with scores kept
-// 117 / 110, 16 of up to 13107 53 / 51; behind a kernel that wrote 1 GB 174 / 118 and 152 / 92.  Where it costs: all of 16 caches of 4000 rows in the last cache from the call before
-// 50 / 58, 16 sequences of 13106 rows on the same pages 58 / 63).
+// Rows are read once, by loads that do not leave them in the caches, where they would push out what other kernels wrote (us by plain loads / so, when scores went to memory as they came:
+// one token after 131071 rows with accounts 117 / 110, behind a kernel that wrote 1 GB 174 / 118; 16 of up to 13106 in 384 workgroups 53 / 51, behind such a kernel 152 / 92.  Where it costs:
+// all of 16 caches of 4000 rows in the last cache from the call before 50 / 58, 16 sequences of 13106 rows on the same pages 58 / 63).
 template <int D, int NW, int NB, bool SCORES>
 __global__ void __launch_bounds__(NW * 64, 2) kvp_few_kernel(const bf16_t* q, PoolView pool, PagedSeqs<NB> sq, int H, int Hkv, float c, Shares sh, float2* __restrict__ stats,
                                                                  float* __restrict__ scores, int kept, bf16_t* out) {
