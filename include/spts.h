@@ -417,7 +417,8 @@ int spts_kvp_append(spts_ctx *ctx, const spts_kv_pool *pool, const void *k, cons
  * of the last rows of caches[b], which have been appended: with n of them, query i of sequence b sees rows 0 .. count - n + i, and
  * out = softmax(q K^T / sqrt(d)) V over these, query head h reading key/value head h / (H / Hkv).  A sequence may have no queries; more queries than
  * rows are SPTS_EINVAL, more in all than the context's max_tokens SPTS_EWORKSPACE.  Rows that a query does not see do not matter, whatever
- * they hold; a query all of whose scores are -inf gives zeros.  Probabilities of chunks are rounded to the element type
+ * they hold; an infinite value gives that infinity, NaN where two meet, to the queries that see it with a weight above 0 (in fp32);
+ * a query all of whose scores are -inf gives zeros.  Probabilities of chunks are rounded to the element type
  * before they meet the values, of single tokens (at most 16 queries and heads of a key/value head) they keep 16 bits or more.
  * add_weights != 0: for every sequence with queries, weight[j] = decay * weight[j] + the softmax weight of row j summed over the
  * call's queries and all heads, for its count rows (0 <= decay <= 1; with decay = 0 the old weights are not read); all caches of such sequences need

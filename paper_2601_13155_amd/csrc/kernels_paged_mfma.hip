@@ -33,6 +33,8 @@ __device__ inline bool any_odd(bf16x8 v) {
     for (int j = 0; j < 4; ++j) odd |= (w[j] & 0x7f80u) == 0x7f80u || (w[j] & 0x7f800000u) == 0x7f800000u;
     return odd;
 }
+// The first of two bf16 parts of a probability: the largest number of that type below it (0 for 0), so that the second is above 0 too and an infinite value times either is that infinity
+__device__ inline uint32_t first_part(float p) { return __builtin_elementwise_sub_sat(__float_as_uint(p), 1u) & 0xffff0000u; }
 // v without its infinities and NaN; up / down: 1 where v is +inf / -inf, both where it is NaN
 __device__ inline bf16x8 split_odd(bf16x8 v, bf16x8* up, bf16x8* down) {
     u32x4 w = __builtin_bit_cast(u32x4, v), u, d;
@@ -367,8 +369,8 @@ __global__ void __launch_bounds__(NW * 64, NW == 8 ? 2 : 1) kvp_many_kernel(cons
 // ------------------------------------------------------------------ few columns
 // Up to 16 columns (single tokens, mostly): bound by the cache's bytes.  The wavefronts of a workgroup take blocks of 32 keys in turn, each on its own, without barriers: keys come into
 // registers, values into its two stages of LDS, a block ahead.  16x16x32: S^T = K Q^T with key 8 (m / 4) + 4 t + m % 4 as operand row m of the t-th product, so that lane group kg
-// has the scores of keys 8 kg .. 8 kg + 7, which is the operand of O^T = V^T P^T as it stands.  Probabilities go in as two bf16 parts (off by 2^-17 of each at most), which costs
-// nothing here.  The maximum moves only when a score is 2^8 above it.
+// has the scores of keys 8 kg .. 8 kg + 7, which is the operand of O^T = V^T P^T as it stands.  Probabilities go in as two bf16 parts, both above 0 (off by 2^-16 of each at most), which
+// costs nothing here.  The maximum moves only when a score is 2^8 above it.
 // Scores for the accounts wait in LDS for the end where a share's fit there and a workgroup has a CU to itself: stores among the reads cost more than their bytes (131071 rows 110 us by these
 // for 97, five of 1600 .. 20000 64 / 55; without accounts 87).
 // Rows are read once, by loads that do not leave them in the caches, where they would push out what other kernels wrote (us by plain loads / so, when scores went to memory as they came:
@@ -485,9 +487,9 @@ __global__ void __launch_bounds__(NW * 64, 2) kvp_few_kernel(const bf16_t* q, Po
         for (int j = 0; j < 8; j += 2) {
             const float p0 = __builtin_amdgcn_exp2f(s[j >> 2][j & 3] - m), p1 = __builtin_amdgcn_exp2f(s[j >> 2][(j & 3) + 1] - m);
             l += p0 + p1;
-            const uint32_t w = cvt_pk_bf16(p0, p1);
-            hi[j >> 1] = w;
-            lo[j >> 1] = cvt_pk_bf16(p0 - __uint_as_float(w << 16), p1 - __uint_as_float(w & 0xffff0000u));
+            const uint32_t h0 = first_part(p0), h1 = first_part(p1);
+            hi[j >> 1] = __builtin_amdgcn_perm(h1, h0, 0x07060302u);
+            lo[j >> 1] = cvt_pk_bf16(p0 - __uint_as_float(h0), p1 - __uint_as_float(h1));
         }
         const bf16x8 ph = __builtin_bit_cast(bf16x8, hi), pl = __builtin_bit_cast(bf16x8, lo);
         const uint32_t at = lds0 + (uint32_t)(stage * BLOCK);

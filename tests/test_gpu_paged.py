@@ -197,6 +197,41 @@ def test_infinite_values_reach_the_queries_that_see_them(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [0.0, 0.3])         # 0: all weights alike, probabilities of exactly 1
+@pytest.mark.parametrize("rows,m", [(40, 1), (600, 1), (600, 4), (5000, 2), (5000, 40)])
+@pytest.mark.parametrize("d", [32, 64, 128])
+def test_infinite_values_wherever_their_row_lies(d, rows, m, scale, dtype):
+    """Infinite and NaN values in blocks of keys that every query sees, in the last ones, in one share or several: each query gets the infinity of the dimensions that it sees one in (NaN
+    where two meet), the other dimensions and the accounts are as without them."""
+    shape = shape_of(8, 2, d, dtype)
+    ctx = context(shape)
+    kv, host = filled(shape, 16, [rows], seed=rows + d)
+    k, v = (t.clone() for t in host[0])
+    late = rows - 1 - m // 2                # not all queries see it
+    for at, e, x in ((0, 1, math.inf), (7, 2, -math.inf), (rows // 2, 3, math.inf), (rows // 2 + 1, 30, -math.inf), (rows // 3, 5, math.nan), (late, 7, math.inf),
+                     (3, 9, math.inf), (rows // 2, 9, math.inf), (3, 11, math.inf), (late, 11, -math.inf), (rows - 1, 13, -math.inf), (rows // 4, d - 1, math.inf)):
+        v[at, :, e] = x
+    put(kv, 0, 0, k, v)
+    q = (scale * torch.randn((m, 8, d), generator=torch.Generator().manual_seed(9))).to(TD[dtype]).cuda()
+    fine = torch.where(torch.isfinite(v), v, torch.zeros_like(v))
+    want, spread, big, got = attend64(q, k, fine, 8, 2)
+    bound = attend_bound(want, spread, big, rows, d, dtype, m * 4 > 16)
+    for add in (0, 1):
+        out = run_attn(ctx, kv, q, [m], add, 0.0).cpu().double()
+        for i in range(m):
+            seen = v[:rows - m + i + 1].double()
+            for h in range(8):
+                col = seen[:, h // 4]
+                nan, up, down = torch.isnan(col).any(0), (col == math.inf).any(0), (col == -math.inf).any(0)
+                nan = nan | (up & down)
+                assert torch.equal(torch.isnan(out[i, h]), nan), (i, h, add)
+                assert bool((out[i, h][up & ~nan] == math.inf).all()) and bool((out[i, h][down & ~nan] == -math.inf).all()), (i, h, add)
+                rest = ~(nan | up | down)
+                assert bool(((out[i, h] - want[i, h]).abs() <= bound[i, h])[rest].all()), (i, h, add)
+    assert bool(((kv.weight[0, :rows].cpu().double() - got).abs() <= got * (2 * score_error(big, d) + 2 * (rows + m * 8 + 64) * 2.0 ** -24) + 1e-30).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("m", [1, 40])
 def test_scores_of_minus_infinity_weigh_nothing(dtype, m):
     shape = shape_of(4, 2, 32, dtype)
