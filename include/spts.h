@@ -395,7 +395,7 @@ typedef struct {
 } spts_kv_pool;
 /* One sequence's cache in the pool: row i is row i % page of page table[i / page].  table [capacity / page], pos [capacity] int32 and
  * weight [capacity] fp32 (NULL = no account of attention is kept) are device arrays, 16-byte aligned; capacity is a multiple of page,
- * 2^30 at most.  count lives on the host, as in spts_kv_out.  The table's entries for the rows in use are pages of the pool; an entry outside
+ * 2^30 at most; 0 for a sequence that has no pages.  count lives on the host, as in spts_kv_out.  The table's entries for the rows in use are pages of the pool; an entry outside
  * [0, pages) is a caller's mistake: its rows are read as the same rows of page 0 and never written.  Sequences may share pages that
  * are only read (a common prompt); the pages that a call appends to or evicts in belong to one sequence.  What lies behind the first
  * count rows is never read as a value: pages need no initialisation. */

@@ -451,6 +451,9 @@ class Context:
         _need(k, "k", n * self.shape.Hkv * self.shape.d, self.elem)
         _need(v, "v", n * self.shape.Hkv * self.shape.d, self.elem)
         _need(pos, "pos", n, self.i32)
+        for b in getattr(caches, "_unreserved", ()):      # of a runtime.PagedKV: no page and a capacity that does not say so yet
+            if off[b + 1] > off[b]:
+                raise ValueError(f"sequence {b}: rows are appended before any page was reserved for it")
         arr, copied = _caches(caches, spts_kvp)
         _check(load().spts_kvp_append(self.handle, C.byref(pool), _ptr(k), _ptr(v), _ptr(pos), off, len(caches), arr), "spts_kvp_append")
         if copied:

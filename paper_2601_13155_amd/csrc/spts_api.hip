@@ -1587,7 +1587,7 @@ int kvp_batch(const spts_kvp* caches, int32_t batch, const PagedPool& pool, Page
     pb->n = batch;
     for (int b = 0; b < batch; ++b) {
         const spts_kvp& k = caches[b];
-        if (!k.table || !k.pos || k.capacity < 1 || k.count < 0 || k.count > k.capacity) return SPTS_EINVAL;
+        if (!k.table || !k.pos || k.capacity < 0 || k.count < 0 || k.count > k.capacity) return SPTS_EINVAL;
         if (!aligned16(k.table) || !aligned16(k.pos) || !aligned16(k.weight)) return SPTS_EALIGN;
         if (k.capacity % (1 << pool.shift) != 0 || k.capacity > KVP_MAX_ROWS) return SPTS_ESHAPE;
         pb->table[b] = k.table; pb->pos[b] = k.pos; pb->weight[b] = k.weight; pb->count[b] = k.count;

@@ -445,6 +445,7 @@ class PagedKV:
     """One layer's caches of several sequences in pages of a pool that they share.  `pool` and `structs` are what the calls take (structs: a ctypes array of
     spts_kvp, its counts kept up to date by them); k, v [pages, Hkv, page, d], table [sequences, capacity / page], pos and weight
     [sequences, capacity] are the tensors behind them.  The host hands out the pages: reserve before appending, release after an eviction.
+    A struct's capacity is what its sequence has pages for, from its first reserve or release on: appending more is refused.
 
     capacity: rows that a sequence may grow to (rounded up to whole pages); free: the order in which pages are handed out (None = 0, 1, 2, ..)."""
 
@@ -468,6 +469,8 @@ class PagedKV:
             s.table, s.pos = self._table.data_ptr() + 4 * stride * b, self.pos.data_ptr() + 4 * per * page * b
             s.weight = self.weight.data_ptr() + 4 * per * page * b if weights else None
             s.capacity = per * page
+        self._most = per * page
+        self.structs._unreserved = set(range(sequences))     # sequences that have never had a page
         every = np.arange(pages, dtype=np.int32)
         self._free = (every if free is None else np.array(free, dtype=np.int32).reshape(-1))[::-1].copy()      # the first _left are free, the last of them is the next
         self._left = pages
@@ -488,8 +491,8 @@ class PagedKV:
         host, in order with what the current stream is given, and with ctx in order with what its stream is given."""
         torch = _torch()
         have, need = len(self.pages[b]), -(-int(rows) // self.page)
-        if need * self.page > self.structs[b].capacity:
-            raise ValueError(f"sequence {b}: {rows} rows exceed its capacity of {self.structs[b].capacity}")
+        if need * self.page > self._most:
+            raise ValueError(f"sequence {b}: {rows} rows exceed its capacity of {self._most}")
         if need - have > self._left:
             raise ValueError(f"{need - have} pages needed, {self._left} free")
         if need > have:
@@ -499,14 +502,24 @@ class PagedKV:
             self.pages[b] += new.tolist()
             with _on_stream_of(ctx) if ctx is not None else contextlib.nullcontext():
                 self.table[b, have:need].copy_(torch.from_numpy(new))
+        self._owns(b)
 
-    def release(self, b: int):
+    def release(self, b: int, ctx: Optional[binding.Context] = None):
         """Hands back the pages behind sequence b's count rows (all of them where it is 0).  Call it when the work on them is in the stream that
-        their next owner uses too."""
-        need = -(-int(self.structs[b].count) // self.page)
+        their next owner uses too.  With ctx the table forgets them as well, in order with what its stream is given, so that a captured append that is
+        replayed later writes nothing there."""
+        have, need = len(self.pages[b]), -(-int(self.structs[b].count) // self.page)
         while len(self.pages[b]) > need:
             self._free[self._left] = self.pages[b].pop()
             self._left += 1
+        if ctx is not None and have > need:
+            with _on_stream_of(ctx):
+                self.table[b, need:have].fill_(-1)
+        self._owns(b)
+
+    def _owns(self, b: int):
+        self.structs[b].capacity = len(self.pages[b]) * self.page
+        self.structs._unreserved.discard(b)
 
     def append_cache(self, ctx: binding.Context, b: int, cache: "KVCache"):
         """Takes over every pair of a prefill's cache behind sequence b's rows (their weights 0); ValueError where it has other heads or

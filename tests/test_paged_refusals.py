@@ -1,6 +1,8 @@
 """Arguments that the calls over caches in pages and the log probabilities refuse, before anything is launched (no GPU: the pointers are never followed)."""
+import contextlib
 import ctypes as C
 import os
+import types
 
 import pytest
 
@@ -195,3 +197,70 @@ def test_pages_are_handed_out_once(monkeypatch):
     for free in ([0, 1, 2, 3, 4], [0, 1, 2, 3, 4, 4], list(range(7))):
         with pytest.raises(ValueError):
             runtime.PagedKV(shape, 6, 16, 3, 70, free=free)
+
+
+@pytest.fixture
+def on_cpu(monkeypatch):
+    """runtime.PagedKV on CPU tensors."""
+    import torch
+    from paper_2601_13155_amd import runtime
+
+    class OnCpu:
+        def __getattr__(self, name):
+            f = getattr(torch, name)
+            return (lambda *a, device=None, **kw: f(*a, **kw)) if name in ("empty", "zeros", "full") else f
+
+    monkeypatch.setattr(runtime, "_torch", lambda: OnCpu())
+    monkeypatch.setattr(runtime, "_on_stream_of", lambda ctx: contextlib.nullcontext())
+    return runtime.PagedKV
+
+
+def test_rows_without_pages_are_not_appended(ctx, on_cpu):
+    """Pages that were handed back may be another sequence's: what is appended has to lie in a sequence's own."""
+    import torch
+    shape = synth.ModelShape(D=256, H=4, Hkv=2, d=64, Dff=256, dtype="f32")
+    me = types.SimpleNamespace(handle=ctx(), shape=shape, elem=torch.float32, i32=torch.int32)
+    kv = on_cpu(shape, 6, 16, 3, 70)
+
+    def append(rows, why, caches=None):
+        offs = [sum(rows[:b]) for b in range(4)]
+        with pytest.raises(binding.SptsError) as e:
+            binding.Context.spts_kvp_append(me, kv.pool, A, A, A, offs, kv.structs if caches is None else caches)
+        assert e.value.status == why
+        assert kv.counts == before
+
+    before = kv.counts
+    for rows in ([0, 1, 0, 0], [0, 0, 0, 16]):
+        with pytest.raises(ValueError):
+            binding.Context.spts_kvp_append(me, kv.pool, A, A, A, [sum(rows[:b + 1]) for b in range(4)], kv.structs)
+    binding.Context.spts_kvp_append(me, kv.pool, A, A, A, [0, 0, 0, 0], kv.structs)
+    kv.reserve(0, 17)
+    kv.reserve(1, 1)
+    assert [s.capacity for s in kv.structs][:2] == [32, 16]
+    kv.structs[0].count, kv.structs[1].count = 20, 3
+    before = kv.counts
+    append([13, 0, 0], INVAL)
+    append([13, 0, 0], INVAL, list(kv.structs))
+    kv.structs[0].count = 10
+    kv.release(0)
+    kv.reserve(1, 32)                          # takes the page that was handed back
+    assert kv.pages[1][1] == kv.table[0, 1] and kv.structs[0].capacity == 16
+    before = kv.counts
+    append([7, 0, 0], INVAL)
+    append([7, 2, 0], INVAL, list(kv.structs))
+    kv.reserve(0, 17)
+    assert kv.structs[0].capacity == 32 and not set(kv.pages[0]) & set(kv.pages[1])
+    # nothing left: no rows, in any call
+    kv.structs[0].count = 0
+    kv.release(0, ctx=me)
+    assert kv.structs[0].capacity == 0 and (kv.table[0] == -1).all() and kv.free_pages == 4
+    before = kv.counts
+    append([1, 0, 0], INVAL)
+    binding.Context.spts_kvp_append(me, kv.pool, A, A, A, [0, 0, 0, 0], kv.structs)
+    binding.Context.spts_kvp_attn(me, kv.pool, A, [0, 0, 0, 0], kv.structs, 4 * A)
+    binding.Context.spts_kvp_evict(me, kv.pool, [5, 3, 1], kv.structs)
+    assert kv.counts == [0, 3, 0]
+    kv.reserve(0, 64)
+    with pytest.raises(ValueError):
+        kv.reserve(0, 81)
+    assert kv.structs[0].capacity == 64 and kv.free_pages == 0
