@@ -498,10 +498,10 @@ class PagedKV:
         if need > have:
             left = self._left - (need - have)
             new = self._free[left:self._left][::-1].copy()
-            self._left = left
-            self.pages[b] += new.tolist()
             with _on_stream_of(ctx) if ctx is not None else contextlib.nullcontext():
                 self.table[b, have:need].copy_(torch.from_numpy(new))
+            self._left = left                           # (the pages are free still where the copy was refused, in a capture for instance)
+            self.pages[b] += new.tolist()
         self._owns(b)
 
     def release(self, b: int, ctx: Optional[binding.Context] = None):
@@ -509,12 +509,12 @@ class PagedKV:
         their next owner uses too.  With ctx the table forgets them as well, in order with what its stream is given, so that a captured append that is
         replayed later writes nothing there."""
         have, need = len(self.pages[b]), -(-int(self.structs[b].count) // self.page)
-        while len(self.pages[b]) > need:
-            self._free[self._left] = self.pages[b].pop()
-            self._left += 1
         if ctx is not None and have > need:
             with _on_stream_of(ctx):
                 self.table[b, need:have].fill_(-1)
+        while len(self.pages[b]) > need:
+            self._free[self._left] = self.pages[b].pop()
+            self._left += 1
         self._owns(b)
 
     def _owns(self, b: int):

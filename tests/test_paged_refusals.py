@@ -264,3 +264,23 @@ def test_rows_without_pages_are_not_appended(ctx, on_cpu):
     with pytest.raises(ValueError):
         kv.reserve(0, 81)
     assert kv.structs[0].capacity == 64 and kv.free_pages == 0
+
+
+def test_a_reservation_that_failed_takes_no_pages(on_cpu, monkeypatch):
+    import torch
+    kv = on_cpu(synth.ModelShape(D=256, H=4, Hkv=2, d=64, Dff=256, dtype="f32"), 6, 16, 2, 70)
+    kv.reserve(0, 20)
+
+    def refused(*a):
+        raise RuntimeError("not now")
+
+    with monkeypatch.context() as m:
+        m.setattr(torch, "from_numpy", refused)
+        with pytest.raises(RuntimeError):
+            kv.reserve(0, 64)
+        with pytest.raises(RuntimeError):
+            kv.reserve(1, 16)
+    assert kv.free_pages == 4 and kv.pages == [[0, 1], []] and kv.structs[0].capacity == 32
+    kv.reserve(1, 16)
+    kv.reserve(0, 64)
+    assert kv.pages == [[0, 1, 3, 4], [2]] and kv.table[0, :4].tolist() == [0, 1, 3, 4] and kv.table[1, 0] == 2
