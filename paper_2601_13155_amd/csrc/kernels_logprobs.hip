@@ -272,21 +272,16 @@ __global__ void __launch_bounds__(PT) logprobs_join_kernel(PartArgs a) {
     });
 }
 
-// Parts of a row: enough workgroups for the chip where rows are few
+// Parts of a row: enough workgroups for the chip where rows are few.  Rows in parts have fewer than 2 * WANT of them in all.
+constexpr int64_t WANT = 256;
+static_assert(2 * WANT * (sizeof(Sums) + LOGPROBS_MAX_TOP * sizeof(Word)) + 64 <= LOGPROBS_SCRATCH_BYTES, "sums and words of all parts");
 static int logprobs_parts(int64_t rows, int32_t V, int32_t* span) {
-    constexpr int64_t WANT = 256;
     int64_t parts = rows >= WANT ? 1 : (WANT + rows - 1) / rows;
     parts = parts > PPARTS ? PPARTS : parts;
     const int64_t least = 8 * PT;   // words of a part
     if (parts > (V + least - 1) / least) parts = (V + least - 1) / least;
     *span = (int32_t)((V + parts - 1) / parts);
     return (int)((V + *span - 1) / *span);
-}
-
-size_t logprobs_scratch_bytes(int64_t rows, int32_t V, int32_t top) {
-    int32_t span;
-    const int parts = logprobs_parts(rows, V, &span);
-    return parts == 1 ? 0 : (size_t)rows * parts * (sizeof(Sums) + top * sizeof(Word)) + 64;
 }
 
 template <typename T>

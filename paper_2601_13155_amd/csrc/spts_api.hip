@@ -1708,7 +1708,7 @@ int spts_token_logprobs(spts_ctx* c, const void* logits, int32_t dtype, int64_t 
     if (!logits) return SPTS_EINVAL;
     const void* ps[] = {logits, tokens, logprob, entropy, top_ids, top_logprobs};
     for (const void* p : ps) if (!aligned16(p)) return SPTS_EALIGN;
-    if (logprobs_scratch_bytes(rows, V, n_top) > c->off.qp - c->off.tmp32) return SPTS_EWORKSPACE;
+    static_assert(LOGPROBS_SCRATCH_BYTES <= TOPK_MULTI_SCRATCH_BYTES, "every workspace has that much behind tmp32, all of it scratch of other calls");
     PHASE(c, PH_LOGPROBS);
     SPTS_HIP(c, launch_token_logprobs(LogprobArgs{logits, stride, V, rows, tokens, logprob, entropy, n_top, top_ids, top_logprobs}, dtype == SPTS_BF16,
                                       c->p<void>(c->off.tmp32), c->stream));

@@ -423,12 +423,12 @@ hipError_t launch_kvp_evict(const PagedPool& pool, const PagedBatch& pb, const P
 
 // ------------------------------------------------------------------ log probabilities
 // Of rows of V logits (stride apart): logprob[i] of word tokens[i] (NaN outside [0, V)), entropy[i], and the `top` words with the largest logits, ties to the lower word
-// (ids -1 and -inf where fewer are above -inf).  tokens with logprob, entropy, ids and top_lp may be null.  scratch: logprobs_scratch_bytes.
+// (ids -1 and -inf where fewer are above -inf).  tokens with logprob, entropy, ids and top_lp may be null.  scratch: LOGPROBS_SCRATCH_BYTES.
 constexpr int LOGPROBS_MAX_TOP = 32;
 struct LogprobArgs {
     const void* logits; int64_t stride; int32_t V; int64_t rows; const int32_t* tokens; float* logprob; float* entropy; int32_t top; int32_t* ids; float* top_lp;
 };
-size_t logprobs_scratch_bytes(int64_t rows, int32_t V, int32_t top);
+constexpr size_t LOGPROBS_SCRATCH_BYTES = 512 * (12 + 8 * LOGPROBS_MAX_TOP) + 64;   // whatever the rows and words
 hipError_t launch_token_logprobs(const LogprobArgs& a, bool bf16, void* scratch, hipStream_t s);
 
 }  // namespace spts

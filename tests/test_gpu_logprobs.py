@@ -131,6 +131,15 @@ def test_only_what_is_wanted(ctx):
             ctx.spts_token_logprobs(x, V, rows, entropy=torch.empty(8, device="cuda"), stride=stride)
 
 
+@pytest.mark.parametrize("rows,V", [(255, 2049), (255, 20011), (129, 5000), (37, 20011), (1, 140000)])
+def test_the_smallest_contexts_serve_every_call(rows, V):
+    """Rows in parts with the longest lists, whose scratch is independent of the context's heads and tokens."""
+    g = torch.Generator().manual_seed(rows + V)
+    x = (3.0 * torch.randn((rows, V), generator=g)).cuda()
+    for H, Hkv, d in ((1, 1, 32), (2, 1, 64)):
+        check(context(shape_of(H, Hkv, d, "f32"), 1), x, torch.randint(0, V, (rows,), generator=g).tolist(), 32)
+
+
 def test_more_elements_than_32_bits(ctx):
     rows, V = 16400, 131072 + 64
     x = torch.empty((rows, V), dtype=torch.bfloat16, device="cuda")
