@@ -441,7 +441,7 @@ int spts_kvp_evict(spts_ctx *ctx, const spts_kv_pool *pool, const int64_t *keep,
  * (<= SPTS_MAX_TOP_LOGPROBS) words with the largest logits, ties to the lower id: top_ids, top_logprobs [rows, n_top].  logprob goes with
  * tokens, top_ids with top_logprobs and n_top > 0; entropy and each of these pairs may be NULL.  Words at -inf have no part in it: where fewer than n_top are
  * above -inf the rest is -1 and -inf; a row without any has entropy 0 and log probabilities of -inf.  A NaN or +inf makes the row's log probabilities and
- * entropy NaN; a NaN is never among the top.  V <= 2^28, rows < 2^31.  spts_process_logits' logits_out are such logits.  Uses the workspace
+ * entropy NaN; a NaN is never among the top.  The results overlap neither the logits nor each other.  V <= 2^28, rows < 2^31.  spts_process_logits' logits_out are such logits.  Uses the workspace
  * of the context, any of which is large enough. */
 #define SPTS_MAX_TOP_LOGPROBS 32
 int spts_token_logprobs(spts_ctx *ctx, const void *logits, int32_t dtype, int64_t stride, int32_t V, int64_t rows, const int32_t *tokens,

@@ -1708,6 +1708,11 @@ int spts_token_logprobs(spts_ctx* c, const void* logits, int32_t dtype, int64_t 
     if (!logits) return SPTS_EINVAL;
     const void* ps[] = {logits, tokens, logprob, entropy, top_ids, top_logprobs};
     for (const void* p : ps) if (!aligned16(p)) return SPTS_EALIGN;
+    const struct { const void* p; int64_t bytes; } out[] = {{logits, ((rows - 1) * stride + V) * (dtype == SPTS_BF16 ? 2 : 4)}, {logprob, 4 * rows}, {entropy, 4 * rows},
+                                                            {top_ids, 4 * rows * n_top}, {top_logprobs, 4 * rows * n_top}};
+    for (const auto& a : out)
+        for (const auto* o = out; o != &a; ++o)
+            if (a.p && o->p && overlap(a.p, a.bytes, o->p, o->bytes)) return SPTS_EINVAL;
     static_assert(LOGPROBS_SCRATCH_BYTES <= TOPK_MULTI_SCRATCH_BYTES, "every workspace has that much behind tmp32, all of it scratch of other calls");
     PHASE(c, PH_LOGPROBS);
     SPTS_HIP(c, launch_token_logprobs(LogprobArgs{logits, stride, V, rows, tokens, logprob, entropy, n_top, top_ids, top_logprobs}, dtype == SPTS_BF16,

@@ -162,6 +162,25 @@ def test_logprobs(lib, ctx):
         assert call(**{name: A + 4}) == ALIGN, name
 
 
+def test_logprobs_results_that_overlap(lib, ctx):
+    h = ctx()
+    rows, stride, V, top = 3, 120, 100, 4
+    places = dict(logits=A, logprob=2 * A, entropy=3 * A, ids=4 * A, top=5 * A)
+    size = dict(logits=4 * (2 * stride + V), logprob=4 * rows, entropy=4 * rows, ids=4 * rows * top, top=4 * rows * top)
+
+    def call(dtype=0, **kw):
+        a = {**places, **kw}
+        return lib.spts_token_logprobs(h, a["logits"], dtype, stride, V, rows, 6 * A, a["logprob"], a["entropy"], top, a["ids"], a["top"])
+
+    for one in places:
+        for other in places:
+            if one == other:
+                continue
+            assert call(**{one: places[other]}) == INVAL, (one, other)
+            assert call(**{one: places[other] + (size[other] - 1) // 16 * 16}) == INVAL, (one, other)
+    assert call(dtype=1, entropy=A + 2 * (2 * stride + V) // 16 * 16) == INVAL
+
+
 def test_pages_are_handed_out_once(monkeypatch):
     """The host's side of runtime.PagedKV, on CPU tensors."""
     import torch
