@@ -68,6 +68,21 @@ def attend64(q, k, v, H, Hkv):
     return out, spread, big, got
 
 
+def attend64_wide(q, k, v, H, Hkv):
+    """attend64 on the GPU, a head's queries at once."""
+    m, n, d, G = q.shape[0], k.shape[0], q.shape[2], H // Hkv
+    q, k, v = (t.cuda().double() for t in (q, k, v))
+    out, spread, big, got = torch.zeros_like(q), torch.zeros_like(q), 0.0, torch.zeros(n, dtype=torch.float64, device="cuda")
+    unseen = torch.ones((m, n), dtype=torch.bool, device="cuda").triu(n - m + 1)
+    for h in range(H):
+        kh, vh, qh = k[:, h // G].contiguous(), v[:, h // G].contiguous(), q[:, h].contiguous()
+        p = torch.softmax(((qh @ kh.t()) / math.sqrt(d)).masked_fill(unseen, -math.inf), 1)
+        out[:, h], spread[:, h] = p @ vh, p @ vh.abs()
+        big = max(big, float((qh.abs() @ kh.t().abs()).masked_fill(unseen, 0.0).max()) / math.sqrt(d))
+        got += p.sum(0)
+    return out.cpu(), spread.cpu(), big, got.cpu()
+
+
 def score_error(big, d):
     """How far a score is off: d products summed in fp32 (each addition and, of fp32 operands, each product half a step), the scaling, the difference to the maximum and the exponential's
     few steps."""

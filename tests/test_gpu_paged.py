@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_2601_13155_amd import binding, runtime, synth
-from tests.paged import attend64, attend_bound, context, evict64, filled, put, score_error, shape_of, TD
+from tests.paged import attend64, attend64_wide, attend_bound, context, evict64, filled, put, score_error, shape_of, TD
 
 pytestmark = pytest.mark.gpu
 
@@ -94,6 +94,43 @@ def test_sixteen_sequences(dtype):
     q = torch.randn((sum(new), 8, 64), generator=torch.Generator().manual_seed(1)).to(TD[dtype]).cuda()
     before = kv.weight.cpu().clone()
     check_attn(shape, kv, host, q, new, run_attn(ctx, kv, q, new, 1, 0.25), 1, 0.25, before)
+
+
+def check_wide(shape, rows, new, page, decay=0.5):
+    """Outputs and accounts of a large call, every query of it."""
+    ctx = context(shape, sum(new))
+    kv, host = filled(shape, page, rows, seed=sum(rows) + shape.d)
+    q = torch.randn((sum(new), shape.H, shape.d), generator=torch.Generator().manual_seed(shape.d)).to(TD[shape.dtype]).cuda()
+    before = kv.weight.cpu().clone()
+    outs, at = (run_attn(ctx, kv, q, new), run_attn(ctx, kv, q, new, 1, decay)), 0
+    for b, m in enumerate(new):
+        n = rows[b]
+        want, spread, big, got = attend64_wide(q[at:at + m], *host[b], shape.H, shape.Hkv)
+        tol = attend_bound(want, spread, big, n, shape.d, shape.dtype, m * shape.H // shape.Hkv > 16)
+        for out in outs:
+            err = (out[at:at + m].cpu().double() - want).abs()
+            assert bool((err <= tol).all()), (b, float((err / tol).max()))
+        w = got + decay * before[b, :n].double()
+        tol = w * (2 * score_error(big, shape.d) + 2 * (n + m * shape.H + 64) * 2.0 ** -24) + 1e-30
+        err = (kv.weight[b, :n].cpu().double() - w).abs()
+        assert bool((err <= tol).all()), (b, float((err / tol).max()))
+        at += m
+
+
+@pytest.mark.parametrize("rows,new,H,Hkv,d,page", [([3300], [1024], 64, 8, 128, 16), ([2600], [600], 64, 64, 32, 16), ([3300, 2100], [1024, 300], 64, 16, 64, 32), ([12000], [32], 64, 32, 64, 16),
+                                                   ([12000], [33], 32, 32, 32, 16), ([9000], [20], 64, 32, 128, 16)])
+def test_chunks_over_more_pages_than_a_wavefront_has_at_hand(rows, new, H, Hkv, d, page):
+    """Shares of more than 64 pages, from the first row on and from later ones: entries of the table come 64 at a time."""
+    check_wide(shape_of(H, Hkv, d, "bf16"), rows, new, page)
+
+
+UNEVEN = [int(4000 * (1 - 0.92 * b / 15)) for b in range(16)]
+
+
+@pytest.mark.parametrize("rows,H,Hkv,d", [([60000], 128, 8, 128), ([150000], 64, 4, 32), (UNEVEN, 32, 8, 32), (UNEVEN, 32, 8, 64), (UNEVEN, 16, 8, 128)])
+def test_accounts_of_single_tokens_whose_scores_leave_at_once(rows, H, Hkv, d):
+    """Scores of shares that are too long for LDS, or of more workgroups than CUs, are stored as they come."""
+    check_wide(shape_of(H, Hkv, d, "bf16"), rows, [1] * len(rows), 16)
 
 
 def test_results_do_not_depend_on_the_batch():
