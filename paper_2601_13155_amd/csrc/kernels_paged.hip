@@ -111,7 +111,6 @@ __global__ void __launch_bounds__(ET) kvp_select_kernel(EvictSeqs<NB> sq, Move* 
 #pragma unroll
         for (int e = 0; e < 4; ++e) key[j][e] = i + e < n ? evict_key(w[e], (int32_t)p[e], below, above) : 0u;
     }
-    auto each_block = [&](auto f) __attribute__((always_inline)) { f(w0); };
     uint32_t prefix = 0, want = (uint32_t)k;   // of the keys that agree with the prefix so far the `want` largest stay
     for (int pass = 0; pass < 3; ++pass) {
         const int sh = pass == 0 ? 21 : pass == 1 ? 10 : 0;
@@ -119,22 +118,20 @@ __global__ void __launch_bounds__(ET) kvp_select_kernel(EvictSeqs<NB> sq, Move* 
         for (int i = tid; i < EBINS; i += ET) hist[i] = 0;
         __syncthreads();
         const uint32_t known = pass == 0 ? 0u : ~0u << (pass == 1 ? 21 : 10);
-        each_block([&](int s0) {
 #pragma unroll
-            for (int j = 0; j < K4; ++j) {
-                if (s0 + 256 * j >= w1) break;
-                // (one count of 256 where rows are all alike, zeros for instance)
-                const uint32_t first = (uint32_t)__builtin_amdgcn_readfirstlane((int)key[j][0]);
-                const bool alike = key[j][0] == first && key[j][1] == first && key[j][2] == first && key[j][3] == first;
-                if (__ballot(alike) == ~0ull) {
-                    if (lane == 0 && (first & known) == prefix) atomicAdd(&hist[(first >> sh) & (bins - 1)], 256u);
-                } else {
+        for (int j = 0; j < K4; ++j) {
+            if (w0 + 256 * j >= w1) break;
+            // (one count of 256 where rows are all alike, zeros for instance)
+            const uint32_t first = (uint32_t)__builtin_amdgcn_readfirstlane((int)key[j][0]);
+            const bool alike = key[j][0] == first && key[j][1] == first && key[j][2] == first && key[j][3] == first;
+            if (__ballot(alike) == ~0ull) {
+                if (lane == 0 && (first & known) == prefix) atomicAdd(&hist[(first >> sh) & (bins - 1)], 256u);
+            } else {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if ((key[j][e] & known) == prefix) atomicAdd(&hist[(key[j][e] >> sh) & (bins - 1)], 1u);
-                }
+                for (int e = 0; e < 4; ++e)
+                    if ((key[j][e] & known) == prefix) atomicAdd(&hist[(key[j][e] >> sh) & (bins - 1)], 1u);
             }
-        });
+        }
         __syncthreads();
         // counts of the bins from the highest down: thread t has bins 2 (ET - 1 - t) + 1 and 2 (ET - 1 - t)
         const int hi = 2 * (ET - 1 - tid) + 1;
@@ -158,14 +155,12 @@ __global__ void __launch_bounds__(ET) kvp_select_kernel(EvictSeqs<NB> sq, Move* 
     }
     // of the rows with the key `prefix` the first `want` stay
     uint32_t ties = 0;
-    each_block([&](int s0) {
 #pragma unroll
-        for (int j = 0; j < K4; ++j) {
-            if (s0 + 256 * j >= w1) break;
+    for (int j = 0; j < K4; ++j) {
+        if (w0 + 256 * j >= w1) break;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) ties += (uint32_t)__popcll(__ballot(key[j][e] == prefix));
-        }
-    });
+        for (int e = 0; e < 4; ++e) ties += (uint32_t)__popcll(__ballot(key[j][e] == prefix));
+    }
     if (lane == 0) swave[wave] = ties;
     __syncthreads();
     uint32_t tie0 = 0, all_ties = 0;
@@ -181,41 +176,39 @@ __global__ void __launch_bounds__(ET) kvp_select_kernel(EvictSeqs<NB> sq, Move* 
     auto quads = [&](auto choose, auto f) __attribute__((always_inline)) {
         uint32_t tie = tie0;
         nfree = nmove = 0;
-        each_block([&](int s0) {
 #pragma unroll
-            for (int j = 0; j < K4; ++j) {
-                const int q0 = s0 + 256 * j, i0 = q0 + 4 * lane;
-                if (q0 >= w1) break;
-                bool stays[4], is_free[4], moves_[4];
-                uint32_t seen = tie;
-                if constexpr (decltype(choose)::value) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint64_t m = __ballot(key[j][e] == prefix);
-                        seen += below_lane(m);
-                        tie += (uint32_t)__popcll(m);
-                    }
-                }
-                uint32_t frank = nfree, mrank = nmove;
+        for (int j = 0; j < K4; ++j) {
+            const int q0 = w0 + 256 * j, i0 = q0 + 4 * lane;
+            if (q0 >= w1) break;
+            bool stays[4], is_free[4], moves_[4];
+            uint32_t seen = tie;
+            if constexpr (decltype(choose)::value) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    stays[e] = key[j][e] >= prefix && i0 + e < n;
-                    if constexpr (decltype(choose)::value) {
-                        const bool t = key[j][e] == prefix;
-                        stays[e] = stays[e] && (!t || seen < want);
-                        seen += t ? 1u : 0u;
-                    }
-                    is_free[e] = i0 + e < k && !stays[e];
-                    moves_[e] = i0 + e >= k && stays[e];
-                    const uint64_t fm = __ballot(is_free[e]), mm = __ballot(moves_[e]);
-                    frank += below_lane(fm);
-                    mrank += below_lane(mm);
-                    nfree += (uint32_t)__popcll(fm);
-                    nmove += (uint32_t)__popcll(mm);
+                    const uint64_t m = __ballot(key[j][e] == prefix);
+                    seen += below_lane(m);
+                    tie += (uint32_t)__popcll(m);
                 }
-                f(i0, is_free, moves_, stays, frank, mrank);
             }
-        });
+            uint32_t frank = nfree, mrank = nmove;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                stays[e] = key[j][e] >= prefix && i0 + e < n;
+                if constexpr (decltype(choose)::value) {
+                    const bool t = key[j][e] == prefix;
+                    stays[e] = stays[e] && (!t || seen < want);
+                    seen += t ? 1u : 0u;
+                }
+                is_free[e] = i0 + e < k && !stays[e];
+                moves_[e] = i0 + e >= k && stays[e];
+                const uint64_t fm = __ballot(is_free[e]), mm = __ballot(moves_[e]);
+                frank += below_lane(fm);
+                mrank += below_lane(mm);
+                nfree += (uint32_t)__popcll(fm);
+                nmove += (uint32_t)__popcll(mm);
+            }
+            f(i0, is_free, moves_, stays, frank, mrank);
+        }
     };
     auto both = [&](auto f) __attribute__((always_inline)) {
         if (all_ties > want) quads(std::true_type{}, f);
@@ -481,7 +474,7 @@ __global__ void __launch_bounds__(256) kvp_move_kernel(u32x4* __restrict__ pk, u
 static int64_t most_moves(const PagedBatch& pb, const PagedEvict& ev, int b) {
     return pb.count[b] > ev.keep[b] ? std::min(ev.keep[b], pb.count[b] - ev.keep[b]) : 0;
 }
-// One workgroup per sequence up to here (us by one / over the chip: 8192 rows 13 / 23, 16384 17 / 26, 65536, keys loaded anew for each pass, 70 / 29)
+// One workgroup per sequence as long as its registers hold the keys (us by one / over the chip: 8192 rows 13 / 23, 16384 17 / 26)
 constexpr int64_t SELECT_ONE = 4096 * K4;
 static int64_t longest_cut(const PagedBatch& pb, const PagedEvict& ev) {
     int64_t n = 0;

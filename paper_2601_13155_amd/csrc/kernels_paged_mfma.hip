@@ -372,7 +372,7 @@ __global__ void __launch_bounds__(NW * 64, NW == 8 ? 2 : 1) kvp_many_kernel(cons
 // has the scores of keys 8 kg .. 8 kg + 7, which is the operand of O^T = V^T P^T as it stands.  Probabilities go in as two bf16 parts, both above 0 (off by 2^-16 of each at most), which
 // costs nothing here.  The maximum moves only when a score is 2^8 above it.
 // Scores for the accounts wait in LDS for the end where a share's fit there and a workgroup has a CU to itself: stores among the reads cost more than their bytes (131071 rows 110 us by these
-// for 97, five of 1600 .. 20000 64 / 55; without accounts 87).
+// for 92, five of 1600 .. 20000 64 / 54; without accounts 87).
 // Rows are read once, by loads that do not leave them in the caches, where they would push out what other kernels wrote (us by plain loads / so, when scores went to memory as they came:
 // one token after 131071 rows with accounts 117 / 110, behind a kernel that wrote 1 GB 174 / 118; 16 of up to 13106 in 384 workgroups 53 / 51, behind such a kernel 152 / 92.  Where it costs:
 // all of 16 caches of 4000 rows in the last cache from the call before 50 / 58, 16 sequences of 13106 rows on the same pages 58 / 63).
