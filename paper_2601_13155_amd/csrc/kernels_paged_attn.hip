@@ -29,10 +29,10 @@ __device__ inline void store4(bf16_t* p, f32x4 v, float f) { *reinterpret_cast<u
 
 // On the fp32 matrix instruction 32x32x2.  S^T = K Q^T: operand rows are keys, columns queries; the two halves of a wavefront multiply every other four of the dimensions, so a lane's
 // operand is half a row and a load takes 32 bytes of each key (halves that are 64 dimensions apart touch twice the lines a load, more than the first cache holds until the rest of them is
-// wanted: 128 tokens after 3872 rows 126 us for 115, one token after 60000 156 for 139, the accounts 57 for 45).  O^T += V^T P^T: result element r of lane (l, half) is key
+// wanted: 128 tokens after 3872 rows of 8 heads of 4, d = 128, 126 us for 115, their accounts 57 for 45).  O^T += V^T P^T: result element r of lane (l, half) is key
 // 8 (r / 4) + 4 half + r % 4 of column l, which is the second operand of the r-th product of V^T as it stands.  The four wavefronts of a workgroup take blocks of 32 keys in turn and meet in
-// LDS; a lane asks for the next piece of a key, and the next 32 dimensions of the values, before it multiplies these: 128 tokens after 3872 rows of 8 heads of 4 (d = 128) 115 us, 72
-// TFLOP/s of the 154 that a large fp32 product reaches here.
+// LDS; a lane asks for the next piece of a key, and the next 32 dimensions of the values, before it multiplies these: those 128 tokens 99 us with the
+// rows in the last cache and 117 behind a kernel that wrote 1 GB, 84 and 71 TFLOP/s of the 154 that a large fp32 product reaches here.
 // A block that some column does not see entirely has its scores set to -inf there, and values that are not finite kept out of the product (0 times them would be NaN): two more products
 // count those that a column does see and put the infinity or NaN where it belongs.
 constexpr int AW = 4;
