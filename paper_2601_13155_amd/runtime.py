@@ -519,7 +519,7 @@ class PagedKV:
 
     def _owns(self, b: int):
         self.structs[b].capacity = len(self.pages[b]) * self.page
-        self.structs._unreserved.discard(b)
+        self.structs._unreserved.discard(b % len(self.structs))
 
     def append_cache(self, ctx: binding.Context, b: int, cache: "KVCache"):
         """Takes over every pair of a prefill's cache behind sequence b's rows (their weights 0); ValueError where it has other heads or

@@ -303,3 +303,9 @@ def test_a_reservation_that_failed_takes_no_pages(on_cpu, monkeypatch):
     kv.reserve(1, 16)
     kv.reserve(0, 64)
     assert kv.pages == [[0, 1, 3, 4], [2]] and kv.table[0, :4].tolist() == [0, 1, 3, 4] and kv.table[1, 0] == 2
+
+
+def test_sequences_counted_from_the_end(on_cpu):
+    kv = on_cpu(synth.ModelShape(D=256, H=4, Hkv=2, d=64, Dff=256, dtype="f32"), 6, 16, 3, 70)
+    kv.reserve(-1, 20)
+    assert kv.pages == [[], [], [0, 1]] and [s.capacity for s in kv.structs] == [80, 80, 32] and kv.structs._unreserved == {0, 1}
